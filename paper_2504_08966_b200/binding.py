@@ -26,7 +26,8 @@ EXPORTS = ["pact_create", "pact_destroy", "pact_workspace_bytes", "pact_status_s
            "pact_prune_static", "pact_reincorporate", "pact_merge", "pact_reduce", "pact_reduce_host",
            "pact_host_staging_bytes", "pact_launch_count", "pact_profile_enable", "pact_profile_read",
            "pact_profile_stage_name", "pact_graph_create", "pact_graph_launch", "pact_graph_destroy",
-           "pact_key_spread", "pact_set_wait_limits"]
+           "pact_key_spread", "pact_set_wait_limits", "pact_cache_plan", "pact_cache_write", "pact_page_select",
+           "pact_paged_attention", "pact_paged_workspace_bytes"]
 
 
 class Params(C.Structure):
@@ -42,6 +43,12 @@ class ImageDesc(C.Structure):
                 ("P_out", C.c_void_p), ("size_out", C.c_void_p), ("label", C.c_void_p),
                 ("score", C.c_void_p), ("keep", C.c_void_p), ("counters", C.c_void_p),
                 ("logw_out", C.c_void_p)]
+
+
+class PagedCacheDesc(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("k_page", C.c_int64), ("k_head", C.c_int64), ("k_row", C.c_int64),
+                ("v_page", C.c_int64), ("v_head", C.c_int64), ("v_row", C.c_int64), ("logw", C.c_void_p),
+                ("bounds", C.c_void_p), ("w_max", C.c_void_p), ("n_pages", C.c_int32), ("page_rows", C.c_int32)]
 
 
 _lib = None
@@ -85,6 +92,13 @@ def lib():
         L.pact_profile_read.argtypes = [vp, C.POINTER(C.c_float), i32]
         L.pact_profile_stage_name.argtypes = [i32]
         L.pact_profile_stage_name.restype = C.c_char_p
+        pc = C.POINTER(PagedCacheDesc)
+        L.pact_cache_plan.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, i64, i32, vp, vp]
+        L.pact_cache_write.argtypes = [vp, pc, vp, vp, i64, i64, vp, vp, i64, vp, vp]
+        L.pact_page_select.argtypes = [vp, pc, vp, i64, i64, i32, vp, i32, vp, C.c_float, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.pact_paged_attention.argtypes = [vp, pc, vp, i64, i64, i32, vp, i32, vp, vp, i32, C.c_float, vp, i64, i64, vp, vp, vp, sz, vp]
+        L.pact_paged_workspace_bytes.argtypes = [vp, i32, i32]
+        L.pact_paged_workspace_bytes.restype = sz
         for name in EXPORTS:
             if getattr(L, name).restype is C.c_int:
                 getattr(L, name).restype = C.c_int
@@ -202,6 +216,40 @@ class Graph:
             pass
 
 
+def _strides(t, what: str):
+    """Strides of a tensor whose last axis is contiguous; an axis of one element gets the stride that it would have if packed."""
+    shape, st = t.shape, list(t.stride())
+    if st[-1] != 1 and shape[-1] != 1:
+        raise PactError(f"{what}: the last axis has to be contiguous")
+    st[-1] = 1
+    for i in range(len(st) - 2, -1, -1):
+        if shape[i] == 1:
+            st[i] = max([st[j] * shape[j] for j in range(len(st)) if shape[j] > 1 or j == len(st) - 1])
+    return st
+
+
+class PagedCache:
+    """One layer's paged cache, the tensors of pact_paged_cache in pact.h: K, V [n_pages, n_kvh, page_rows, d_h] (any strides with a contiguous last
+    axis; rows before heads is a transposed view), logw [n_pages, page_rows] fp32, bounds [n_pages, n_kvh, 2, d_h], w_max [n_pages] fp32.  The
+    caller owns them; the handle keeps them alive."""
+
+    def __init__(self, K, V, logw=None, bounds=None, w_max=None):
+        if K.dim() != 4 or V.shape != K.shape or V.dtype != K.dtype:
+            raise PactError("K and V are [n_pages, n_kvh, page_rows, d_h] of one type")
+        self.K, self.V, self.logw, self.bounds, self.w_max = K, V, logw, bounds, w_max
+        self.n_pages, self.n_kvh, self.page_rows, self.d_h = K.shape
+        self.dtype, self.device = K.dtype, K.get_device()
+        for t, dtype, shape, what in ((logw, torch.float32, (self.n_pages, self.page_rows), "logw"), (w_max, torch.float32, (self.n_pages,), "w_max"),
+                                      (bounds, K.dtype, (self.n_pages, self.n_kvh, 2, self.d_h), "bounds")):
+            if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+                raise PactError(f"{what}: a contiguous {dtype} tensor of shape {shape} is wanted")
+        if any(t is not None and t.get_device() != self.device for t in (V, logw, bounds, w_max)):
+            raise PactError("the tensors of a cache are on one device")
+        k, v = _strides(K, "K"), _strides(V, "V")
+        self.desc = PagedCacheDesc(_ptr(K), _ptr(V), k[0], k[1], k[2], v[0], v[1], v[2], _ptr(logw), _ptr(bounds), _ptr(w_max),
+                                   self.n_pages, self.page_rows)
+
+
 PRUNE_STATIC_MAX_N = 65536
 
 
@@ -223,6 +271,9 @@ class Context:
         _check(None, self._L.pact_create(C.byref(self.handle), d, n_qh, n_kvh, d_h, _dt(in_dtype), _dt(out_dtype)))
         self.ws = None
         self._need = {}                      # (max_batch, max_N) -> workspace bytes, asked from the library once
+        self.device = torch.cuda.current_device()
+        self._paged_ws = []                  # workspaces of the paged cache's calls, the last one in use
+        self._paged_need = {}
 
     def close(self):
         if self.handle:
@@ -326,6 +377,113 @@ class Context:
         h = C.c_void_p()
         _check(self.handle, self._L.pact_graph_create(self.handle, arr, B, parr, stride, w, n, C.byref(h)))
         return Graph(self, h, images, self.ws)
+
+    # ---- the paged cache ------------------------------------------------------------------
+    def _on_device(self, t, dtype, shape, what):
+        """A contiguous tensor of this type and shape on the context's device; its address, None for None."""
+        if t is None:
+            return None
+        if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != self.device:
+            raise PactError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{self.device} is wanted")
+        return t.data_ptr()
+
+    def _heads(self, t, dtype, n, what):
+        """Address and strides of a [.., n, d_h] tensor on the context's device."""
+        if t.dtype != dtype or t.dim() != 3 or t.shape[1] != n or t.shape[2] != self.d_h or t.get_device() != self.device:
+            raise PactError(f"{what}: a {dtype} tensor of shape [.., {n}, {self.d_h}] on cuda:{self.device} is wanted")
+        s0, s1, s2 = t.stride()
+        if s2 != 1 or t.shape[0] == 1 or n == 1:
+            s0, s1, _ = _strides(t, what)
+        return t.data_ptr(), s0, s1
+
+    def _cache(self, cache):
+        if cache.n_kvh != self.n_kvh or cache.d_h != self.d_h or cache.dtype != self.in_dtype or cache.device != self.device:
+            raise PactError(f"the cache is not one of {self.n_kvh} key heads of {self.d_h} {self.in_dtype} on cuda:{self.device}")
+        return C.byref(cache.desc)
+
+    def _paged_workspace(self, B, max_pages):
+        """Address and size of the workspace.  One that is outgrown is kept: a captured graph may hold its address."""
+        need = self._paged_need.get((B, max_pages))
+        if need is None:
+            if len(self._paged_need) >= 4096:
+                self._paged_need.clear()
+            need = self._paged_need[(B, max_pages)] = int(self._L.pact_paged_workspace_bytes(self.handle, B, max_pages))
+        if not self._paged_ws or self._paged_ws[-1].numel() < need:
+            self._paged_ws.append(torch.empty(max(need, 2 * self._paged_ws[-1].numel() if self._paged_ws else 0), dtype=torch.uint8, device=self._cuda()))
+        return self._paged_ws[-1].data_ptr(), self._paged_ws[-1].numel()
+
+    def _cuda(self):
+        return torch.device("cuda", self.device)
+
+    def pact_cache_plan(self, page_rows, block_table, length, n_new, free_pages, n_free, length_out, n_free_out, row_start=None, slot=None,
+                        n_rows=None, row_stride=0, status=None):
+        """Pages and slots of the rows that come next (pact_cache_plan in pact.h).  block_table [B, max_pages], length, length_out [B], n_new [B] (may be a
+        strided view, such as the N_OUT column of the counters of a batch; negative: the request has ended), free_pages [n_pages], n_free, n_free_out
+        [1], row_start [B + 1], all int32; slot [n_rows] int64; n_rows: rows that the caller has room for, where slot is not given."""
+        i32 = torch.int32
+        if block_table.dim() != 2 or n_new.dim() != 1 or n_new.dtype != i32 or n_new.get_device() != self.device:
+            raise PactError("block_table is [B, max_pages], n_new an int32 [B] on the context's device")
+        B, W = block_table.shape
+        if n_new.shape[0] != B or free_pages.dim() != 1:
+            raise PactError("n_new is [B], free_pages [n_pages]")
+        if slot is not None:
+            if n_rows is not None and n_rows != slot.numel():
+                raise PactError("n_rows is the length of slot")
+            n_rows = slot.numel()
+        elif n_rows is None:
+            raise PactError("slot or n_rows is wanted")
+        _check(self.handle, self._L.pact_cache_plan(
+            self.handle, page_rows, free_pages.shape[0], B, W, self._on_device(block_table, i32, (B, W), "block_table"), self._on_device(length, i32, (B,), "length"),
+            n_new.data_ptr(), n_new.stride(0) if B > 1 else 1, self._on_device(free_pages, i32, free_pages.shape, "free_pages"),
+            self._on_device(n_free, i32, (1,), "n_free"), self._on_device(length_out, i32, (B,), "length_out"), self._on_device(n_free_out, i32, (1,), "n_free_out"),
+            self._on_device(row_start, i32, (B + 1,), "row_start"), self._on_device(slot, torch.int64, (n_rows,), "slot"), n_rows, row_stride,
+            self._on_device(status, i32, (1,), "status"), _stream()))
+
+    def pact_cache_write(self, cache: PagedCache, K_new, V_new, logw_new, slot, status=None):
+        """Rows K_new, V_new [n, n_kvh, d_h] (alike in their strides) and logw_new [n] fp32 (None: 0) into slot [n] int64."""
+        ref = self._cache(cache)
+        k, ld_row, ld_head = self._heads(K_new, self.in_dtype, self.n_kvh, "K_new")
+        v, v_row, v_head = self._heads(V_new, self.in_dtype, self.n_kvh, "V_new")
+        n = K_new.shape[0]
+        if V_new.shape[0] != n or (v_row, v_head) != (ld_row, ld_head):
+            raise PactError("K_new and V_new have the same shape and strides")
+        _check(self.handle, self._L.pact_cache_write(self.handle, ref, k, v, ld_row, ld_head, self._on_device(logw_new, torch.float32, (n,), "logw_new"),
+                                                     self._on_device(slot, torch.int64, (n,), "slot"), n, self._on_device(status, torch.int32, (1,), "status"), _stream()))
+
+    def pact_page_select(self, cache: PagedCache, Q, block_table, length, selected, n_first=1, n_last=1, scale=None, status=None):
+        """Places of the pages that each request's token attends to, into selected [B, n_kvh, n_select] int32.  Q [B, n_qh, d_h]; scale: 1 / sqrt(d_h) if not given."""
+        ref = self._cache(cache)
+        q, ldq, ldqh = self._heads(Q, self.in_dtype, self.n_qh, "Q")
+        B, W = block_table.shape
+        if Q.shape[0] != B or selected.dim() != 3:
+            raise PactError("Q is [B, n_qh, d_h], selected [B, n_kvh, n_select]")
+        n_select = selected.shape[2]
+        w, n = self._paged_workspace(B, W)
+        _check(self.handle, self._L.pact_page_select(
+            self.handle, ref, q, ldq, ldqh, B, self._on_device(block_table, torch.int32, (B, W), "block_table"), W, self._on_device(length, torch.int32, (B,), "length"),
+            self.d_h ** -0.5 if scale is None else scale, n_first, n_last, n_select, self._on_device(selected, torch.int32, (B, self.n_kvh, n_select), "selected"),
+            self._on_device(status, torch.int32, (1,), "status"), w, n, _stream()))
+
+    def pact_paged_attention(self, cache: PagedCache, Q, block_table, length, out, lse=None, selected=None, scale=None, status=None):
+        """Attention of one token per request, Q [B, n_qh, d_h] -> out [B, n_qh, d_h] (the context's output type), lse [B, n_qh] fp32, over the cached rows or
+        those of the pages in selected [B, n_kvh, n_select]; scale: 1 / sqrt(d_h) if not given."""
+        ref = self._cache(cache)
+        q, ldq, ldqh = self._heads(Q, self.in_dtype, self.n_qh, "Q")
+        o, ldo, ldoh = self._heads(out, self.out_dtype, self.n_qh, "out")
+        B, W = block_table.shape
+        if Q.shape[0] != B or out.shape[0] != B:
+            raise PactError("Q and out are [B, n_qh, d_h]")
+        n_select = 0
+        if selected is not None:
+            if selected.dim() != 3:
+                raise PactError("selected is [B, n_kvh, n_select]")
+            n_select = selected.shape[2]
+            selected = self._on_device(selected, torch.int32, (B, self.n_kvh, n_select), "selected")
+        w, n = self._paged_workspace(1, 1)
+        _check(self.handle, self._L.pact_paged_attention(
+            self.handle, ref, q, ldq, ldqh, B, self._on_device(block_table, torch.int32, (B, W), "block_table"), W, self._on_device(length, torch.int32, (B,), "length"),
+            selected, n_select, self.d_h ** -0.5 if scale is None else scale, o, ldo, ldoh, self._on_device(lse, torch.float32, (B, self.n_qh), "lse"),
+            self._on_device(status, torch.int32, (1,), "status"), w, n, _stream()))
 
     def set_wait_limits(self, barrier_polls: int = 0, center_sweeps: int = 0):
         """Bounds of the device-side waits (0 = default); see pact_set_wait_limits in pact.h."""

@@ -1,37 +1,12 @@
 // Host side of the C ABI: argument checks, workspace layout, launch sequences.
 #include <math.h>
-#include <stdio.h>
 #include <string.h>
 
-#include <atomic>
 #include <new>
 
-#include "kernels.cuh"
+#include "context.h"
 
 using namespace pact;
-
-constexpr int kProfStages = 9;
-
-struct pact_ctx {
-  int d, n_qh, n_kvh, d_h, d_k, n_qcols;
-  pact_dtype in, out;
-  int elt;                 // bytes per input element
-  DeviceCfg dev;           // of the device the context was created on
-  bool umma;               // bf16 keys of a width the tcgen05 tile kernels take
-  int device;
-  char err[256];
-  long long launches;      // kernels launched by this context so far
-  int spin_limit;          // polls the barrier of the member-list kernel makes before it raises PACT_ERR_TIMEOUT
-  int sweep_limit;         // sweeps the centre selection makes before it raises PACT_ERR_TIMEOUT
-  int prof_on;             // record an event after every stage of pact_reduce
-  int prof_n;              // stages recorded by the last profiled call
-  cudaEvent_t ev[kProfStages + 1];
-  // pact_reduce_host: a stream for the copies in, used by one call at a time (another thread's call does without)
-  std::atomic_flag feed_busy = ATOMIC_FLAG_INIT;
-  bool fed_before = false;                             // there has been a call large enough for it
-  cudaStream_t feed_stream = nullptr;
-  cudaEvent_t feed_start = nullptr, feed_keys = nullptr, feed_part[kFeedParts] = {};
-};
 
 struct pact_graph {
   pact_ctx *ctx;
@@ -103,18 +78,6 @@ size_t carve_image(const pact_ctx *c, int N, char *base, ImgDesc *im) {
   return cv.off;
 }
 
-pact_status fail_cuda(pact_ctx *c, cudaError_t e, const char *where) {
-  snprintf(c->err, sizeof(c->err), "%s: %s", where, cudaGetErrorString(e));
-  return PACT_ERR_CUDA;
-}
-
-#define CK(call)                                                     \
-  do {                                                               \
-    cudaError_t e_ = (call);                                         \
-    if (e_ != cudaSuccess) return fail_cuda(ctx, e_, #call);         \
-  } while (0)
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool ld_ok(const pact_ctx *c, int64_t ld, int width) {
   return ld >= width && ((size_t)ld * c->elt) % 16 == 0;
 }
@@ -219,6 +182,7 @@ const char *pact_status_string(pact_status s) {
     case PACT_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
     case PACT_ERR_CUDA: return "CUDA runtime error";
     case PACT_ERR_TIMEOUT: return "a bounded device wait ran out";
+    case PACT_ERR_NO_PAGES: return "fewer free pages than the new rows need";
   }
   return "unknown status";
 }
@@ -259,6 +223,12 @@ pact_status pact_create(pact_ctx **out, int d, int n_qh, int n_kvh, int d_h, pac
     return PACT_ERR_CUDA;
   }
   c->umma = in == PACT_BF16 && umma_supported(c->d_k);
+  e = paged_configure(&c->paged, c->dev, n_qh, n_kvh, d_h, in == PACT_BF16);
+  if (e != cudaSuccess) {
+    fail_cuda(ctx, e, "pact_create");
+    delete c;
+    return PACT_ERR_CUDA;
+  }
   c->spin_limit = kSpinLimit;
   c->sweep_limit = kSpinLimit;
   *out = c;

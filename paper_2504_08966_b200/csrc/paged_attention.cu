@@ -1,0 +1,848 @@
+// Attention of one new token per request over a paged cache (pact_paged_attention): Eq. 11 of the paper for the tokens that follow.
+//
+//   s_p = scale q.k_p + logw_p,   out = sum_p exp(s_p - m) v_p / sum_p exp(s_p - m),   m = max_p s_p
+//
+// Keys and values are read once and each is used by the few query heads of its key head, so HBM bounds it: 4 d_h bytes per row and key
+// head in bf16 against 4 d_h g operations for g query heads.
+//
+// Split.  The rows of all requests and key heads, in tiles of 64, form one line of T tiles that G CTAs share out evenly: CTA i takes tiles
+// [i T / G, (i + 1) T / G).  No length, batch or number of heads leaves SMs idle, at most G - 1 cuts are made in all, and k_attend_join puts
+// the parts of what was cut together.  The shares follow from prefix sums over the lengths, which every CTA forms itself: lengths are known on
+// the device only.
+//
+// Pipeline.  One warp copies: each lane works out page ids and row counts of one tile, 32 tiles at a time, and tiles arrive as boxes of
+// 128-byte columns through the tensor-copy unit (swizzled, so that ldmatrix meets no bank conflicts) in a ring that runs on across requests.
+// Four warps compute; each has 16 rows of every tile and its own running maximum, sum and output, so they meet only at the end of a request.
+//
+// bf16: logits as K (16 rows x 16) by q^T (16 x 8 heads) on mma.sync, so that eight heads are one operand; the output as V^T (16 columns x 16 rows)
+// by P^T (16 rows x 8 heads), also without padding.  tcgen05 would want 64 or 128 rows per instruction and its results through tensor memory,
+// where HBM delivers a tile every 1400 clocks of an SM and the warps need less.  Probabilities go in as two bf16 terms (p = hi + lo to
+// 2^-17): one term would put an error of 2^-9 on every product, as large as the rounding of a bf16 result and far above that of an fp32 one.
+// fp32: fused multiply-adds; for the logits a lane has one row and half of the columns, for the output four columns of all rows.
+#include "paged.cuh"
+#include "umma.cuh"
+
+namespace pact {
+namespace {
+
+constexpr int kTile = 64;                  // rows of a tile
+constexpr int kRowsOfWarp = 16;
+constexpr int kConsumers = 4;              // computing warps
+constexpr int kAttendThreads = (kConsumers + 1) * 32;
+constexpr int kMaxAttendStages = 8;
+constexpr int kBoxBytes = 128;             // columns of a box
+constexpr int kBlockBytes = kTile * kBoxBytes;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kScratch = kRowsOfWarp * 8 + 8;   // fp32: floats of a warp for probabilities and factors
+
+// Offsets in dynamic shared memory (the ring comes first: swizzled boxes lie at multiples of 1024 bytes).
+struct AttendSmem {
+  int stage;                               // bytes of K and V of a stage
+  int bias, q, q_row, q_own, slots, ml, meta, bars, pre, total;
+};
+__host__ __device__ inline AttendSmem attend_smem(int stages, int blocks, int heads, int elt, int B) {
+  AttendSmem m;
+  m.stage = 2 * blocks * kBlockBytes;
+  m.bias = stages * m.stage;
+  m.q = m.bias + stages * kTile * 4;
+  m.q_row = blocks * kBoxBytes + 16;       // (16 bytes more: rows of different heads begin in different banks)
+  m.q_own = m.q + stages * heads * m.q_row;
+  m.slots = m.q_own + (elt == 4 ? heads * m.q_row : 0);
+  m.ml = m.slots + 2 * heads * (blocks * kBoxBytes / elt + 4) * 4;
+  m.bars = m.ml + kConsumers * heads * 8;
+  m.meta = m.bars + (2 * stages + 1) * 8;
+  m.pre = m.meta + stages * 4;
+  m.total = m.pre + (B + 1 + kAttendThreads / 32) * 4;
+  return m;
+}
+
+__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y, int z, int w) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ float4 lds4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float fma4(const float4 &x, const float4 &y, float s) { return fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s)))); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+__device__ __forceinline__ void consumers_meet() { asm volatile("bar.sync 1, %0;" ::"n"(kConsumers * 32) : "memory"); }
+
+// One warp's part of a request and key head: running maximum (of the logits times log2 e), sum and output of its rows.
+template <typename T, int NB, int NT> struct Part;
+
+template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
+  static constexpr int kHeads = 8 * NT, kCols = NB * 64;
+  uint32_t q[NB * 4][NT][2];               // q^T: columns 16 k + 2 (lane % 4) + {0, 1} (+ 8), head lane / 4
+  float m[NT][2], l[NT][2];                // heads 2 (lane % 4) + {0, 1}; the sums are of this lane's rows
+  float o[NB * 4][NT][4];                  // columns 16 c + lane / 4 (+ 8 in the upper two), the same heads
+
+  __device__ __forceinline__ void begin(const char *sq, int q_row, char *, int lane, int) {
+#pragma unroll
+    for (int k = 0; k < NB * 4; ++k)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          q[k][n][i] = *reinterpret_cast<const uint32_t *>(sq + (n * 8 + lane / 4) * q_row + (k * 16 + i * 8 + (lane % 4) * 2) * 2);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NB * 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[c][n][i] = 0.f;
+    }
+  }
+
+  // rows [row0, row0 + 16) of the tile, of which the first `rows` count
+  __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, const float *bias, bool has_bias, int row0, int rows, float scale, int lane, float *) {
+    float s[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
+    {
+      const int r = row0 + (lane & 15), x = r & 7;
+      const uint32_t at = sk + r * kBoxBytes;
+#pragma unroll
+      for (int k = 0; k < NB * 4; ++k) {
+        uint32_t a[4];
+        ldsm4(a, at + (k / 4) * kBlockBytes + ((((k % 4) * 2 + (lane >> 4)) ^ x) << 4));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma_bf16(s[n], a, q[k][n][0], q[k][n][1]);
+      }
+    }
+    const int r0 = lane / 4, r1 = r0 + 8;
+    float b0 = 0.f, b1 = 0.f;
+    if (has_bias) {
+      b0 = bias[row0 + r0];
+      b1 = bias[row0 + r1];
+    }
+    const bool in0 = r0 < rows && b0 != -INFINITY, in1 = r1 < rows && b1 != -INFINITY;
+    b0 *= kLog2e;
+    b1 *= kLog2e;
+    float top[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        s[n][i] = in0 ? fmaf(s[n][i], scale, b0) : -INFINITY;
+        s[n][2 + i] = in1 ? fmaf(s[n][2 + i], scale, b1) : -INFINITY;
+        top[n][i] = fmaxf(s[n][i], s[n][2 + i]);
+      }
+#pragma unroll
+    for (int w = 4; w < 32; w <<= 1)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) top[n][i] = fmaxf(top[n][i], __shfl_xor_sync(0xffffffffu, top[n][i], w));
+    bool grows = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) grows = grows || top[n][i] > m[n][i];
+    if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float to = fmaxf(m[n][i], top[n][i]), f = m[n][i] == to ? 1.f : ex2_approx(m[n][i] - to);   // (m - to is NaN where both are infinite)
+          m[n][i] = to;
+          l[n][i] *= f;
+#pragma unroll
+          for (int c = 0; c < NB * 4; ++c) {
+            o[c][n][i] *= f;
+            o[c][n][2 + i] *= f;
+          }
+        }
+    }
+    uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = ex2_approx(s[n][i] - (m[n][i & 1] == -INFINITY ? 0.f : m[n][i & 1]));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) l[n][i] += p[i] + p[2 + i];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t h = pack_bf16(p[2 * i], p[2 * i + 1]);
+        hi[n][i] = transpose8(h);
+        lo[n][i] = transpose8(pack_bf16(p[2 * i] - __uint_as_float(h << 16), p[2 * i + 1] - __uint_as_float(h & 0xFFFF0000u)));
+      }
+    }
+    // values of rows that do not count are cleared: zero times an infinity or a NaN would not be zero
+    uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
+    const uint32_t rows0 = __ballot_sync(0xffffffffu, in0), rows1 = __ballot_sync(0xffffffffu, in1);
+    const bool clear = (rows0 & rows1) != 0xffffffffu;
+    if (clear) {                               // lane 4 r speaks for row r; this lane's registers hold rows 2 (lane % 4) + {0, 1} (+ 8)
+      const int r = (lane % 4) * 8;
+      keep0 = ((rows0 >> r) & 1 ? 0xFFFFu : 0u) | ((rows0 >> (r + 4)) & 1 ? 0xFFFF0000u : 0u);
+      keep1 = ((rows1 >> r) & 1 ? 0xFFFFu : 0u) | ((rows1 >> (r + 4)) & 1 ? 0xFFFF0000u : 0u);
+    }
+    {
+      const int r = row0 + (lane & 7) + (lane >> 4) * 8, x = r & 7;
+      const uint32_t at = sv + r * kBoxBytes;
+#pragma unroll
+      for (int c = 0; c < NB * 4; ++c) {
+        uint32_t a[4];
+        ldsm4_t(a, at + (c / 4) * kBlockBytes + ((((c % 4) * 2 + ((lane >> 3) & 1)) ^ x) << 4));
+        if (clear) {
+          a[0] &= keep0;
+          a[1] &= keep0;
+          a[2] &= keep1;
+          a[3] &= keep1;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          mma_bf16(o[c][n], a, hi[n][0], hi[n][1]);
+          mma_bf16(o[c][n], a, lo[n][0], lo[n][1]);
+        }
+      }
+    }
+  }
+
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int w = 4; w < 32; w <<= 1)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], w);
+  }
+  // f(head, m, l), once for every head
+  template <typename F> __device__ __forceinline__ void each_head(int lane, F f) {
+    if (lane < 4)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) f(n * 8 + lane * 2 + i, m[n][i], l[n][i]);
+  }
+  // x = f(head, m), then g(x, o, head, column) for every element of o of this lane
+  template <typename F, typename G> __device__ __forceinline__ void each(int lane, F f, G g) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int head = n * 8 + (lane % 4) * 2 + i;
+        const auto x = f(head, m[n][i]);
+#pragma unroll
+        for (int c = 0; c < NB * 4; ++c) {
+          g(x, o[c][n][i], head, c * 16 + lane / 4);
+          g(x, o[c][n][2 + i], head, c * 16 + lane / 4 + 8);
+        }
+      }
+  }
+};
+
+template <int NB> struct Part<float, NB, 1> {
+  static constexpr int kHeads = 8, kCols = NB * 32;
+  static constexpr int kChunks = NB * 8;                       // 16-byte columns of a row
+  static constexpr int kGroups = kChunks <= 8 ? 4 : kChunks <= 16 ? 2 : 1;   // groups of lanes that share out the rows for the output
+  static constexpr int kGroupLanes = 32 / kGroups;
+  uint32_t q;                              // in shared memory
+  int q_row;
+  float m[4], l[4];                        // heads 4 (lane / 16) + {0 .. 3}; the sums are of this lane's row
+  float o[8][4];                           // columns 4 (lane % kGroupLanes) + {0 .. 3}, rows of the lane's group
+
+  // q is read in every step, and the copying warp may be ahead by now with the next request's in the same stage: the warps make a copy.
+  // (The barrier also parts the probabilities to come, which lie in the slots, from reads of the slots at the end of the request before.)
+  __device__ __forceinline__ void begin(const char *sq, int row, char *own, int, int tid) {
+    for (int i = tid * 16; i < kHeads * row; i += kConsumers * 32 * 16) *reinterpret_cast<uint4 *>(own + i) = *reinterpret_cast<const uint4 *>(sq + i);
+    consumers_meet();
+    q = smem_u32(own);
+    q_row = row;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+    }
+#pragma unroll
+    for (int h = 0; h < 8; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[h][i] = 0.f;
+  }
+
+  // scratch: 16 rows x 8 heads of probabilities and 8 factors, this warp's
+  __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, const float *bias, bool has_bias, int row0, int rows, float scale, int lane, float *scratch) {
+    const int r = lane & 15, half = lane >> 4, row = row0 + r, x = row & 7;
+    float s[8];
+#pragma unroll
+    for (int h = 0; h < 8; ++h) s[h] = 0.f;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int c = 2 * i + half;
+        const float4 k = lds4(sk + nb * kBlockBytes + row * kBoxBytes + ((c ^ x) << 4));
+#pragma unroll
+        for (int h = 0; h < 8; ++h) s[h] = fma4(k, lds4(q + h * q_row + nb * kBoxBytes + c * 16), s[h]);
+      }
+    float b = has_bias ? bias[row] : 0.f;
+    const bool in = r < rows && b != -INFINITY;
+    b *= kLog2e;
+    float t[4], top[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {             // both halves of the columns; a lane goes on with four heads
+      const float give = half ? s[i] : s[4 + i], got = __shfl_xor_sync(0xffffffffu, give, 16);
+      t[i] = in ? fmaf((half ? s[4 + i] : s[i]) + got, scale, b) : -INFINITY;
+      top[i] = t[i];
+    }
+#pragma unroll
+    for (int w = 1; w < 16; w <<= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], w));
+    bool grows = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) grows = grows || top[i] > m[i];
+    const bool rescale = __any_sync(0xffffffffu, grows);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (rescale) {
+        const float to = fmaxf(m[i], top[i]), f = m[i] == to ? 1.f : ex2_approx(m[i] - to);
+        m[i] = to;
+        l[i] *= f;
+        if (r == 0) scratch[kRowsOfWarp * 8 + half * 4 + i] = f;
+      }
+      t[i] = ex2_approx(t[i] - (m[i] == -INFINITY ? 0.f : m[i]));
+      l[i] += t[i];
+    }
+    *reinterpret_cast<float4 *>(scratch + r * 8 + half * 4) = make_float4(t[0], t[1], t[2], t[3]);
+    const uint32_t live = __ballot_sync(0xffffffffu, in) & 0xffffu;
+    __syncwarp();
+    if (rescale) {
+#pragma unroll
+      for (int h = 0; h < 8; ++h) {
+        const float f = scratch[kRowsOfWarp * 8 + h];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[h][i] *= f;
+      }
+    }
+    const int c = lane % kGroupLanes;
+    if (c < kChunks) {
+#pragma unroll 4
+      for (int k = lane / kGroupLanes; k < kRowsOfWarp; k += kGroups) {
+        if (!(live >> k & 1)) continue;       // zero times an infinity or a NaN would not be zero
+        const int vr = row0 + k;
+        const float4 v = lds4(sv + (c / 8) * kBlockBytes + vr * kBoxBytes + (((c % 8) ^ (vr & 7)) << 4));
+        const float4 p0 = *reinterpret_cast<const float4 *>(scratch + k * 8), p1 = *reinterpret_cast<const float4 *>(scratch + k * 8 + 4);
+        const float p[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+          o[h][0] = fmaf(p[h], v.x, o[h][0]);
+          o[h][1] = fmaf(p[h], v.y, o[h][1]);
+          o[h][2] = fmaf(p[h], v.z, o[h][2]);
+          o[h][3] = fmaf(p[h], v.w, o[h][3]);
+        }
+      }
+    }
+    __syncwarp();
+  }
+
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int w = 1; w < 16; w <<= 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
+#pragma unroll
+    for (int w = kGroupLanes; w < 32; w <<= 1)
+#pragma unroll
+      for (int h = 0; h < 8; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[h][i] += __shfl_xor_sync(0xffffffffu, o[h][i], w);
+  }
+  template <typename F> __device__ __forceinline__ void each_head(int lane, F f) {
+    if ((lane & 15) == 0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f((lane >> 4) * 4 + i, m[i], l[i]);
+  }
+  template <typename F, typename G> __device__ __forceinline__ void each(int lane, F f, G g) {
+    float mh[8];
+#pragma unroll
+    for (int h = 0; h < 8; ++h) mh[h] = __shfl_sync(0xffffffffu, m[h & 3], (h >> 2) * 16);
+    if (lane < kGroupLanes && lane < kChunks)
+#pragma unroll
+      for (int h = 0; h < 8; ++h) {
+        const auto x = f(h, mh[h]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g(x, o[h][i], h, lane * 4 + i);
+      }
+  }
+};
+
+// how much a sum with maximum m counts beside one with maximum `to`
+__device__ __forceinline__ float weight(float m, float to) { return m == -INFINITY ? 0.f : m == to ? 1.f : ex2_approx(m - to); }
+
+__device__ __forceinline__ void store4(const AttendArgs &a, int b, int head, int c, const float4 &v) {
+  const long long at = b * a.ldO + head * a.ldOh + c;
+  if (a.out_bf16) *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.out) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+  else *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = v;
+}
+
+constexpr int attend_ctas(int blocks, int tiles_of_heads) { return blocks <= 2 && tiles_of_heads == 1 ? 2 : 1; }   // of an SM
+
+template <typename T, int NB, int NT>
+__global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
+    k_attend(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendArgs a) {
+  using P = Part<T, NB, NT>;
+  extern __shared__ __align__(1024) char sm[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const AttendSmem at = attend_smem(a.stages, NB, P::kHeads, sizeof(T), a.B);
+  uint64_t *full = reinterpret_cast<uint64_t *>(sm + at.bars), *empty = full + a.stages;
+  int *abort = reinterpret_cast<int *>(empty + a.stages);
+  uint32_t *meta = reinterpret_cast<uint32_t *>(sm + at.meta);
+  int *pre = reinterpret_cast<int *>(sm + at.pre), *w_sum = pre + a.B + 1;
+  if (tid < a.stages) {
+    mbar_init(full + tid, 1);
+    mbar_init(empty + tid, kConsumers);
+  }
+  if (tid == 0) *abort = 0;
+  // columns past d_h and heads past the last are zero in q (of K and V the copies fill them in)
+  for (int i = tid * 16; i < at.q_own - at.q; i += kAttendThreads * 16) *reinterpret_cast<uint4 *>(sm + at.q + i) = make_uint4(0, 0, 0, 0);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+
+  pdl_wait();
+  pdl_trigger();
+  // tiles before each request, of one key head
+  const long long room = (long long)a.width * a.page;
+  const auto rows_of = [&](int b) {
+    const int len = a.length[b];
+    return len < 0 ? 0 : len > room ? (int)room : len;
+  };
+  const auto tiles_of = [&](int b) {
+    const unsigned rows = (unsigned)rows_of(b);
+    if (!a.selected) return (int)((rows + kTile - 1u) / kTile);
+    const long long pages = min((long long)a.n_select, (long long)((rows + (unsigned)a.page - 1u) / (unsigned)a.page));
+    return (int)((pages * a.page + kTile - 1) / kTile);
+  };
+  const int Hn = a.n_kvh * a.head_tiles;
+  {
+    const int per = (a.B + kAttendThreads - 1) / kAttendThreads, b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
+    int mine = 0;
+    for (int b = b0; b < b1; ++b) {
+      mine += tiles_of(b);
+      if (blockIdx.x == 0 && a.status && (a.length[b] < 0 || a.length[b] > room)) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
+    }
+    int x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) w_sum[warp] = x;
+    __syncthreads();
+    int sum = x - mine;
+    for (int w = 0; w < warp; ++w) sum += w_sum[w];
+    for (int b = b0; b < b1; ++b) {
+      pre[b] = sum;
+      sum += tiles_of(b);
+    }
+    if (b0 < a.B && b1 == a.B) pre[a.B] = sum;
+    __syncthreads();
+  }
+  const long long T_all = (long long)pre[a.B] * Hn;
+  const long long G = min((long long)gridDim.x, T_all);
+  const long long me = blockIdx.x;
+  const long long t0 = me < G ? me * T_all / G : T_all, t1 = me < G ? (me + 1) * T_all / G : T_all;
+  // requests without any row
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x)
+    if (pre[b + 1] == pre[b]) {
+      for (int i = tid * 4; i < a.n_kvh * a.group * a.d_h; i += kAttendThreads * 4) store4(a, b, i / a.d_h, i % a.d_h, make_float4(0.f, 0.f, 0.f, 0.f));
+      if (a.lse)
+        for (int i = tid; i < a.n_kvh * a.group; i += kAttendThreads) a.lse[(long long)b * a.n_kvh * a.group + i] = -INFINITY;
+    }
+  // where tile t lies: request, key head and head tile, place
+  const auto find = [&](long long t, int &b, int &h, int &j) {
+    int lo = 0, hi = a.B;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if ((long long)pre[mid] * Hn <= t) lo = mid;
+      else hi = mid;
+    }
+    b = lo;
+    const long long u = t - (long long)pre[lo] * Hn;
+    const int n = pre[lo + 1] - pre[lo];
+    h = (int)(u / n);
+    j = (int)(u - (long long)h * n);
+  };
+
+  if (t0 == t1) {
+    if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+  } else if (warp == kConsumers) {
+    // ---- the copying warp ----
+    int st = 0;
+    uint32_t ph = 0;
+    bool given_up = false;
+    const int boxes = kTile / a.box_rows, per_box = a.box_rows / kRowsOfWarp, copies = 2 * NB + (a.logw ? 1 : 0);
+    for (long long base = t0; base < t1 && !given_up; base += 32) {
+      const int n = (int)min(32ll, t1 - base);
+      int b = 0, h = 0, j = 0, id[4] = {-1, -1, -1, -1}, off[4] = {0, 0, 0, 0};   // page and place of every 16 rows
+      uint32_t rows = 0;                                       // rows that count of every 16, a byte each
+      if (lane < n) {
+        find(base + lane, b, h, j);
+        const int len = rows_of(b), kv = h / a.head_tiles;
+        const int pages = (int)(((unsigned)len + (unsigned)a.page - 1u) / (unsigned)a.page), listed = a.selected ? min(a.n_select, pages) : pages;
+        long long left = 0;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          if (g % per_box == 0) {                              // a box lies in one page
+            const long long r = (long long)j * kTile + g * kRowsOfWarp;
+            int place = (int)(r / a.page);
+            off[g] = (int)(r - (long long)place * a.page);
+            if (place >= listed) place = -1;
+            else if (a.selected) place = a.selected[((long long)b * a.n_kvh + kv) * a.n_select + place];
+            left = place < 0 || place >= pages ? 0 : len - ((long long)place * a.page + off[g]);
+            if (left > 0) {
+              id[g] = a.table[(long long)b * a.width + place];
+              if (id[g] < 0 || id[g] >= a.n_pages) {
+                left = 0;
+                if (a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
+              }
+            }
+          } else {
+            left -= kRowsOfWarp;
+          }
+          if (left > 0) rows |= (uint32_t)min(left, (long long)kRowsOfWarp) << (8 * g);
+        }
+      }
+      for (int i = 0; i < n; ++i) {
+        const uint32_t rows_i = __shfl_sync(0xffffffffu, rows, i);
+        const int bi = __shfl_sync(0xffffffffu, b, i), hi = __shfl_sync(0xffffffffu, h, i), ji = __shfl_sync(0xffffffffu, j, i);
+        const int kv = hi / a.head_tiles, ht = hi - kv * a.head_tiles;
+        const bool first = base + i == t0 || ji == 0;
+        const int heads = min(P::kHeads, a.group - ht * P::kHeads);
+        uint32_t load = 0;                                     // a box is copied if any of its rows counts: its first 16 do then
+        for (int x = 0; x < boxes; ++x)
+          if (rows_i >> (8 * x * per_box) & 0xffu) load |= 1u << x;
+        if (!mbar_wait_warp(empty + st, ph ^ 1)) {
+          given_up = true;
+          if (lane == 0) {
+            atomicExch(abort, 1);
+            if (a.status) atomicMin(a.status, (int)PACT_ERR_TIMEOUT);
+          }
+          break;
+        }
+        if (lane == 0) {
+          meta[st] = rows_i;
+          mbar_arrive_expect_tx(full + st, (uint32_t)(__popc(load) * a.box_rows * (2 * NB * kBoxBytes + (a.logw ? 4 : 0)) + (first ? heads * a.d_h * (int)sizeof(T) : 0)));
+        }
+        __syncwarp();
+        char *stage = sm + st * at.stage;
+        for (int c = lane; c < ((boxes * copies + 31) & ~31); c += 32) {
+          const int x = min(c / copies, boxes - 1), k = c - x * copies, g = x * per_box;
+          int page = 0, row = 0;
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {                        // (each lane wants another register of lane i)
+            const int p = __shfl_sync(0xffffffffu, id[y], i), o = __shfl_sync(0xffffffffu, off[y], i);
+            if (y == g) {
+              page = p;
+              row = o;
+            }
+          }
+          if (k < copies && (load >> x & 1)) {
+            if (k < 2 * NB) {
+              char *to = stage + k * kBlockBytes + x * a.box_rows * kBoxBytes;
+              tma_load_4d(to, k < NB ? &map_k : &map_v, full + st, (k < NB ? k : k - NB) * (kBoxBytes / (int)sizeof(T)), row, kv, page);
+            } else {
+              bulk_load(sm + at.bias + (st * kTile + x * a.box_rows) * 4, a.logw + (long long)page * a.page + row, a.box_rows * 4, full + st);
+            }
+          }
+        }
+        if (first && lane < heads) {
+          const T *q = static_cast<const T *>(a.Q) + bi * a.ldQ + (long long)(kv * a.group + ht * P::kHeads + lane) * a.ldQh;
+          bulk_load(sm + at.q + (st * P::kHeads + lane) * at.q_row, q, a.d_h * (int)sizeof(T), full + st);
+        }
+        __syncwarp();
+        if (++st == a.stages) {
+          st = 0;
+          ph ^= 1;
+        }
+      }
+    }
+  } else {
+    // ---- the computing warps ----
+    P part;
+    int st = 0;
+    uint32_t ph = 0;
+    int b, h, j;
+    find(t0, b, h, j);
+    if (tid == 0) {                                            // what the CTAs before this one have of the request at t0
+      int4 d = make_int4(0, 0, 0, 0);
+      if (j > 0) {
+        const long long ts = t0 - j, te = ts + (pre[b + 1] - pre[b]);
+        const long long i0 = ((ts + 1) * G - 1) / T_all, i1 = (te * G - 1) / T_all;
+        if (i0 == me - 1) d = make_int4(ts == i0 * T_all / G ? 1 : 2, (int)i1, b, h);
+      }
+      a.desc[blockIdx.x] = d;
+    }
+    float *slots = reinterpret_cast<float *>(sm + at.slots);
+    float2 *ml = reinterpret_cast<float2 *>(sm + at.ml);
+    constexpr int kRow = P::kCols + 4, kSlot = P::kHeads * kRow;
+    static_assert(sizeof(T) == 2 || 2 * kSlot >= kConsumers * kScratch, "the probabilities lie in the slots, which are free between ends");
+    bool ok = true;
+    for (long long t = t0; t < t1;) {
+      const int n = pre[b + 1] - pre[b], j1 = (int)min((long long)n, j + (t1 - t));
+      for (int i = j; i < j1; ++i) {
+        if (ok && !mbar_wait_warp_unless(abort, full + st, ph)) {
+          ok = false;
+          if (lane == 0) {
+            atomicExch(abort, 1);
+            if (a.status) atomicMin(a.status, (int)PACT_ERR_TIMEOUT);
+          }
+        }
+        if (i == j) part.begin(sm + at.q + st * P::kHeads * at.q_row, at.q_row, sm + at.q_own, lane, tid);
+        const int rows = (int)(meta[st] >> (8 * warp) & 0xffu);
+        if (rows > 0 && ok) {
+          const uint32_t sk = smem_u32(sm + st * at.stage);
+          part.step(sk, sk + NB * kBlockBytes, reinterpret_cast<const float *>(sm + at.bias) + st * kTile, a.logw != nullptr, warp * kRowsOfWarp, rows, a.scale_log2,
+                    lane, slots + warp * kScratch);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty + st);
+        if (++st == a.stages) {
+          st = 0;
+          ph ^= 1;
+        }
+      }
+      // ---- the four warps' parts, two and two ----
+      part.finish();
+      consumers_meet();                                        // (the slots of the request before have been read)
+      if (warp >= 2) {
+        float *slot = slots + (warp - 2) * kSlot;
+        part.each(lane, [](int, float) { return 0; }, [&](int, float o, int head, int c) { slot[head * kRow + c] = o; });
+      }
+      part.each_head(lane, [&](int head, float m, float l) { ml[warp * P::kHeads + head] = make_float2(m, l); });
+      consumers_meet();
+      if (warp < 2) {
+        float *slot = slots + warp * kSlot;
+        part.each(
+            lane,
+            [&](int head, float m) {
+              const float mo = ml[(warp + 2) * P::kHeads + head].x, to = fmaxf(m, mo);
+              return make_float2(weight(m, to), weight(mo, to));
+            },
+            [&](float2 f, float o, int head, int c) {
+              float &s = slot[head * kRow + c];
+              s = o * f.x + s * f.y;
+            });
+        part.each_head(lane, [&](int head, float m, float l) {
+          const float2 other = ml[(warp + 2) * P::kHeads + head];
+          const float to = fmaxf(m, other.x);
+          ml[warp * P::kHeads + head] = make_float2(to, l * weight(m, to) + other.y * weight(other.x, to));
+        });
+      }
+      consumers_meet();
+      const int kv = h / a.head_tiles, ht = h - kv * a.head_tiles, heads = min(P::kHeads, a.group - ht * P::kHeads);
+      const bool whole = j == 0 && j1 == n;
+      const long long slot_out = 2 * me + (t == t0 ? 0 : 1);
+      for (int i = tid; i < heads * (P::kCols / 4); i += kConsumers * 32) {
+        const int hd = i / (P::kCols / 4), c = (i - hd * (P::kCols / 4)) * 4;
+        const float2 x = ml[hd], y = ml[P::kHeads + hd];
+        const float to = fmaxf(x.x, y.x), fx = weight(x.x, to), fy = weight(y.x, to), l = x.y * fx + y.y * fy;
+        const float4 u = *reinterpret_cast<const float4 *>(slots + hd * kRow + c), v = *reinterpret_cast<const float4 *>(slots + kSlot + hd * kRow + c);
+        const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+        const float4 o = make_float4((u.x * fx + v.x * fy) * inv, (u.y * fx + v.y * fy) * inv, (u.z * fx + v.z * fy) * inv, (u.w * fx + v.w * fy) * inv);
+        if (whole) {
+          const int head = kv * a.group + ht * P::kHeads + hd;
+          if (c < a.d_h) store4(a, b, head, c, o);
+          if (c == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : (to + log2f(l)) * kLn2;
+        } else {
+          *reinterpret_cast<float4 *>(a.part_o + (slot_out * P::kHeads + hd) * P::kCols + c) = o;
+          if (c == 0) a.part_ml[slot_out * P::kHeads + hd] = make_float2(to, l);
+        }
+      }
+      t += j1 - j;
+      j = 0;
+      if (++h == Hn) {
+        h = 0;
+        do ++b;
+        while (b < a.B && pre[b + 1] == pre[b]);
+      }
+    }
+  }
+  __syncthreads();
+  if (*abort) land_copies(full, a.stages);
+}
+
+// Parts of the request and key head that was cut at the beginning of CTA blockIdx.x's share and not before it; one head per CTA.
+constexpr int kJoinThreads = 256;
+constexpr int kMaxParts = 1024;
+
+__global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_constant__ AttendArgs a, int tile_heads, int cols) {
+  __shared__ float s_w[kMaxParts], s_l[kMaxParts], s_red[kJoinThreads / 32];
+  __shared__ float4 s_o[kJoinThreads];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, hd = blockIdx.y;
+  pdl_wait();
+  pdl_trigger();
+  const int4 d = a.desc[blockIdx.x];
+  if (!d.x) return;
+  const int i0 = blockIdx.x - 1, n = d.y - i0 + 1, b = d.z, kv = d.w / a.head_tiles, ht = d.w - kv * a.head_tiles;
+  if (ht * tile_heads + hd >= a.group) return;
+  const auto slot = [&](int p) { return 2 * (long long)(i0 + p) + (p == 0 ? d.x - 1 : 0); };
+  float top = -INFINITY;
+  for (int p = tid; p < n; p += kJoinThreads) {
+    const float2 x = a.part_ml[slot(p) * tile_heads + hd];
+    s_w[p] = x.x;
+    s_l[p] = x.y;
+    top = fmaxf(top, x.x);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 0) s_red[warp] = top;
+  __syncthreads();
+  for (int w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, s_red[w]);
+  __syncthreads();
+  float l = 0.f;
+  for (int p = tid; p < n; p += kJoinThreads) {
+    const float f = weight(s_w[p], top);
+    l += s_l[p] * f;
+    s_w[p] = f;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  if (lane == 0) s_red[warp] = l;
+  __syncthreads();
+  l = 0.f;
+  for (int w = 0; w < kJoinThreads / 32; ++w) l += s_red[w];
+  const int quads = cols / 4, groups = kJoinThreads / quads, c = tid % quads, g = tid / quads;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (g < groups) {
+#pragma unroll 4
+    for (int p = g; p < n; p += groups) {
+      const float4 x = *reinterpret_cast<const float4 *>(a.part_o + (slot(p) * tile_heads + hd) * cols + c * 4);
+      const float f = s_w[p];
+      o.x = fmaf(x.x, f, o.x);
+      o.y = fmaf(x.y, f, o.y);
+      o.z = fmaf(x.z, f, o.z);
+      o.w = fmaf(x.w, f, o.w);
+    }
+    s_o[tid] = o;
+  }
+  __syncthreads();
+  if (tid < quads && tid * 4 < a.d_h) {
+    for (int i = 1; i < groups; ++i) {
+      const float4 x = s_o[i * quads + tid];
+      o.x += x.x;
+      o.y += x.y;
+      o.z += x.z;
+      o.w += x.w;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int head = kv * a.group + ht * tile_heads + hd;
+    store4(a, b, head, tid * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (tid == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+  }
+}
+
+// ---- host side -----------------------------------------------------------------------------------
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// pages as [page][head][row][column], boxes of 128 bytes x box_rows
+bool encode_pages(const PagedCfg &cfg, CUtensorMap *map, void *base, bool bf16, const AttendArgs &a, long long ld_page, long long ld_head, long long ld_row) {
+  const int elt = bf16 ? 2 : 4;
+  const cuuint64_t dims[4] = {(cuuint64_t)a.d_h, (cuuint64_t)a.page, (cuuint64_t)a.n_kvh, (cuuint64_t)a.n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)ld_row * elt, (cuuint64_t)ld_head * elt, (cuuint64_t)ld_page * elt};
+  const cuuint32_t box[4] = {(cuuint32_t)(kBoxBytes / elt), (cuuint32_t)a.box_rows, 1, 1}, estr[4] = {1, 1, 1, 1};
+  return reinterpret_cast<EncodeTiledFn>(cfg.encode_tiled)(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base, dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+using AttendKernel = void (*)(CUtensorMap, CUtensorMap, AttendArgs);
+AttendKernel attend_kernel(const PagedCfg &cfg, bool bf16) {
+  const bool wide = cfg.tile_heads == 16;
+  switch (bf16 ? cfg.blocks : 4 + cfg.blocks) {
+    case 1: return wide ? k_attend<__nv_bfloat16, 1, 2> : k_attend<__nv_bfloat16, 1, 1>;
+    case 2: return wide ? k_attend<__nv_bfloat16, 2, 2> : k_attend<__nv_bfloat16, 2, 1>;
+    case 3: return wide ? k_attend<__nv_bfloat16, 3, 2> : k_attend<__nv_bfloat16, 3, 1>;
+    case 4: return wide ? k_attend<__nv_bfloat16, 4, 2> : k_attend<__nv_bfloat16, 4, 1>;
+    case 5: return k_attend<float, 1, 1>;
+    case 6: return k_attend<float, 2, 1>;
+    case 7: return k_attend<float, 3, 1>;
+    case 8: return k_attend<float, 4, 1>;
+  }
+  return nullptr;
+}
+
+constexpr size_t kSmSmem = 228 * 1024, kCtaReserve = 1024;   // shared memory of an SM, and what the system takes of it for each CTA
+
+}  // namespace
+
+cudaError_t paged_configure(PagedCfg *cfg, const DeviceCfg &dev, int n_qh, int n_kvh, int d_h, bool bf16) {
+  void *fn = nullptr;
+  cudaDriverEntryPointQueryResult qres;
+  cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+  if (e != cudaSuccess) return e;
+  if (qres != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
+  cfg->encode_tiled = fn;
+  e = plan_configure();
+  if (e == cudaSuccess) e = select_pages_configure();
+  if (e != cudaSuccess) return e;
+  const int blocks = (d_h * (bf16 ? 2 : 4) + kBoxBytes - 1) / kBoxBytes, group = n_qh / n_kvh;
+  if (blocks > 4) return cudaSuccess;
+  cfg->blocks = blocks;
+  cfg->tile_heads = bf16 && group > 8 ? 16 : 8;
+  cfg->head_tiles = (group + cfg->tile_heads - 1) / cfg->tile_heads;
+  return cudaFuncSetAttribute(attend_kernel(*cfg, bf16), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dev.smem_optin);
+}
+
+size_t attend_scratch(const PagedCfg &cfg, const DeviceCfg &dev, bool bf16, AttendArgs *a, char *base) {
+  if (!cfg.blocks) return 0;
+  const size_t slots = (size_t)dev.sm_count * attend_ctas(cfg.blocks, cfg.tile_heads / 8) * 2 * cfg.tile_heads;
+  const size_t o = slots * (cfg.blocks * kBoxBytes / (bf16 ? 2 : 4)) * sizeof(float), ml = slots * sizeof(float2);   // multiples of 256 bytes
+  if (a) {
+    a->part_o = reinterpret_cast<float *>(base);
+    a->part_ml = reinterpret_cast<float2 *>(base + o);
+    a->desc = reinterpret_cast<int4 *>(base + o + ml);
+  }
+  return (o + ml + slots * sizeof(int4) + 255) / 256 * 256;
+}
+
+cudaError_t launch_attend(AttendArgs a, const pact_paged_cache &cache, const PagedCfg &cfg, const DeviceCfg &dev, bool bf16, cudaStream_t st, int *launches) {
+  a.head_tiles = cfg.head_tiles;
+  a.box_rows = a.page % 64 == 0 ? 64 : a.page % 32 == 0 ? 32 : 16;
+  CUtensorMap mk, mv;
+  if (!encode_pages(cfg, &mk, cache.K, bf16, a, cache.k_page, cache.k_head, cache.k_row) ||
+      !encode_pages(cfg, &mv, cache.V, bf16, a, cache.v_page, cache.v_head, cache.v_row))
+    return cudaErrorInvalidValue;
+  const int per_sm = attend_ctas(cfg.blocks, cfg.tile_heads / 8), ctas = dev.sm_count * per_sm, elt = bf16 ? 2 : 4;
+  const size_t most = kSmSmem / per_sm - kCtaReserve;
+  a.stages = kMaxAttendStages;
+  while (a.stages > 2 && (size_t)attend_smem(a.stages, cfg.blocks, cfg.tile_heads, elt, a.B).total > most) --a.stages;
+  const int smem = attend_smem(a.stages, cfg.blocks, cfg.tile_heads, elt, a.B).total;
+  *launches = 1;
+  cudaError_t e = launch_k(attend_kernel(cfg, bf16), dim3((unsigned)ctas), dim3(kAttendThreads), (size_t)smem, st, true, mk, mv, a);
+  if (e != cudaSuccess) return e;
+  const long long rows = (long long)(a.selected && a.n_select < a.width ? a.n_select : a.width) * a.page;
+  if (rows <= kTile) return e;                                 // a request and key head is one tile: nothing is cut
+  *launches = 2;
+  const int group = a.group < cfg.tile_heads ? a.group : cfg.tile_heads;
+  return launch_k(k_attend_join, dim3((unsigned)ctas, (unsigned)group), dim3(kJoinThreads), 0, st, true, a, cfg.tile_heads, cfg.blocks * kBoxBytes / elt);
+}
+
+}  // namespace pact
