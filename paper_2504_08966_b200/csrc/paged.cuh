@@ -75,7 +75,7 @@ struct AttendArgs {
   float *part_o;         // [2 CTAs][heads of a tile][columns] sums of the parts of a request that several CTAs share
   float2 *part_ml;       // [2 CTAs][heads of a tile] their running maximum and sum
   int4 *desc;            // [CTAs] what was cut at the beginning of a CTA's share
-  float scale_log2;      // scale * log2(e)
+  float scale;
   int B, width, page, n_pages, n_select;
   int n_kvh, group, d_h, head_tiles;
   int box_rows;          // rows of one copy: the largest of 64, 32, 16 that divides the page

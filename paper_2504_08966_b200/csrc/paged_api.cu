@@ -141,7 +141,7 @@ pact_status pact_paged_attention(pact_ctx *ctx, const pact_paged_cache *cache, c
   if (s != PACT_OK) return s;
   a.Q = Q; a.ldQ = ldQ; a.ldQh = ldQh; a.logw = cache->logw; a.table = block_table; a.length = length; a.selected = selected;
   a.out = out; a.ldO = ldO; a.ldOh = ldOh; a.lse = lse; a.status = status;
-  a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.scale = scale;
   a.B = n_requests; a.width = max_pages; a.page = cache->page_rows; a.n_pages = cache->n_pages; a.n_select = selected ? n_select : 0;
   a.n_kvh = ctx->n_kvh; a.group = ctx->n_qh / ctx->n_kvh; a.d_h = ctx->d_h; a.out_bf16 = ctx->out == PACT_BF16;
   int launches = 0;

@@ -20,19 +20,18 @@
 // 2^-17): one term would put an error of 2^-9 on every product, as large as the rounding of a bf16 result and far above that of an fp32 one.
 // fp32: fused multiply-adds; for the logits a lane has one row and half of the columns, for the output four columns of all rows.
 #include "paged.cuh"
+#include "paged_tiles.h"
 #include "umma.cuh"
 
 namespace pact {
 namespace {
 
-constexpr int kTile = 64;                  // rows of a tile
-constexpr int kRowsOfWarp = 16;
 constexpr int kConsumers = 4;              // computing warps
 constexpr int kAttendThreads = (kConsumers + 1) * 32;
 constexpr int kMaxAttendStages = 8;
 constexpr int kBoxBytes = 128;             // columns of a box
 constexpr int kBlockBytes = kTile * kBoxBytes;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kScratch = kRowsOfWarp * 8 + 8;   // fp32: floats of a warp for probabilities and factors
 
 // Offsets in dynamic shared memory (the ring comes first: swizzled boxes lie at multiples of 1024 bytes).
@@ -89,7 +88,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 
 __device__ __forceinline__ void consumers_meet() { asm volatile("bar.sync 1, %0;" ::"n"(kConsumers * 32) : "memory"); }
 
-// One warp's part of a request and key head: running maximum (of the logits times log2 e), sum and output of its rows.
+// Logits stay in natural units: a bias of the lowest float times log2 e would be minus infinity, and rows that all have it share the attention.
+// exp(s - m), 0 for s = -inf whatever m is
+__device__ __forceinline__ float exp_below(float s, float m) { return ex2_approx((s - (m == -INFINITY ? 0.f : m)) * kLog2e); }
+// how much a sum with maximum m counts beside one with maximum `to` (m - to is NaN where both are infinite)
+__device__ __forceinline__ float weight(float m, float to) { return m == -INFINITY ? 0.f : m == to ? 1.f : ex2_approx((m - to) * kLog2e); }
+
+// One warp's part of a request and key head: running maximum of the logits, sum and output of its rows.
 template <typename T, int NB, int NT> struct Part;
 
 template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
@@ -142,8 +147,6 @@ template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
       b1 = bias[row0 + r1];
     }
     const bool in0 = r0 < rows && b0 != -INFINITY, in1 = r1 < rows && b1 != -INFINITY;
-    b0 *= kLog2e;
-    b1 *= kLog2e;
     float top[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -169,7 +172,7 @@ template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float to = fmaxf(m[n][i], top[n][i]), f = m[n][i] == to ? 1.f : ex2_approx(m[n][i] - to);   // (m - to is NaN where both are infinite)
+          const float to = fmaxf(m[n][i], top[n][i]), f = weight(m[n][i], to);
           m[n][i] = to;
           l[n][i] *= f;
 #pragma unroll
@@ -184,7 +187,7 @@ template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
     for (int n = 0; n < NT; ++n) {
       float p[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = ex2_approx(s[n][i] - (m[n][i & 1] == -INFINITY ? 0.f : m[n][i & 1]));
+      for (int i = 0; i < 4; ++i) p[i] = exp_below(s[n][i], m[n][i & 1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) l[n][i] += p[i] + p[2 + i];
 #pragma unroll
@@ -301,9 +304,8 @@ template <int NB> struct Part<float, NB, 1> {
 #pragma unroll
         for (int h = 0; h < 8; ++h) s[h] = fma4(k, lds4(q + h * q_row + nb * kBoxBytes + c * 16), s[h]);
       }
-    float b = has_bias ? bias[row] : 0.f;
+    const float b = has_bias ? bias[row] : 0.f;
     const bool in = r < rows && b != -INFINITY;
-    b *= kLog2e;
     float t[4], top[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {             // both halves of the columns; a lane goes on with four heads
@@ -322,12 +324,12 @@ template <int NB> struct Part<float, NB, 1> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (rescale) {
-        const float to = fmaxf(m[i], top[i]), f = m[i] == to ? 1.f : ex2_approx(m[i] - to);
+        const float to = fmaxf(m[i], top[i]), f = weight(m[i], to);
         m[i] = to;
         l[i] *= f;
         if (r == 0) scratch[kRowsOfWarp * 8 + half * 4 + i] = f;
       }
-      t[i] = ex2_approx(t[i] - (m[i] == -INFINITY ? 0.f : m[i]));
+      t[i] = exp_below(t[i], m[i]);
       l[i] += t[i];
     }
     *reinterpret_cast<float4 *>(scratch + r * 8 + half * 4) = make_float4(t[0], t[1], t[2], t[3]);
@@ -393,9 +395,6 @@ template <int NB> struct Part<float, NB, 1> {
   }
 };
 
-// how much a sum with maximum m counts beside one with maximum `to`
-__device__ __forceinline__ float weight(float m, float to) { return m == -INFINITY ? 0.f : m == to ? 1.f : ex2_approx(m - to); }
-
 __device__ __forceinline__ void store4(const AttendArgs &a, int b, int head, int c, const float4 &v) {
   const long long at = b * a.ldO + head * a.ldOh + c;
   if (a.out_bf16) *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.out) + at) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
@@ -434,10 +433,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
     return len < 0 ? 0 : len > room ? (int)room : len;
   };
   const auto tiles_of = [&](int b) {
-    const unsigned rows = (unsigned)rows_of(b);
-    if (!a.selected) return (int)((rows + kTile - 1u) / kTile);
-    const long long pages = min((long long)a.n_select, (long long)((rows + (unsigned)a.page - 1u) / (unsigned)a.page));
-    return (int)((pages * a.page + kTile - 1) / kTile);
+    return tiles_of_request(rows_of(b), a.page, a.selected != nullptr, a.n_select);
   };
   const int Hn = a.n_kvh * a.head_tiles;
   {
@@ -467,7 +463,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
   const long long T_all = (long long)pre[a.B] * Hn;
   const long long G = min((long long)gridDim.x, T_all);
   const long long me = blockIdx.x;
-  const long long t0 = me < G ? me * T_all / G : T_all, t1 = me < G ? (me + 1) * T_all / G : T_all;
+  const long long t0 = me < G ? share_begin(me, G, T_all) : T_all, t1 = me < G ? share_begin(me + 1, G, T_all) : T_all;
   // requests without any row
   for (int b = blockIdx.x; b < a.B; b += gridDim.x)
     if (pre[b + 1] == pre[b]) {
@@ -504,30 +500,16 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
       uint32_t rows = 0;                                       // rows that count of every 16, a byte each
       if (lane < n) {
         find(base + lane, b, h, j);
-        const int len = rows_of(b), kv = h / a.head_tiles;
-        const int pages = (int)(((unsigned)len + (unsigned)a.page - 1u) / (unsigned)a.page), listed = a.selected ? min(a.n_select, pages) : pages;
-        long long left = 0;
+        const int kv = h / a.head_tiles;
+        const TileRows at_rows = locate_rows(j, rows_of(b), a.page, per_box, a.table + (long long)b * a.width, a.n_pages,
+                                             a.selected ? a.selected + ((long long)b * a.n_kvh + kv) * a.n_select : nullptr, a.n_select);
+        rows = at_rows.rows;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          if (g % per_box == 0) {                              // a box lies in one page
-            const long long r = (long long)j * kTile + g * kRowsOfWarp;
-            int place = (int)(r / a.page);
-            off[g] = (int)(r - (long long)place * a.page);
-            if (place >= listed) place = -1;
-            else if (a.selected) place = a.selected[((long long)b * a.n_kvh + kv) * a.n_select + place];
-            left = place < 0 || place >= pages ? 0 : len - ((long long)place * a.page + off[g]);
-            if (left > 0) {
-              id[g] = a.table[(long long)b * a.width + place];
-              if (id[g] < 0 || id[g] >= a.n_pages) {
-                left = 0;
-                if (a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
-              }
-            }
-          } else {
-            left -= kRowsOfWarp;
-          }
-          if (left > 0) rows |= (uint32_t)min(left, (long long)kRowsOfWarp) << (8 * g);
+          id[g] = at_rows.id[g];
+          off[g] = at_rows.off[g];
         }
+        if (at_rows.bad && a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
       }
       for (int i = 0; i < n; ++i) {
         const uint32_t rows_i = __shfl_sync(0xffffffffu, rows, i);
@@ -594,8 +576,8 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
       int4 d = make_int4(0, 0, 0, 0);
       if (j > 0) {
         const long long ts = t0 - j, te = ts + (pre[b + 1] - pre[b]);
-        const long long i0 = ((ts + 1) * G - 1) / T_all, i1 = (te * G - 1) / T_all;
-        if (i0 == me - 1) d = make_int4(ts == i0 * T_all / G ? 1 : 2, (int)i1, b, h);
+        const long long i0 = share_of(ts, G, T_all), i1 = share_of(te - 1, G, T_all);
+        if (i0 == me - 1) d = make_int4(ts == share_begin(i0, G, T_all) ? 1 : 2, (int)i1, b, h);
       }
       a.desc[blockIdx.x] = d;
     }
@@ -618,7 +600,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
         const int rows = (int)(meta[st] >> (8 * warp) & 0xffu);
         if (rows > 0 && ok) {
           const uint32_t sk = smem_u32(sm + st * at.stage);
-          part.step(sk, sk + NB * kBlockBytes, reinterpret_cast<const float *>(sm + at.bias) + st * kTile, a.logw != nullptr, warp * kRowsOfWarp, rows, a.scale_log2,
+          part.step(sk, sk + NB * kBlockBytes, reinterpret_cast<const float *>(sm + at.bias) + st * kTile, a.logw != nullptr, warp * kRowsOfWarp, rows, a.scale,
                     lane, slots + warp * kScratch);
         }
         __syncwarp();
@@ -669,7 +651,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
         if (whole) {
           const int head = kv * a.group + ht * P::kHeads + hd;
           if (c < a.d_h) store4(a, b, head, c, o);
-          if (c == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : (to + log2f(l)) * kLn2;
+          if (c == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : to + logf(l);
         } else {
           *reinterpret_cast<float4 *>(a.part_o + (slot_out * P::kHeads + hd) * P::kCols + c) = o;
           if (c == 0) a.part_ml[slot_out * P::kHeads + hd] = make_float2(to, l);
@@ -754,7 +736,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_const
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int head = kv * a.group + ht * tile_heads + hd;
     store4(a, b, head, tid * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-    if (tid == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+    if (tid == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : top + logf(l);
   }
 }
 

@@ -1,0 +1,70 @@
+// How the attention over a paged cache shares out its work: which tiles a CTA has, and where the rows of a tile lie.  Plain functions, so that
+// they can be run on the host as well.
+#pragma once
+#include <stdint.h>
+
+#ifdef __CUDACC__
+#define PACT_HD __host__ __device__ __forceinline__
+#else
+#define PACT_HD inline
+#endif
+
+namespace pact {
+
+constexpr int kTile = 64;                  // rows of a tile
+constexpr int kRowsOfWarp = 16;
+
+// Tiles of one key head of a request with `rows` cached rows: of all its rows, or of the first n_select entries of its list of pages (but no more entries
+// than it has pages).
+PACT_HD int tiles_of_request(int rows, int page, bool selected, int n_select) {
+  if (!selected) return (int)(((unsigned)rows + kTile - 1u) / kTile);
+  const long long have = (long long)(((unsigned)rows + (unsigned)page - 1u) / (unsigned)page), pages = have < n_select ? have : n_select;
+  return (int)((pages * page + kTile - 1) / kTile);
+}
+
+// T tiles in G shares of floor(T / G) or one more, G <= T: the first tile of share i, and the share that tile t is in.
+PACT_HD long long share_begin(long long i, long long G, long long T) { return i * T / G; }
+PACT_HD long long share_of(long long t, long long G, long long T) { return ((t + 1) * G - 1) / T; }
+
+// Page and place of every 16 rows of tile j, and how many of them count (a byte each).  A page id outside the cache makes its rows count for nothing and
+// sets `bad`.  per_box: 16 rows times this always lie in one page.
+struct TileRows {
+  int id[4], off[4];
+  uint32_t rows;
+  bool bad;
+};
+PACT_HD TileRows locate_rows(int j, int len, int page, int per_box, const int32_t *table, int n_pages, const int32_t *selected, int n_select) {
+  TileRows t;
+  t.rows = 0;
+  t.bad = false;
+  const int pages = (int)(((unsigned)len + (unsigned)page - 1u) / (unsigned)page), listed = selected && n_select < pages ? n_select : pages;
+  long long left = 0;
+#ifdef __CUDACC__
+#pragma unroll
+#endif
+  for (int g = 0; g < 4; ++g) {
+    t.id[g] = -1;
+    t.off[g] = 0;
+    if (g % per_box == 0) {
+      const long long r = (long long)j * kTile + g * kRowsOfWarp;
+      long long place = r / page;
+      t.off[g] = (int)(r - place * page);
+      if (place >= listed) place = -1;
+      else if (selected) place = selected[place];
+      left = place < 0 || place >= pages ? 0 : len - (place * page + t.off[g]);
+      if (left > 0) {
+        t.id[g] = table[place];
+        if (t.id[g] < 0 || t.id[g] >= n_pages) {
+          t.bad = true;
+          left = 0;
+        }
+      }
+    } else {
+      left -= kRowsOfWarp;
+    }
+    if (left > 0) t.rows |= (uint32_t)(left < kRowsOfWarp ? left : kRowsOfWarp) << (8 * g);
+  }
+  return t;
+}
+
+}  // namespace pact
