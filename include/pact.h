@@ -364,7 +364,7 @@ pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache /*host
  * pages are skipped, and a page named twice counts twice.  Rows with logw = minus infinity and rows past the length have no effect, whatever their keys and values hold.  Without any row out
  * is 0 and lse minus infinity.
  * Logits, softmax statistics and sums are fp32; bf16 probabilities are carried as two bf16 terms (error 2^-17).
- * out: element [b][j][c] at b * ldO + j * ldOh + c, type `out`; lse [n_requests][n_qh], may be NULL.
+ * out: element [b][j][c] at b * ldO + j * ldOh + c, type `out` (pointer and strides: multiples of four elements); lse [n_requests][n_qh], may be NULL.
  * d_h <= 256 for bf16, <= 128 for fp32 (UNSUPPORTED above).  Lengths are clamped to 0 .. max_pages * page_rows and rows of pages outside
  * the cache are left out; both set status to INVALID_ARG. */
 pact_status pact_paged_attention(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const void *Q, int64_t ldQ, int64_t ldQh,

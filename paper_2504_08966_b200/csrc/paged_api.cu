@@ -129,8 +129,8 @@ pact_status pact_paged_attention(pact_ctx *ctx, const pact_paged_cache *cache, c
   if (s == PACT_OK) s = check_cache(ctx, cache);
   if (s != PACT_OK) return s;
   const size_t oe = ctx->out == PACT_BF16 ? 2 : 4;
-  if (!Q || !out || !aligned16(Q) || !aligned16(out) || !stride_ok(ctx, ldQ) || !stride_ok(ctx, ldQh)) return PACT_ERR_INVALID_ARG;
-  if (ldO < ctx->d_h || ldOh < ctx->d_h || ((size_t)ldO * oe) % 16 != 0 || ((size_t)ldOh * oe) % 16 != 0) return PACT_ERR_INVALID_ARG;
+  if (!Q || !out || !aligned16(Q) || reinterpret_cast<uintptr_t>(out) % (4 * oe) != 0 || !stride_ok(ctx, ldQ) || !stride_ok(ctx, ldQh)) return PACT_ERR_INVALID_ARG;
+  if (ldO < ctx->d_h || ldOh < ctx->d_h || ldO % 4 != 0 || ldOh % 4 != 0) return PACT_ERR_INVALID_ARG;
   if (!isfinite(scale) || (selected && n_select < 1)) return PACT_ERR_INVALID_ARG;
   if (!ctx->paged.blocks) return PACT_ERR_UNSUPPORTED;
   const int64_t rows = (int64_t)(selected && n_select < max_pages ? n_select : max_pages) * cache->page_rows;

@@ -25,7 +25,7 @@ _ctx = {}
 def context(pb, n_qh=8, n_kvh=2, d_h=64, dtype=BF, out=None):
     key = (n_qh, n_kvh, d_h, dtype, out or dtype)
     if key not in _ctx:
-        _ctx[key] = pb.Context(max(8, n_qh * d_h), n_qh, n_kvh, d_h, dtype, out or dtype)
+        _ctx[key] = pb.Context((n_qh * d_h + 7) // 8 * 8, n_qh, n_kvh, d_h, dtype, out or dtype)
     return _ctx[key]
 
 
@@ -102,7 +102,7 @@ def test_a_plan_that_cannot_be_served_changes_nothing(pb, fault, in_place, rows)
     lens, table, free, n_free = plan_state(rng, B, width, page, B * width, 50)
     new, n_rows, row_stride = [rows, 1, -1, 2], rows + 3, 0
     if fault == "pages":
-        n_free = 1
+        n_free, lens[2] = 1, 0                         # the request that ends has none to give back
     elif fault == "length":
         lens[1] = width * page
     elif fault == "negative":
@@ -359,7 +359,7 @@ def attend_and_check(pb, dtype, out_dtype, n_qh, H, D, page, lens, heads_first=T
     assert np.isfinite(got).all() and (err <= tol).all(), (err / tol).max()
     none = lse_ref == -np.inf
     assert np.array_equal(got_lse == -np.inf, none) and not got[none].any()
-    err = np.abs(got_lse - lse_ref)[~none]
+    err = np.abs(got_lse[~none] - lse_ref[~none])
     assert (err <= (delta + 2.0 ** -20 + steps * 2.0 ** -21 + 2.0 ** -22 * np.abs(lse_ref, where=~none, out=np.zeros_like(lse_ref)))[~none]).all()
     first = out.clone(), lse.clone()
     call()
@@ -497,7 +497,8 @@ def test_offsets_past_32_bits(pb):
     ctx.pact_paged_attention(cache, Q, i32([ids]), i32([n]), out)
     s = torch.einsum("hc,nhc->hn", Q[0].double(), K_new.double()) * D ** -0.5
     ref = torch.einsum("hn,nhc->hc", torch.softmax(s, 1), V_new.double())
-    assert (out[0].double() - ref).abs().max() <= 2.0 ** -9 * ref.abs().max() + 2.0 ** -15
+    # a bf16 number has eight significant bits, so its rounding is off by up to 2^-8 of the value (half of eps = 2^-7); 2^-15: two-term probabilities
+    assert ((out[0].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -15).all()
 
 
 # ---- as a serving program uses them --------------------------------------------------------------------------------
@@ -566,7 +567,7 @@ def test_cache_behind_a_reduction(pb):
         im = pb.device_image(wl.images[0], F32)
         im.H_out, im.logw_out, im.counters = H_out[i], logw[i], counters[i]
         ims.append(im)
-    ctx.pact_reduce(ims, [pb.make_params(lam=lam, d_c=wl.d_c) for lam in (0.1, 0.3, 0.6)])
+    ctx.pact_reduce(ims, [pb.make_params(lam=lam, d_c=d_c) for lam, d_c in ((0.1, 0.01), (0.3, wl.d_c), (0.6, 0.02))])
     page, width, n_pages = 16, 20, 60
     K, V = torch.full((2, n_pages, n_kvh, page, d_h), float("nan"), device="cuda")
     w, b, wm = (torch.full(s, float("nan"), device="cuda") for s in ((n_pages, page), (n_pages, n_kvh, 2, d_h), (n_pages,)))

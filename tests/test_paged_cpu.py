@@ -184,7 +184,7 @@ int main() {
     ctx.paged.blocks = 2;
   };
   common(true);
-  REFUSED(x.out = nullptr, PACT_ERR_INVALID_ARG) REFUSED(x.out = buf + 8, PACT_ERR_INVALID_ARG) REFUSED(x.ldo = 100, PACT_ERR_INVALID_ARG) REFUSED(x.ldoh = 130, PACT_ERR_INVALID_ARG)
+  REFUSED(x.out = nullptr, PACT_ERR_INVALID_ARG) REFUSED(x.out = buf + 4, PACT_ERR_INVALID_ARG) REFUSED(x.ldo = 100, PACT_ERR_INVALID_ARG) REFUSED(x.ldoh = 130, PACT_ERR_INVALID_ARG)
   // ---- selection
   ok.f = [&](Args &x) { return pact_page_select(x.ctx, cache(x), x.q, x.ldq, x.ldqh, x.B, x.table, x.width, x.length, x.scale, x.n_first, x.n_last, x.n_select, x.sel, nullptr, x.ws,
                                                 x.ws_bytes, nullptr); };
