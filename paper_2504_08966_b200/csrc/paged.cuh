@@ -53,7 +53,8 @@ struct SelectArgs {
   const float *w_max;
   const int32_t *table, *length;
   int32_t *selected, *status;
-  unsigned long long *keys;   // [B][n_kvh][width] scores as integers that order like them
+  uint2 *approx;              // [B][n_kvh][width] scores in fp32 as integers that order like them, and bounds of their errors
+  unsigned long long *keys;   // [B][n_kvh][width] scores in double, those that were needed
   float scale;
   int B, width, page, n_pages, n_kvh, group, d_h;
   int n_first, n_last, n_select;

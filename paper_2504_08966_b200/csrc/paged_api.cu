@@ -40,8 +40,9 @@ pact_status check_ws(void *ws, size_t have, size_t need) {
   return ws && reinterpret_cast<uintptr_t>(ws) % kAlign == 0 && have >= need ? PACT_OK : PACT_ERR_WORKSPACE;
 }
 
+size_t select_scores(const pact_ctx *c, int requests, int pages) { return (size_t)requests * c->n_kvh * pages; }
 size_t select_bytes(const pact_ctx *c, int requests, int pages) {
-  return ((size_t)requests * c->n_kvh * pages * sizeof(unsigned long long) + kAlign - 1) / kAlign * kAlign;
+  return (select_scores(c, requests, pages) * (sizeof(uint2) + sizeof(unsigned long long)) + kAlign - 1) / kAlign * kAlign;
 }
 
 }  // namespace
@@ -110,7 +111,7 @@ pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache, const
   if (s != PACT_OK) return s;
   SelectArgs a;
   a.Q = Q; a.ldQ = ldQ; a.ldQh = ldQh; a.bounds = cache->bounds; a.w_max = cache->w_max; a.table = block_table; a.length = length;
-  a.selected = selected; a.status = status; a.keys = (unsigned long long *)ws; a.scale = scale;
+  a.selected = selected; a.status = status; a.approx = (uint2 *)ws; a.keys = (unsigned long long *)ws + select_scores(ctx, n_requests, max_pages); a.scale = scale;
   a.B = n_requests; a.width = max_pages; a.page = cache->page_rows; a.n_pages = cache->n_pages;
   a.n_kvh = ctx->n_kvh; a.group = ctx->n_qh / ctx->n_kvh; a.d_h = ctx->d_h;
   a.n_first = n_first; a.n_last = n_last; a.n_select = n_select;
