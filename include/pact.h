@@ -316,61 +316,90 @@ typedef struct {
 /* Block tables and slots of the rows that come next.  length[b] rows of request b are cached, n_new[b * n_new_stride] rows
  * (0 or more) are to follow: a count array of its own, or the N_OUT counters of a batch that pact_reduce has just written
  * (stride PACT_N_COUNTERS).  A negative count ends the request: its pages go back and its length becomes 0.
- * free_pages is a stack of page ids, its top at free_pages[*n_free - 1] (capacity n_pages).  Ended requests push their pages first,
- * by ascending request and ascending place; then the others take pages off the top in the same order.
- * Writes the new entries of block_table [n_requests][max_pages] (entries that no new row needs are left alone), length_out,
- * n_free_out, free_pages above the old top, row_start[n_requests + 1] (prefix sums of the counts; may be NULL) and slot[n_rows] (may
- * be NULL): the slot of every new row, -1 behind the last.  New rows are packed (row_stride 0: row i of request b is
- * row_start[b] + i, and n_rows is what the caller has room for), or each request has row_stride of them (row
- * b * row_stride + i; n_rows = n_requests * row_stride).  length_out may be length and n_free_out may be n_free.
+ * free_pages is a stack of page ids, its top at free_pages[*n_free - 1].  Ended requests push their pages first, by ascending request and
+ * ascending place; then the others take pages off the top in the same order.
+ * New rows are packed (row_stride 0: row i of request b is row_start[b] + i, and n_rows is what the caller has room for), or each request has
+ * row_stride of them (row b * row_stride + i; n_rows = n_requests * row_stride).
  * A call that cannot be served as a whole changes nothing: length_out and n_free_out repeat the old values, row_start is 0, every
  * slot -1, and status becomes PACT_ERR_NO_PAGES (more pages needed than free) or PACT_ERR_INVALID_ARG (a length that is negative or, with
  * the new rows, more than max_pages hold; more new rows than n_rows or row_stride; n_free outside 0 .. n_pages, or above n_pages once
  * ended requests have pushed their pages). */
-pact_status pact_cache_plan(pact_ctx *ctx, int page_rows, int n_pages, int n_requests, int max_pages, int32_t *block_table,
-                            const int32_t *length, const int32_t *n_new, int64_t n_new_stride, int32_t *free_pages,
-                            const int32_t *n_free, int32_t *length_out, int32_t *n_free_out, int32_t *row_start,
-                            int64_t *slot, int64_t n_rows, int row_stride, int32_t *status, void *stream);
+typedef struct {
+  int32_t page_rows, n_pages; /* of the cache (the same for all layers)                             */
+  int32_t n_requests, max_pages;
+  int32_t *block_table;       /* [n_requests][max_pages]; entries of new pages are written, the others left alone */
+  const int32_t *length;      /* [n_requests]                                                       */
+  const int32_t *n_new;       /* [n_requests] with stride n_new_stride >= 1                         */
+  int64_t n_new_stride;
+  int32_t *free_pages;        /* [n_pages]; changes above the old top only                          */
+  const int32_t *n_free;      /* [1]                                                                */
+  int32_t *length_out;        /* [n_requests]; may be length                                        */
+  int32_t *n_free_out;        /* [1]; may be n_free                                                 */
+  int32_t *row_start;         /* [n_requests + 1] prefix sums of the counts; may be NULL            */
+  int64_t *slot;              /* [n_rows] slot of every new row, -1 behind the last; may be NULL    */
+  int64_t n_rows;
+  int32_t row_stride;
+  int32_t reserved;
+  int32_t *status;
+} pact_plan;
+pact_status pact_cache_plan(pact_ctx *ctx, const pact_plan *p /*host*/, void *stream);
 
-/* Rows into their slots: row r of K_new and V_new (element [r][head][c] at r * ld_row + head * ld_head + c) and logw_new[r] (NULL: 0) go
- * to slot[r]; a negative slot is skipped, one that no page of the cache has is skipped and sets status to INVALID_ARG.
+/* Rows into their slots: row r of K and V (element [r][head][c] at r * ld_row + head * ld_head + c, type `in`) and logw[r] go to slot[r]; a
+ * negative slot is skipped, one that no page of the cache has is skipped and sets status to INVALID_ARG.
  * Slots of a call differ.  Where the cache keeps bounds, the rows of a page are neighbours in the call, in ascending slots without a gap, as
  * pact_cache_plan lays them out: a page whose place 0 is written begins new bounds, those of other pages are widened. */
-pact_status pact_cache_write(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const void *K_new, const void *V_new,
-                             int64_t ld_row, int64_t ld_head, const float *logw_new, const int64_t *slot, int64_t n_rows,
-                             int32_t *status, void *stream);
+typedef struct {
+  const void *K, *V;
+  int64_t ld_row, ld_head;
+  const float *logw;          /* [n_rows]; NULL: 0                                                  */
+  const int64_t *slot;        /* [n_rows]                                                           */
+  int64_t n_rows;
+  int32_t *status;
+} pact_new_rows;
+pact_status pact_cache_write(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_new_rows *r /*host*/, void *stream);
 
-/* Bytes of device workspace (256-byte aligned) that pact_page_select and pact_paged_attention need for at most max_requests requests
- * and max_pages entries per block table.  It needs no initialisation and keeps nothing between calls. */
+/* One new token per request: what pact_page_select and pact_paged_attention take. */
+typedef struct {
+  const void *Q;              /* element [b][j][c] at b * ldQ + j * ldQh + c, type `in`             */
+  int64_t ldQ, ldQh;
+  const int32_t *block_table; /* [n_requests][max_pages]                                            */
+  const int32_t *length;      /* [n_requests] cached rows, the new token's own among them           */
+  int32_t n_requests, max_pages;
+  int32_t *selected;          /* [n_requests][n_kvh][n_select] places in the block table: written by pact_page_select, read by
+                                 pact_paged_attention (NULL: all pages)                             */
+  int32_t n_select;
+  int32_t n_first, n_last;    /* pact_page_select: pages that are always selected                   */
+  float scale;                /* of the logits; 1 / sqrt(d_h) as a rule                             */
+  void *out;                  /* pact_paged_attention: element [b][j][c] at b * ldO + j * ldOh + c, type `out` (pointer and
+                                 strides: multiples of four elements)                               */
+  int64_t ldO, ldOh;
+  float *lse;                 /* [n_requests][n_qh]; may be NULL                                    */
+  int32_t *status;
+  void *ws;                   /* workspace, 256-byte aligned                                        */
+  size_t ws_bytes;
+} pact_query;
+
+/* Bytes of device workspace that pact_page_select and pact_paged_attention need for at most max_requests requests and max_pages entries per
+ * block table.  It needs no initialisation and keeps nothing between calls. */
 size_t pact_paged_workspace_bytes(const pact_ctx *ctx, int max_requests, int max_pages);
 
-/* Pages that one new token per request should attend to.  Q: element [b][j][c] at b * ldQ + j * ldQh + c, type `in`.  For a page
- * with bounds lo, hi and every query head j of a key head, scale * sum_c (max(q_c, 0) hi_c + min(q_c, 0) lo_c) + w_max is at least
- * every logit scale * q.k + logw of its rows (scale >= 0); the page's score is the largest of these over the heads (a sum that is not a
- * number is left out), formed in double.  Selected are the first n_first and the last n_last pages of the request, then those with the largest
- * scores, ties to the lower page, n_select in all.
- * selected [n_requests][n_kvh][n_select]: their places in the block table in ascending order, -1 behind the last.  n_first, n_last >= 0,
- * n_first + n_last <= n_select; max_pages <= 65536.  Lengths outside 0 .. max_pages * page_rows are clamped and page ids outside the
- * cache score minus infinity; both set status to INVALID_ARG. */
-pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const void *Q, int64_t ldQ, int64_t ldQh,
-                             int n_requests, const int32_t *block_table, int max_pages, const int32_t *length, float scale,
-                             int n_first, int n_last, int n_select, int32_t *selected, int32_t *status, void *ws,
-                             size_t ws_bytes, void *stream);
+/* Pages that the new token should attend to.  For a page with bounds lo, hi and every query head j of a key head,
+ * scale * sum_c (max(q_c, 0) hi_c + min(q_c, 0) lo_c) + w_max is at least every logit scale * q.k + logw of its rows (scale >= 0); the page's
+ * score is the largest of these over the heads (a sum that is not a number is left out), in the order of double precision.  Selected are the first
+ * n_first and the last n_last pages of the request, then those with the largest scores, ties to the lower page, n_select in all.
+ * selected: their places in ascending order, -1 behind the last.  n_first, n_last >= 0, n_first + n_last <= n_select; max_pages <= 65536.  Lengths
+ * outside 0 .. max_pages * page_rows are clamped and page ids outside the cache score minus infinity; both set status to INVALID_ARG. */
+pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_query *q /*host*/, void *stream);
 
-/* Attention of one new token per request over its cached rows (Eq. 11): with s_p = scale * q.k_p + logw_p over the rows p in 0 .. length[b] - 1,
- * out = sum_p exp(s_p - lse) v_p and lse = log sum_p exp(s_p), for every query head, which reads key head
- * floor(j * n_kvh / n_qh).  With `selected` [n_requests][n_kvh][n_select] (places in the block table as pact_page_select writes them; NULL: all
- * pages) only the rows of those pages count: of the first min(n_select, pages of the request) entries, those below 0 or beyond the request's
- * pages are skipped, and a page named twice counts twice.  Rows with logw = minus infinity and rows past the length have no effect, whatever their keys and values hold.  Without any row out
- * is 0 and lse minus infinity.
+/* Attention of the new token over its request's cached rows (Eq. 11): with s_p = scale * q.k_p + logw_p over the rows p in
+ * 0 .. length[b] - 1, out = sum_p exp(s_p - lse) v_p and lse = log sum_p exp(s_p), for every query head, which reads key head
+ * floor(j * n_kvh / n_qh).  With `selected` only the rows of those pages count: of the first min(n_select, pages of the request) entries,
+ * those below 0 or beyond the request's pages are skipped, and a page named twice counts twice.  Rows with logw = minus infinity and
+ * rows past the length have no effect, whatever their keys and values hold.  Without any row out is 0 and lse minus infinity.
  * Logits, softmax statistics and sums are fp32; bf16 probabilities are carried as two bf16 terms (error 2^-17).
- * out: element [b][j][c] at b * ldO + j * ldOh + c, type `out` (pointer and strides: multiples of four elements); lse [n_requests][n_qh], may be NULL.
  * d_h <= 256 for bf16, <= 128 for fp32 (UNSUPPORTED above).  Lengths are clamped to 0 .. max_pages * page_rows and rows of pages outside
  * the cache are left out; both set status to INVALID_ARG. */
-pact_status pact_paged_attention(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const void *Q, int64_t ldQ, int64_t ldQh,
-                                 int n_requests, const int32_t *block_table, int max_pages, const int32_t *length,
-                                 const int32_t *selected, int n_select, float scale, void *out, int64_t ldO, int64_t ldOh,
-                                 float *lse, int32_t *status, void *ws, size_t ws_bytes, void *stream);
+pact_status pact_paged_attention(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_query *q /*host*/, void *stream);
 
 #ifdef __cplusplus
 }

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -51,6 +52,11 @@ class PagedCacheDesc(C.Structure):
                 ("bounds", C.c_void_p), ("w_max", C.c_void_p), ("n_pages", C.c_int32), ("page_rows", C.c_int32)]
 
 
+# pact_plan, pact_new_rows and pact_query of pact.h: packed into a buffer of the context, a tenth of the time of as many ctypes arguments
+_PLAN = struct.Struct("@4iPPPqPPPPPPqiiP")
+_NEW_ROWS = struct.Struct("@PPqqPPqP")
+_QUERY = struct.Struct("@PqqPPiiPiiifPqqPPPN")
+
 _lib = None
 
 
@@ -93,10 +99,10 @@ def lib():
         L.pact_profile_stage_name.argtypes = [i32]
         L.pact_profile_stage_name.restype = C.c_char_p
         pc = C.POINTER(PagedCacheDesc)
-        L.pact_cache_plan.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, i64, i32, vp, vp]
-        L.pact_cache_write.argtypes = [vp, pc, vp, vp, i64, i64, vp, vp, i64, vp, vp]
-        L.pact_page_select.argtypes = [vp, pc, vp, i64, i64, i32, vp, i32, vp, C.c_float, i32, i32, i32, vp, vp, vp, sz, vp]
-        L.pact_paged_attention.argtypes = [vp, pc, vp, i64, i64, i32, vp, i32, vp, vp, i32, C.c_float, vp, i64, i64, vp, vp, vp, sz, vp]
+        L.pact_cache_plan.argtypes = [vp, vp, vp]
+        L.pact_cache_write.argtypes = [vp, pc, vp, vp]
+        L.pact_page_select.argtypes = [vp, pc, vp, vp]
+        L.pact_paged_attention.argtypes = [vp, pc, vp, vp]
         L.pact_paged_workspace_bytes.argtypes = [vp, i32, i32]
         L.pact_paged_workspace_bytes.restype = sz
         for name in EXPORTS:
@@ -248,6 +254,7 @@ class PagedCache:
         k, v = _strides(K, "K"), _strides(V, "V")
         self.desc = PagedCacheDesc(_ptr(K), _ptr(V), k[0], k[1], k[2], v[0], v[1], v[2], _ptr(logw), _ptr(bounds), _ptr(w_max),
                                    self.n_pages, self.page_rows)
+        self.ref = C.byref(self.desc)
 
 
 PRUNE_STATIC_MAX_N = 65536
@@ -272,8 +279,9 @@ class Context:
         self.ws = None
         self._need = {}                      # (max_batch, max_N) -> workspace bytes, asked from the library once
         self.device = torch.cuda.current_device()
-        self._paged_ws = []                  # workspaces of the paged cache's calls, the last one in use
+        self._paged_ws = []                  # workspaces of the paged cache's calls: address, size, tensor; the last one is in use
         self._paged_need = {}
+        self._make_args()
 
     def close(self):
         if self.handle:
@@ -379,27 +387,39 @@ class Context:
         return Graph(self, h, images, self.ws)
 
     # ---- the paged cache ------------------------------------------------------------------
-    def _on_device(self, t, dtype, shape, what):
-        """A contiguous tensor of this type and shape on the context's device; its address, None for None."""
+    def _make_args(self):
+        self._args = C.create_string_buffer(max(_PLAN.size, _NEW_ROWS.size, _QUERY.size))
+        self._args_at = C.addressof(self._args)
+
+    def _flat(self, t, dtype, n, what):
+        """Address of a contiguous tensor of n elements of this type on the context's device; 0 for None."""
         if t is None:
-            return None
-        if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != self.device:
-            raise PactError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{self.device} is wanted")
+            return 0
+        if t.dtype is not dtype or t.numel() != n or t.get_device() != self.device or not t.is_contiguous():
+            raise PactError(f"{what}: a contiguous {dtype} tensor of {n} elements on cuda:{self.device} is wanted")
         return t.data_ptr()
 
-    def _heads(self, t, dtype, n, what):
-        """Address and strides of a [.., n, d_h] tensor on the context's device."""
-        if t.dtype != dtype or t.dim() != 3 or t.shape[1] != n or t.shape[2] != self.d_h or t.get_device() != self.device:
-            raise PactError(f"{what}: a {dtype} tensor of shape [.., {n}, {self.d_h}] on cuda:{self.device} is wanted")
+    def _table(self, t):
+        """Address, requests and width of a block table."""
+        if t.dtype is not torch.int32 or t.ndim != 2 or t.get_device() != self.device or not t.is_contiguous():
+            raise PactError(f"block_table: a contiguous {torch.int32} tensor of shape [B, max_pages] on cuda:{self.device} is wanted")
+        B, W = t.shape
+        return t.data_ptr(), B, W
+
+    def _heads(self, t, dtype, heads, n, what):
+        """Address and strides of a [n, heads, d_h] tensor on the context's device (n None: any)."""
+        shape = t.shape
+        if t.dtype is not dtype or len(shape) != 3 or shape[1] != heads or shape[2] != self.d_h or t.get_device() != self.device or (n is not None and shape[0] != n):
+            raise PactError(f"{what}: a {dtype} tensor of shape [{'..' if n is None else n}, {heads}, {self.d_h}] on cuda:{self.device} is wanted")
         s0, s1, s2 = t.stride()
-        if s2 != 1 or t.shape[0] == 1 or n == 1:
+        if s2 != 1 or shape[0] == 1 or heads == 1:
             s0, s1, _ = _strides(t, what)
         return t.data_ptr(), s0, s1
 
     def _cache(self, cache):
-        if cache.n_kvh != self.n_kvh or cache.d_h != self.d_h or cache.dtype != self.in_dtype or cache.device != self.device:
+        if cache.n_kvh != self.n_kvh or cache.d_h != self.d_h or cache.dtype is not self.in_dtype or cache.device != self.device:
             raise PactError(f"the cache is not one of {self.n_kvh} key heads of {self.d_h} {self.in_dtype} on cuda:{self.device}")
-        return C.byref(cache.desc)
+        return cache.ref
 
     def _paged_workspace(self, B, max_pages):
         """Address and size of the workspace.  One that is outgrown is kept: a captured graph may hold its address."""
@@ -408,9 +428,12 @@ class Context:
             if len(self._paged_need) >= 4096:
                 self._paged_need.clear()
             need = self._paged_need[(B, max_pages)] = int(self._L.pact_paged_workspace_bytes(self.handle, B, max_pages))
-        if not self._paged_ws or self._paged_ws[-1].numel() < need:
-            self._paged_ws.append(torch.empty(max(need, 2 * self._paged_ws[-1].numel() if self._paged_ws else 0), dtype=torch.uint8, device=self._cuda()))
-        return self._paged_ws[-1].data_ptr(), self._paged_ws[-1].numel()
+        have = self._paged_ws[-1] if self._paged_ws else None
+        if have is None or have[1] < need:
+            size = max(need, 2 * have[1] if have else 0)
+            ws = torch.empty(size, dtype=torch.uint8, device=self._cuda())
+            self._paged_ws.append((ws.data_ptr(), size, ws))
+        return self._paged_ws[-1]
 
     def _cuda(self):
         return torch.device("cuda", self.device)
@@ -420,70 +443,63 @@ class Context:
         """Pages and slots of the rows that come next (pact_cache_plan in pact.h).  block_table [B, max_pages], length, length_out [B], n_new [B] (may be a
         strided view, such as the N_OUT column of the counters of a batch; negative: the request has ended), free_pages [n_pages], n_free, n_free_out
         [1], row_start [B + 1], all int32; slot [n_rows] int64; n_rows: rows that the caller has room for, where slot is not given."""
-        i32 = torch.int32
-        if block_table.dim() != 2 or n_new.dim() != 1 or n_new.dtype != i32 or n_new.get_device() != self.device:
-            raise PactError("block_table is [B, max_pages], n_new an int32 [B] on the context's device")
-        B, W = block_table.shape
-        if n_new.shape[0] != B or free_pages.dim() != 1:
-            raise PactError("n_new is [B], free_pages [n_pages]")
+        i32, flat = torch.int32, self._flat
+        table, B, W = self._table(block_table)
+        if n_new.dtype is not i32 or n_new.ndim != 1 or n_new.numel() != B or n_new.get_device() != self.device:
+            raise PactError(f"n_new: an int32 tensor of shape [{B}] on cuda:{self.device} is wanted")
+        n_pages = free_pages.numel()
         if slot is not None:
             if n_rows is not None and n_rows != slot.numel():
                 raise PactError("n_rows is the length of slot")
             n_rows = slot.numel()
         elif n_rows is None:
             raise PactError("slot or n_rows is wanted")
-        _check(self.handle, self._L.pact_cache_plan(
-            self.handle, page_rows, free_pages.shape[0], B, W, self._on_device(block_table, i32, (B, W), "block_table"), self._on_device(length, i32, (B,), "length"),
-            n_new.data_ptr(), n_new.stride(0) if B > 1 else 1, self._on_device(free_pages, i32, free_pages.shape, "free_pages"),
-            self._on_device(n_free, i32, (1,), "n_free"), self._on_device(length_out, i32, (B,), "length_out"), self._on_device(n_free_out, i32, (1,), "n_free_out"),
-            self._on_device(row_start, i32, (B + 1,), "row_start"), self._on_device(slot, torch.int64, (n_rows,), "slot"), n_rows, row_stride,
-            self._on_device(status, i32, (1,), "status"), _stream()))
+        _PLAN.pack_into(self._args, 0, page_rows, n_pages, B, W, table, flat(length, i32, B, "length"), n_new.data_ptr(), n_new.stride()[0] if B > 1 else 1,
+                        flat(free_pages, i32, n_pages, "free_pages"), flat(n_free, i32, 1, "n_free"), flat(length_out, i32, B, "length_out"),
+                        flat(n_free_out, i32, 1, "n_free_out"), flat(row_start, i32, B + 1, "row_start"), flat(slot, torch.int64, n_rows, "slot"), n_rows, row_stride, 0,
+                        flat(status, i32, 1, "status"))
+        _check(self.handle, self._L.pact_cache_plan(self.handle, self._args_at, _stream()))
 
     def pact_cache_write(self, cache: PagedCache, K_new, V_new, logw_new, slot, status=None):
         """Rows K_new, V_new [n, n_kvh, d_h] (alike in their strides) and logw_new [n] fp32 (None: 0) into slot [n] int64."""
         ref = self._cache(cache)
-        k, ld_row, ld_head = self._heads(K_new, self.in_dtype, self.n_kvh, "K_new")
-        v, v_row, v_head = self._heads(V_new, self.in_dtype, self.n_kvh, "V_new")
+        k, ld_row, ld_head = self._heads(K_new, self.in_dtype, self.n_kvh, None, "K_new")
         n = K_new.shape[0]
-        if V_new.shape[0] != n or (v_row, v_head) != (ld_row, ld_head):
-            raise PactError("K_new and V_new have the same shape and strides")
-        _check(self.handle, self._L.pact_cache_write(self.handle, ref, k, v, ld_row, ld_head, self._on_device(logw_new, torch.float32, (n,), "logw_new"),
-                                                     self._on_device(slot, torch.int64, (n,), "slot"), n, self._on_device(status, torch.int32, (1,), "status"), _stream()))
+        v, v_row, v_head = self._heads(V_new, self.in_dtype, self.n_kvh, n, "V_new")
+        if v_row != ld_row or v_head != ld_head:
+            raise PactError("K_new and V_new have the same strides")
+        _NEW_ROWS.pack_into(self._args, 0, k, v, ld_row, ld_head, self._flat(logw_new, torch.float32, n, "logw_new"), self._flat(slot, torch.int64, n, "slot"), n,
+                            self._flat(status, torch.int32, 1, "status"))
+        _check(self.handle, self._L.pact_cache_write(self.handle, ref, self._args_at, _stream()))
 
     def pact_page_select(self, cache: PagedCache, Q, block_table, length, selected, n_first=1, n_last=1, scale=None, status=None):
         """Places of the pages that each request's token attends to, into selected [B, n_kvh, n_select] int32.  Q [B, n_qh, d_h]; scale: 1 / sqrt(d_h) if not given."""
+        i32 = torch.int32
         ref = self._cache(cache)
-        q, ldq, ldqh = self._heads(Q, self.in_dtype, self.n_qh, "Q")
-        B, W = block_table.shape
-        if Q.shape[0] != B or selected.dim() != 3:
-            raise PactError("Q is [B, n_qh, d_h], selected [B, n_kvh, n_select]")
-        n_select = selected.shape[2]
-        w, n = self._paged_workspace(B, W)
-        _check(self.handle, self._L.pact_page_select(
-            self.handle, ref, q, ldq, ldqh, B, self._on_device(block_table, torch.int32, (B, W), "block_table"), W, self._on_device(length, torch.int32, (B,), "length"),
-            self.d_h ** -0.5 if scale is None else scale, n_first, n_last, n_select, self._on_device(selected, torch.int32, (B, self.n_kvh, n_select), "selected"),
-            self._on_device(status, torch.int32, (1,), "status"), w, n, _stream()))
+        table, B, W = self._table(block_table)
+        q, ldq, ldqh = self._heads(Q, self.in_dtype, self.n_qh, B, "Q")
+        n_select = selected.shape[-1]
+        w, n, _ = self._paged_workspace(B, W)
+        _QUERY.pack_into(self._args, 0, q, ldq, ldqh, table, self._flat(length, i32, B, "length"), B, W, self._flat(selected, i32, B * self.n_kvh * n_select, "selected"),
+                         n_select, n_first, n_last, self.d_h ** -0.5 if scale is None else scale, 0, 0, 0, 0, self._flat(status, i32, 1, "status"), w, n)
+        _check(self.handle, self._L.pact_page_select(self.handle, ref, self._args_at, _stream()))
 
     def pact_paged_attention(self, cache: PagedCache, Q, block_table, length, out, lse=None, selected=None, scale=None, status=None):
         """Attention of one token per request, Q [B, n_qh, d_h] -> out [B, n_qh, d_h] (the context's output type), lse [B, n_qh] fp32, over the cached rows or
         those of the pages in selected [B, n_kvh, n_select]; scale: 1 / sqrt(d_h) if not given."""
+        i32 = torch.int32
         ref = self._cache(cache)
-        q, ldq, ldqh = self._heads(Q, self.in_dtype, self.n_qh, "Q")
-        o, ldo, ldoh = self._heads(out, self.out_dtype, self.n_qh, "out")
-        B, W = block_table.shape
-        if Q.shape[0] != B or out.shape[0] != B:
-            raise PactError("Q and out are [B, n_qh, d_h]")
-        n_select = 0
+        table, B, W = self._table(block_table)
+        q, ldq, ldqh = self._heads(Q, self.in_dtype, self.n_qh, B, "Q")
+        o, ldo, ldoh = self._heads(out, self.out_dtype, self.n_qh, B, "out")
+        n_select = sel = 0
         if selected is not None:
-            if selected.dim() != 3:
-                raise PactError("selected is [B, n_kvh, n_select]")
-            n_select = selected.shape[2]
-            selected = self._on_device(selected, torch.int32, (B, self.n_kvh, n_select), "selected")
-        w, n = self._paged_workspace(1, 1)
-        _check(self.handle, self._L.pact_paged_attention(
-            self.handle, ref, q, ldq, ldqh, B, self._on_device(block_table, torch.int32, (B, W), "block_table"), W, self._on_device(length, torch.int32, (B,), "length"),
-            selected, n_select, self.d_h ** -0.5 if scale is None else scale, o, ldo, ldoh, self._on_device(lse, torch.float32, (B, self.n_qh), "lse"),
-            self._on_device(status, torch.int32, (1,), "status"), w, n, _stream()))
+            n_select = selected.shape[-1]
+            sel = self._flat(selected, i32, B * self.n_kvh * n_select, "selected")
+        w, n, _ = self._paged_workspace(1, 1)
+        _QUERY.pack_into(self._args, 0, q, ldq, ldqh, table, self._flat(length, i32, B, "length"), B, W, sel, n_select, 0, 0, self.d_h ** -0.5 if scale is None else scale,
+                         o, ldo, ldoh, self._flat(lse, torch.float32, B * self.n_qh, "lse"), self._flat(status, i32, 1, "status"), w, n)
+        _check(self.handle, self._L.pact_paged_attention(self.handle, ref, self._args_at, _stream()))
 
     def set_wait_limits(self, barrier_polls: int = 0, center_sweeps: int = 0):
         """Bounds of the device-side waits (0 = default); see pact_set_wait_limits in pact.h."""

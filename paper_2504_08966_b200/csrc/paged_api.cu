@@ -49,20 +49,19 @@ size_t select_bytes(const pact_ctx *c, int requests, int pages) {
 
 extern "C" {
 
-pact_status pact_cache_plan(pact_ctx *ctx, int page_rows, int n_pages, int n_requests, int max_pages, int32_t *block_table, const int32_t *length,
-                            const int32_t *n_new, int64_t n_new_stride, int32_t *free_pages, const int32_t *n_free, int32_t *length_out,
-                            int32_t *n_free_out, int32_t *row_start, int64_t *slot, int64_t n_rows, int row_stride, int32_t *status, void *stream) {
-  const pact_status s = check_requests(ctx, page_rows, n_pages, n_requests, max_pages, block_table, length);
+pact_status pact_cache_plan(pact_ctx *ctx, const pact_plan *p, void *stream) {
+  if (!ctx || !p) return PACT_ERR_INVALID_ARG;
+  const pact_status s = check_requests(ctx, p->page_rows, p->n_pages, p->n_requests, p->max_pages, p->block_table, p->length);
   if (s != PACT_OK) return s;
-  if (!n_new || n_new_stride < 1 || !free_pages || !n_free || !length_out || !n_free_out) return PACT_ERR_INVALID_ARG;
-  if (n_rows < 0 || row_stride < 0 || (row_stride && n_rows != (int64_t)n_requests * row_stride)) return PACT_ERR_INVALID_ARG;
-  if (n_rows > INT32_MAX) return PACT_ERR_UNSUPPORTED;
+  if (!p->n_new || p->n_new_stride < 1 || !p->free_pages || !p->n_free || !p->length_out || !p->n_free_out) return PACT_ERR_INVALID_ARG;
+  if (p->n_rows < 0 || p->row_stride < 0 || (p->row_stride && p->n_rows != (int64_t)p->n_requests * p->row_stride)) return PACT_ERR_INVALID_ARG;
+  if (p->n_rows > INT32_MAX) return PACT_ERR_UNSUPPORTED;
   PlanArgs a;
   memset(&a, 0, sizeof(a));
-  a.table = block_table; a.length = length; a.n_new = n_new; a.n_new_stride = n_new_stride;
-  a.free_pages = free_pages; a.n_free = n_free; a.length_out = length_out; a.n_free_out = n_free_out;
-  a.row_start = row_start; a.slot = slot; a.n_rows = n_rows; a.status = status;
-  a.B = n_requests; a.width = max_pages; a.page = page_rows; a.n_pages = n_pages; a.row_stride = row_stride;
+  a.table = p->block_table; a.length = p->length; a.n_new = p->n_new; a.n_new_stride = p->n_new_stride;
+  a.free_pages = p->free_pages; a.n_free = p->n_free; a.length_out = p->length_out; a.n_free_out = p->n_free_out;
+  a.row_start = p->row_start; a.slot = p->slot; a.n_rows = p->n_rows; a.status = p->status;
+  a.B = p->n_requests; a.width = p->max_pages; a.page = p->page_rows; a.n_pages = p->n_pages; a.row_stride = p->row_stride;
   int launches = 0;
   CK(launch_cache_plan(a, ctx->dev.sm_count, (cudaStream_t)stream, &launches));
   ctx->launches += launches;
@@ -70,20 +69,19 @@ pact_status pact_cache_plan(pact_ctx *ctx, int page_rows, int n_pages, int n_req
   return PACT_OK;
 }
 
-pact_status pact_cache_write(pact_ctx *ctx, const pact_paged_cache *cache, const void *K_new, const void *V_new, int64_t ld_row, int64_t ld_head,
-                             const float *logw_new, const int64_t *slot, int64_t n_rows, int32_t *status, void *stream) {
-  if (!ctx || !on_device(ctx) || n_rows < 0) return PACT_ERR_INVALID_ARG;
+pact_status pact_cache_write(pact_ctx *ctx, const pact_paged_cache *cache, const pact_new_rows *r, void *stream) {
+  if (!ctx || !r || !on_device(ctx) || r->n_rows < 0) return PACT_ERR_INVALID_ARG;
   const pact_status s = check_cache(ctx, cache);
   if (s != PACT_OK) return s;
-  if (n_rows == 0) return PACT_OK;
-  if (!K_new || !V_new || !slot || !aligned16(K_new) || !aligned16(V_new) || !stride_ok(ctx, ld_row) || !stride_ok(ctx, ld_head)) return PACT_ERR_INVALID_ARG;
-  if (n_rows > INT32_MAX) return PACT_ERR_UNSUPPORTED;
+  if (r->n_rows == 0) return PACT_OK;
+  if (!r->K || !r->V || !r->slot || !aligned16(r->K) || !aligned16(r->V) || !stride_ok(ctx, r->ld_row) || !stride_ok(ctx, r->ld_head)) return PACT_ERR_INVALID_ARG;
+  if (r->n_rows > INT32_MAX) return PACT_ERR_UNSUPPORTED;
   if (ctx->d_h * ctx->elt > 4096) return PACT_ERR_UNSUPPORTED;   // (a CTA's threads have to hold a row)
   WriteArgs a;
-  a.Kn = K_new; a.Vn = V_new; a.ld_row = ld_row; a.ld_head = ld_head; a.logw_new = logw_new; a.slot = slot; a.n_rows = n_rows;
+  a.Kn = r->K; a.Vn = r->V; a.ld_row = r->ld_row; a.ld_head = r->ld_head; a.logw_new = r->logw; a.slot = r->slot; a.n_rows = r->n_rows;
   a.K = cache->K; a.V = cache->V; a.k_page = cache->k_page; a.k_head = cache->k_head; a.k_row = cache->k_row;
   a.v_page = cache->v_page; a.v_head = cache->v_head; a.v_row = cache->v_row;
-  a.logw = cache->logw; a.bounds = cache->bounds; a.w_max = cache->w_max; a.status = status;
+  a.logw = cache->logw; a.bounds = cache->bounds; a.w_max = cache->w_max; a.status = r->status;
   a.n_pages = cache->n_pages; a.page = cache->page_rows; a.n_kvh = ctx->n_kvh; a.d_h = ctx->d_h;
   CK(launch_cache_write(a, ctx->in == PACT_BF16, ctx->dev.sm_count, (cudaStream_t)stream));
   ctx->launches += 1;
@@ -97,24 +95,31 @@ size_t pact_paged_workspace_bytes(const pact_ctx *ctx, int max_requests, int max
   return x > y ? x : y;
 }
 
-pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache, const void *Q, int64_t ldQ, int64_t ldQh, int n_requests,
-                             const int32_t *block_table, int max_pages, const int32_t *length, float scale, int n_first, int n_last, int n_select,
-                             int32_t *selected, int32_t *status, void *ws, size_t ws_bytes, void *stream) {
-  if (!ctx || !cache) return PACT_ERR_INVALID_ARG;
-  pact_status s = check_requests(ctx, cache->page_rows, cache->n_pages, n_requests, max_pages, block_table, length);
+static pact_status check_query(const pact_ctx *ctx, const pact_paged_cache *cache, const pact_query *q) {
+  if (!ctx || !cache || !q) return PACT_ERR_INVALID_ARG;
+  pact_status s = check_requests(ctx, cache->page_rows, cache->n_pages, q->n_requests, q->max_pages, q->block_table, q->length);
   if (s == PACT_OK) s = check_cache(ctx, cache);
   if (s != PACT_OK) return s;
-  if (!cache->bounds || !Q || !selected || !aligned16(Q) || !stride_ok(ctx, ldQ) || !stride_ok(ctx, ldQh)) return PACT_ERR_INVALID_ARG;
-  if (!isfinite(scale) || n_first < 0 || n_last < 0 || n_select < 1 || n_first > n_select || n_last > n_select - n_first) return PACT_ERR_INVALID_ARG;
-  if (max_pages > kMaxSelectPages || !ctx->paged.blocks) return PACT_ERR_UNSUPPORTED;
-  s = check_ws(ws, ws_bytes, select_bytes(ctx, n_requests, max_pages));
+  if (!q->Q || !aligned16(q->Q) || !stride_ok(ctx, q->ldQ) || !stride_ok(ctx, q->ldQh) || !isfinite(q->scale)) return PACT_ERR_INVALID_ARG;
+  if (q->selected && q->n_select < 1) return PACT_ERR_INVALID_ARG;
+  return ctx->paged.blocks ? PACT_OK : PACT_ERR_UNSUPPORTED;
+}
+
+pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache, const pact_query *q, void *stream) {
+  pact_status s = check_query(ctx, cache, q);
+  if (s != PACT_OK) return s;
+  if (!cache->bounds || !q->selected || q->n_first < 0 || q->n_last < 0 || q->n_first > q->n_select || q->n_last > q->n_select - q->n_first)
+    return PACT_ERR_INVALID_ARG;
+  if (q->max_pages > kMaxSelectPages) return PACT_ERR_UNSUPPORTED;
+  s = check_ws(q->ws, q->ws_bytes, select_bytes(ctx, q->n_requests, q->max_pages));
   if (s != PACT_OK) return s;
   SelectArgs a;
-  a.Q = Q; a.ldQ = ldQ; a.ldQh = ldQh; a.bounds = cache->bounds; a.w_max = cache->w_max; a.table = block_table; a.length = length;
-  a.selected = selected; a.status = status; a.approx = (uint2 *)ws; a.keys = (unsigned long long *)ws + select_scores(ctx, n_requests, max_pages); a.scale = scale;
-  a.B = n_requests; a.width = max_pages; a.page = cache->page_rows; a.n_pages = cache->n_pages;
+  a.Q = q->Q; a.ldQ = q->ldQ; a.ldQh = q->ldQh; a.bounds = cache->bounds; a.w_max = cache->w_max; a.table = q->block_table; a.length = q->length;
+  a.selected = q->selected; a.status = q->status; a.scale = q->scale;
+  a.approx = (uint2 *)q->ws; a.keys = (unsigned long long *)q->ws + select_scores(ctx, q->n_requests, q->max_pages);
+  a.B = q->n_requests; a.width = q->max_pages; a.page = cache->page_rows; a.n_pages = cache->n_pages;
   a.n_kvh = ctx->n_kvh; a.group = ctx->n_qh / ctx->n_kvh; a.d_h = ctx->d_h;
-  a.n_first = n_first; a.n_last = n_last; a.n_select = n_select;
+  a.n_first = q->n_first; a.n_last = q->n_last; a.n_select = q->n_select;
   int launches = 0;
   CK(launch_page_select(a, ctx->in == PACT_BF16, (cudaStream_t)stream, &launches));
   ctx->launches += launches;
@@ -122,28 +127,21 @@ pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache, const
   return PACT_OK;
 }
 
-pact_status pact_paged_attention(pact_ctx *ctx, const pact_paged_cache *cache, const void *Q, int64_t ldQ, int64_t ldQh, int n_requests,
-                                 const int32_t *block_table, int max_pages, const int32_t *length, const int32_t *selected, int n_select, float scale,
-                                 void *out, int64_t ldO, int64_t ldOh, float *lse, int32_t *status, void *ws, size_t ws_bytes, void *stream) {
-  if (!ctx || !cache) return PACT_ERR_INVALID_ARG;
-  pact_status s = check_requests(ctx, cache->page_rows, cache->n_pages, n_requests, max_pages, block_table, length);
-  if (s == PACT_OK) s = check_cache(ctx, cache);
+pact_status pact_paged_attention(pact_ctx *ctx, const pact_paged_cache *cache, const pact_query *q, void *stream) {
+  pact_status s = check_query(ctx, cache, q);
   if (s != PACT_OK) return s;
   const size_t oe = ctx->out == PACT_BF16 ? 2 : 4;
-  if (!Q || !out || !aligned16(Q) || reinterpret_cast<uintptr_t>(out) % (4 * oe) != 0 || !stride_ok(ctx, ldQ) || !stride_ok(ctx, ldQh)) return PACT_ERR_INVALID_ARG;
-  if (ldO < ctx->d_h || ldOh < ctx->d_h || ldO % 4 != 0 || ldOh % 4 != 0) return PACT_ERR_INVALID_ARG;
-  if (!isfinite(scale) || (selected && n_select < 1)) return PACT_ERR_INVALID_ARG;
-  if (!ctx->paged.blocks) return PACT_ERR_UNSUPPORTED;
-  const int64_t rows = (int64_t)(selected && n_select < max_pages ? n_select : max_pages) * cache->page_rows;
-  if (n_requests * ((rows + 63) / 64) > INT32_MAX) return PACT_ERR_UNSUPPORTED;
+  if (!q->out || reinterpret_cast<uintptr_t>(q->out) % (4 * oe) != 0) return PACT_ERR_INVALID_ARG;
+  if (q->ldO < ctx->d_h || q->ldOh < ctx->d_h || q->ldO % 4 != 0 || q->ldOh % 4 != 0) return PACT_ERR_INVALID_ARG;
+  const int64_t rows = (int64_t)(q->selected && q->n_select < q->max_pages ? q->n_select : q->max_pages) * cache->page_rows;
+  if (q->n_requests * ((rows + 63) / 64) > INT32_MAX) return PACT_ERR_UNSUPPORTED;
   AttendArgs a;
   memset(&a, 0, sizeof(a));
-  s = check_ws(ws, ws_bytes, attend_scratch(ctx->paged, ctx->dev, ctx->in == PACT_BF16, &a, (char *)ws));
+  s = check_ws(q->ws, q->ws_bytes, attend_scratch(ctx->paged, ctx->dev, ctx->in == PACT_BF16, &a, (char *)q->ws));
   if (s != PACT_OK) return s;
-  a.Q = Q; a.ldQ = ldQ; a.ldQh = ldQh; a.logw = cache->logw; a.table = block_table; a.length = length; a.selected = selected;
-  a.out = out; a.ldO = ldO; a.ldOh = ldOh; a.lse = lse; a.status = status;
-  a.scale = scale;
-  a.B = n_requests; a.width = max_pages; a.page = cache->page_rows; a.n_pages = cache->n_pages; a.n_select = selected ? n_select : 0;
+  a.Q = q->Q; a.ldQ = q->ldQ; a.ldQh = q->ldQh; a.logw = cache->logw; a.table = q->block_table; a.length = q->length; a.selected = q->selected;
+  a.out = q->out; a.ldO = q->ldO; a.ldOh = q->ldOh; a.lse = q->lse; a.status = q->status; a.scale = q->scale;
+  a.B = q->n_requests; a.width = q->max_pages; a.page = cache->page_rows; a.n_pages = cache->n_pages; a.n_select = q->selected ? q->n_select : 0;
   a.n_kvh = ctx->n_kvh; a.group = ctx->n_qh / ctx->n_kvh; a.d_h = ctx->d_h; a.out_bf16 = ctx->out == PACT_BF16;
   int launches = 0;
   CK(launch_attend(a, *cache, ctx->paged, ctx->dev, ctx->in == PACT_BF16, (cudaStream_t)stream, &launches));

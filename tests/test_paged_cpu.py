@@ -24,18 +24,41 @@ def _run(tmp_path, text, cmd):
     return r.stdout
 
 
-def test_cache_struct_layout(tmp_path):
+def test_struct_layouts(tmp_path):
+    """The binding packs the three argument structs with the struct module and the cache with ctypes."""
     from paper_2504_08966_b200 import binding
     out = _run(tmp_path, r"""
 #include <stdio.h>
 #include <stddef.h>
+#include <string.h>
 #include "pact.h"
+template <typename T> void dump(const T &x) {
+  for (size_t i = 0; i < sizeof(x); ++i) printf("%02x", ((const unsigned char *)&x)[i]);
+  printf("\n");
+}
+#define P(n) ((char *)0 + n)
 int main() {
-  printf("%zu %zu %zu %zu %zu %zu %zu\n", sizeof(pact_paged_cache), offsetof(pact_paged_cache, k_row), offsetof(pact_paged_cache, v_page),
-         offsetof(pact_paged_cache, logw), offsetof(pact_paged_cache, bounds), offsetof(pact_paged_cache, w_max), offsetof(pact_paged_cache, page_rows));
-}""", ["g++", "-I", os.path.join(ROOT, "include")])
-    D = binding.PagedCacheDesc
-    assert [int(x) for x in out.split()] == [C.sizeof(D), D.k_row.offset, D.v_page.offset, D.logw.offset, D.bounds.offset, D.w_max.offset, D.page_rows.offset]
+  pact_paged_cache c; memset(&c, 0, sizeof c);
+  c.K = P(1); c.V = P(2); c.k_page = 3; c.k_head = 4; c.k_row = 5; c.v_page = 6; c.v_head = 7; c.v_row = 8; c.logw = (float *)P(9); c.bounds = P(10); c.w_max = (float *)P(11);
+  c.n_pages = 12; c.page_rows = 13;
+  dump(c);
+  pact_plan p; memset(&p, 0, sizeof p);
+  p.page_rows = 1; p.n_pages = 2; p.n_requests = 3; p.max_pages = 4; p.block_table = (int32_t *)P(5); p.length = (int32_t *)P(6); p.n_new = (int32_t *)P(7); p.n_new_stride = 8;
+  p.free_pages = (int32_t *)P(9); p.n_free = (int32_t *)P(10); p.length_out = (int32_t *)P(11); p.n_free_out = (int32_t *)P(12); p.row_start = (int32_t *)P(13); p.slot = (int64_t *)P(14);
+  p.n_rows = 15; p.row_stride = 16; p.status = (int32_t *)P(18);
+  dump(p);
+  pact_new_rows r; memset(&r, 0, sizeof r);
+  r.K = P(1); r.V = P(2); r.ld_row = 3; r.ld_head = 4; r.logw = (float *)P(5); r.slot = (int64_t *)P(6); r.n_rows = 7; r.status = (int32_t *)P(8);
+  dump(r);
+  pact_query q; memset(&q, 0, sizeof q);
+  q.Q = P(1); q.ldQ = 2; q.ldQh = 3; q.block_table = (int32_t *)P(4); q.length = (int32_t *)P(5); q.n_requests = 6; q.max_pages = 7; q.selected = (int32_t *)P(8); q.n_select = 9;
+  q.n_first = 10; q.n_last = 11; q.scale = 12; q.out = P(13); q.ldO = 14; q.ldOh = 15; q.lse = (float *)P(16); q.status = (int32_t *)P(17); q.ws = P(18); q.ws_bytes = 19;
+  dump(q);
+}""", ["g++", "-I", os.path.join(ROOT, "include")]).split()
+    assert bytes(binding.PagedCacheDesc(*range(1, 14))).hex() == out[0]
+    assert binding._PLAN.pack(*range(1, 17), 0, 18).hex() == out[1]
+    assert binding._NEW_ROWS.pack(*range(1, 9)).hex() == out[2]
+    assert binding._QUERY.pack(*range(1, 20)).hex() == out[3]
 
 
 def test_status_text():
@@ -157,9 +180,14 @@ int main() {
   ok.ctx = &ctx;
   ok.c = {buf, buf, 2 * 32 * 128, 32 * 128, 128, 2 * 32 * 128, 32 * 128, 128, (float *)buf, buf, (float *)buf, 8, 32};
   const auto cache = [](Args &x) { return x.cache_null ? nullptr : &x.c; };
+  const auto query = [](Args &x) {
+    return pact_query{x.q, x.ldq, x.ldqh, x.table, x.length, x.B, x.width, x.sel, x.n_select, x.n_first, x.n_last, x.scale, x.out, x.ldo, x.ldoh, nullptr, nullptr, x.ws, x.ws_bytes};
+  };
+  if (pact_paged_attention(&ctx, nullptr, nullptr, nullptr) != -1 || pact_page_select(&ctx, nullptr, nullptr, nullptr) != -1 || pact_cache_write(&ctx, nullptr, nullptr, nullptr) != -1 ||
+      pact_cache_plan(&ctx, nullptr, nullptr) != -1)
+    return 1;
   // ---- attention
-  ok.f = [&](Args &x) { return pact_paged_attention(x.ctx, cache(x), x.q, x.ldq, x.ldqh, x.B, x.table, x.width, x.length, x.sel, x.n_select, x.scale, x.out, x.ldo, x.ldoh,
-                                                    nullptr, nullptr, x.ws, x.ws_bytes, nullptr); };
+  ok.f = [&](Args &x) { const pact_query q = query(x); return pact_paged_attention(x.ctx, cache(x), &q, nullptr); };
   want("attention", ok.call(), PACT_OK, 1);
   { Args x = ok; x.sel = nullptr; x.n_select = 0; want("no list", x.call(), PACT_OK, 1); }
   { Args x = ok; x.c.bounds = nullptr; x.c.w_max = nullptr; x.c.logw = nullptr; want("no biases", x.call(), PACT_OK, 1); }
@@ -186,22 +214,21 @@ int main() {
   common(true);
   REFUSED(x.out = nullptr, PACT_ERR_INVALID_ARG) REFUSED(x.out = buf + 4, PACT_ERR_INVALID_ARG) REFUSED(x.ldo = 100, PACT_ERR_INVALID_ARG) REFUSED(x.ldoh = 130, PACT_ERR_INVALID_ARG)
   // ---- selection
-  ok.f = [&](Args &x) { return pact_page_select(x.ctx, cache(x), x.q, x.ldq, x.ldqh, x.B, x.table, x.width, x.length, x.scale, x.n_first, x.n_last, x.n_select, x.sel, nullptr, x.ws,
-                                                x.ws_bytes, nullptr); };
+  ok.f = [&](Args &x) { const pact_query q = query(x); return pact_page_select(x.ctx, cache(x), &q, nullptr); };
   want("selection", ok.call(), PACT_OK, 1);
   common(true);
   REFUSED(x.sel = nullptr, PACT_ERR_INVALID_ARG) REFUSED(x.n_first = -1, PACT_ERR_INVALID_ARG) REFUSED(x.n_last = 3, PACT_ERR_INVALID_ARG) REFUSED(x.n_first = 1 << 30; x.n_last = 1 << 30, PACT_ERR_INVALID_ARG)
   REFUSED(x.width = 65537, PACT_ERR_UNSUPPORTED) REFUSED(x.c.bounds = nullptr; x.c.w_max = nullptr, PACT_ERR_INVALID_ARG)
   // ---- writing
-  ok.f = [&](Args &x) { return pact_cache_write(x.ctx, cache(x), x.q, x.out, x.ldq, x.ldqh, nullptr, x.slot, x.n_rows, nullptr, nullptr); };
+  ok.f = [&](Args &x) { const pact_new_rows r = {x.q, x.out, x.ldq, x.ldqh, nullptr, x.slot, x.n_rows, nullptr}; return pact_cache_write(x.ctx, cache(x), &r, nullptr); };
   want("writing", ok.call(), PACT_OK, 1);
   { Args x = ok; x.n_rows = 0; x.q = nullptr; want("no rows", x.call(), PACT_OK, 0); }
   common(false);
   REFUSED(x.q = nullptr, PACT_ERR_INVALID_ARG) REFUSED(x.out = buf + 4, PACT_ERR_INVALID_ARG) REFUSED(x.slot = nullptr, PACT_ERR_INVALID_ARG) REFUSED(x.n_rows = -1, PACT_ERR_INVALID_ARG)
   REFUSED(x.ldq = 64, PACT_ERR_INVALID_ARG) REFUSED(x.n_rows = 1ll << 31, PACT_ERR_UNSUPPORTED)
   // ---- planning
-  ok.f = [&](Args &x) { return pact_cache_plan(x.ctx, x.page, x.n_pages, x.B, x.width, x.table, x.length, x.n_new, x.new_stride, x.free_pages, x.n_free, x.length_out, x.n_free_out, nullptr,
-                                               x.slot, x.n_rows, x.row_stride, nullptr, nullptr); };
+  ok.f = [&](Args &x) { const pact_plan p = {x.page, x.n_pages, x.B, x.width, x.table, x.length, x.n_new, x.new_stride, x.free_pages, x.n_free, x.length_out, x.n_free_out, nullptr,
+                                              x.slot, x.n_rows, x.row_stride, 0, nullptr}; return pact_cache_plan(x.ctx, &p, nullptr); };
   want("planning", ok.call(), PACT_OK, 1);
   { Args x = ok; x.slot = nullptr; want("no slots", x.call(), PACT_OK, 1); }
   { Args x = ok; x.row_stride = 4; want("padded", x.call(), PACT_OK, 1); }
@@ -225,7 +252,8 @@ def _stub_context(n_qh=4, n_kvh=2, d_h=64):
     ctx._L, ctx.handle = binding.lib(), C.c_void_p()
     ctx.n_qh, ctx.n_kvh, ctx.d_h, ctx.in_dtype, ctx.out_dtype, ctx.device = n_qh, n_kvh, d_h, torch.bfloat16, torch.float32, -1
     ctx._paged_ws, ctx._paged_need = [], {}
-    ctx._paged_workspace = lambda B, W: (0, 0)
+    ctx._paged_workspace = lambda B, W: (0, 0, None)
+    ctx._make_args()
     return ctx
 
 
@@ -258,13 +286,14 @@ def test_refusals_of_the_binding(monkeypatch):
     refused(ctx.pact_paged_attention, cache, Q, table, length, out, word=null)
     refused(ctx.pact_paged_attention, cache, Q, table, length, out, selected=sel, word=null)
     refused(ctx.pact_page_select, cache, Q, table, length, sel, word=null)
-    for change in (dict(Q=Q.float()), dict(Q=Q[:, :3]), dict(Q=Q[..., :32]), dict(table=table.long()), dict(table=table.t().contiguous().t()), dict(length=length[:2]),
+    for change in (dict(Q=Q.float()), dict(Q=Q[:, :3]), dict(Q=Q[..., :32]), dict(table=table.long()), dict(table=table[0]), dict(table=table.t().contiguous().t()), dict(length=length[:2]),
                    dict(length=length.long()), dict(out=out.to(bf)), dict(out=out[:, :2]), dict(lse=torch.zeros(3, 5)), dict(selected=sel[:, :1]), dict(selected=sel.long()),
                    dict(status=torch.zeros(2, dtype=i32))):
         kw = dict(Q=Q, table=table, length=length, out=out, lse=None, selected=None, status=None)
         kw.update(change)
         refused(ctx.pact_paged_attention, cache, kw["Q"], kw["table"], kw["length"], kw["out"], lse=kw["lse"], selected=kw["selected"], status=kw["status"])
-    refused(ctx.pact_paged_attention, cache, Q[:2], table, length, out, word="B, n_qh")
+    refused(ctx.pact_paged_attention, cache, Q[:2], table, length, out)
+    refused(ctx.pact_paged_attention, cache, Q, table, length, out[:2])
     refused(ctx.pact_paged_attention, turned, Q.transpose(1, 2).contiguous().transpose(1, 2), table, length, out, word="last axis")
     refused(_stub_context(n_kvh=1).pact_paged_attention, cache, Q, table, length, out, word="not one of")
     refused(ctx.pact_page_select, cache, Q, table, length, sel[:2])
@@ -272,7 +301,7 @@ def test_refusals_of_the_binding(monkeypatch):
     refused(ctx.pact_cache_write, cache, rows, rows, None, slot, word=null)
     refused(ctx.pact_cache_write, cache, rows, rows, None, slot.int())
     refused(ctx.pact_cache_write, cache, rows, rows, torch.zeros(6), slot)
-    refused(ctx.pact_cache_write, cache, rows, torch.zeros(7, 2, 128, dtype=bf)[..., :64], None, slot, word="same shape and strides")
+    refused(ctx.pact_cache_write, cache, rows, torch.zeros(7, 2, 128, dtype=bf)[..., :64], None, slot, word="same strides")
     refused(ctx.pact_cache_write, cache, rows[:, :1], rows[:, :1], None, slot)
     one_i = torch.zeros(1, dtype=i32)
 
@@ -287,8 +316,8 @@ def test_refusals_of_the_binding(monkeypatch):
     refused(plan, n_new=torch.zeros(3, 16, dtype=i32)[:, 0], word=null)
     refused(plan, slot=None)
     refused(plan, n_rows=9, word="length of slot")
-    refused(plan, n_new=length[:2], word="n_new is")
-    refused(plan, n_new=length.long(), word="n_new an int32")
+    refused(plan, n_new=length[:2])
+    refused(plan, n_new=length.long())
     refused(plan, length_out=length[:2])
     refused(plan, row_start=length)
     refused(plan, slot=slot.int())
@@ -303,8 +332,8 @@ def test_workspaces_that_are_outgrown_are_kept(monkeypatch):
     monkeypatch.setattr(type(ctx), "_cuda", lambda self: torch.device("cpu"))
     ctx._paged_need.update(sizes)
     got = [ctx._paged_workspace(*k) for k in ((1, 1), (4, 4), (1, 1), (9, 9), (4, 4))]
-    assert [n for _, n in got] == [1000, 2000, 2000, 9000, 9000]
-    assert len({a for a, _ in got}) == 3 and len(ctx._paged_ws) == 3
+    assert [n for _, n, _ in got] == [1000, 2000, 2000, 9000, 9000]
+    assert len({a for a, _, _ in got}) == 3 and len(ctx._paged_ws) == 3
 
 
 # ---- pins of the plain implementations ------------------------------------------------------------------------------
