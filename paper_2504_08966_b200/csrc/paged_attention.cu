@@ -8,7 +8,9 @@
 // Split.  The rows of all requests and key heads, in tiles of 64, form one line of T tiles that G CTAs share out evenly: CTA i takes tiles
 // [i T / G, (i + 1) T / G).  No length, batch or number of heads leaves SMs idle, at most G - 1 cuts are made in all, and k_attend_join puts
 // the parts of what was cut together.  The shares follow from prefix sums over the lengths, which every CTA forms itself: lengths are known on
-// the device only.
+// the device only.  (Smaller units behind shares of four fifths, which CTAs took over as they were done: the CTAs ended within 3 us instead of
+// 9, but no earlier, since HBM was busy all the time, and the more parts cost the join 3 to 25 us.)
+// Short tables and few requests: a cluster of CTAs per request and key head instead, which put their parts together through shared memory.
 //
 // Pipeline.  One warp copies: each lane works out page ids and row counts of one tile, 32 tiles at a time, and tiles arrive as boxes of
 // 128-byte columns through the tensor-copy unit (swizzled, so that ldmatrix meets no bank conflicts) in a ring that runs on across requests.
@@ -32,12 +34,23 @@ constexpr int kMaxAttendStages = 8;
 constexpr int kBoxBytes = 128;             // columns of a box
 constexpr int kBlockBytes = kTile * kBoxBytes;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxCluster = 16;
+constexpr int kClusterTiles = 8;           // most tiles of a CTA of a cluster
 constexpr int kScratch = kRowsOfWarp * 8 + 8;   // fp32: floats of a warp for probabilities and factors
+
+// What the copying warp has worked out about a tile.
+struct __align__(16) TilePlan {
+  int id[4];                               // page of every 16 rows
+  uint32_t rows, place;                    // rows that count of every 16, their place in the page in 16 rows: a byte each
+  uint32_t bytes;                          // to be copied
+  int first;                               // the first of its part of a request
+  int b, h;
+};
 
 // Offsets in dynamic shared memory (the ring comes first: swizzled boxes lie at multiples of 1024 bytes).
 struct AttendSmem {
   int stage;                               // bytes of K and V of a stage
-  int bias, q, q_row, q_own, slots, ml, meta, bars, pre, total;
+  int bias, q, q_row, q_own, slots, ml, tiles, bars, meta, pre, total;
 };
 __host__ __device__ inline AttendSmem attend_smem(int stages, int blocks, int heads, int elt, int B) {
   AttendSmem m;
@@ -48,9 +61,10 @@ __host__ __device__ inline AttendSmem attend_smem(int stages, int blocks, int he
   m.q_own = m.q + stages * heads * m.q_row;
   m.slots = m.q_own + (elt == 4 ? heads * m.q_row : 0);
   m.ml = m.slots + 2 * heads * (blocks * kBoxBytes / elt + 4) * 4;
-  m.bars = m.ml + kConsumers * heads * 8;
-  m.meta = m.bars + (2 * stages + 1) * 8;
-  m.pre = m.meta + stages * 4;
+  m.tiles = m.ml + kConsumers * heads * 8;
+  m.bars = m.tiles + 32 * (int)sizeof(TilePlan);
+  m.meta = m.bars + 2 * stages * 8;
+  m.pre = m.meta + stages * 4 + 4;
   m.total = m.pre + (B + 1 + kAttendThreads / 32) * 4;
   return m;
 }
@@ -84,6 +98,32 @@ __device__ __forceinline__ float fma4(const float4 &x, const float4 &y, float s)
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t in_cta(const void *p, uint32_t rank) {   // the same place in the shared memory of another CTA of the cluster
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 ld_cluster2(uint32_t at) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+  return v;
 }
 
 __device__ __forceinline__ void consumers_meet() { asm volatile("bar.sync 1, %0;" ::"n"(kConsumers * 32) : "memory"); }
@@ -403,17 +443,19 @@ __device__ __forceinline__ void store4(const AttendArgs &a, int b, int head, int
 
 constexpr int attend_ctas(int blocks, int tiles_of_heads) { return blocks <= 2 && tiles_of_heads == 1 ? 2 : 1; }   // of an SM
 
-template <typename T, int NB, int NT>
+// CLUSTER: CTA (rank, key head and head tile, request) has a share of that request's tiles alone.
+template <typename T, int NB, int NT, bool CLUSTER>
 __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
     k_attend(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendArgs a) {
   using P = Part<T, NB, NT>;
   extern __shared__ __align__(1024) char sm[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const AttendSmem at = attend_smem(a.stages, NB, P::kHeads, sizeof(T), a.B);
+  const AttendSmem at = attend_smem(a.stages, NB, P::kHeads, sizeof(T), CLUSTER ? 1 : a.B);
   uint64_t *full = reinterpret_cast<uint64_t *>(sm + at.bars), *empty = full + a.stages;
-  int *abort = reinterpret_cast<int *>(empty + a.stages);
   uint32_t *meta = reinterpret_cast<uint32_t *>(sm + at.meta);
-  int *pre = reinterpret_cast<int *>(sm + at.pre), *w_sum = pre + a.B + 1;
+  int *abort = reinterpret_cast<int *>(meta + a.stages);
+  int *pre = reinterpret_cast<int *>(sm + at.pre), *w_sum = pre + (CLUSTER ? 1 : a.B) + 1;
+  TilePlan *plan = reinterpret_cast<TilePlan *>(sm + at.tiles);
   if (tid < a.stages) {
     mbar_init(full + tid, 1);
     mbar_init(empty + tid, kConsumers);
@@ -423,25 +465,39 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
   for (int i = tid * 16; i < at.q_own - at.q; i += kAttendThreads * 16) *reinterpret_cast<uint4 *>(sm + at.q + i) = make_uint4(0, 0, 0, 0);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  // what this lane copies of a tile: box `x` of rows, and of it a 128-byte block of K or V, or the biases
+  const int boxes = kTile / a.box_rows, per_box = a.box_rows / kRowsOfWarp, copies = 2 * NB + (a.logw ? 1 : 0);
+  constexpr int kRoles = (4 * (2 * NB + 1) + 31) / 32;
+  int my_box[kRoles], my_copy[kRoles];
+#pragma unroll
+  for (int r = 0; r < kRoles; ++r) {
+    my_box[r] = (lane + 32 * r) / copies;
+    my_copy[r] = lane + 32 * r - my_box[r] * copies;
+  }
 
   pdl_wait();
   pdl_trigger();
-  // tiles before each request, of one key head
   const long long room = (long long)a.width * a.page;
-  const auto rows_of = [&](int b) {
-    const int len = a.length[b];
-    return len < 0 ? 0 : len > room ? (int)room : len;
-  };
-  const auto tiles_of = [&](int b) {
-    return tiles_of_request(rows_of(b), a.page, a.selected != nullptr, a.n_select);
-  };
+  const auto rows_of = [&](int len) { return len < 0 ? 0 : len > room ? (int)room : len; };
+  const auto tiles_of = [&](int len) { return tiles_of_request(rows_of(len), a.page, a.selected != nullptr, a.n_select); };
   const int Hn = a.n_kvh * a.head_tiles;
-  {
+  if constexpr (CLUSTER) {
+    const int b = blockIdx.z, len = a.length[b];
+    if (tid == 0) {
+      pre[0] = 0;
+      pre[1] = tiles_of(len);
+      if (blockIdx.x == 0 && blockIdx.y == 0 && a.status && (len < 0 || len > room)) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
+    }
+    __syncthreads();
+  } else {
+    // tiles before each request, of one key head
     const int per = (a.B + kAttendThreads - 1) / kAttendThreads, b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
     int mine = 0;
     for (int b = b0; b < b1; ++b) {
-      mine += tiles_of(b);
-      if (blockIdx.x == 0 && a.status && (a.length[b] < 0 || a.length[b] > room)) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
+      const int len = a.length[b], n = tiles_of(len);
+      if (blockIdx.x == 0 && a.status && (len < 0 || len > room)) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
+      pre[b] = mine;
+      mine += n;
     }
     int x = mine;
 #pragma unroll
@@ -453,73 +509,78 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
     __syncthreads();
     int sum = x - mine;
     for (int w = 0; w < warp; ++w) sum += w_sum[w];
-    for (int b = b0; b < b1; ++b) {
-      pre[b] = sum;
-      sum += tiles_of(b);
-    }
+    for (int b = b0; b < b1; ++b) pre[b] += sum;
+    sum += mine;
     if (b0 < a.B && b1 == a.B) pre[a.B] = sum;
     __syncthreads();
   }
-  const long long T_all = (long long)pre[a.B] * Hn;
-  const long long G = min((long long)gridDim.x, T_all);
-  const long long me = blockIdx.x;
+  // this CTA's tiles
+  const long long T_all = CLUSTER ? pre[1] : (long long)pre[a.B] * Hn;
+  const long long G = CLUSTER ? cluster_size() : min((long long)gridDim.x, T_all), me = CLUSTER ? cluster_rank() : blockIdx.x;
   const long long t0 = me < G ? share_begin(me, G, T_all) : T_all, t1 = me < G ? share_begin(me + 1, G, T_all) : T_all;
-  // requests without any row
-  for (int b = blockIdx.x; b < a.B; b += gridDim.x)
-    if (pre[b + 1] == pre[b]) {
-      for (int i = tid * 4; i < a.n_kvh * a.group * a.d_h; i += kAttendThreads * 4) store4(a, b, i / a.d_h, i % a.d_h, make_float4(0.f, 0.f, 0.f, 0.f));
-      if (a.lse)
-        for (int i = tid; i < a.n_kvh * a.group; i += kAttendThreads) a.lse[(long long)b * a.n_kvh * a.group + i] = -INFINITY;
-    }
   // where tile t lies: request, key head and head tile, place
   const auto find = [&](long long t, int &b, int &h, int &j) {
-    int lo = 0, hi = a.B;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if ((long long)pre[mid] * Hn <= t) lo = mid;
-      else hi = mid;
+    if constexpr (CLUSTER) {
+      b = blockIdx.z;
+      h = blockIdx.y;
+      j = (int)t;
+    } else {
+      int lo = 0, hi = a.B;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((long long)pre[mid] * Hn <= t) lo = mid;
+        else hi = mid;
+      }
+      b = lo;
+      h = divide_small(t - (long long)pre[lo] * Hn, pre[lo + 1] - pre[lo], &j);
     }
-    b = lo;
-    const long long u = t - (long long)pre[lo] * Hn;
-    const int n = pre[lo + 1] - pre[lo];
-    h = (int)(u / n);
-    j = (int)(u - (long long)h * n);
   };
+  if constexpr (CLUSTER) {
+    if (t0 == t1 && tid < P::kHeads) reinterpret_cast<float2 *>(sm + at.ml)[2 * P::kHeads + tid] = make_float2(-INFINITY, 0.f);   // this CTA has no part
+  } else {
+    // requests without any row
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x)
+      if (pre[b + 1] == pre[b]) {
+        for (int i = tid * 4; i < a.n_kvh * a.group * a.d_h; i += kAttendThreads * 4) store4(a, b, i / a.d_h, i % a.d_h, make_float4(0.f, 0.f, 0.f, 0.f));
+        if (a.lse)
+          for (int i = tid; i < a.n_kvh * a.group; i += kAttendThreads) a.lse[(long long)b * a.n_kvh * a.group + i] = -INFINITY;
+      }
+    if (t0 == t1 && tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+  }
 
-  if (t0 == t1) {
-    if (tid == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
-  } else if (warp == kConsumers) {
+  if (warp == kConsumers) {
     // ---- the copying warp ----
     int st = 0;
     uint32_t ph = 0;
     bool given_up = false;
-    const int boxes = kTile / a.box_rows, per_box = a.box_rows / kRowsOfWarp, copies = 2 * NB + (a.logw ? 1 : 0);
     for (long long base = t0; base < t1 && !given_up; base += 32) {
       const int n = (int)min(32ll, t1 - base);
-      int b = 0, h = 0, j = 0, id[4] = {-1, -1, -1, -1}, off[4] = {0, 0, 0, 0};   // page and place of every 16 rows
-      uint32_t rows = 0;                                       // rows that count of every 16, a byte each
       if (lane < n) {
+        int b, h, j;
         find(base + lane, b, h, j);
-        const int kv = h / a.head_tiles;
-        const TileRows at_rows = locate_rows(j, rows_of(b), a.page, per_box, a.table + (long long)b * a.width, a.n_pages,
+        const int kv = h / a.head_tiles, ht = h - kv * a.head_tiles;
+        const TileRows at_rows = locate_rows(j, rows_of(a.length[b]), a.page, per_box, a.table + (long long)b * a.width, a.n_pages,
                                              a.selected ? a.selected + ((long long)b * a.n_kvh + kv) * a.n_select : nullptr, a.n_select);
-        rows = at_rows.rows;
+        if (at_rows.bad && a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
+        TilePlan p;
+        p.rows = at_rows.rows;
+        p.place = 0;
+        p.first = j == 0 || base + lane == t0;
+        p.bytes = p.first ? min(P::kHeads, a.group - ht * P::kHeads) * a.d_h * (int)sizeof(T) : 0;
+        p.b = b;
+        p.h = h;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          id[g] = at_rows.id[g];
-          off[g] = at_rows.off[g];
+          p.id[g] = at_rows.id[g];
+          p.place |= (uint32_t)(at_rows.off[g] / kRowsOfWarp) << (8 * g);
+          // a box is copied if any of its rows counts: its first 16 do then
+          if (g % per_box == 0 && (at_rows.rows >> (8 * g) & 0xffu)) p.bytes += a.box_rows * (2 * NB * kBoxBytes + (a.logw ? 4 : 0));
         }
-        if (at_rows.bad && a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
+        plan[lane] = p;
       }
+      __syncwarp();
       for (int i = 0; i < n; ++i) {
-        const uint32_t rows_i = __shfl_sync(0xffffffffu, rows, i);
-        const int bi = __shfl_sync(0xffffffffu, b, i), hi = __shfl_sync(0xffffffffu, h, i), ji = __shfl_sync(0xffffffffu, j, i);
-        const int kv = hi / a.head_tiles, ht = hi - kv * a.head_tiles;
-        const bool first = base + i == t0 || ji == 0;
-        const int heads = min(P::kHeads, a.group - ht * P::kHeads);
-        uint32_t load = 0;                                     // a box is copied if any of its rows counts: its first 16 do then
-        for (int x = 0; x < boxes; ++x)
-          if (rows_i >> (8 * x * per_box) & 0xffu) load |= 1u << x;
+        const uint32_t rows = plan[i].rows, place = plan[i].place;
         if (!mbar_wait_warp(empty + st, ph ^ 1)) {
           given_up = true;
           if (lane == 0) {
@@ -529,65 +590,63 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
           break;
         }
         if (lane == 0) {
-          meta[st] = rows_i;
-          mbar_arrive_expect_tx(full + st, (uint32_t)(__popc(load) * a.box_rows * (2 * NB * kBoxBytes + (a.logw ? 4 : 0)) + (first ? heads * a.d_h * (int)sizeof(T) : 0)));
+          meta[st] = rows;
+          mbar_arrive_expect_tx(full + st, plan[i].bytes);
         }
         __syncwarp();
-        char *stage = sm + st * at.stage;
-        for (int c = lane; c < ((boxes * copies + 31) & ~31); c += 32) {
-          const int x = min(c / copies, boxes - 1), k = c - x * copies, g = x * per_box;
-          int page = 0, row = 0;
+        const int h = plan[i].h, kv = h / a.head_tiles;
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {                        // (each lane wants another register of lane i)
-            const int p = __shfl_sync(0xffffffffu, id[y], i), o = __shfl_sync(0xffffffffu, off[y], i);
-            if (y == g) {
-              page = p;
-              row = o;
-            }
-          }
-          if (k < copies && (load >> x & 1)) {
+        for (int r = 0; r < kRoles; ++r) {
+          const int x = my_box[r], k = my_copy[r], g = 8 * x * per_box;
+          if (x < boxes && (rows >> g & 0xffu)) {
+            const int page = plan[i].id[x * per_box], row = (int)(place >> g & 0xffu) * kRowsOfWarp;
             if (k < 2 * NB) {
-              char *to = stage + k * kBlockBytes + x * a.box_rows * kBoxBytes;
+              char *to = sm + st * at.stage + k * kBlockBytes + x * a.box_rows * kBoxBytes;
               tma_load_4d(to, k < NB ? &map_k : &map_v, full + st, (k < NB ? k : k - NB) * (kBoxBytes / (int)sizeof(T)), row, kv, page);
             } else {
               bulk_load(sm + at.bias + (st * kTile + x * a.box_rows) * 4, a.logw + (long long)page * a.page + row, a.box_rows * 4, full + st);
             }
           }
         }
-        if (first && lane < heads) {
-          const T *q = static_cast<const T *>(a.Q) + bi * a.ldQ + (long long)(kv * a.group + ht * P::kHeads + lane) * a.ldQh;
-          bulk_load(sm + at.q + (st * P::kHeads + lane) * at.q_row, q, a.d_h * (int)sizeof(T), full + st);
+        if (plan[i].first) {
+          const int ht = h - kv * a.head_tiles;
+          if (lane < min(P::kHeads, a.group - ht * P::kHeads)) {
+            const T *q = static_cast<const T *>(a.Q) + plan[i].b * a.ldQ + (long long)(kv * a.group + ht * P::kHeads + lane) * a.ldQh;
+            bulk_load(sm + at.q + (st * P::kHeads + lane) * at.q_row, q, a.d_h * (int)sizeof(T), full + st);
+          }
         }
-        __syncwarp();
         if (++st == a.stages) {
           st = 0;
           ph ^= 1;
         }
       }
+      __syncwarp();
     }
   } else {
     // ---- the computing warps ----
     P part;
     int st = 0;
     uint32_t ph = 0;
-    int b, h, j;
-    find(t0, b, h, j);
-    if (tid == 0) {                                            // what the CTAs before this one have of the request at t0
-      int4 d = make_int4(0, 0, 0, 0);
-      if (j > 0) {
-        const long long ts = t0 - j, te = ts + (pre[b + 1] - pre[b]);
-        const long long i0 = share_of(ts, G, T_all), i1 = share_of(te - 1, G, T_all);
-        if (i0 == me - 1) d = make_int4(ts == share_begin(i0, G, T_all) ? 1 : 2, (int)i1, b, h);
-      }
-      a.desc[blockIdx.x] = d;
-    }
     float *slots = reinterpret_cast<float *>(sm + at.slots);
     float2 *ml = reinterpret_cast<float2 *>(sm + at.ml);
     constexpr int kRow = P::kCols + 4, kSlot = P::kHeads * kRow;
     static_assert(sizeof(T) == 2 || 2 * kSlot >= kConsumers * kScratch, "the probabilities lie in the slots, which are free between ends");
     bool ok = true;
+    int b = 0, h = 0, j = 0;
+    if (t0 < t1) {
+      find(t0, b, h, j);
+      if (!CLUSTER && tid == 0) {                            // what the CTAs before this one have of the request at t0
+        int4 d = make_int4(0, 0, 0, 0);
+        if (j > 0) {
+          const long long ts = t0 - j, te = ts + (pre[b + 1] - pre[b]);
+          const long long i0 = share_of(ts, G, T_all), i1 = share_of(te - 1, G, T_all);
+          if (i0 == me - 1) d = make_int4(ts == share_begin(i0, G, T_all) ? 1 : 2, (int)i1, b, h);
+        }
+        a.desc[blockIdx.x] = d;
+      }
+    }
     for (long long t = t0; t < t1;) {
-      const int n = pre[b + 1] - pre[b], j1 = (int)min((long long)n, j + (t1 - t));
+      const int n = CLUSTER ? pre[1] : pre[b + 1] - pre[b], j1 = (int)min((long long)n, j + (t1 - t));
       for (int i = j; i < j1; ++i) {
         if (ok && !mbar_wait_warp_unless(abort, full + st, ph)) {
           ok = false;
@@ -612,7 +671,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
       }
       // ---- the four warps' parts, two and two ----
       part.finish();
-      consumers_meet();                                        // (the slots of the request before have been read)
+      consumers_meet();                                      // (the slots of the request before have been read)
       if (warp >= 2) {
         float *slot = slots + (warp - 2) * kSlot;
         part.each(lane, [](int, float) { return 0; }, [&](int, float o, int head, int c) { slot[head * kRow + c] = o; });
@@ -639,7 +698,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
       }
       consumers_meet();
       const int kv = h / a.head_tiles, ht = h - kv * a.head_tiles, heads = min(P::kHeads, a.group - ht * P::kHeads);
-      const bool whole = j == 0 && j1 == n;
+      const bool whole = !CLUSTER && j == 0 && j1 == n;
       const long long slot_out = 2 * me + (t == t0 ? 0 : 1);
       for (int i = tid; i < heads * (P::kCols / 4); i += kConsumers * 32) {
         const int hd = i / (P::kCols / 4), c = (i - hd * (P::kCols / 4)) * 4;
@@ -648,7 +707,10 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
         const float4 u = *reinterpret_cast<const float4 *>(slots + hd * kRow + c), v = *reinterpret_cast<const float4 *>(slots + kSlot + hd * kRow + c);
         const float inv = whole ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
         const float4 o = make_float4((u.x * fx + v.x * fy) * inv, (u.y * fx + v.y * fy) * inv, (u.z * fx + v.z * fy) * inv, (u.w * fx + v.w * fy) * inv);
-        if (whole) {
+        if constexpr (CLUSTER) {                             // for the other CTAs to read
+          *reinterpret_cast<float4 *>(slots + hd * kRow + c) = o;
+          if (c == 0) ml[2 * P::kHeads + hd] = make_float2(to, l);
+        } else if (whole) {
           const int head = kv * a.group + ht * P::kHeads + hd;
           if (c < a.d_h) store4(a, b, head, c, o);
           if (c == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : to + logf(l);
@@ -659,7 +721,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
       }
       t += j1 - j;
       j = 0;
-      if (++h == Hn) {
+      if (!CLUSTER && ++h == Hn) {
         h = 0;
         do ++b;
         while (b < a.B && pre[b + 1] == pre[b]);
@@ -667,76 +729,131 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
     }
   }
   __syncthreads();
+  if constexpr (CLUSTER) {
+    // the parts of the CTAs of a request and key head, each by all of them
+    cluster_sync();
+    const int b = blockIdx.z, h = blockIdx.y, kv = h / a.head_tiles, ht = h - kv * a.head_tiles, heads = min(P::kHeads, a.group - ht * P::kHeads);
+    const int rank = cluster_rank(), size = cluster_size();
+    constexpr int kRow = P::kCols + 4;
+    const float *slots = reinterpret_cast<const float *>(sm + at.slots);
+    const float2 *ml = reinterpret_cast<const float2 *>(sm + at.ml) + 2 * P::kHeads;
+    for (int i = rank * kAttendThreads + tid; i < heads * (P::kCols / 4); i += size * kAttendThreads) {
+      const int hd = i / (P::kCols / 4), c = (i - hd * (P::kCols / 4)) * 4;
+      float top = -INFINITY, l = 0.f;
+      float2 x[kMaxCluster];
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        x[r] = r < size ? ld_cluster2(in_cta(ml + hd, r)) : make_float2(-INFINITY, 0.f);
+        top = fmaxf(top, x[r].x);
+      }
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        if (x[r].x == -INFINITY && x[r].y == 0.f) continue;    // no part, or none of its rows counts
+        const float f = weight(x[r].x, top);
+        const float4 v = ld_cluster4(in_cta(slots + hd * kRow + c, r));
+        l = fmaf(x[r].y, f, l);
+        o.x = fmaf(v.x, f, o.x);
+        o.y = fmaf(v.y, f, o.y);
+        o.z = fmaf(v.z, f, o.z);
+        o.w = fmaf(v.w, f, o.w);
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int head = kv * a.group + ht * P::kHeads + hd;
+      if (c < a.d_h) store4(a, b, head, c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+      if (c == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : top + logf(l);
+    }
+    cluster_sync();                                            // (the others have read)
+  }
   if (*abort) land_copies(full, a.stages);
 }
 
-// Parts of the request and key head that was cut at the beginning of CTA blockIdx.x's share and not before it; one head per CTA.
-constexpr int kJoinThreads = 256;
-constexpr int kMaxParts = 1024;
+// Parts of the request and key head that was cut at the beginning of CTA blockIdx.x's share and not before it.  Few parts (a batch): one CTA, a warp per
+// head.  Many (a long request): a CTA per head, whose warps share out the parts.  A warp asks for its first sums together with the maxima.
+constexpr int kJoinWarps = 8;
+constexpr int kMaxParts = 512;             // most CTAs of k_attend
+constexpr int kFewParts = 8;
 
-__global__ void __launch_bounds__(kJoinThreads) k_attend_join(const __grid_constant__ AttendArgs a, int tile_heads, int cols) {
-  __shared__ float s_w[kMaxParts], s_l[kMaxParts], s_red[kJoinThreads / 32];
-  __shared__ float4 s_o[kJoinThreads];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, hd = blockIdx.y;
+template <int CH>                          // 16-byte columns of a lane
+__global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(const __grid_constant__ AttendArgs a, int tile_heads, int cols) {
+  __shared__ float s_w[kJoinWarps][kMaxParts / kJoinWarps + 1];
+  __shared__ float4 s_o[kJoinWarps][CH * 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quads = cols / 4;
   pdl_wait();
   pdl_trigger();
   const int4 d = a.desc[blockIdx.x];
-  if (!d.x) return;
   const int i0 = blockIdx.x - 1, n = d.y - i0 + 1, b = d.z, kv = d.w / a.head_tiles, ht = d.w - kv * a.head_tiles;
-  if (ht * tile_heads + hd >= a.group) return;
-  const auto slot = [&](int p) { return 2 * (long long)(i0 + p) + (p == 0 ? d.x - 1 : 0); };
-  float top = -INFINITY;
-  for (int p = tid; p < n; p += kJoinThreads) {
-    const float2 x = a.part_ml[slot(p) * tile_heads + hd];
-    s_w[p] = x.x;
-    s_l[p] = x.y;
-    top = fmaxf(top, x.x);
-  }
+  const bool few = n <= kFewParts;
+  if (!d.x || (few && blockIdx.y)) return;
+  const int heads = min(tile_heads, a.group - ht * tile_heads);
+  const int p0 = few ? 0 : warp * n / kJoinWarps, p1 = few ? n : (warp + 1) * n / kJoinWarps;
+  for (int hd = few ? warp : blockIdx.y; hd < heads; hd += few ? kJoinWarps : gridDim.y) {
+    const auto slot = [&](int p) { return (2 * (long long)(i0 + p) + (p == 0 ? d.x - 1 : 0)) * tile_heads + hd; };
+    const auto sum_of = [&](int p, int k) { return *reinterpret_cast<const float4 *>(a.part_o + slot(p) * cols + (lane + 32 * k) * 4); };
+    const auto add = [&](const float4 &v, float f, float4 &to) {
+      to.x = fmaf(v.x, f, to.x);
+      to.y = fmaf(v.y, f, to.y);
+      to.z = fmaf(v.z, f, to.z);
+      to.w = fmaf(v.w, f, to.w);
+    };
+    constexpr int U = 8;
+    float4 x[U][CH], o[CH];
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < n) ml = a.part_ml[slot(lane)];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (lane == 0) s_red[warp] = top;
-  __syncthreads();
-  for (int w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, s_red[w]);
-  __syncthreads();
-  float l = 0.f;
-  for (int p = tid; p < n; p += kJoinThreads) {
-    const float f = weight(s_w[p], top);
-    l += s_l[p] * f;
-    s_w[p] = f;
-  }
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-  if (lane == 0) s_red[warp] = l;
-  __syncthreads();
-  l = 0.f;
-  for (int w = 0; w < kJoinThreads / 32; ++w) l += s_red[w];
-  const int quads = cols / 4, groups = kJoinThreads / quads, c = tid % quads, g = tid / quads;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (g < groups) {
-#pragma unroll 4
-    for (int p = g; p < n; p += groups) {
-      const float4 x = *reinterpret_cast<const float4 *>(a.part_o + (slot(p) * tile_heads + hd) * cols + c * 4);
-      const float f = s_w[p];
-      o.x = fmaf(x.x, f, o.x);
-      o.y = fmaf(x.y, f, o.y);
-      o.z = fmaf(x.z, f, o.z);
-      o.w = fmaf(x.w, f, o.w);
+      for (int k = 0; k < CH; ++k)
+        if (p0 + u < p1 && lane + 32 * k < quads) x[u][k] = sum_of(p0 + u, k);
+    float top = ml.x, l = 0.f;
+    for (int p = 32 + lane; p < n; p += 32) top = fmaxf(top, a.part_ml[slot(p)].x);
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+    for (int p = lane; p < n; p += 32) {
+      const float2 y = p < 32 ? ml : a.part_ml[slot(p)];
+      const float f = weight(y.x, top);
+      l += y.y * f;
+      if (p >= p0 && p < p1) s_w[warp][p - p0] = f;
     }
-    s_o[tid] = o;
-  }
-  __syncthreads();
-  if (tid < quads && tid * 4 < a.d_h) {
-    for (int i = 1; i < groups; ++i) {
-      const float4 x = s_o[i * quads + tid];
-      o.x += x.x;
-      o.y += x.y;
-      o.z += x.z;
-      o.w += x.w;
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) l += __shfl_xor_sync(0xffffffffu, l, w);
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < CH; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p = p0; p < p1; p += U) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (p + u < p1)
+#pragma unroll
+          for (int k = 0; k < CH; ++k)
+            if (lane + 32 * k < quads) add(x[u][k], s_w[warp][p + u - p0], o[k]);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < CH; ++k)
+          if (p + U + u < p1 && lane + 32 * k < quads) x[u][k] = sum_of(p + U + u, k);
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int head = kv * a.group + ht * tile_heads + hd;
-    store4(a, b, head, tid * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-    if (tid == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : top + logf(l);
+    if (!few) {
+#pragma unroll
+      for (int k = 0; k < CH; ++k) s_o[warp][lane + 32 * k] = o[k];
+      __syncthreads();
+      if (warp == 0)
+        for (int w = 1; w < kJoinWarps; ++w)
+#pragma unroll
+          for (int k = 0; k < CH; ++k) add(s_o[w][lane + 32 * k], 1.f, o[k]);
+      __syncthreads();
+    }
+    if (few || warp == 0) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int head = kv * a.group + ht * tile_heads + hd;
+#pragma unroll
+      for (int k = 0; k < CH; ++k) {
+        const int c = (lane + 32 * k) * 4;
+        if (c < a.d_h) store4(a, b, head, c, make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
+      }
+      if (lane == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : top + logf(l);
+    }
+    __syncwarp();
   }
 }
 
@@ -756,22 +873,31 @@ bool encode_pages(const PagedCfg &cfg, CUtensorMap *map, void *base, bool bf16, 
 }
 
 using AttendKernel = void (*)(CUtensorMap, CUtensorMap, AttendArgs);
-AttendKernel attend_kernel(const PagedCfg &cfg, bool bf16) {
+template <bool CLUSTER> AttendKernel attend_kernel(const PagedCfg &cfg, bool bf16) {
   const bool wide = cfg.tile_heads == 16;
   switch (bf16 ? cfg.blocks : 4 + cfg.blocks) {
-    case 1: return wide ? k_attend<__nv_bfloat16, 1, 2> : k_attend<__nv_bfloat16, 1, 1>;
-    case 2: return wide ? k_attend<__nv_bfloat16, 2, 2> : k_attend<__nv_bfloat16, 2, 1>;
-    case 3: return wide ? k_attend<__nv_bfloat16, 3, 2> : k_attend<__nv_bfloat16, 3, 1>;
-    case 4: return wide ? k_attend<__nv_bfloat16, 4, 2> : k_attend<__nv_bfloat16, 4, 1>;
-    case 5: return k_attend<float, 1, 1>;
-    case 6: return k_attend<float, 2, 1>;
-    case 7: return k_attend<float, 3, 1>;
-    case 8: return k_attend<float, 4, 1>;
+    case 1: return wide ? k_attend<__nv_bfloat16, 1, 2, CLUSTER> : k_attend<__nv_bfloat16, 1, 1, CLUSTER>;
+    case 2: return wide ? k_attend<__nv_bfloat16, 2, 2, CLUSTER> : k_attend<__nv_bfloat16, 2, 1, CLUSTER>;
+    case 3: return wide ? k_attend<__nv_bfloat16, 3, 2, CLUSTER> : k_attend<__nv_bfloat16, 3, 1, CLUSTER>;
+    case 4: return wide ? k_attend<__nv_bfloat16, 4, 2, CLUSTER> : k_attend<__nv_bfloat16, 4, 1, CLUSTER>;
+    case 5: return k_attend<float, 1, 1, CLUSTER>;
+    case 6: return k_attend<float, 2, 1, CLUSTER>;
+    case 7: return k_attend<float, 3, 1, CLUSTER>;
+    case 8: return k_attend<float, 4, 1, CLUSTER>;
   }
   return nullptr;
 }
 
 constexpr size_t kSmSmem = 228 * 1024, kCtaReserve = 1024;   // shared memory of an SM, and what the system takes of it for each CTA
+
+// CTAs of a cluster per request and key head, 0: no clusters.  `n` tiles of one at most, `heads` of them.
+int cluster_for(const PagedCfg &cfg, long long n, long long heads) {
+  for (int size = cfg.cluster; size >= 2; size /= 2) {
+    const int i = size == 2 ? 0 : size == 4 ? 1 : size == 8 ? 2 : 3;
+    if (heads <= cfg.clusters[i] && n <= (long long)size * kClusterTiles) return size;
+  }
+  return 0;
+}
 
 }  // namespace
 
@@ -790,19 +916,45 @@ cudaError_t paged_configure(PagedCfg *cfg, const DeviceCfg &dev, int n_qh, int n
   cfg->blocks = blocks;
   cfg->tile_heads = bf16 && group > 8 ? 16 : 8;
   cfg->head_tiles = (group + cfg->tile_heads - 1) / cfg->tile_heads;
-  return cudaFuncSetAttribute(attend_kernel(*cfg, bf16), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dev.smem_optin);
+  e = cudaFuncSetAttribute(attend_kernel<false>(*cfg, bf16), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dev.smem_optin);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attend_kernel<true>(*cfg, bf16), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dev.smem_optin);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attend_kernel<true>(*cfg, bf16), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess) return e;
+  // clusters of how many CTAs can be launched at all
+  cfg->cluster = 1;
+  for (int size = 2; size <= kMaxCluster; size *= 2) {
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3(size);
+    lc.blockDim = dim3(kAttendThreads);
+    lc.dynamicSmemBytes = kSmSmem / attend_ctas(cfg->blocks, cfg->tile_heads / 8) - kCtaReserve;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = size;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, attend_kernel<true>(*cfg, bf16), &lc);
+    if (e != cudaSuccess || n < 1) {
+      (void)cudaGetLastError();
+      break;
+    }
+    cfg->cluster = size;
+    cfg->clusters[size == 2 ? 0 : size == 4 ? 1 : size == 8 ? 2 : 3] = n;
+  }
+  return cudaSuccess;
 }
 
 size_t attend_scratch(const PagedCfg &cfg, const DeviceCfg &dev, bool bf16, AttendArgs *a, char *base) {
   if (!cfg.blocks) return 0;
-  const size_t slots = (size_t)dev.sm_count * attend_ctas(cfg.blocks, cfg.tile_heads / 8) * 2 * cfg.tile_heads;
-  const size_t o = slots * (cfg.blocks * kBoxBytes / (bf16 ? 2 : 4)) * sizeof(float), ml = slots * sizeof(float2);   // multiples of 256 bytes
+  const size_t ctas = (size_t)dev.sm_count * attend_ctas(cfg.blocks, cfg.tile_heads / 8), slots = ctas * 2 * cfg.tile_heads;
+  const size_t o = slots * (cfg.blocks * kBoxBytes / (bf16 ? 2 : 4)) * sizeof(float), ml = slots * sizeof(float2);   // multiples of 128 bytes
   if (a) {
     a->part_o = reinterpret_cast<float *>(base);
     a->part_ml = reinterpret_cast<float2 *>(base + o);
     a->desc = reinterpret_cast<int4 *>(base + o + ml);
   }
-  return (o + ml + slots * sizeof(int4) + 255) / 256 * 256;
+  return (o + ml + ctas * sizeof(int4) + 255) / 256 * 256;
 }
 
 cudaError_t launch_attend(AttendArgs a, const pact_paged_cache &cache, const PagedCfg &cfg, const DeviceCfg &dev, bool bf16, cudaStream_t st, int *launches) {
@@ -812,19 +964,27 @@ cudaError_t launch_attend(AttendArgs a, const pact_paged_cache &cache, const Pag
   if (!encode_pages(cfg, &mk, cache.K, bf16, a, cache.k_page, cache.k_head, cache.k_row) ||
       !encode_pages(cfg, &mv, cache.V, bf16, a, cache.v_page, cache.v_head, cache.v_row))
     return cudaErrorInvalidValue;
-  const int per_sm = attend_ctas(cfg.blocks, cfg.tile_heads / 8), ctas = dev.sm_count * per_sm, elt = bf16 ? 2 : 4;
+  const int per_sm = attend_ctas(cfg.blocks, cfg.tile_heads / 8), elt = bf16 ? 2 : 4, Hn = a.n_kvh * cfg.head_tiles;
+  const int ctas = dev.sm_count * per_sm;
+  // the most tiles that a request and key head can have
+  const long long n = ((long long)(a.selected && a.n_select < a.width ? a.n_select : a.width) * a.page + kTile - 1) / kTile;
+  const int size = cluster_for(cfg, n, (long long)a.B * Hn);
+  const int B = size ? 1 : a.B;
   const size_t most = kSmSmem / per_sm - kCtaReserve;
   a.stages = kMaxAttendStages;
-  while (a.stages > 2 && (size_t)attend_smem(a.stages, cfg.blocks, cfg.tile_heads, elt, a.B).total > most) --a.stages;
-  const int smem = attend_smem(a.stages, cfg.blocks, cfg.tile_heads, elt, a.B).total;
+  while (a.stages > 2 && (size_t)attend_smem(a.stages, cfg.blocks, cfg.tile_heads, elt, B).total > most) --a.stages;
+  const int smem = attend_smem(a.stages, cfg.blocks, cfg.tile_heads, elt, B).total;
   *launches = 1;
-  cudaError_t e = launch_k(attend_kernel(cfg, bf16), dim3((unsigned)ctas), dim3(kAttendThreads), (size_t)smem, st, true, mk, mv, a);
-  if (e != cudaSuccess) return e;
-  const long long rows = (long long)(a.selected && a.n_select < a.width ? a.n_select : a.width) * a.page;
-  if (rows <= kTile) return e;                                 // a request and key head is one tile: nothing is cut
+  if (size) {
+    LaunchOpt opt;
+    opt.cluster = size;
+    return launch_opt(opt, attend_kernel<true>(cfg, bf16), dim3((unsigned)size, (unsigned)Hn, (unsigned)a.B), dim3(kAttendThreads), (size_t)smem, st, mk, mv, a);
+  }
+  cudaError_t e = launch_k(attend_kernel<false>(cfg, bf16), dim3((unsigned)ctas), dim3(kAttendThreads), (size_t)smem, st, true, mk, mv, a);
+  if (e != cudaSuccess || n == 1) return e;                    // (a request and key head of one tile is never cut)
   *launches = 2;
-  const int group = a.group < cfg.tile_heads ? a.group : cfg.tile_heads;
-  return launch_k(k_attend_join, dim3((unsigned)ctas, (unsigned)group), dim3(kJoinThreads), 0, st, true, a, cfg.tile_heads, cfg.blocks * kBoxBytes / elt);
+  const int cols = cfg.blocks * kBoxBytes / elt, heads = a.group < 8 ? a.group : 8;
+  return launch_k(cols <= 128 ? k_attend_join<1> : k_attend_join<2>, dim3((unsigned)ctas, (unsigned)heads), dim3(kJoinWarps * 32), 0, st, true, a, cfg.tile_heads, cols);
 }
 
 }  // namespace pact

@@ -4,9 +4,9 @@
 #include <stdint.h>
 
 #ifdef __CUDACC__
-#define PACT_HD __host__ __device__ __forceinline__
+#define PAGED_HD __host__ __device__ __forceinline__
 #else
-#define PACT_HD inline
+#define PAGED_HD inline
 #endif
 
 namespace pact {
@@ -16,15 +16,30 @@ constexpr int kRowsOfWarp = 16;
 
 // Tiles of one key head of a request with `rows` cached rows: of all its rows, or of the first n_select entries of its list of pages (but no more entries
 // than it has pages).
-PACT_HD int tiles_of_request(int rows, int page, bool selected, int n_select) {
+PAGED_HD int tiles_of_request(int rows, int page, bool selected, int n_select) {
   if (!selected) return (int)(((unsigned)rows + kTile - 1u) / kTile);
   const long long have = (long long)(((unsigned)rows + (unsigned)page - 1u) / (unsigned)page), pages = have < n_select ? have : n_select;
   return (int)((pages * page + kTile - 1) / kTile);
 }
 
 // T tiles in G shares of floor(T / G) or one more, G <= T: the first tile of share i, and the share that tile t is in.
-PACT_HD long long share_begin(long long i, long long G, long long T) { return i * T / G; }
-PACT_HD long long share_of(long long t, long long G, long long T) { return ((t + 1) * G - 1) / T; }
+PAGED_HD long long share_begin(long long i, long long G, long long T) { return i * T / G; }
+PAGED_HD long long share_of(long long t, long long G, long long T) { return ((t + 1) * G - 1) / T; }
+
+// u / n and the rest for 0 <= u < 256 n, 1 <= n < 2^26: the quotient in fp32 is off by one at most.
+PAGED_HD int divide_small(long long u, int n, int *rest) {
+  int h = (int)((float)u / (float)n);
+  long long r = u - (long long)h * n;
+  if (r < 0) {
+    --h;
+    r += n;
+  } else if (r >= n) {
+    ++h;
+    r -= n;
+  }
+  *rest = (int)r;
+  return h;
+}
 
 // Page and place of every 16 rows of tile j, and how many of them count (a byte each).  A page id outside the cache makes its rows count for nothing and
 // sets `bad`.  per_box: 16 rows times this always lie in one page.
@@ -33,12 +48,12 @@ struct TileRows {
   uint32_t rows;
   bool bad;
 };
-PACT_HD TileRows locate_rows(int j, int len, int page, int per_box, const int32_t *table, int n_pages, const int32_t *selected, int n_select) {
+PAGED_HD TileRows locate_rows(int j, int len, int page, int per_box, const int32_t *table, int n_pages, const int32_t *selected, int n_select) {
   TileRows t;
   t.rows = 0;
   t.bad = false;
   const int pages = (int)(((unsigned)len + (unsigned)page - 1u) / (unsigned)page), listed = selected && n_select < pages ? n_select : pages;
-  long long left = 0;
+  int left = 0;
 #ifdef __CUDACC__
 #pragma unroll
 #endif
@@ -46,12 +61,12 @@ PACT_HD TileRows locate_rows(int j, int len, int page, int per_box, const int32_
     t.id[g] = -1;
     t.off[g] = 0;
     if (g % per_box == 0) {
-      const long long r = (long long)j * kTile + g * kRowsOfWarp;
-      long long place = r / page;
-      t.off[g] = (int)(r - place * page);
+      const unsigned r = (unsigned)j * kTile + g * kRowsOfWarp, at = r / (unsigned)page;   // (below 2^31 + 64 * 1024)
+      int place = (int)at;
+      t.off[g] = (int)(r - at * (unsigned)page);
       if (place >= listed) place = -1;
       else if (selected) place = selected[place];
-      left = place < 0 || place >= pages ? 0 : len - (place * page + t.off[g]);
+      left = place < 0 || place >= pages ? 0 : len - (int)((unsigned)place * (unsigned)page + (unsigned)t.off[g]);
       if (left > 0) {
         t.id[g] = table[place];
         if (t.id[g] < 0 || t.id[g] >= n_pages) {

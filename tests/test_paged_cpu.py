@@ -92,6 +92,22 @@ int main() {
     for (long long i = 0; i < 296; ++i)
       for (long long t : {share_begin(i, 296, T), share_begin(i + 1, 296, T) - 1})
         if (share_of(t, 296, T) != i) BAD("owner, long\n");
+  for (int trial = 0; trial < 2000000; ++trial) {
+    const int n = trial % 2 ? 1 + rand() % 1000 : 1 + rand() % (1 << 26), h = rand() % 256;
+    const long long u = (long long)h * n + (trial % 5 == 0 ? 0 : trial % 5 == 1 ? n - 1 : rand() % n);
+    int rest;
+    if (divide_small(u, n, &rest) != h || rest != u - (long long)h * n) BAD("%lld / %d\n", u, n);
+  }
+  // the ends of the range: a request of almost 2^31 rows
+  {
+    const int32_t last[1] = {5};
+    std::vector<int32_t> table((1 << 21) - 1, 3);
+    const int len = ((1 << 21) - 1) * 1024, j = tiles_of_request(len, 1024, false, 0) - 1;
+    const TileRows t = locate_rows(j, len, 1024, 4, table.data(), 4, nullptr, 0);
+    if (t.bad || t.id[0] != 3 || t.off[0] != 960 || t.rows != 0x10101010u) BAD("last tile\n");
+    const TileRows s = locate_rows(0, len, 1024, 4, table.data(), 4, last, 1);
+    if (s.bad || s.id[0] != 3 || s.rows != 0x10101010u) BAD("listed\n");
+  }
   // rows: whatever page size, length, list of pages and bad ids, every row that counts is found exactly once, none else, ids stay inside the cache
   srand(1);
   for (int trial = 0; trial < 60000; ++trial) {
