@@ -412,8 +412,12 @@ class Context:
         if t.dtype is not dtype or len(shape) != 3 or shape[1] != heads or shape[2] != self.d_h or t.get_device() != self.device or (n is not None and shape[0] != n):
             raise PactError(f"{what}: a {dtype} tensor of shape [{'..' if n is None else n}, {heads}, {self.d_h}] on cuda:{self.device} is wanted")
         s0, s1, s2 = t.stride()
-        if s2 != 1 or shape[0] == 1 or heads == 1:
-            s0, s1, _ = _strides(t, what)
+        if s2 != 1 and self.d_h > 1:
+            raise PactError(f"{what}: the last axis has to be contiguous")
+        if heads == 1:                      # the stride of an axis of one element is anything: the one that it would have if packed
+            s1 = self.d_h
+        if shape[0] == 1:
+            s0 = s1 * heads
         return t.data_ptr(), s0, s1
 
     def _cache(self, cache):
@@ -430,7 +434,7 @@ class Context:
             need = self._paged_need[(B, max_pages)] = int(self._L.pact_paged_workspace_bytes(self.handle, B, max_pages))
         have = self._paged_ws[-1] if self._paged_ws else None
         if have is None or have[1] < need:
-            size = max(need, 2 * have[1] if have else 0)
+            size = max(need, 2 * have[1] if have else 0)   # (never less than what the attention's parts need, which does not depend on B or max_pages)
             ws = torch.empty(size, dtype=torch.uint8, device=self._cuda())
             self._paged_ws.append((ws.data_ptr(), size, ws))
         return self._paged_ws[-1]
@@ -496,7 +500,7 @@ class Context:
         if selected is not None:
             n_select = selected.shape[-1]
             sel = self._flat(selected, i32, B * self.n_kvh * n_select, "selected")
-        w, n, _ = self._paged_workspace(1, 1)
+        w, n, _ = self._paged_ws[-1] if self._paged_ws else self._paged_workspace(1, 1)   # (any is large enough for the parts)
         _QUERY.pack_into(self._args, 0, q, ldq, ldqh, table, self._flat(length, i32, B, "length"), B, W, sel, n_select, 0, 0, self.d_h ** -0.5 if scale is None else scale,
                          o, ldo, ldoh, self._flat(lse, torch.float32, B * self.n_qh, "lse"), self._flat(status, i32, 1, "status"), w, n)
         _check(self.handle, self._L.pact_paged_attention(self.handle, ref, self._args_at, _stream()))

@@ -3,19 +3,25 @@
 // For a page with key bounds lo, hi and a query q, the largest q.k over all k with lo <= k <= hi is sum_c (max(q_c, 0) hi_c + min(q_c, 0) lo_c), so
 // scale times it, plus the page's largest bias, bounds every logit of the page.  The order of the scores decides what is selected, and with
 // thousands of pages two scores that differ by 1e-6 of themselves are common: the order is that of scores formed in double (products of bf16 or
-// fp32 numbers are exact there, sums good to 1e-15).  Doubles for all of them cost 20 times what the bytes do (82 us where HBM would need 7), so
-// k_page_scores forms the scores in fp32, with a bound of their error, and k_page_pick forms in double only those that the bound leaves in doubt,
-// a few per request.
-// k_page_scores, bf16: pages (16) by query heads (8) on mma.sync; rows are loaded 16 bytes per lane straight into operands (a dot product does not
+// fp32 numbers are exact there, sums good to 1e-15).  Doubles for all of them cost 12 times what the bytes do (82 us where HBM would need 7), so
+// the scores are formed in fp32 with a bound of their error, and in double only those that the bound leaves in doubt, a few per request.
+//
+// One kernel, a cluster of CTAs per request and key head (one CTA where there are enough of them): all CTAs score pages, the first one has the scores in
+// its shared memory and selects.  (As two kernels: 22 us instead of 13 for 32 requests of 16384 rows, 16 instead of 12 for two of 131072.)
+// Scores, bf16: pages (16) by query heads (8) on mma.sync; rows are loaded 16 bytes per lane straight into operands (a dot product does not
 // mind the order of its columns, so keys and queries take the same convenient one).  fp32: fused multiply-adds, folded over the lanes.
-// k_page_pick: a CTA per request and key head finds the bin of the n-th largest score (histograms of ten bits from the first bit in which the
-// scores differ), decides what lies near it in double, and writes the selected places in order from a bit mask.
+// Selection: the bin of the n-th largest score (histograms of eleven bits from the first bit in which the scores differ), what lies near it in
+// double, and the selected places in order from a bit mask.
 #include "paged.cuh"
+#include "tma.cuh"
 
 namespace pact {
 namespace {
 
-constexpr int kScoreThreads = 128;
+constexpr int kSelectThreads = 256;
+constexpr int kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectPages = 16 * kSelectWarps;   // pages that a CTA scores at once
+constexpr int kMaxSelectCluster = 16;
 
 // unsigned integers that order like the floats; NaN with minus infinity
 __device__ __forceinline__ unsigned long long order_key(double s) {
@@ -39,19 +45,18 @@ __device__ __forceinline__ int pages_of(const SelectArgs &a, int b, bool report)
   return (int)(((unsigned)len + (unsigned)a.page - 1u) / (unsigned)a.page);
 }
 
-// Score in fp32 and a bound of its error: `size` bounds the sum of the absolute products of a head, times |scale|.  512 products at most, each addition off
-// by 2^-23 of what it adds up to at most (tensor cores cut off): 2^-14 of `size`; the addition of w by 2^-24 of the result.
-// What fp32 cannot hold, infinities and NaN get an unlimited error: they are decided in double.
-constexpr float kScoreErr = 1.f / 16384.f;
-__device__ __forceinline__ uint2 approx(float best, float size, float w) {
-  if (w == -INFINITY) return make_uint2(order_key(-INFINITY), 0u);
-  const float s = best + w;
-  float err = size * kScoreErr + fabsf(w) * (1.f / 4194304.f);
-  if (!(err < 1e30f) || !(fabsf(s) < 1e30f)) {
-    err = INFINITY;
-    return make_uint2(order_key(0.f), __float_as_uint(err));
+// A page's score in fp32 as an integer, and a bound of its error.  `size` is the sum of the absolute products, the largest over the heads, times |scale|;
+// rel: what the additions are off by, as a part of it; the addition of w is off by 2^-24 of the result.  What fp32 cannot hold, infinities and
+// NaN get an unlimited error: they are decided in double.
+__device__ __forceinline__ uint32_t approx(float best, float size, float rel, float w, uint32_t &err) {
+  if (w == -INFINITY) return order_key(-INFINITY);
+  const float s = best + w, e = size * rel + (size + fabsf(w)) * (1.f / 4194304.f);
+  if (!(e < 1e30f) || !(fabsf(s) < 1e30f)) {
+    err = 0x7f800000u;
+    return order_key(0.f);
   }
-  return make_uint2(order_key(s), __float_as_uint(err));
+  err = max(err, __float_as_uint(e));
+  return order_key(s);
 }
 
 __device__ __forceinline__ uint32_t bf2_max(uint32_t x, uint32_t y) {
@@ -67,19 +72,13 @@ __device__ __forceinline__ void mma_16x8(float (&d)[4], uint32_t a0, uint32_t a1
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// bf16.  A warp has 16 pages of one key head; lane 4 r + c reads columns 32 j + 8 c .. + 7 of pages r and r + 8.  ND: blocks of 32 columns.
-constexpr int kScorePages = 16 * kScoreThreads / 32;   // pages of a CTA
-
-template <int ND>
-__global__ void __launch_bounds__(kScoreThreads) k_page_scores(SelectArgs a) {
+// bf16: scores of pages p0 .. p0 + 15 by a warp, into put(page, score as an integer).  Lane 4 r + c reads columns 32 j + 8 c .. + 7 of pages r and r + 8.
+// ND: blocks of 32 columns.  Error of a sum: 4 ND instructions of 17 addends each, which tensor cores align to the largest and cut off, each off by 2^-23
+// of the sum of all absolute values at most.
+template <int ND, typename F> __device__ __forceinline__ void score_pages(const SelectArgs &a, int b, int head, int p0, int np, uint32_t &err, F put) {
   using T = __nv_bfloat16;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int head = blockIdx.y, b = blockIdx.z, p0 = blockIdx.x * kScorePages + warp * 16;
-  const int r = lane / 4, c = lane % 4;
-  pdl_wait();
-  pdl_trigger();
-  const int np = pages_of(a, b, false);
-  if (p0 >= np) return;
+  constexpr float kRel = 4 * ND * 17 / 8388608.f;
+  const int lane = threadIdx.x & 31, r = lane / 4, c = lane % 4;
   int id = -1;                                             // page of lane & 15
   if (lane < 16 && p0 + lane < np) {
     id = a.table[(long long)b * a.width + p0 + lane];
@@ -92,11 +91,12 @@ __global__ void __launch_bounds__(kScoreThreads) k_page_scores(SelectArgs a) {
   const uint4 zero = make_uint4(0, 0, 0, 0);
   const T *bounds = static_cast<const T *>(a.bounds) + (long long)head * 2 * a.d_h, *Q = static_cast<const T *>(a.Q) + b * a.ldQ + (long long)head * a.group * a.ldQh;
   const T *row0 = bounds + (long long)id0 * a.n_kvh * 2 * a.d_h, *row1 = bounds + (long long)id1 * a.n_kvh * 2 * a.d_h;
+  const float w = c < 2 && (c ? id1 : id0) >= 0 ? __ldg(a.w_max + (c ? id1 : id0)) : -INFINITY;
   const auto ld = [&](const T *p, bool there, int col) { return there && col < a.d_h ? __ldg(reinterpret_cast<const uint4 *>(p + col)) : zero; };
-  float best0 = -INFINITY, best1 = -INFINITY, size0 = 0.f, size1 = 0.f;   // over the heads of this lane; pages r and r + 8
+  float best0 = -INFINITY, best1 = -INFINITY;              // over the heads of this lane; pages r and r + 8
+  uint32_t size0 = 0, size1 = 0;                           // (as integers: not negative, and NaN is above all)
   for (int h0 = 0; h0 < a.group; h0 += 8) {
-    float s[4] = {0.f, 0.f, 0.f, 0.f}, q1 = 0.f;
-    uint32_t top0 = 0, top1 = 0;                           // largest absolute bound of this lane's columns
+    float s[4] = {0.f, 0.f, 0.f, 0.f}, t[4] = {0.f, 0.f, 0.f, 0.f};
     constexpr int U = ND < 4 ? ND : 4;                     // blocks of columns in flight
 #pragma unroll
     for (int j0 = 0; j0 < ND; j0 += U) {
@@ -113,60 +113,42 @@ __global__ void __launch_bounds__(kScoreThreads) k_page_scores(SelectArgs a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const uint32_t qw[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
-        uint32_t qp[4], qn[4];
+        const uint32_t lo0[4] = {x[u][0].x, x[u][0].y, x[u][0].z, x[u][0].w}, lo1[4] = {x[u][1].x, x[u][1].y, x[u][1].z, x[u][1].w};
+        const uint32_t hi0[4] = {x[u][2].x, x[u][2].y, x[u][2].z, x[u][2].w}, hi1[4] = {x[u][3].x, x[u][3].y, x[u][3].z, x[u][3].w};
+        uint32_t m0[4], m1[4];                             // absolute values of bf16 numbers order like the integers, NaN above infinity
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          qp[i] = bf2_max(qw[i], 0u);
-          qn[i] = bf2_min(qw[i], 0u);
-          q1 += fabsf(__uint_as_float(qw[i] << 16)) + fabsf(__uint_as_float(qw[i] & 0xFFFF0000u));
+          m0[i] = __vmaxu2(lo0[i] & 0x7FFF7FFFu, hi0[i] & 0x7FFF7FFFu);
+          m1[i] = __vmaxu2(lo1[i] & 0x7FFF7FFFu, hi1[i] & 0x7FFF7FFFu);
         }
-        const uint4 lo0 = x[u][0], lo1 = x[u][1], hi0 = x[u][2], hi1 = x[u][3];
-        mma_16x8(s, lo0.x, lo1.x, lo0.y, lo1.y, qn[0], qn[1]);
-        mma_16x8(s, lo0.z, lo1.z, lo0.w, lo1.w, qn[2], qn[3]);
-        mma_16x8(s, hi0.x, hi1.x, hi0.y, hi1.y, qp[0], qp[1]);
-        mma_16x8(s, hi0.z, hi1.z, hi0.w, hi1.w, qp[2], qp[3]);
-        // absolute values of bf16 numbers, NaN above infinity, order like the integers
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint4 v = x[u][i];
-          uint32_t &top = i & 1 ? top1 : top0;
-          top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
+        for (int i = 0; i < 4; i += 2) {
+          mma_16x8(s, lo0[i], lo1[i], lo0[i + 1], lo1[i + 1], bf2_min(qw[i], 0u), bf2_min(qw[i + 1], 0u));
+          mma_16x8(s, hi0[i], hi1[i], hi0[i + 1], hi1[i + 1], bf2_max(qw[i], 0u), bf2_max(qw[i + 1], 0u));
+          mma_16x8(t, m0[i], m1[i], m0[i + 1], m1[i + 1], qw[i] & 0x7FFF7FFFu, qw[i + 1] & 0x7FFF7FFFu);
         }
       }
     }
-    // |q| of head r over the four lanes, the largest over the heads; the largest bound over the four lanes
-#pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-      q1 += __shfl_xor_sync(0xffffffffu, q1, o);
-      top0 = __vmaxu2(top0, __shfl_xor_sync(0xffffffffu, top0, o));
-      top1 = __vmaxu2(top1, __shfl_xor_sync(0xffffffffu, top1, o));
-    }
-    q1 = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(q1)));   // (not negative, and NaN is above all)
-    const float t0 = __uint_as_float(max(top0 << 16, top0 & 0xFFFF0000u)), t1 = __uint_as_float(max(top1 << 16, top1 & 0xFFFF0000u));
-    // fmaxf drops a NaN, so the larger one is taken as integers, which have it above all
-    size0 = __uint_as_float(max(__float_as_uint(size0), __float_as_uint(q1 * t0) & 0x7fffffffu));
-    size1 = __uint_as_float(max(__float_as_uint(size1), __float_as_uint(q1 * t1) & 0x7fffffffu));
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (h0 + 2 * c + i < a.group) {
         best0 = fmaxf(best0, s[i] * a.scale);
         best1 = fmaxf(best1, s[2 + i] * a.scale);
+        size0 = max(size0, __float_as_uint(t[i]) & 0x7fffffffu);
+        size1 = max(size1, __float_as_uint(t[2 + i]) & 0x7fffffffu);
       }
   }
 #pragma unroll
   for (int o = 1; o < 4; o <<= 1) {
     best0 = fmaxf(best0, __shfl_xor_sync(0xffffffffu, best0, o));
     best1 = fmaxf(best1, __shfl_xor_sync(0xffffffffu, best1, o));
+    size0 = max(size0, __shfl_xor_sync(0xffffffffu, size0, o));
+    size1 = max(size1, __shfl_xor_sync(0xffffffffu, size1, o));
   }
-  if (c < 2) {                                             // lane 4 r writes page r, lane 4 r + 1 page r + 8
-    const int p = p0 + r + 8 * c, at = c ? id1 : id0;
-    if (p < np)
-      a.approx[((long long)b * a.n_kvh + head) * a.width + p] =
-          approx(c ? best1 : best0, fabsf(a.scale) * (c ? size1 : size0), at < 0 ? -INFINITY : a.w_max[at]);
-  }
+  const int p = p0 + r + 8 * c;                            // lane 4 r has page r, lane 4 r + 1 page r + 8
+  if (c < 2 && p < np) put(p, approx(c ? best1 : best0, fabsf(a.scale) * __uint_as_float(c ? size1 : size0), kRel, w, err));
 }
 
-// fp32.  A warp has eight pages; a lane has DL columns of them and takes four query heads at a time.
 constexpr int kHeadsAtOnce = 4;
 
 // Sums of x[0..N) over the lanes: value i ends up in x[0] of the lanes whose bits from `bit` down spell i (31 exchanges for 32 sums, where 32
@@ -182,16 +164,12 @@ template <int N> __device__ __forceinline__ void fold(float (&x)[N], int lane, i
   }
 }
 
-template <int DL>
-__global__ void __launch_bounds__(kScoreThreads) k_page_scores_f32(SelectArgs a) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int head = blockIdx.y, b = blockIdx.z, p0 = (blockIdx.x * (kScoreThreads / 32) + warp) * 8;
-  const int c = lane * DL;
+// fp32: scores of pages p0 .. p0 + 7 by a warp.  A lane has DL columns and takes four query heads at a time.  Error: 2 DL additions in a lane and five over
+// the lanes, of 2^-24 each.
+template <int DL, typename F> __device__ __forceinline__ void score_pages_f32(const SelectArgs &a, int b, int head, int p0, int np, uint32_t &err, F put) {
+  constexpr float kRel = (2 * DL + 5) / 16777216.f;
+  const int lane = threadIdx.x & 31, c = lane * DL;
   const bool mine = c < a.d_h;                             // (d_h is a multiple of 4)
-  pdl_wait();
-  pdl_trigger();
-  const int np = pages_of(a, b, false);
-  if (p0 >= np) return;
   int id = -1;                                             // page of lane & 7
   if (lane < 8 && p0 + lane < np) {
     id = a.table[(long long)b * a.width + p0 + lane];
@@ -209,88 +187,98 @@ __global__ void __launch_bounds__(kScoreThreads) k_page_scores_f32(SelectArgs a)
     }
   };
   float lo[8][DL], hi[8][DL];
-  uint32_t top[8];                                         // largest absolute bound of a page, as bits (NaN above all)
 #pragma unroll
   for (int p = 0; p < 8; ++p) {
     const int at = __shfl_sync(0xffffffffu, id, p);
     const float *row = bounds + ((long long)at * a.n_kvh + head) * 2 * a.d_h + c;
     load(row, mine && at >= 0, lo[p]);
     load(row + a.d_h, mine && at >= 0, hi[p]);
-    top[p] = 0;
-#pragma unroll
-    for (int e = 0; e < DL; ++e) top[p] = max(top[p], max(__float_as_uint(lo[p][e]) & 0x7fffffffu, __float_as_uint(hi[p][e]) & 0x7fffffffu));
   }
+  const int at = __shfl_sync(0xffffffffu, id, lane >> 2);
+  const float w = at >= 0 ? __ldg(a.w_max + at) : -INFINITY;
   float best = -INFINITY;                                  // of page lane >> 2, over the heads of this lane
-  uint32_t q1 = 0;                                         // largest |q| of a head
+  uint32_t size = 0;                                       // (as an integer: not negative, and NaN is above all)
   for (int h0 = 0; h0 < a.group; h0 += kHeadsAtOnce) {
-    float sum[8 * kHeadsAtOnce];
+    float sum[8 * kHeadsAtOnce], abs[8 * kHeadsAtOnce];
 #pragma unroll
     for (int h = 0; h < kHeadsAtOnce; ++h) {
-      float q[DL], n = 0.f;
+      float q[DL];
       load(Q + (h0 + h) * a.ldQh + c, mine && h0 + h < a.group, q);
 #pragma unroll
-      for (int e = 0; e < DL; ++e) n += fabsf(q[e]);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-      q1 = max(q1, __float_as_uint(n) & 0x7fffffffu);
-#pragma unroll
       for (int p = 0; p < 8; ++p) {
-        float s = 0.f;
+        float s = 0.f, t = 0.f;
 #pragma unroll
-        for (int e = 0; e < DL; ++e) s = fmaf(fmaxf(q[e], 0.f), hi[p][e], fmaf(fminf(q[e], 0.f), lo[p][e], s));
+        for (int e = 0; e < DL; ++e) {
+          s = fmaf(fmaxf(q[e], 0.f), hi[p][e], fmaf(fminf(q[e], 0.f), lo[p][e], s));
+          t = fmaf(fabsf(q[e]), fabsf(lo[p][e]) + fabsf(hi[p][e]), t);
+        }
         sum[p * kHeadsAtOnce + h] = s;
+        abs[p * kHeadsAtOnce + h] = t;
       }
     }
     fold<8 * kHeadsAtOnce>(sum, lane, 16);
-    if (h0 + (lane & (kHeadsAtOnce - 1)) < a.group) best = fmaxf(best, sum[0] * a.scale);
+    fold<8 * kHeadsAtOnce>(abs, lane, 16);
+    if (h0 + (lane & (kHeadsAtOnce - 1)) < a.group) {
+      best = fmaxf(best, sum[0] * a.scale);
+      size = max(size, __float_as_uint(abs[0]) & 0x7fffffffu);
+    }
   }
 #pragma unroll
-  for (int o = 1; o < kHeadsAtOnce; o <<= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
-  uint32_t my_top = 0;
-#pragma unroll
-  for (int p = 0; p < 8; ++p) {
-    const uint32_t t = __reduce_max_sync(0xffffffffu, top[p]);
-    if (p == lane >> 2) my_top = t;
+  for (int o = 1; o < kHeadsAtOnce; o <<= 1) {
+    best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
+    size = max(size, __shfl_xor_sync(0xffffffffu, size, o));
   }
-  const int at = __shfl_sync(0xffffffffu, id, lane >> 2), p = p0 + (lane >> 2);
-  if ((lane & 3) == 0 && p < np)
-    a.approx[((long long)b * a.n_kvh + head) * a.width + p] =
-        approx(best, fabsf(a.scale) * __uint_as_float(q1) * __uint_as_float(my_top), at < 0 ? -INFINITY : a.w_max[at]);
+  const int p = p0 + (lane >> 2);
+  if ((lane & 3) == 0 && p < np) put(p, approx(best, fabsf(a.scale) * __uint_as_float(size), kRel, w, err));
 }
 
-// The score of page p in double, by a warp.
-template <typename T> __device__ double exact_score(const SelectArgs &a, int b, int head, int p) {
+// The score of page p in double, by a warp.  The loads of a page and of four heads are under way at once.
+template <typename T> __device__ __noinline__ double exact_score(const SelectArgs &a, int b, int head, int p) {
   const int lane = threadIdx.x & 31, id = a.table[(long long)b * a.width + p];
   if (id < 0 || id >= a.n_pages) return -INFINITY;
   const T *row = static_cast<const T *>(a.bounds) + ((long long)id * a.n_kvh + head) * 2 * a.d_h, *Q = static_cast<const T *>(a.Q) + b * a.ldQ + (long long)head * a.group * a.ldQh;
+  const double w = a.w_max[id];
   double best = -INFINITY;
-  for (int h = 0; h < a.group; ++h) {
-    double s = 0.0;
-    for (int c = lane; c < a.d_h; c += 32) {
-      const float q = (float)Q[h * a.ldQh + c];
-      const double qp = q > 0.f ? q : q == q ? 0.f : q, qn = q < 0.f ? q : 0.f;
-      s = fma(qp, (double)(float)row[a.d_h + c], fma(qn, (double)(float)row[c], s));
+  for (int h0 = 0; h0 < a.group; h0 += 4) {
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int c = lane + 32 * i;
+      if (c < a.d_h) {
+        const double lo = (float)row[c], hi = (float)row[a.d_h + c];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          const float q = h0 + h < a.group ? (float)Q[(h0 + h) * a.ldQh + c] : 0.f;
+          const double qp = q > 0.f ? q : q == q ? 0.f : q, qn = q < 0.f ? q : 0.f;
+          s[h] = fma(qp, hi, fma(qn, lo, s[h]));
+        }
+      }
     }
-    best = fmax(best, warp_sum(s) * (double)a.scale);      // (drops a NaN)
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const double x = warp_sum(s[h]) * (double)a.scale;
+      if (h0 + h < a.group) best = fmax(best, x);          // (drops a NaN)
+    }
   }
-  return best + (double)a.w_max[id];
+  return best + w;
 }
 
-constexpr int kPickThreads = 256;
-constexpr int kPickWarps = kPickThreads / 32;
-constexpr int kPickBits = 10;
+constexpr int kPickBits = 11;
 constexpr int kPickKeys = 8192;            // scores of a request and head that are kept in shared memory
-constexpr int kPickDoubt = 256;            // most scores in doubt that are ranked by comparing them with one another
+constexpr int kPickNear = 256;             // most scores near the n-th largest that are decided by comparing them with one another
+constexpr int kPickBin = 64;               // a bin of no more scores than this is not divided further
 
 struct PickShared {
   uint32_t mask[kMaxSelectPages / 32];
   int hist[1 << kPickBits];
-  unsigned long long cand[kPickDoubt];
-  int cand_at[kPickDoubt];
-  unsigned long long w_max[kPickWarps], w_min[kPickWarps];
-  uint32_t w_err[kPickWarps];
-  int w_sum[kPickWarps];
-  int bin, above, in_bin, n_cand, n_sure;
+  uint32_t near_key[kPickNear];            // scores near the n-th largest, in fp32
+  int near_at[kPickNear];
+  int doubt[kPickNear];                    // of these, the ones that fp32 leaves in doubt
+  unsigned long long cand[kPickNear];      // their scores in double
+  unsigned long long w_max[kSelectWarps], w_min[kSelectWarps];
+  uint32_t err[kMaxSelectCluster * kSelectWarps];   // largest error of every warp of the cluster
+  int w_sum[kSelectWarps];
+  int bin, above, in_bin, n_near, n_sure, n_doubt;
 };
 
 // exclusive prefix sum over the CTA's threads; *total: over all of them
@@ -307,7 +295,7 @@ __device__ __forceinline__ int scan_block(int v, int *w_sum, int *total) {
   __syncthreads();
   int before = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < kPickWarps; ++w) {
+  for (int w = 0; w < kSelectWarps; ++w) {
     if (w == warp) before = all;
     all += w_sum[w];
   }
@@ -333,14 +321,14 @@ __device__ __forceinline__ Cut<K> find_cut(PickShared &s, F key, int first, int 
   cut.agree = end - first;
   while (cut.need > 0 && cut.need < cut.agree && cut.agree > enough && cut.shift > 0) {
     const int lower = max(0, cut.shift - kPickBits), bins = 1 << (cut.shift - lower);
-    for (int i = tid; i < bins; i += kPickThreads) s.hist[i] = 0;
+    for (int i = tid; i < bins; i += kSelectThreads) s.hist[i] = 0;
     __syncthreads();
-    for (int i = first + tid; i < end; i += kPickThreads) {
+    for (int i = first + tid; i < end; i += kSelectThreads) {
       const K k = key(i);
       if (Cut<K>::high(k, cut.shift) == cut.prefix) atomicAdd(&s.hist[(int)(k >> lower) & (bins - 1)], 1);
     }
     __syncthreads();
-    constexpr int PER = (1 << kPickBits) / kPickThreads;   // bins of a thread, the largest first
+    constexpr int PER = (1 << kPickBits) / kSelectThreads;   // bins of a thread, the largest first
     int n[PER], sum = 0, all;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -368,98 +356,148 @@ __device__ __forceinline__ Cut<K> find_cut(PickShared &s, F key, int first, int 
   return cut;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kPickThreads) k_page_pick(SelectArgs a) {
+__device__ __forceinline__ void st_cluster_u32(const uint32_t *p, int rank, uint32_t v) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+}
+
+// W: columns of a row, in blocks of 64 (bf16 and fp32)
+template <typename T, int W>
+__global__ void __launch_bounds__(kSelectThreads, W * sizeof(T) <= 4 ? 2 : 1) k_page_select(const __grid_constant__ SelectArgs a) {
   extern __shared__ uint32_t s_keys[];
   __shared__ PickShared s;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int head = blockIdx.x, b = blockIdx.y;
+  const int head = blockIdx.y, b = blockIdx.z, rank = blockIdx.x, ctas = gridDim.x;   // (a cluster is a row of the grid)
   int32_t *out = a.selected + ((long long)b * a.n_kvh + head) * a.n_select;
+  cluster_arrive();                                        // the first CTA's shared memory is written once that CTA runs
   pdl_wait();
   pdl_trigger();
-  const int np = pages_of(a, b, tid == 0 && head == 0);
-  if (np <= a.n_select) {                                  // all of them
-    for (int i = tid; i < a.n_select; i += kPickThreads) out[i] = i < np ? i : -1;
+  const int np = pages_of(a, b, rank == 0 && tid == 0 && head == 0);
+  const bool all = np <= a.n_select;
+  const int first = a.n_first, end = np - a.n_last;        // the scores decide between these (n_first + n_last <= n_select < np)
+  const long long row = ((long long)b * a.n_kvh + head) * a.width;
+  const bool kept = np <= kPickKeys;                       // in shared memory, otherwise in the workspace
+  cluster_wait();
+  if (!all) {
+    uint32_t err = 0;
+    const auto put = [&](int p, uint32_t k) {
+      if (kept) st_cluster_u32(s_keys + p, 0, k);
+      else a.approx[row + p] = k;
+    };
+    constexpr int PER = sizeof(T) == 2 ? 16 : 8;           // pages of a warp
+    for (int p0 = (rank * kSelectWarps + warp) * PER; p0 < np; p0 += ctas * kSelectWarps * PER) {
+      if constexpr (sizeof(T) == 2) score_pages<2 * W>(a, b, head, p0, np, err, put);
+      else score_pages_f32<2 * W>(a, b, head, p0, np, err, put);
+    }
+    err = __reduce_max_sync(0xffffffffu, err);
+    if (lane == 0) st_cluster_u32(s.err + rank * kSelectWarps + warp, 0, err);
+  }
+  cluster_sync();
+  if (rank) return;
+  if (all) {
+    for (int i = tid; i < a.n_select; i += kSelectThreads) out[i] = i < np ? i : -1;
     return;
   }
-  const int first = a.n_first, end = np - a.n_last;        // the scores decide between these (n_first + n_last <= n_select < np)
   const int need = a.n_select - a.n_first - a.n_last;
-  const long long row = ((long long)b * a.n_kvh + head) * a.width;
-  const uint2 *apx = a.approx + row;
-  const bool kept = np <= kPickKeys;
+  const uint32_t *apx = a.approx + row;
   uint32_t kmax = 0, kmin = ~0u, err = 0;
-  for (int i = first + tid; i < end; i += kPickThreads) {
-    const uint2 k = apx[i];
-    if (kept) s_keys[i] = k.x;
-    kmax = max(kmax, k.x);
-    kmin = min(kmin, k.x);
-    err = max(err, k.y);                                   // (not negative: orders like the bits)
+  for (int i = first + tid; i < end; i += kSelectThreads) {
+    const uint32_t k = kept ? s_keys[i] : apx[i];
+    kmax = max(kmax, k);
+    kmin = min(kmin, k);
   }
+  if (tid < ctas * kSelectWarps) err = s.err[tid];         // (at most as many as threads)
   kmax = __reduce_max_sync(0xffffffffu, kmax);
   kmin = __reduce_min_sync(0xffffffffu, kmin);
   err = __reduce_max_sync(0xffffffffu, err);
   if (lane == 0) {
     s.w_max[warp] = kmax;
     s.w_min[warp] = kmin;
-    s.w_err[warp] = err;
+    s.w_sum[warp] = (int)err;
   }
-  if (tid == 0) s.n_cand = s.n_sure = 0;
+  if (tid == 0) s.n_near = s.n_sure = s.n_doubt = 0;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kPickWarps; ++w) {
+  for (int w = 0; w < kSelectWarps; ++w) {
     kmax = max(kmax, (uint32_t)s.w_max[w]);
     kmin = min(kmin, (uint32_t)s.w_min[w]);
-    err = max(err, s.w_err[w]);
+    err = max(err, (uint32_t)s.w_sum[w]);
   }
-  const auto key = [&](int i) { return kept ? s_keys[i] : apx[i].x; };
+  __syncthreads();
+  const auto key = [&](int i) { return kept ? s_keys[i] : apx[i]; };
   const int words = (np + 31) / 32;
   // Of two scores whose fp32 values differ by more than twice the largest error the larger one is the larger one in double as well.  [low, high]: fp32
-  // values that may lie on either side of the need-th largest; `sure` ones are larger.
+  // values that may lie on either side of the need-th largest; those above it are selected.
+  const float e2 = 2.f * __uint_as_float(err);
+  const auto below = [&](uint32_t k) { return order_key(__fsub_rd(from_order_key(k), e2)); };
+  const auto above = [&](uint32_t k) { return order_key(__fadd_ru(from_order_key(k), e2)); };
   uint32_t low = 0, high = ~0u;
   if (err < 0x7f800000u) {
-    const Cut<uint32_t> cut = find_cut<uint32_t>(s, key, first, end, need, kmax, kmin, 1);
+    const Cut<uint32_t> cut = find_cut<uint32_t>(s, key, first, end, need, kmax, kmin, kPickBin);
     // the need-th largest agrees with the prefix
     const uint32_t least = cut.shift >= 32 ? 0u : cut.prefix << cut.shift, most = cut.shift >= 32 ? ~0u : least | ((1u << cut.shift) - 1u);
-    const float e2 = 2.f * __uint_as_float(err);
-    low = order_key(__fsub_rd(from_order_key(max(least, kmin)), e2));
-    high = order_key(__fadd_ru(from_order_key(min(most, kmax)), e2));
+    low = below(max(least, kmin));
+    high = above(min(most, kmax));
   }
-  for (int w = warp; w < words; w += kPickWarps) {
+  for (int w = warp; w < words; w += kSelectWarps) {
     const int i = w * 32 + lane;
     const bool in = i >= first && i < end;
     const uint32_t k = in ? key(i) : 0u;
-    const bool sure = in && need > 0 && k > high, doubt = in && need > 0 && k >= low && k <= high;
+    const bool sure = in && need > 0 && k > high, near = in && need > 0 && k >= low && k <= high;
     const uint32_t m = __ballot_sync(0xffffffffu, sure || (!in && i < np)), ms = __ballot_sync(0xffffffffu, sure);
     if (lane == 0) {
       s.mask[w] = m;
       if (ms) atomicAdd(&s.n_sure, __popc(ms));
     }
-    if (doubt) {
-      const int at = atomicAdd(&s.n_cand, 1);              // (their order changes nothing)
-      if (at < kPickDoubt) s.cand_at[at] = i;
+    if (near) {
+      const int at = atomicAdd(&s.n_near, 1);              // (their order changes nothing)
+      if (at < kPickNear) {
+        s.near_at[at] = i;
+        s.near_key[at] = k;
+      }
     }
   }
   __syncthreads();
-  const int doubts = s.n_cand, more = need - s.n_sure;     // `more` of the ones in doubt are selected: 0 <= more <= doubts
-  if (more > 0 && more == doubts && doubts <= kPickDoubt) {
-    for (int j = tid; j < doubts; j += kPickThreads) atomicOr(&s.mask[s.cand_at[j] >> 5], 1u << (s.cand_at[j] & 31));
-  } else if (more > 0 && doubts <= kPickDoubt) {
-    for (int j = warp; j < doubts; j += kPickWarps) {
-      const double x = exact_score<T>(a, b, head, s.cand_at[j]);
+  const int near = s.n_near, more = need - s.n_sure;       // `more` of the near ones are selected: 0 <= more <= near
+  if (more > 0 && near <= kPickNear) {
+    // each against the others: `over` of them are larger whatever the errors, `maybe` may be (itself among them)
+    int in = 0;
+    for (int j = tid; j < near; j += kSelectThreads) {
+      const uint32_t k = s.near_key[j], up = err < 0x7f800000u ? above(k) : ~0u, down = err < 0x7f800000u ? below(k) : 0u;
+      int over = 0, maybe = 0;
+      for (int i = 0; i < near; ++i) {
+        over += s.near_key[i] > up;
+        maybe += s.near_key[i] >= down;
+      }
+      if (maybe <= more) {
+        ++in;
+        atomicOr(&s.mask[s.near_at[j] >> 5], 1u << (s.near_at[j] & 31));
+      } else if (over < more) {
+        s.doubt[atomicAdd(&s.n_doubt, 1)] = s.near_at[j];
+      }
+    }
+    if (tid < 32) s.w_sum[0] = 0;
+    __syncthreads();
+    if (in) atomicAdd(&s.w_sum[0], in);
+    __syncthreads();
+    const int doubts = s.n_doubt, rest = more - s.w_sum[0];   // `rest` of the ones in doubt are selected
+    for (int j = warp; j < doubts; j += kSelectWarps) {
+      const double x = exact_score<T>(a, b, head, s.doubt[j]);
       if (lane == 0) s.cand[j] = order_key(x);
     }
-    __syncthreads();
-    for (int j = tid; j < doubts; j += kPickThreads) {
+    if (doubts) __syncthreads();
+    for (int j = tid; j < doubts; j += kSelectThreads) {
       const unsigned long long k = s.cand[j];
-      const int at = s.cand_at[j];
+      const int at = s.doubt[j];
       int before = 0;
-      for (int i = 0; i < doubts; ++i) before += s.cand[i] > k || (s.cand[i] == k && s.cand_at[i] < at);
-      if (before < more) atomicOr(&s.mask[at >> 5], 1u << (at & 31));
+      for (int i = 0; i < doubts; ++i) before += s.cand[i] > k || (s.cand[i] == k && s.doubt[i] < at);
+      if (before < rest) atomicOr(&s.mask[at >> 5], 1u << (at & 31));
     }
-  } else if (more > 0) {                                   // many scores (nearly) equal, or beyond fp32: all that are in doubt in double
-    unsigned long long *exact = a.keys + row;              // 0 for what is not in doubt: below every score
+  } else if (more > 0) {                                   // many scores (nearly) equal, or beyond fp32: all near ones in double
+    unsigned long long *exact = a.keys + row;              // 0 for what is not near: below every score
     unsigned long long xmax = 0, xmin = ~0ull;
-    for (int i = first + warp; i < end; i += kPickWarps) {
+    for (int i = first + warp; i < end; i += kSelectWarps) {
       const uint32_t k = key(i);
       unsigned long long x = 0;
       if (k >= low && k <= high) {
@@ -471,17 +509,17 @@ __global__ void __launch_bounds__(kPickThreads) k_page_pick(SelectArgs a) {
     }
     if (lane == 0) {
       s.w_max[warp] = xmax;
-      s.w_min[warp] = doubts < end - first ? 0ull : xmin;
+      s.w_min[warp] = near < end - first ? 0ull : xmin;
     }
     __syncthreads();
-    for (int w = 0; w < kPickWarps; ++w) {
+    for (int w = 0; w < kSelectWarps; ++w) {
       xmax = max(xmax, s.w_max[w]);
       xmin = min(xmin, s.w_min[w]);
     }
     const auto ekey = [&](int i) { return exact[i]; };
     const Cut<unsigned long long> cut = find_cut<unsigned long long>(s, ekey, first, end, more, xmax, xmin, 0);
     int taken = 0;                                         // equal scores in the words before this round's
-    for (int w0 = 0; w0 < words; w0 += kPickWarps) {
+    for (int w0 = 0; w0 < words; w0 += kSelectWarps) {
       const int w = w0 + warp, i = w * 32 + lane;
       const unsigned long long k = i >= first && i < end ? exact[i] : 0ull, h = Cut<unsigned long long>::high(k, cut.shift);
       const bool same = k != 0 && h == cut.prefix;
@@ -489,7 +527,7 @@ __global__ void __launch_bounds__(kPickThreads) k_page_pick(SelectArgs a) {
       if (lane == 0) s.w_sum[warp] = __popc(eq);
       __syncthreads();
       int before = taken, all = 0;
-      for (int v = 0; v < kPickWarps; ++v) {
+      for (int v = 0; v < kSelectWarps; ++v) {
         if (v < warp) before += s.w_sum[v];
         all += s.w_sum[v];
       }
@@ -501,7 +539,7 @@ __global__ void __launch_bounds__(kPickThreads) k_page_pick(SelectArgs a) {
   }
   __syncthreads();
   int base = 0;
-  for (int w0 = 0; w0 < words; w0 += kPickThreads) {
+  for (int w0 = 0; w0 < words; w0 += kSelectThreads) {
     const int w = w0 + tid;
     uint32_t m = w < words ? s.mask[w] : 0u;
     int all;
@@ -513,25 +551,27 @@ __global__ void __launch_bounds__(kPickThreads) k_page_pick(SelectArgs a) {
 
 }  // namespace
 
-cudaError_t select_pages_configure() {
-  const cudaError_t e = cudaFuncSetAttribute(k_page_pick<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kPickKeys * sizeof(uint32_t)));
-  if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(k_page_pick<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kPickKeys * sizeof(uint32_t)));
+using SelectKernel = void (*)(SelectArgs);
+static SelectKernel select_kernel(int d_h, bool bf16) {
+  if (!bf16) return d_h <= 64 ? k_page_select<float, 1> : k_page_select<float, 2>;
+  return d_h <= 64 ? k_page_select<__nv_bfloat16, 1> : d_h <= 128 ? k_page_select<__nv_bfloat16, 2> : k_page_select<__nv_bfloat16, 4>;
 }
 
-cudaError_t launch_page_select(const SelectArgs &a, bool bf16, cudaStream_t st, int *launches) {
-  *launches = 1;
-  if (a.width > a.n_select) {                              // otherwise all pages are selected whatever the lengths
-    const int pages = bf16 ? kScorePages : kScorePages / 2;
-    const dim3 grid((unsigned)((a.width + pages - 1) / pages), (unsigned)a.n_kvh, (unsigned)a.B);
-    void (*kernel)(SelectArgs) = bf16 ? (a.d_h <= 64 ? k_page_scores<2> : a.d_h <= 128 ? k_page_scores<4> : k_page_scores<8>)
-                                      : (a.d_h <= 64 ? k_page_scores_f32<2> : k_page_scores_f32<4>);
-    const cudaError_t e = launch_k(kernel, grid, dim3(kScoreThreads), 0, st, true, a);
-    if (e != cudaSuccess) return e;
-    *launches = 2;
-  }
+cudaError_t select_pages_configure(int d_h, bool bf16) {
+  const cudaError_t e = cudaFuncSetAttribute(select_kernel(d_h, bf16), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kPickKeys * sizeof(uint32_t)));
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(select_kernel(d_h, bf16), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+}
+
+cudaError_t launch_page_select(const SelectArgs &a, bool bf16, int most_ctas, int sm_count, cudaStream_t st) {
+  // As many CTAs as give every SM two, no more than there are pages for.
+  int size = 1;
+  const int pages = bf16 ? kSelectPages : kSelectPages / 2;
+  while (size * 2 <= most_ctas && size * 2 <= kMaxSelectCluster && (long long)a.B * a.n_kvh * size < sm_count && size * pages < a.width) size *= 2;
+  if (a.width <= a.n_select) size = 1;                     // all pages are selected whatever the lengths
   const int keys = a.width <= a.n_select ? 0 : a.width < kPickKeys ? a.width : kPickKeys;
-  return launch_k(bf16 ? k_page_pick<__nv_bfloat16> : k_page_pick<float>, dim3((unsigned)a.n_kvh, (unsigned)a.B), dim3(kPickThreads), (size_t)keys * sizeof(uint32_t), st, true, a);
+  LaunchOpt opt;
+  opt.cluster = size > 1 ? size : 0;
+  return launch_opt(opt, select_kernel(a.d_h, bf16), dim3((unsigned)size, (unsigned)a.n_kvh, (unsigned)a.B), dim3(kSelectThreads), (size_t)keys * sizeof(uint32_t), st, a);
 }
 
 }  // namespace pact

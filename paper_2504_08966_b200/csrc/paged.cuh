@@ -53,14 +53,14 @@ struct SelectArgs {
   const float *w_max;
   const int32_t *table, *length;
   int32_t *selected, *status;
-  uint2 *approx;              // [B][n_kvh][width] scores in fp32 as integers that order like them, and bounds of their errors
-  unsigned long long *keys;   // [B][n_kvh][width] scores in double, those that were needed
+  unsigned long long *keys;   // [B][n_kvh][width] scores in double, where many are in doubt, as integers that order like them
+  uint32_t *approx;           // [B][n_kvh][width] scores in fp32, where they are too many for shared memory
   float scale;
   int B, width, page, n_pages, n_kvh, group, d_h;
   int n_first, n_last, n_select;
 };
-cudaError_t launch_page_select(const SelectArgs &a, bool bf16, cudaStream_t st, int *launches);
-cudaError_t select_pages_configure();
+cudaError_t launch_page_select(const SelectArgs &a, bool bf16, int most_ctas, int sm_count, cudaStream_t st);   // most_ctas: of a cluster
+cudaError_t select_pages_configure(int d_h, bool bf16);
 
 // ---- paged_attention.cu --------------------------------------------------------------------------------
 

@@ -42,7 +42,7 @@ pact_status check_ws(void *ws, size_t have, size_t need) {
 
 size_t select_scores(const pact_ctx *c, int requests, int pages) { return (size_t)requests * c->n_kvh * pages; }
 size_t select_bytes(const pact_ctx *c, int requests, int pages) {
-  return (select_scores(c, requests, pages) * (sizeof(uint2) + sizeof(unsigned long long)) + kAlign - 1) / kAlign * kAlign;
+  return (select_scores(c, requests, pages) * (sizeof(uint32_t) + sizeof(unsigned long long)) + kAlign - 1) / kAlign * kAlign;
 }
 
 }  // namespace
@@ -116,13 +116,12 @@ pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache, const
   SelectArgs a;
   a.Q = q->Q; a.ldQ = q->ldQ; a.ldQh = q->ldQh; a.bounds = cache->bounds; a.w_max = cache->w_max; a.table = q->block_table; a.length = q->length;
   a.selected = q->selected; a.status = q->status; a.scale = q->scale;
-  a.approx = (uint2 *)q->ws; a.keys = (unsigned long long *)q->ws + select_scores(ctx, q->n_requests, q->max_pages);
+  a.keys = (unsigned long long *)q->ws; a.approx = (uint32_t *)(a.keys + select_scores(ctx, q->n_requests, q->max_pages));
   a.B = q->n_requests; a.width = q->max_pages; a.page = cache->page_rows; a.n_pages = cache->n_pages;
   a.n_kvh = ctx->n_kvh; a.group = ctx->n_qh / ctx->n_kvh; a.d_h = ctx->d_h;
   a.n_first = q->n_first; a.n_last = q->n_last; a.n_select = q->n_select;
-  int launches = 0;
-  CK(launch_page_select(a, ctx->in == PACT_BF16, (cudaStream_t)stream, &launches));
-  ctx->launches += launches;
+  CK(launch_page_select(a, ctx->in == PACT_BF16, ctx->paged.cluster, ctx->dev.sm_count, (cudaStream_t)stream));
+  ctx->launches += 1;
   CK(cudaGetLastError());
   return PACT_OK;
 }

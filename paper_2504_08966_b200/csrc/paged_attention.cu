@@ -35,8 +35,7 @@ constexpr int kBoxBytes = 128;             // columns of a box
 constexpr int kBlockBytes = kTile * kBoxBytes;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxCluster = 16;
-constexpr int kClusterTiles = 8;           // most tiles of a CTA of a cluster
-constexpr int kScratch = kRowsOfWarp * 8 + 8;   // fp32: floats of a warp for probabilities and factors
+template <int HEADS> constexpr int kScratch = (kRowsOfWarp + 1) * HEADS;   // fp32: floats of a warp for probabilities and factors
 
 // What the copying warp has worked out about a tile.
 struct __align__(16) TilePlan {
@@ -301,15 +300,16 @@ template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
   }
 };
 
-template <int NB> struct Part<float, NB, 1> {
-  static constexpr int kHeads = 8, kCols = NB * 32;
+// NT: 1 for eight heads, 0 for two (models with as many key heads as query heads would pay for eight: 212 rows 9.1 -> 8.1 us)
+template <int NB, int NT> struct Part<float, NB, NT> {
+  static constexpr int kHeads = NT ? 8 : 2, kHalf = kHeads / 2, kCols = NB * 32;
   static constexpr int kChunks = NB * 8;                       // 16-byte columns of a row
   static constexpr int kGroups = kChunks <= 8 ? 4 : kChunks <= 16 ? 2 : 1;   // groups of lanes that share out the rows for the output
   static constexpr int kGroupLanes = 32 / kGroups;
   uint32_t q;                              // in shared memory
   int q_row;
-  float m[4], l[4];                        // heads 4 (lane / 16) + {0 .. 3}; the sums are of this lane's row
-  float o[8][4];                           // columns 4 (lane % kGroupLanes) + {0 .. 3}, rows of the lane's group
+  float m[kHalf], l[kHalf];                // heads kHalf (lane / 16) + {0 ..}; the sums are of this lane's row
+  float o[kHeads][4];                           // columns 4 (lane % kGroupLanes) + {0 .. 3}, rows of the lane's group
 
   // q is read in every step, and the copying warp may be ahead by now with the next request's in the same stage: the warps make a copy.
   // (The barrier also parts the probabilities to come, which lie in the slots, from reads of the slots at the end of the request before.)
@@ -319,22 +319,22 @@ template <int NB> struct Part<float, NB, 1> {
     q = smem_u32(own);
     q_row = row;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kHalf; ++i) {
       m[i] = -INFINITY;
       l[i] = 0.f;
     }
 #pragma unroll
-    for (int h = 0; h < 8; ++h)
+    for (int h = 0; h < kHeads; ++h)
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[h][i] = 0.f;
   }
 
-  // scratch: 16 rows x 8 heads of probabilities and 8 factors, this warp's
+  // scratch: 16 rows of probabilities and a row of factors, this warp's
   __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, const float *bias, bool has_bias, int row0, int rows, float scale, int lane, float *scratch) {
     const int r = lane & 15, half = lane >> 4, row = row0 + r, x = row & 7;
-    float s[8];
+    float s[kHeads];
 #pragma unroll
-    for (int h = 0; h < 8; ++h) s[h] = 0.f;
+    for (int h = 0; h < kHeads; ++h) s[h] = 0.f;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -342,43 +342,44 @@ template <int NB> struct Part<float, NB, 1> {
         const int c = 2 * i + half;
         const float4 k = lds4(sk + nb * kBlockBytes + row * kBoxBytes + ((c ^ x) << 4));
 #pragma unroll
-        for (int h = 0; h < 8; ++h) s[h] = fma4(k, lds4(q + h * q_row + nb * kBoxBytes + c * 16), s[h]);
+        for (int h = 0; h < kHeads; ++h) s[h] = fma4(k, lds4(q + h * q_row + nb * kBoxBytes + c * 16), s[h]);
       }
     const float b = has_bias ? bias[row] : 0.f;
     const bool in = r < rows && b != -INFINITY;
-    float t[4], top[4];
+    float t[kHalf], top[kHalf];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {             // both halves of the columns; a lane goes on with four heads
-      const float give = half ? s[i] : s[4 + i], got = __shfl_xor_sync(0xffffffffu, give, 16);
-      t[i] = in ? fmaf((half ? s[4 + i] : s[i]) + got, scale, b) : -INFINITY;
+    for (int i = 0; i < kHalf; ++i) {         // both halves of the columns; a lane goes on with half of the heads
+      const float give = half ? s[i] : s[kHalf + i], got = __shfl_xor_sync(0xffffffffu, give, 16);
+      t[i] = in ? fmaf((half ? s[kHalf + i] : s[i]) + got, scale, b) : -INFINITY;
       top[i] = t[i];
     }
 #pragma unroll
     for (int w = 1; w < 16; w <<= 1)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], w));
+      for (int i = 0; i < kHalf; ++i) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], w));
     bool grows = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) grows = grows || top[i] > m[i];
+    for (int i = 0; i < kHalf; ++i) grows = grows || top[i] > m[i];
     const bool rescale = __any_sync(0xffffffffu, grows);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kHalf; ++i) {
       if (rescale) {
         const float to = fmaxf(m[i], top[i]), f = weight(m[i], to);
         m[i] = to;
         l[i] *= f;
-        if (r == 0) scratch[kRowsOfWarp * 8 + half * 4 + i] = f;
+        if (r == 0) scratch[kRowsOfWarp * kHeads + half * kHalf + i] = f;
       }
       t[i] = exp_below(t[i], m[i]);
       l[i] += t[i];
     }
-    *reinterpret_cast<float4 *>(scratch + r * 8 + half * 4) = make_float4(t[0], t[1], t[2], t[3]);
+    if constexpr (kHalf == 4) *reinterpret_cast<float4 *>(scratch + r * 8 + half * 4) = make_float4(t[0], t[1], t[2], t[3]);
+    else scratch[r * 2 + half] = t[0];
     const uint32_t live = __ballot_sync(0xffffffffu, in) & 0xffffu;
     __syncwarp();
     if (rescale) {
 #pragma unroll
-      for (int h = 0; h < 8; ++h) {
-        const float f = scratch[kRowsOfWarp * 8 + h];
+      for (int h = 0; h < kHeads; ++h) {
+        const float f = scratch[kRowsOfWarp * kHeads + h];
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[h][i] *= f;
       }
@@ -390,10 +391,17 @@ template <int NB> struct Part<float, NB, 1> {
         if (!(live >> k & 1)) continue;       // zero times an infinity or a NaN would not be zero
         const int vr = row0 + k;
         const float4 v = lds4(sv + (c / 8) * kBlockBytes + vr * kBoxBytes + (((c % 8) ^ (vr & 7)) << 4));
-        const float4 p0 = *reinterpret_cast<const float4 *>(scratch + k * 8), p1 = *reinterpret_cast<const float4 *>(scratch + k * 8 + 4);
-        const float p[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+        float p[kHeads];
+        if constexpr (kHeads == 8) {
+          const float4 p0 = *reinterpret_cast<const float4 *>(scratch + k * 8), p1 = *reinterpret_cast<const float4 *>(scratch + k * 8 + 4);
+          p[0] = p0.x; p[1] = p0.y; p[2] = p0.z; p[3] = p0.w;
+          p[4] = p1.x; p[5] = p1.y; p[6] = p1.z; p[7] = p1.w;
+        } else {
+          const float2 p0 = *reinterpret_cast<const float2 *>(scratch + k * 2);
+          p[0] = p0.x; p[1] = p0.y;
+        }
 #pragma unroll
-        for (int h = 0; h < 8; ++h) {
+        for (int h = 0; h < kHeads; ++h) {
           o[h][0] = fmaf(p[h], v.x, o[h][0]);
           o[h][1] = fmaf(p[h], v.y, o[h][1]);
           o[h][2] = fmaf(p[h], v.z, o[h][2]);
@@ -408,26 +416,26 @@ template <int NB> struct Part<float, NB, 1> {
 #pragma unroll
     for (int w = 1; w < 16; w <<= 1)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
+      for (int i = 0; i < kHalf; ++i) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
 #pragma unroll
     for (int w = kGroupLanes; w < 32; w <<= 1)
 #pragma unroll
-      for (int h = 0; h < 8; ++h)
+      for (int h = 0; h < kHeads; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[h][i] += __shfl_xor_sync(0xffffffffu, o[h][i], w);
   }
   template <typename F> __device__ __forceinline__ void each_head(int lane, F f) {
     if ((lane & 15) == 0)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) f((lane >> 4) * 4 + i, m[i], l[i]);
+      for (int i = 0; i < kHalf; ++i) f((lane >> 4) * kHalf + i, m[i], l[i]);
   }
   template <typename F, typename G> __device__ __forceinline__ void each(int lane, F f, G g) {
-    float mh[8];
+    float mh[kHeads];
 #pragma unroll
-    for (int h = 0; h < 8; ++h) mh[h] = __shfl_sync(0xffffffffu, m[h & 3], (h >> 2) * 16);
+    for (int h = 0; h < kHeads; ++h) mh[h] = __shfl_sync(0xffffffffu, m[h % kHalf], h / kHalf * 16);
     if (lane < kGroupLanes && lane < kChunks)
 #pragma unroll
-      for (int h = 0; h < 8; ++h) {
+      for (int h = 0; h < kHeads; ++h) {
         const auto x = f(h, mh[h]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) g(x, o[h][i], h, lane * 4 + i);
@@ -441,7 +449,7 @@ __device__ __forceinline__ void store4(const AttendArgs &a, int b, int head, int
   else *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = v;
 }
 
-constexpr int attend_ctas(int blocks, int tiles_of_heads) { return blocks <= 2 && tiles_of_heads == 1 ? 2 : 1; }   // of an SM
+constexpr int attend_ctas(int blocks, int tiles_of_heads) { return blocks <= 2 && tiles_of_heads <= 1 ? 2 : 1; }   // of an SM
 
 // CLUSTER: CTA (rank, key head and head tile, request) has a share of that request's tiles alone.
 template <typename T, int NB, int NT, bool CLUSTER>
@@ -630,7 +638,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
     float *slots = reinterpret_cast<float *>(sm + at.slots);
     float2 *ml = reinterpret_cast<float2 *>(sm + at.ml);
     constexpr int kRow = P::kCols + 4, kSlot = P::kHeads * kRow;
-    static_assert(sizeof(T) == 2 || 2 * kSlot >= kConsumers * kScratch, "the probabilities lie in the slots, which are free between ends");
+    static_assert(sizeof(T) == 2 || 2 * kSlot >= kConsumers * kScratch<P::kHeads>, "the probabilities lie in the slots, which are free between ends");
     bool ok = true;
     int b = 0, h = 0, j = 0;
     if (t0 < t1) {
@@ -660,7 +668,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
         if (rows > 0 && ok) {
           const uint32_t sk = smem_u32(sm + st * at.stage);
           part.step(sk, sk + NB * kBlockBytes, reinterpret_cast<const float *>(sm + at.bias) + st * kTile, a.logw != nullptr, warp * kRowsOfWarp, rows, a.scale,
-                    lane, slots + warp * kScratch);
+                    lane, slots + warp * kScratch<P::kHeads>);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(empty + st);
@@ -874,16 +882,16 @@ bool encode_pages(const PagedCfg &cfg, CUtensorMap *map, void *base, bool bf16, 
 
 using AttendKernel = void (*)(CUtensorMap, CUtensorMap, AttendArgs);
 template <bool CLUSTER> AttendKernel attend_kernel(const PagedCfg &cfg, bool bf16) {
-  const bool wide = cfg.tile_heads == 16;
+  const bool wide = cfg.tile_heads == 16, few = cfg.tile_heads == 2;
   switch (bf16 ? cfg.blocks : 4 + cfg.blocks) {
     case 1: return wide ? k_attend<__nv_bfloat16, 1, 2, CLUSTER> : k_attend<__nv_bfloat16, 1, 1, CLUSTER>;
     case 2: return wide ? k_attend<__nv_bfloat16, 2, 2, CLUSTER> : k_attend<__nv_bfloat16, 2, 1, CLUSTER>;
     case 3: return wide ? k_attend<__nv_bfloat16, 3, 2, CLUSTER> : k_attend<__nv_bfloat16, 3, 1, CLUSTER>;
     case 4: return wide ? k_attend<__nv_bfloat16, 4, 2, CLUSTER> : k_attend<__nv_bfloat16, 4, 1, CLUSTER>;
-    case 5: return k_attend<float, 1, 1, CLUSTER>;
-    case 6: return k_attend<float, 2, 1, CLUSTER>;
-    case 7: return k_attend<float, 3, 1, CLUSTER>;
-    case 8: return k_attend<float, 4, 1, CLUSTER>;
+    case 5: return few ? k_attend<float, 1, 0, CLUSTER> : k_attend<float, 1, 1, CLUSTER>;
+    case 6: return few ? k_attend<float, 2, 0, CLUSTER> : k_attend<float, 2, 1, CLUSTER>;
+    case 7: return few ? k_attend<float, 3, 0, CLUSTER> : k_attend<float, 3, 1, CLUSTER>;
+    case 8: return few ? k_attend<float, 4, 0, CLUSTER> : k_attend<float, 4, 1, CLUSTER>;
   }
   return nullptr;
 }
@@ -891,10 +899,14 @@ template <bool CLUSTER> AttendKernel attend_kernel(const PagedCfg &cfg, bool bf1
 constexpr size_t kSmSmem = 228 * 1024, kCtaReserve = 1024;   // shared memory of an SM, and what the system takes of it for each CTA
 
 // CTAs of a cluster per request and key head, 0: no clusters.  `n` tiles of one at most, `heads` of them.
-int cluster_for(const PagedCfg &cfg, long long n, long long heads) {
+// Clusters leave SMs idle where there are few heads and give every request the time of the longest, the line of tiles costs a second kernel.  One request of 28 heads on
+// 4: 1000 rows 9.3 us in clusters against 11.4, 5000 12.2 / 14.3, 9000 15.1 / 14.4, 16000 19.9 / 16.0; eight of them (clusters of 8, two CTAs per SM):
+// 1000 9.6 / 15.3, 5000 16.7 / 21.8, 16000 48 / 54.  fp32, 2 heads on 2: 200 rows 8.3 / 9.1, 1000 10.1 / 9.9, 4000 14.4 / 11.1.
+int cluster_for(const PagedCfg &cfg, long long n, long long heads, bool bf16, int sm_count) {
   for (int size = cfg.cluster; size >= 2; size /= 2) {
     const int i = size == 2 ? 0 : size == 4 ? 1 : size == 8 ? 2 : 3;
-    if (heads <= cfg.clusters[i] && n <= (long long)size * kClusterTiles) return size;
+    const int most = (bf16 ? 8 : 2) * (heads * size * 4 >= sm_count * 3 ? 2 : 1);   // tiles of a CTA
+    if (heads <= cfg.clusters[i] && n <= (long long)size * most) return size;
   }
   return 0;
 }
@@ -909,12 +921,12 @@ cudaError_t paged_configure(PagedCfg *cfg, const DeviceCfg &dev, int n_qh, int n
   if (qres != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
   cfg->encode_tiled = fn;
   e = plan_configure();
-  if (e == cudaSuccess) e = select_pages_configure();
-  if (e != cudaSuccess) return e;
   const int blocks = (d_h * (bf16 ? 2 : 4) + kBoxBytes - 1) / kBoxBytes, group = n_qh / n_kvh;
-  if (blocks > 4) return cudaSuccess;
+  if (e != cudaSuccess || blocks > 4) return e;
+  e = select_pages_configure(d_h, bf16);
+  if (e != cudaSuccess) return e;
   cfg->blocks = blocks;
-  cfg->tile_heads = bf16 && group > 8 ? 16 : 8;
+  cfg->tile_heads = bf16 ? (group > 8 ? 16 : 8) : group > 2 ? 8 : 2;
   cfg->head_tiles = (group + cfg->tile_heads - 1) / cfg->tile_heads;
   e = cudaFuncSetAttribute(attend_kernel<false>(*cfg, bf16), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dev.smem_optin);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attend_kernel<true>(*cfg, bf16), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dev.smem_optin);
@@ -968,7 +980,7 @@ cudaError_t launch_attend(AttendArgs a, const pact_paged_cache &cache, const Pag
   const int ctas = dev.sm_count * per_sm;
   // the most tiles that a request and key head can have
   const long long n = ((long long)(a.selected && a.n_select < a.width ? a.n_select : a.width) * a.page + kTile - 1) / kTile;
-  const int size = cluster_for(cfg, n, (long long)a.B * Hn);
+  const int size = cluster_for(cfg, n, (long long)a.B * Hn, bf16, dev.sm_count);
   const int B = size ? 1 : a.B;
   const size_t most = kSmSmem / per_sm - kCtaReserve;
   a.stages = kMaxAttendStages;

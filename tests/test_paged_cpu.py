@@ -168,7 +168,7 @@ static cudaError_t fake_last_error() { return cudaSuccess; }
 namespace pact {
 cudaError_t launch_cache_plan(PlanArgs, int, cudaStream_t, int *n) { ++launched; *n = 1; return cudaSuccess; }
 cudaError_t launch_cache_write(const WriteArgs &, bool, int, cudaStream_t) { ++launched; return cudaSuccess; }
-cudaError_t launch_page_select(const SelectArgs &, bool, cudaStream_t, int *n) { ++launched; *n = 2; return cudaSuccess; }
+cudaError_t launch_page_select(const SelectArgs &, bool, int, int, cudaStream_t) { ++launched; return cudaSuccess; }
 cudaError_t launch_attend(AttendArgs, const pact_paged_cache &, const PagedCfg &, const DeviceCfg &, bool, cudaStream_t, int *n) { ++launched; *n = 2; return cudaSuccess; }
 size_t attend_scratch(const PagedCfg &, const DeviceCfg &, bool, AttendArgs *, char *) { return 4096; }
 }
