@@ -10,7 +10,7 @@
 // its shared memory and selects.  (As two kernels: 22 us instead of 13 for 32 requests of 16384 rows, 16 instead of 12 for two of 131072.)
 // Scores, bf16: pages (16) by query heads (8) on mma.sync; rows are loaded 16 bytes per lane straight into operands (a dot product does not
 // mind the order of its columns, so keys and queries take the same convenient one).  fp32: fused multiply-adds, folded over the lanes.
-// Selection: the bin of the n-th largest score (histograms of eleven bits from the first bit in which the scores differ), what lies near it in
+// Selection: the bin of the n-th largest score (histograms of ten bits from the first bit in which the scores differ), what lies near it in
 // double, and the selected places in order from a bit mask.
 #include "paged.cuh"
 #include "tma.cuh"
@@ -72,21 +72,14 @@ __device__ __forceinline__ void mma_16x8(float (&d)[4], uint32_t a0, uint32_t a1
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// bf16: scores of pages p0 .. p0 + 15 by a warp, into put(page, score as an integer).  Lane 4 r + c reads columns 32 j + 8 c .. + 7 of pages r and r + 8.
-// ND: blocks of 32 columns.  Error of a sum: 4 ND instructions of 17 addends each, which tensor cores align to the largest and cut off, each off by 2^-23
-// of the sum of all absolute values at most.
-template <int ND, typename F> __device__ __forceinline__ void score_pages(const SelectArgs &a, int b, int head, int p0, int np, uint32_t &err, F put) {
+// bf16: scores of pages p0 .. p0 + 15 by a warp, into put(page, score as an integer); id: page of this lane, of the first 16 (fp32: 8).  Lane 4 r + c reads columns 32 j + 8 c .. + 7 of pages r and r + 8.
+// ND: blocks of 32 columns.  Error of a sum: an instruction adds 17 numbers, which tensor cores align to the largest and cut off, each off by 2^-23 of the absolute sum at most; four
+// of them make the sum of a block, and the sums of the blocks are added with rounding.  (All in one chain: the same time, but every instruction off by a part of
+// the whole, four times as many scores in doubt; every instruction's result added by itself: 2 to 4 us more.)
+template <int ND, typename F> __device__ __forceinline__ void score_pages(const SelectArgs &a, int b, int head, int p0, int id, int np, uint32_t &err, F put) {
   using T = __nv_bfloat16;
-  constexpr float kRel = 4 * ND * 17 / 8388608.f;
+  constexpr float kRel = (4 * 17 + ND) / 8388608.f;
   const int lane = threadIdx.x & 31, r = lane / 4, c = lane % 4;
-  int id = -1;                                             // page of lane & 15
-  if (lane < 16 && p0 + lane < np) {
-    id = a.table[(long long)b * a.width + p0 + lane];
-    if (id < 0 || id >= a.n_pages) {
-      id = -1;
-      if (a.status && head == 0) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
-    }
-  }
   const int id0 = __shfl_sync(0xffffffffu, id, r), id1 = __shfl_sync(0xffffffffu, id, r + 8);
   const uint4 zero = make_uint4(0, 0, 0, 0);
   const T *bounds = static_cast<const T *>(a.bounds) + (long long)head * 2 * a.d_h, *Q = static_cast<const T *>(a.Q) + b * a.ldQ + (long long)head * a.group * a.ldQh;
@@ -121,12 +114,15 @@ template <int ND, typename F> __device__ __forceinline__ void score_pages(const 
           m0[i] = __vmaxu2(lo0[i] & 0x7FFF7FFFu, hi0[i] & 0x7FFF7FFFu);
           m1[i] = __vmaxu2(lo1[i] & 0x7FFF7FFFu, hi1[i] & 0x7FFF7FFFu);
         }
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
-          mma_16x8(s, lo0[i], lo1[i], lo0[i + 1], lo1[i + 1], bf2_min(qw[i], 0u), bf2_min(qw[i + 1], 0u));
-          mma_16x8(s, hi0[i], hi1[i], hi0[i + 1], hi1[i + 1], bf2_max(qw[i], 0u), bf2_max(qw[i + 1], 0u));
+          mma_16x8(y, lo0[i], lo1[i], lo0[i + 1], lo1[i + 1], bf2_min(qw[i], 0u), bf2_min(qw[i + 1], 0u));
+          mma_16x8(y, hi0[i], hi1[i], hi0[i + 1], hi1[i + 1], bf2_max(qw[i], 0u), bf2_max(qw[i + 1], 0u));
           mma_16x8(t, m0[i], m1[i], m0[i + 1], m1[i + 1], qw[i] & 0x7FFF7FFFu, qw[i + 1] & 0x7FFF7FFFu);
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += y[e];
       }
     }
 #pragma unroll
@@ -166,18 +162,10 @@ template <int N> __device__ __forceinline__ void fold(float (&x)[N], int lane, i
 
 // fp32: scores of pages p0 .. p0 + 7 by a warp.  A lane has DL columns and takes four query heads at a time.  Error: 2 DL additions in a lane and five over
 // the lanes, of 2^-24 each.
-template <int DL, typename F> __device__ __forceinline__ void score_pages_f32(const SelectArgs &a, int b, int head, int p0, int np, uint32_t &err, F put) {
+template <int DL, typename F> __device__ __forceinline__ void score_pages_f32(const SelectArgs &a, int b, int head, int p0, int id, int np, uint32_t &err, F put) {
   constexpr float kRel = (2 * DL + 5) / 16777216.f;
   const int lane = threadIdx.x & 31, c = lane * DL;
   const bool mine = c < a.d_h;                             // (d_h is a multiple of 4)
-  int id = -1;                                             // page of lane & 7
-  if (lane < 8 && p0 + lane < np) {
-    id = a.table[(long long)b * a.width + p0 + lane];
-    if (id < 0 || id >= a.n_pages) {
-      id = -1;
-      if (a.status && head == 0) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
-    }
-  }
   const float *bounds = static_cast<const float *>(a.bounds), *Q = static_cast<const float *>(a.Q) + b * a.ldQ + (long long)head * a.group * a.ldQh;
   const auto load = [&](const float *p, bool there, float (&x)[DL]) {
 #pragma unroll
@@ -263,7 +251,7 @@ template <typename T> __device__ __noinline__ double exact_score(const SelectArg
   return best + w;
 }
 
-constexpr int kPickBits = 11;
+constexpr int kPickBits = 10;
 constexpr int kPickKeys = 8192;            // scores of a request and head that are kept in shared memory
 constexpr int kPickNear = 256;             // most scores near the n-th largest that are decided by comparing them with one another
 constexpr int kPickBin = 64;               // a bin of no more scores than this is not divided further
@@ -276,7 +264,7 @@ struct PickShared {
   int doubt[kPickNear];                    // of these, the ones that fp32 leaves in doubt
   unsigned long long cand[kPickNear];      // their scores in double
   unsigned long long w_max[kSelectWarps], w_min[kSelectWarps];
-  uint32_t err[kMaxSelectCluster * kSelectWarps];   // largest error of every warp of the cluster
+  uint32_t range[3][kMaxSelectCluster * kSelectWarps];   // largest and smallest score and largest error of every warp of the cluster
   int w_sum[kSelectWarps];
   int bin, above, in_bin, n_near, n_sure, n_doubt;
 };
@@ -380,18 +368,31 @@ __global__ void __launch_bounds__(kSelectThreads, W * sizeof(T) <= 4 ? 2 : 1) k_
   const bool kept = np <= kPickKeys;                       // in shared memory, otherwise in the workspace
   cluster_wait();
   if (!all) {
-    uint32_t err = 0;
+    uint32_t kmax = 0, kmin = ~0u, err = 0;                // (of all pages; the range may be wider than that of the ones the scores decide between)
     const auto put = [&](int p, uint32_t k) {
+      kmax = max(kmax, k);
+      kmin = min(kmin, k);
       if (kept) st_cluster_u32(s_keys + p, 0, k);
       else a.approx[row + p] = k;
     };
     constexpr int PER = sizeof(T) == 2 ? 16 : 8;           // pages of a warp
-    for (int p0 = (rank * kSelectWarps + warp) * PER; p0 < np; p0 += ctas * kSelectWarps * PER) {
-      if constexpr (sizeof(T) == 2) score_pages<2 * W>(a, b, head, p0, np, err, put);
-      else score_pages_f32<2 * W>(a, b, head, p0, np, err, put);
+    const int step = ctas * kSelectWarps * PER;
+    const auto page_at = [&](int p) { return lane < PER && p + lane < np ? a.table[(long long)b * a.width + p + lane] : -1; };
+    int p0 = (rank * kSelectWarps + warp) * PER, next = page_at(p0);
+    for (; p0 < np; p0 += step) {
+      int id = next;
+      next = page_at(p0 + step);                           // (a trip ahead of the pages themselves)
+      if (lane < PER && p0 + lane < np && (id < 0 || id >= a.n_pages)) {
+        id = -1;
+        if (a.status && head == 0) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
+      }
+      if constexpr (sizeof(T) == 2) score_pages<2 * W>(a, b, head, p0, id, np, err, put);
+      else score_pages_f32<2 * W>(a, b, head, p0, id, np, err, put);
     }
+    kmax = __reduce_max_sync(0xffffffffu, kmax);
+    kmin = __reduce_min_sync(0xffffffffu, kmin);
     err = __reduce_max_sync(0xffffffffu, err);
-    if (lane == 0) st_cluster_u32(s.err + rank * kSelectWarps + warp, 0, err);
+    if (lane < 3) st_cluster_u32(s.range[lane] + rank * kSelectWarps + warp, 0, lane == 0 ? kmax : lane == 1 ? kmin : err);
   }
   cluster_sync();
   if (rank) return;
@@ -401,29 +402,16 @@ __global__ void __launch_bounds__(kSelectThreads, W * sizeof(T) <= 4 ? 2 : 1) k_
   }
   const int need = a.n_select - a.n_first - a.n_last;
   const uint32_t *apx = a.approx + row;
-  uint32_t kmax = 0, kmin = ~0u, err = 0;
-  for (int i = first + tid; i < end; i += kSelectThreads) {
-    const uint32_t k = kept ? s_keys[i] : apx[i];
-    kmax = max(kmax, k);
-    kmin = min(kmin, k);
+  uint32_t kmax = 0, kmin = ~0u, err = 0;                  // (every warp for itself)
+  for (int i = lane; i < ctas * kSelectWarps; i += 32) {
+    kmax = max(kmax, s.range[0][i]);
+    kmin = min(kmin, s.range[1][i]);
+    err = max(err, s.range[2][i]);
   }
-  if (tid < ctas * kSelectWarps) err = s.err[tid];         // (at most as many as threads)
   kmax = __reduce_max_sync(0xffffffffu, kmax);
   kmin = __reduce_min_sync(0xffffffffu, kmin);
   err = __reduce_max_sync(0xffffffffu, err);
-  if (lane == 0) {
-    s.w_max[warp] = kmax;
-    s.w_min[warp] = kmin;
-    s.w_sum[warp] = (int)err;
-  }
   if (tid == 0) s.n_near = s.n_sure = s.n_doubt = 0;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kSelectWarps; ++w) {
-    kmax = max(kmax, (uint32_t)s.w_max[w]);
-    kmin = min(kmin, (uint32_t)s.w_min[w]);
-    err = max(err, (uint32_t)s.w_sum[w]);
-  }
   __syncthreads();
   const auto key = [&](int i) { return kept ? s_keys[i] : apx[i]; };
   const int words = (np + 31) / 32;
