@@ -11,9 +11,9 @@
 namespace pact {
 namespace {
 
-constexpr int kPlanThreads = 1024;
-constexpr int kPlanRowsAlone = 8192;       // new rows up to which one CTA does everything
-constexpr int kPlanRowsPerCta = 4096;
+constexpr int kPlanRequests = 256;         // requests up to which CTAs have 256 threads, beyond 1024
+constexpr int kPlanRowsAlone = 1024;       // new rows up to which one CTA does everything
+constexpr int kPlanRowsInPlace = 8192;     // the same where lengths are updated in place
 
 struct Sums {
   long long need, freed, rows;
@@ -32,27 +32,37 @@ __device__ __forceinline__ int find_share(const int *pre, int n, int k) {
   return lo;
 }
 
-__global__ void __launch_bounds__(kPlanThreads) k_cache_plan(PlanArgs a) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) k_cache_plan(PlanArgs a) {
   extern __shared__ int s_plan[];
-  __shared__ Sums s_warp[kPlanThreads / 32];
+  __shared__ Sums s_warp[THREADS / 32];
   int *s_need = s_plan, *s_freed = s_need + a.B + 1, *s_rows = s_freed + a.B + 1, *s_len = s_rows + a.B + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (a.B + kPlanThreads - 1) / kPlanThreads;       // requests of a thread
+  const int per = (a.B + THREADS - 1) / THREADS;                   // requests of a thread
   pdl_wait();
   pdl_trigger();
   const long long n_free = *a.n_free;
   const long long room = (long long)a.width * a.page;
+  const auto sums_of = [&](int len, int add_rows) {
+    const bool ended = add_rows < 0;
+    const unsigned rows = ended ? 0u : (unsigned)add_rows, had = ((unsigned)len + (unsigned)a.page - 1u) / (unsigned)a.page;
+    // (len + rows < 2^32: both are below 2^31; what does not fit the table is refused before these are used)
+    const unsigned all = (unsigned)(((unsigned long long)(unsigned)len + rows + (unsigned)a.page - 1u) / (unsigned)a.page);
+    return Sums{ended ? 0ll : (long long)all - had, ended ? (long long)had : 0ll, (long long)rows};
+  };
   Sums mine = {0, 0, 0};
   bool bad = n_free < 0 || n_free > a.n_pages;
   for (int i = 0; i < per; ++i) {
     const int b = tid * per + i;
     if (b >= a.B) break;
-    const long long len = a.length[b], add_rows = a.n_new[b * a.n_new_stride];
-    const bool ended = add_rows < 0;
-    const long long rows = ended ? 0 : add_rows, had = (len + a.page - 1) / a.page;
-    bad = bad || len < 0 || len + rows > room || (a.row_stride && rows > a.row_stride);
-    mine = add(mine, {ended ? 0 : (len + rows + a.page - 1) / a.page - had, ended ? had : 0, rows});
-    s_len[b] = (int)len;
+    const int len = a.length[b], add_rows = a.n_new[b * a.n_new_stride];
+    bad = bad || len < 0 || len + (long long)max(add_rows, 0) > room || (a.row_stride && add_rows > a.row_stride);
+    const Sums x = sums_of(max(len, 0), add_rows);
+    s_need[b] = (int)mine.need;                                    // so far: before this request, of this thread's
+    s_freed[b] = (int)mine.freed;
+    s_rows[b] = (int)mine.rows;
+    s_len[b] = len;
+    mine = add(mine, x);
   }
   Sums upto = mine;                                                // inclusive over the warp
 #pragma unroll
@@ -63,30 +73,25 @@ __global__ void __launch_bounds__(kPlanThreads) k_cache_plan(PlanArgs a) {
   if (lane == 31) s_warp[warp] = upto;
   const bool any_bad = __syncthreads_or(bad);
   Sums total = {0, 0, 0}, before = {0, 0, 0};
-  for (int w = 0; w < kPlanThreads / 32; ++w) {
+#pragma unroll 8
+  for (int w = 0; w < THREADS / 32; ++w) {
     if (w == warp) before = total;
     total = add(total, s_warp[w]);
   }
   const bool invalid = any_bad || total.rows > a.n_rows || n_free + total.freed > a.n_pages;
-  const bool ok = !invalid && total.need <= n_free + total.freed;
-  if (ok) {                                                        // every sum fits 32 bits
-    Sums at = {before.need + upto.need - mine.need, before.freed + upto.freed - mine.freed, before.rows + upto.rows - mine.rows};
-    for (int i = 0; i < per; ++i) {
-      const int b = tid * per + i;
-      if (b >= a.B) break;
-      const long long len = s_len[b], add_rows = a.n_new[b * a.n_new_stride];
-      const bool ended = add_rows < 0;
-      const long long rows = ended ? 0 : add_rows, had = (len + a.page - 1) / a.page;
-      s_need[b] = (int)at.need;
-      s_freed[b] = (int)at.freed;
-      s_rows[b] = (int)at.rows;
-      at = add(at, {ended ? 0 : (len + rows + a.page - 1) / a.page - had, ended ? had : 0, rows});
-    }
-    if (tid == 0) {
-      s_need[a.B] = (int)total.need;
-      s_freed[a.B] = (int)total.freed;
-      s_rows[a.B] = (int)total.rows;
-    }
+  const bool ok = !invalid && total.need <= n_free + total.freed;  // then every sum fits 32 bits
+  const Sums at = {before.need + upto.need - mine.need, before.freed + upto.freed - mine.freed, before.rows + upto.rows - mine.rows};
+  for (int i = 0; i < per; ++i) {
+    const int b = tid * per + i;
+    if (b >= a.B) break;
+    s_need[b] += (int)at.need;
+    s_freed[b] += (int)at.freed;
+    s_rows[b] += (int)at.rows;
+  }
+  if (tid == 0) {
+    s_need[a.B] = (int)total.need;
+    s_freed[a.B] = (int)total.freed;
+    s_rows[a.B] = (int)total.rows;
   }
   __syncthreads();
 
@@ -97,7 +102,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_cache_plan(PlanArgs a) {
     const int b = find_share(s_freed, a.B, i - nf);
     return a.table[(long long)b * a.width + (i - nf - s_freed[b])];
   };
-  const long long first = (long long)blockIdx.x * kPlanThreads + tid, step = (long long)gridDim.x * kPlanThreads;
+  const long long first = (long long)blockIdx.x * THREADS + tid, step = (long long)gridDim.x * THREADS;
   if (a.rows && ok) {
     for (long long k = first; k < total.need; k += step) {
       const int b = find_share(s_need, a.B, (int)k);
@@ -130,7 +135,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_cache_plan(PlanArgs a) {
     }
   }
   if (a.commit && blockIdx.x == 0) {
-    for (int b = tid; b < a.B; b += kPlanThreads) {
+    for (int b = tid; b < a.B; b += THREADS) {
       const int add_rows = ok ? a.n_new[b * a.n_new_stride] : 0;
       a.length_out[b] = add_rows < 0 ? 0 : s_len[b] + add_rows;
       if (a.row_start) a.row_start[b] = ok ? s_rows[b] : 0;
@@ -147,22 +152,24 @@ __global__ void __launch_bounds__(kPlanThreads) k_cache_plan(PlanArgs a) {
 
 cudaError_t launch_cache_plan(PlanArgs a, int sm_count, cudaStream_t st, int *launches) {
   const size_t smem = ((size_t)a.B * 4 + 3) * sizeof(int);
+  const bool in_place = a.length_out == a.length || a.n_free_out == a.n_free, wide = a.B > kPlanRequests || (in_place && a.n_rows > kPlanRowsAlone);
+  void (*kernel)(PlanArgs) = wide ? k_cache_plan<1024> : k_cache_plan<256>;
+  const int threads = wide ? 1024 : 256;
   a.rows = a.commit = true;
   *launches = 1;
-  if (a.n_rows <= kPlanRowsAlone) return launch_k(k_cache_plan, dim3(1), dim3(kPlanThreads), smem, st, true, a);
-  const bool in_place = a.length_out == a.length || a.n_free_out == a.n_free;
-  const long long ctas = (a.n_rows + kPlanRowsPerCta - 1) / kPlanRowsPerCta;
+  if (a.n_rows <= (in_place ? kPlanRowsInPlace : kPlanRowsAlone)) return launch_k(kernel, dim3(1), dim3(threads), smem, st, true, a);
+  const long long ctas = (a.n_rows + 4 * threads - 1) / (4 * threads), most = wide ? sm_count : 4 * sm_count;
   a.commit = !in_place;
-  cudaError_t e = launch_k(k_cache_plan, dim3((unsigned)(ctas < sm_count ? ctas : sm_count)), dim3(kPlanThreads), smem, st, true, a);
+  cudaError_t e = launch_k(kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(threads), smem, st, true, a);
   if (e != cudaSuccess || !in_place) return e;
   a.rows = false;
   a.commit = true;
   *launches = 2;
-  return launch_k(k_cache_plan, dim3(1), dim3(kPlanThreads), smem, st, true, a);
+  return launch_k(kernel, dim3(1), dim3(threads), smem, st, true, a);
 }
 
 cudaError_t plan_configure() {
-  return cudaFuncSetAttribute(k_cache_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(((size_t)PACT_MAX_REQUESTS * 4 + 3) * sizeof(int)));
+  return cudaFuncSetAttribute(k_cache_plan<1024>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(((size_t)PACT_MAX_REQUESTS * 4 + 3) * sizeof(int)));
 }
 
 }  // namespace pact
