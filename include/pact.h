@@ -296,7 +296,8 @@ size_t pact_host_staging_bytes(const pact_ctx *ctx, int n_total, int N);
  *
  * `status` (device int32[1], may be NULL) is lowered to a negative pact_status when the device meets something that it cannot
  * serve, and never raised again: the caller clears it.  Whatever lengths, tables and slots hold, nothing outside the given buffers is read or
- * written.  The context's device must be the current one.  n_requests is at most PACT_MAX_REQUESTS. */
+ * written.  The context's device must be the current one.  n_requests is at most PACT_MAX_REQUESTS.  Heads are at most 256 wide in bf16 and 128 in fp32
+ * (PACT_ERR_UNSUPPORTED above). */
 #define PACT_MAX_REQUESTS 4096
 
 /* One layer's cache.  K and V: element [page][head][row][c] lies at page * k_page + head * k_head + row * k_row + c (elements;
@@ -397,7 +398,7 @@ pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache /*host
  * those below 0 or beyond the request's pages are skipped, and a page named twice counts twice.  Rows with logw = minus infinity and
  * rows past the length have no effect, whatever their keys and values hold.  Without any row out is 0 and lse minus infinity.
  * Logits, softmax statistics and sums are fp32; bf16 probabilities are carried as two bf16 terms (error 2^-17).
- * d_h <= 256 for bf16, <= 128 for fp32 (UNSUPPORTED above).  Lengths are clamped to 0 .. max_pages * page_rows and rows of pages outside
+ * Lengths are clamped to 0 .. max_pages * page_rows and rows of pages outside
  * the cache are left out; both set status to INVALID_ARG. */
 pact_status pact_paged_attention(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_query *q /*host*/, void *stream);
 

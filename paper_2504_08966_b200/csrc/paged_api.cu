@@ -76,7 +76,7 @@ pact_status pact_cache_write(pact_ctx *ctx, const pact_paged_cache *cache, const
   if (r->n_rows == 0) return PACT_OK;
   if (!r->K || !r->V || !r->slot || !aligned16(r->K) || !aligned16(r->V) || !stride_ok(ctx, r->ld_row) || !stride_ok(ctx, r->ld_head)) return PACT_ERR_INVALID_ARG;
   if (r->n_rows > INT32_MAX) return PACT_ERR_UNSUPPORTED;
-  if (ctx->d_h * ctx->elt > 4096) return PACT_ERR_UNSUPPORTED;   // (a CTA's threads have to hold a row)
+  if (!ctx->paged.blocks) return PACT_ERR_UNSUPPORTED;
   WriteArgs a;
   a.Kn = r->K; a.Vn = r->V; a.ld_row = r->ld_row; a.ld_head = r->ld_head; a.logw_new = r->logw; a.slot = r->slot; a.n_rows = r->n_rows;
   a.K = cache->K; a.V = cache->V; a.k_page = cache->k_page; a.k_head = cache->k_head; a.k_row = cache->k_row;
