@@ -68,10 +68,16 @@ __host__ __device__ inline AttendSmem attend_smem(int stages, int blocks, int he
   return m;
 }
 
-__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y, int z, int w) {
+__device__ __forceinline__ void tma_load_5d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y, int z, int w, int v) {
   asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-      ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+      ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(v) : "memory");
+}
+__device__ __forceinline__ void copy16(void *dst, const void *src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void arrive_after_copies(uint64_t *bar) {   // once this thread's 16-byte copies so far have landed
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
@@ -161,20 +167,20 @@ template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
     }
   }
 
-  // rows [row0, row0 + 16) of the tile, of which the first `rows` count
-  __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, const float *bias, bool has_bias, int row0, int rows, float scale, int lane, float *) {
+  // 16 rows, of which the first `rows` count: K from sk on, V from sv on, 128 bytes of each and `block` bytes to the next 128 of their columns
+  __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, uint32_t block, const float *bias, bool has_bias, int rows, float scale, int lane, float *) {
     float s[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
     {
-      const int r = row0 + (lane & 15), x = r & 7;
+      const int r = lane & 15, x = r & 7;
       const uint32_t at = sk + r * kBoxBytes;
 #pragma unroll
       for (int k = 0; k < NB * 4; ++k) {
         uint32_t a[4];
-        ldsm4(a, at + (k / 4) * kBlockBytes + ((((k % 4) * 2 + (lane >> 4)) ^ x) << 4));
+        ldsm4(a, at + (k / 4) * block + ((((k % 4) * 2 + (lane >> 4)) ^ x) << 4));
 #pragma unroll
         for (int n = 0; n < NT; ++n) mma_bf16(s[n], a, q[k][n][0], q[k][n][1]);
       }
@@ -182,8 +188,8 @@ template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
     const int r0 = lane / 4, r1 = r0 + 8;
     float b0 = 0.f, b1 = 0.f;
     if (has_bias) {
-      b0 = bias[row0 + r0];
-      b1 = bias[row0 + r1];
+      b0 = bias[r0];
+      b1 = bias[r1];
     }
     const bool in0 = r0 < rows && b0 != -INFINITY, in1 = r1 < rows && b1 != -INFINITY;
     float top[NT][2];
@@ -246,12 +252,12 @@ template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
       keep1 = ((rows1 >> r) & 1 ? 0xFFFFu : 0u) | ((rows1 >> (r + 4)) & 1 ? 0xFFFF0000u : 0u);
     }
     {
-      const int r = row0 + (lane & 7) + (lane >> 4) * 8, x = r & 7;
+      const int r = (lane & 7) + (lane >> 4) * 8, x = r & 7;
       const uint32_t at = sv + r * kBoxBytes;
 #pragma unroll
       for (int c = 0; c < NB * 4; ++c) {
         uint32_t a[4];
-        ldsm4_t(a, at + (c / 4) * kBlockBytes + ((((c % 4) * 2 + ((lane >> 3) & 1)) ^ x) << 4));
+        ldsm4_t(a, at + (c / 4) * block + ((((c % 4) * 2 + ((lane >> 3) & 1)) ^ x) << 4));
         if (clear) {
           a[0] &= keep0;
           a[1] &= keep0;
@@ -330,8 +336,8 @@ template <int NB, int NT> struct Part<float, NB, NT> {
   }
 
   // scratch: 16 rows of probabilities and a row of factors, this warp's
-  __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, const float *bias, bool has_bias, int row0, int rows, float scale, int lane, float *scratch) {
-    const int r = lane & 15, half = lane >> 4, row = row0 + r, x = row & 7;
+  __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, uint32_t block, const float *bias, bool has_bias, int rows, float scale, int lane, float *scratch) {
+    const int r = lane & 15, half = lane >> 4, x = r & 7;
     float s[kHeads];
 #pragma unroll
     for (int h = 0; h < kHeads; ++h) s[h] = 0.f;
@@ -340,11 +346,11 @@ template <int NB, int NT> struct Part<float, NB, NT> {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int c = 2 * i + half;
-        const float4 k = lds4(sk + nb * kBlockBytes + row * kBoxBytes + ((c ^ x) << 4));
+        const float4 k = lds4(sk + nb * block + r * kBoxBytes + ((c ^ x) << 4));
 #pragma unroll
         for (int h = 0; h < kHeads; ++h) s[h] = fma4(k, lds4(q + h * q_row + nb * kBoxBytes + c * 16), s[h]);
       }
-    const float b = has_bias ? bias[row] : 0.f;
+    const float b = has_bias ? bias[r] : 0.f;
     const bool in = r < rows && b != -INFINITY;
     float t[kHalf], top[kHalf];
 #pragma unroll
@@ -389,8 +395,7 @@ template <int NB, int NT> struct Part<float, NB, NT> {
 #pragma unroll 4
       for (int k = lane / kGroupLanes; k < kRowsOfWarp; k += kGroups) {
         if (!(live >> k & 1)) continue;       // zero times an infinity or a NaN would not be zero
-        const int vr = row0 + k;
-        const float4 v = lds4(sv + (c / 8) * kBlockBytes + vr * kBoxBytes + (((c % 8) ^ (vr & 7)) << 4));
+        const float4 v = lds4(sv + (c / 8) * block + k * kBoxBytes + (((c % 8) ^ (k & 7)) << 4));
         float p[kHeads];
         if constexpr (kHeads == 8) {
           const float4 p0 = *reinterpret_cast<const float4 *>(scratch + k * 8), p1 = *reinterpret_cast<const float4 *>(scratch + k * 8 + 4);
@@ -465,7 +470,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
   int *pre = reinterpret_cast<int *>(sm + at.pre), *w_sum = pre + (CLUSTER ? 1 : a.B) + 1;
   TilePlan *plan = reinterpret_cast<TilePlan *>(sm + at.tiles);
   if (tid < a.stages) {
-    mbar_init(full + tid, 1);
+    mbar_init(full + tid, a.logw ? 1 + kTile / 4 : 1);          // (the biases: 16 bytes of a lane each)
     mbar_init(empty + tid, kConsumers);
   }
   if (tid == 0) *abort = 0;
@@ -473,9 +478,10 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
   for (int i = tid * 16; i < at.q_own - at.q; i += kAttendThreads * 16) *reinterpret_cast<uint4 *>(sm + at.q + i) = make_uint4(0, 0, 0, 0);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  // what this lane copies of a tile: box `x` of rows, and of it a 128-byte block of K or V, or the biases
-  const int boxes = kTile / a.box_rows, per_box = a.box_rows / kRowsOfWarp, copies = 2 * NB + (a.logw ? 1 : 0);
-  constexpr int kRoles = (4 * (2 * NB + 1) + 31) / 32;
+  // What this lane copies of a tile: of box `x` of rows K, then V, all of their 128-byte blocks at once if they are whole, otherwise one after
+  // the other (columns past d_h are filled in then).  A box lies in a stage as its blocks, each with all rows of the box.
+  const int boxes = kTile / a.box_rows, per_box = a.box_rows / kRowsOfWarp, at_once = a.whole_blocks ? NB : 1, copies = 2 * NB / at_once;
+  constexpr int kRoles = (4 * 2 * NB + 31) / 32;
   int my_box[kRoles], my_copy[kRoles];
 #pragma unroll
   for (int r = 0; r < kRoles; ++r) {
@@ -582,7 +588,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
           p.id[g] = at_rows.id[g];
           p.place |= (uint32_t)(at_rows.off[g] / kRowsOfWarp) << (8 * g);
           // a box is copied if any of its rows counts: its first 16 do then
-          if (g % per_box == 0 && (at_rows.rows >> (8 * g) & 0xffu)) p.bytes += a.box_rows * (2 * NB * kBoxBytes + (a.logw ? 4 : 0));
+          if (g % per_box == 0 && (at_rows.rows >> (8 * g) & 0xffu)) p.bytes += a.box_rows * 2 * NB * kBoxBytes;
         }
         plan[lane] = p;
       }
@@ -608,13 +614,16 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
           const int x = my_box[r], k = my_copy[r], g = 8 * x * per_box;
           if (x < boxes && (rows >> g & 0xffu)) {
             const int page = plan[i].id[x * per_box], row = (int)(place >> g & 0xffu) * kRowsOfWarp;
-            if (k < 2 * NB) {
-              char *to = sm + st * at.stage + k * kBlockBytes + x * a.box_rows * kBoxBytes;
-              tma_load_4d(to, k < NB ? &map_k : &map_v, full + st, (k < NB ? k : k - NB) * (kBoxBytes / (int)sizeof(T)), row, kv, page);
-            } else {
-              bulk_load(sm + at.bias + (st * kTile + x * a.box_rows) * 4, a.logw + (long long)page * a.page + row, a.box_rows * 4, full + st);
-            }
+            const int nb = k * at_once % NB, of_v = k * at_once / NB, block = a.box_rows * kBoxBytes;
+            char *to = sm + st * at.stage + of_v * NB * kBlockBytes + (x * NB + nb) * block;
+            tma_load_5d(to, of_v ? &map_v : &map_k, full + st, nb * (kBoxBytes / (int)sizeof(T)), row, 0, kv, page);
           }
+        }
+        if (a.logw && lane < kTile / 4) {
+          const int g = lane / 4, box = g / per_box * per_box;   // (16 rows of four lanes)
+          if (rows >> (8 * g) & 0xffu)
+            copy16(sm + at.bias + (st * kTile + lane * 4) * 4, a.logw + (long long)plan[i].id[box] * a.page + (place >> (8 * box) & 0xffu) * kRowsOfWarp + (lane * 4 - box * kRowsOfWarp));
+          arrive_after_copies(full + st);
         }
         if (plan[i].first) {
           const int ht = h - kv * a.head_tiles;
@@ -639,6 +648,8 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
     float2 *ml = reinterpret_cast<float2 *>(sm + at.ml);
     constexpr int kRow = P::kCols + 4, kSlot = P::kHeads * kRow;
     static_assert(sizeof(T) == 2 || 2 * kSlot >= kConsumers * kScratch<P::kHeads>, "the probabilities lie in the slots, which are free between ends");
+    // this warp's rows of a stage
+    const uint32_t block = a.box_rows * kBoxBytes, of_warp = warp / per_box * NB * block + warp % per_box * kRowsOfWarp * kBoxBytes;
     bool ok = true;
     int b = 0, h = 0, j = 0;
     if (t0 < t1) {
@@ -666,9 +677,9 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
         if (i == j) part.begin(sm + at.q + st * P::kHeads * at.q_row, at.q_row, sm + at.q_own, lane, tid);
         const int rows = (int)(meta[st] >> (8 * warp) & 0xffu);
         if (rows > 0 && ok) {
-          const uint32_t sk = smem_u32(sm + st * at.stage);
-          part.step(sk, sk + NB * kBlockBytes, reinterpret_cast<const float *>(sm + at.bias) + st * kTile, a.logw != nullptr, warp * kRowsOfWarp, rows, a.scale,
-                    lane, slots + warp * kScratch<P::kHeads>);
+          const uint32_t sk = smem_u32(sm + st * at.stage) + of_warp;
+          part.step(sk, sk + NB * kBlockBytes, block, reinterpret_cast<const float *>(sm + at.bias) + st * kTile + warp * kRowsOfWarp, a.logw != nullptr, rows, a.scale, lane,
+                    slots + warp * kScratch<P::kHeads>);
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(empty + st);
@@ -870,13 +881,14 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(const __grid_co
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                   const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// pages as [page][head][row][column], boxes of 128 bytes x box_rows
+// Pages as [page][head][128-byte block][row][column], boxes of box_rows rows and all blocks; rows that are no whole number of blocks as one block, boxes
+// of 128 bytes of it.
 bool encode_pages(const PagedCfg &cfg, CUtensorMap *map, void *base, bool bf16, const AttendArgs &a, long long ld_page, long long ld_head, long long ld_row) {
-  const int elt = bf16 ? 2 : 4;
-  const cuuint64_t dims[4] = {(cuuint64_t)a.d_h, (cuuint64_t)a.page, (cuuint64_t)a.n_kvh, (cuuint64_t)a.n_pages};
-  const cuuint64_t strides[3] = {(cuuint64_t)ld_row * elt, (cuuint64_t)ld_head * elt, (cuuint64_t)ld_page * elt};
-  const cuuint32_t box[4] = {(cuuint32_t)(kBoxBytes / elt), (cuuint32_t)a.box_rows, 1, 1}, estr[4] = {1, 1, 1, 1};
-  return reinterpret_cast<EncodeTiledFn>(cfg.encode_tiled)(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base, dims, strides, box, estr,
+  const int elt = bf16 ? 2 : 4, blocks = a.whole_blocks ? cfg.blocks : 1;
+  const cuuint64_t dims[5] = {(cuuint64_t)(a.whole_blocks ? kBoxBytes / elt : a.d_h), (cuuint64_t)a.page, (cuuint64_t)blocks, (cuuint64_t)a.n_kvh, (cuuint64_t)a.n_pages};
+  const cuuint64_t strides[4] = {(cuuint64_t)ld_row * elt, (cuuint64_t)kBoxBytes, (cuuint64_t)ld_head * elt, (cuuint64_t)ld_page * elt};
+  const cuuint32_t box[5] = {(cuuint32_t)(kBoxBytes / elt), (cuuint32_t)a.box_rows, (cuuint32_t)blocks, 1, 1}, estr[5] = {1, 1, 1, 1, 1};
+  return reinterpret_cast<EncodeTiledFn>(cfg.encode_tiled)(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 5, base, dims, strides, box, estr,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -972,6 +984,7 @@ size_t attend_scratch(const PagedCfg &cfg, const DeviceCfg &dev, bool bf16, Atte
 cudaError_t launch_attend(AttendArgs a, const pact_paged_cache &cache, const PagedCfg &cfg, const DeviceCfg &dev, bool bf16, cudaStream_t st, int *launches) {
   a.head_tiles = cfg.head_tiles;
   a.box_rows = a.page % 64 == 0 ? 64 : a.page % 32 == 0 ? 32 : 16;
+  a.whole_blocks = a.d_h * (bf16 ? 2 : 4) % kBoxBytes == 0;
   CUtensorMap mk, mv;
   if (!encode_pages(cfg, &mk, cache.K, bf16, a, cache.k_page, cache.k_head, cache.k_row) ||
       !encode_pages(cfg, &mv, cache.V, bf16, a, cache.v_page, cache.v_head, cache.v_row))
