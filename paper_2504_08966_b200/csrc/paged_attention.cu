@@ -787,26 +787,53 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
   if (*abort) land_copies(full, a.stages);
 }
 
-// Parts of the request and key head that was cut at the beginning of CTA blockIdx.x's share and not before it.  Few parts (a batch): one CTA, a warp per
-// head.  Many (a long request): a CTA per head, whose warps share out the parts.  A warp asks for its first sums together with the maxima.
+// Parts of the requests and key heads that were cut.  Few parts (a batch): CTA i < `shares` has what was cut at the beginning of share i and not before it, a
+// warp per head.  Many (a long request): a CTA per head, whose warps share out the parts; there are at most shares / kFewParts of these, and
+// the CTAs from `shares` on look for the one that is theirs.  A warp asks for its first sums together with the maxima.
 constexpr int kJoinWarps = 8;
 constexpr int kMaxParts = 512;             // most CTAs of k_attend
 constexpr int kFewParts = 8;
 
 template <int CH>                          // 16-byte columns of a lane
-__global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(const __grid_constant__ AttendArgs a, int tile_heads, int cols) {
+__global__ void __launch_bounds__(kJoinWarps * 32) k_attend_join(const __grid_constant__ AttendArgs a, int tile_heads, int cols, int shares, int head_ctas) {
   __shared__ float s_w[kJoinWarps][kMaxParts / kJoinWarps + 1];
   __shared__ float4 s_o[kJoinWarps][CH * 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quads = cols / 4;
   pdl_wait();
   pdl_trigger();
-  const int4 d = a.desc[blockIdx.x];
-  const int i0 = blockIdx.x - 1, n = d.y - i0 + 1, b = d.z, kv = d.w / a.head_tiles, ht = d.w - kv * a.head_tiles;
-  const bool few = n <= kFewParts;
-  if (!d.x || (few && blockIdx.y)) return;
+  const bool few = blockIdx.x < shares;
+  int unit = blockIdx.x, first_head = warp;
+  if (!few) {
+    __shared__ int s_count[kJoinWarps], s_unit;
+    const int e = blockIdx.x - shares;
+    first_head = e % head_ctas;
+    int before = e / head_ctas;                                // of the requests of many parts
+    if (threadIdx.x == 0) s_unit = -1;
+    for (int u0 = 0; u0 < shares; u0 += kJoinWarps * 32) {
+      const int u = u0 + threadIdx.x;
+      const int4 x = u < shares ? a.desc[u] : make_int4(0, 0, 0, 0);
+      const bool many = x.x && x.y - (u - 1) + 1 > kFewParts;
+      const uint32_t bits = __ballot_sync(0xffffffffu, many);
+      if (lane == 0) s_count[warp] = __popc(bits);
+      __syncthreads();
+      int at = before, all = 0;
+      for (int w = 0; w < kJoinWarps; ++w) {
+        if (w < warp) at -= s_count[w];
+        all += s_count[w];
+      }
+      if (many && at == __popc(bits & ((1u << lane) - 1u))) s_unit = u;
+      before -= all;
+      __syncthreads();
+    }
+    unit = s_unit;
+    if (unit < 0) return;
+  }
+  const int4 d = a.desc[unit];
+  const int i0 = unit - 1, n = d.y - i0 + 1, b = d.z, kv = d.w / a.head_tiles, ht = d.w - kv * a.head_tiles;
+  if (!d.x || (few && n > kFewParts)) return;
   const int heads = min(tile_heads, a.group - ht * tile_heads);
   const int p0 = few ? 0 : warp * n / kJoinWarps, p1 = few ? n : (warp + 1) * n / kJoinWarps;
-  for (int hd = few ? warp : blockIdx.y; hd < heads; hd += few ? kJoinWarps : gridDim.y) {
+  for (int hd = first_head; hd < heads; hd += few ? kJoinWarps : head_ctas) {
     const auto slot = [&](int p) { return (2 * (long long)(i0 + p) + (p == 0 ? d.x - 1 : 0)) * tile_heads + hd; };
     const auto sum_of = [&](int p, int k) { return *reinterpret_cast<const float4 *>(a.part_o + slot(p) * cols + (lane + 32 * k) * 4); };
     const auto add = [&](const float4 &v, float f, float4 &to) {
@@ -1009,7 +1036,8 @@ cudaError_t launch_attend(AttendArgs a, const pact_paged_cache &cache, const Pag
   if (e != cudaSuccess || n == 1) return e;                    // (a request and key head of one tile is never cut)
   *launches = 2;
   const int cols = cfg.blocks * kBoxBytes / elt, heads = a.group < 8 ? a.group : 8;
-  return launch_k(cols <= 128 ? k_attend_join<1> : k_attend_join<2>, dim3((unsigned)ctas, (unsigned)heads), dim3(kJoinWarps * 32), 0, st, true, a, cfg.tile_heads, cols);
+  return launch_k(cols <= 128 ? k_attend_join<1> : k_attend_join<2>, dim3((unsigned)(ctas + ctas / kFewParts * heads)), dim3(kJoinWarps * 32), 0, st, true, a, cfg.tile_heads,
+                  cols, ctas, heads);
 }
 
 }  // namespace pact
