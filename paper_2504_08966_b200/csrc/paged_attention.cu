@@ -747,42 +747,45 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
       }
     }
   }
-  __syncthreads();
   if constexpr (CLUSTER) {
-    // the parts of the CTAs of a request and key head, each by all of them
+    // The parts of the CTAs of a request and key head: a group of lanes per four columns, a lane per CTA, so that all is asked for in one trip.
     cluster_sync();
     const int b = blockIdx.z, h = blockIdx.y, kv = h / a.head_tiles, ht = h - kv * a.head_tiles, heads = min(P::kHeads, a.group - ht * P::kHeads);
-    const int rank = cluster_rank(), size = cluster_size();
+    const int rank = cluster_rank(), size = cluster_size(), r = tid & (size - 1), items = heads * (P::kCols / 4);
     constexpr int kRow = P::kCols + 4;
     const float *slots = reinterpret_cast<const float *>(sm + at.slots);
     const float2 *ml = reinterpret_cast<const float2 *>(sm + at.ml) + 2 * P::kHeads;
-    for (int i = rank * kAttendThreads + tid; i < heads * (P::kCols / 4); i += size * kAttendThreads) {
-      const int hd = i / (P::kCols / 4), c = (i - hd * (P::kCols / 4)) * 4;
-      float top = -INFINITY, l = 0.f;
-      float2 x[kMaxCluster];
-#pragma unroll
-      for (int r = 0; r < kMaxCluster; ++r) {
-        x[r] = r < size ? ld_cluster2(in_cta(ml + hd, r)) : make_float2(-INFINITY, 0.f);
-        top = fmaxf(top, x[r].x);
+    for (int i0 = 0; i0 < items; i0 += kAttendThreads) {       // (as many groups in all CTAs together)
+      const int i = i0 + (rank * kAttendThreads + tid) / size, hd = i / (P::kCols / 4), c = (i - hd * (P::kCols / 4)) * 4;
+      float2 x = make_float2(-INFINITY, 0.f);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i < items) {
+        x = ld_cluster2(in_cta(ml + hd, r));
+        v = ld_cluster4(in_cta(slots + hd * kRow + c, r));
+        if (x.x == -INFINITY && x.y == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);   // no part, or none of its rows counts
       }
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int r = 0; r < kMaxCluster; ++r) {
-        if (x[r].x == -INFINITY && x[r].y == 0.f) continue;    // no part, or none of its rows counts
-        const float f = weight(x[r].x, top);
-        const float4 v = ld_cluster4(in_cta(slots + hd * kRow + c, r));
-        l = fmaf(x[r].y, f, l);
-        o.x = fmaf(v.x, f, o.x);
-        o.y = fmaf(v.y, f, o.y);
-        o.z = fmaf(v.z, f, o.z);
-        o.w = fmaf(v.w, f, o.w);
+      float top = x.x;
+      for (int o = 1; o < size; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float f = weight(x.x, top);
+      float l = x.y * f;
+      v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+      for (int o = 1; o < size; o <<= 1) {
+        l += __shfl_xor_sync(0xffffffffu, l, o);
+        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+        v.z += __shfl_xor_sync(0xffffffffu, v.z, o);
+        v.w += __shfl_xor_sync(0xffffffffu, v.w, o);
       }
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int head = kv * a.group + ht * P::kHeads + hd;
-      if (c < a.d_h) store4(a, b, head, c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-      if (c == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : top + logf(l);
+      if (i < items && r == 0) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int head = kv * a.group + ht * P::kHeads + hd;
+        if (c < a.d_h) store4(a, b, head, c, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+        if (c == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : top + logf(l);
+      }
     }
     cluster_sync();                                            // (the others have read)
+  } else {
+    __syncthreads();
   }
   if (*abort) land_copies(full, a.stages);
 }
