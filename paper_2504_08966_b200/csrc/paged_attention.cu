@@ -538,7 +538,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
       b = blockIdx.z;
       h = blockIdx.y;
       j = (int)t;
-    } else {
+    } else if (T_all >> 31) {
       int lo = 0, hi = a.B;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -547,6 +547,15 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
       }
       b = lo;
       h = divide_small(t - (long long)pre[lo] * Hn, pre[lo + 1] - pre[lo], &j);
+    } else {                                                   // (the same in 32 bits)
+      int lo = 0, hi = a.B;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (pre[mid] * Hn <= (int)t) lo = mid;
+        else hi = mid;
+      }
+      b = lo;
+      h = divide_small((int)t - pre[lo] * Hn, pre[lo + 1] - pre[lo], &j);
     }
   };
   if constexpr (CLUSTER) {
@@ -748,39 +757,37 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
     }
   }
   if constexpr (CLUSTER) {
-    // The parts of the CTAs of a request and key head: a group of lanes per four columns, a lane per CTA, so that all is asked for in one trip.
+    // The parts of the CTAs of a request and key head: a group of lanes per eight columns, a lane per CTA, so that all is asked for in one trip.
     cluster_sync();
     const int b = blockIdx.z, h = blockIdx.y, kv = h / a.head_tiles, ht = h - kv * a.head_tiles, heads = min(P::kHeads, a.group - ht * P::kHeads);
-    const int rank = cluster_rank(), size = cluster_size(), r = tid & (size - 1), items = heads * (P::kCols / 4);
+    const int rank = cluster_rank(), size = cluster_size(), r = tid & (size - 1), items = heads * (P::kCols / 8);
     constexpr int kRow = P::kCols + 4;
     const float *slots = reinterpret_cast<const float *>(sm + at.slots);
     const float2 *ml = reinterpret_cast<const float2 *>(sm + at.ml) + 2 * P::kHeads;
     for (int i0 = 0; i0 < items; i0 += kAttendThreads) {       // (as many groups in all CTAs together)
-      const int i = i0 + (rank * kAttendThreads + tid) / size, hd = i / (P::kCols / 4), c = (i - hd * (P::kCols / 4)) * 4;
+      const int i = i0 + (rank * kAttendThreads + tid) / size, hd = i / (P::kCols / 8), c = (i - hd * (P::kCols / 8)) * 8;
       float2 x = make_float2(-INFINITY, 0.f);
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      float4 u = make_float4(0.f, 0.f, 0.f, 0.f), v = u;
       if (i < items) {
+        const uint32_t from = in_cta(slots + hd * kRow + c, r);
         x = ld_cluster2(in_cta(ml + hd, r));
-        v = ld_cluster4(in_cta(slots + hd * kRow + c, r));
-        if (x.x == -INFINITY && x.y == 0.f) v = make_float4(0.f, 0.f, 0.f, 0.f);   // no part, or none of its rows counts
+        u = ld_cluster4(from);
+        v = ld_cluster4(from + 16);
+        if (x.x == -INFINITY && x.y == 0.f) u = v = make_float4(0.f, 0.f, 0.f, 0.f);   // no part, or none of its rows counts
       }
       float top = x.x;
       for (int o = 1; o < size; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
       const float f = weight(x.x, top);
-      float l = x.y * f;
-      v = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-      for (int o = 1; o < size; o <<= 1) {
-        l += __shfl_xor_sync(0xffffffffu, l, o);
-        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-        v.z += __shfl_xor_sync(0xffffffffu, v.z, o);
-        v.w += __shfl_xor_sync(0xffffffffu, v.w, o);
-      }
-      if (i < items && r == 0) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+      float y[9] = {u.x * f, u.y * f, u.z * f, u.w * f, v.x * f, v.y * f, v.z * f, v.w * f, x.y * f};
+      for (int o = 1; o < size; o <<= 1)
+#pragma unroll
+        for (int e = 0; e < 9; ++e) y[e] += __shfl_xor_sync(0xffffffffu, y[e], o);
+      if (i < items && r < 2) {                                // a lane for each four of them
+        const float l = y[8], inv = l == 0.f ? 0.f : 1.f / l;
         const int head = kv * a.group + ht * P::kHeads + hd;
-        if (c < a.d_h) store4(a, b, head, c, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
-        if (c == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : top + logf(l);
+        const float4 z = r ? make_float4(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv) : make_float4(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+        if (c + 4 * r < a.d_h) store4(a, b, head, c + 4 * r, z);
+        if (c + 4 * r == 0 && a.lse) a.lse[(long long)b * a.n_kvh * a.group + head] = l == 0.f ? -INFINITY : top + logf(l);
       }
     }
     cluster_sync();                                            // (the others have read)

@@ -26,10 +26,14 @@ PAGED_HD int tiles_of_request(int rows, int page, bool selected, int n_select) {
 PAGED_HD long long share_begin(long long i, long long G, long long T) { return i * T / G; }
 PAGED_HD long long share_of(long long t, long long G, long long T) { return ((t + 1) * G - 1) / T; }
 
-// u / n and the rest for 0 <= u < 256 n, 1 <= n < 2^26: the quotient in fp32 is off by one at most.
-PAGED_HD int divide_small(long long u, int n, int *rest) {
+// u / n and the rest for 0 <= u < 256 n, 1 <= n < 2^26: the quotient in fp32, a few units in its last place off, is off by one at most.
+template <typename I> PAGED_HD int divide_small(I u, int n, int *rest) {
+#ifdef __CUDA_ARCH__
+  int h = (int)__fdividef((float)u, (float)n);
+#else
   int h = (int)((float)u / (float)n);
-  long long r = u - (long long)h * n;
+#endif
+  I r = u - (I)h * n;
   if (r < 0) {
     --h;
     r += n;

@@ -97,6 +97,7 @@ int main() {
     const long long u = (long long)h * n + (trial % 5 == 0 ? 0 : trial % 5 == 1 ? n - 1 : rand() % n);
     int rest;
     if (divide_small(u, n, &rest) != h || rest != u - (long long)h * n) BAD("%lld / %d\n", u, n);
+    if (u <= 0x7fffffff && (divide_small((int)u, n, &rest) != h || rest != u - (long long)h * n)) BAD("%lld / %d, 32 bits\n", u, n);
   }
   // the ends of the range: a request of almost 2^31 rows
   {
