@@ -57,32 +57,45 @@ PAGED_HD TileRows locate_rows(int j, int len, int page, int per_box, const int32
   t.rows = 0;
   t.bad = false;
   const int pages = (int)(((unsigned)len + (unsigned)page - 1u) / (unsigned)page), listed = selected && n_select < pages ? n_select : pages;
-  int left = 0;
+  const unsigned r = (unsigned)j * kTile, first = r / (unsigned)page;   // (below 2^31 + 64 * 1024)
+  int place[4], at = (int)first, off = (int)(r - first * (unsigned)page);
+#define PAGED_EACH(g) for (int g = 0; g < 4; ++g)
 #ifdef __CUDACC__
-#pragma unroll
+#define PAGED_UNROLL _Pragma("unroll")
+#else
+#define PAGED_UNROLL
 #endif
-  for (int g = 0; g < 4; ++g) {
-    t.id[g] = -1;
-    t.off[g] = 0;
-    if (g % per_box == 0) {
-      const unsigned r = (unsigned)j * kTile + g * kRowsOfWarp, at = r / (unsigned)page;   // (below 2^31 + 64 * 1024)
-      int place = (int)at;
-      t.off[g] = (int)(r - at * (unsigned)page);
-      if (place >= listed) place = -1;
-      else if (selected) place = selected[place];
-      left = place < 0 || place >= pages ? 0 : len - (int)((unsigned)place * (unsigned)page + (unsigned)t.off[g]);
-      if (left > 0) {
-        t.id[g] = table[place];
-        if (t.id[g] < 0 || t.id[g] >= n_pages) {
-          t.bad = true;
-          left = 0;
-        }
+  PAGED_UNROLL PAGED_EACH(g) {
+    t.off[g] = off;
+    place[g] = at < listed ? at : -1;
+    off += kRowsOfWarp;
+    if (off >= page) {                     // (a page is a multiple of 16 rows)
+      off = 0;
+      ++at;
+    }
+  }
+  // first all places, then all pages: a trip to memory each
+  if (selected) PAGED_UNROLL PAGED_EACH(g) if (g % per_box == 0 && place[g] >= 0) place[g] = selected[place[g]];
+  PAGED_UNROLL PAGED_EACH(g) {
+    const bool there = g % per_box == 0 && place[g] >= 0 && place[g] < pages && len - (int)((unsigned)place[g] * (unsigned)page + (unsigned)t.off[g]) > 0;
+    t.id[g] = there ? table[place[g]] : -1;
+    if (!there) place[g] = -1;
+  }
+  int left = 0;
+  PAGED_UNROLL PAGED_EACH(g) {
+    if (g % per_box == 0) {                // a box lies in one page
+      left = place[g] < 0 ? 0 : len - (int)((unsigned)place[g] * (unsigned)page + (unsigned)t.off[g]);
+      if (left > 0 && (t.id[g] < 0 || t.id[g] >= n_pages)) {
+        t.bad = true;
+        left = 0;
       }
     } else {
       left -= kRowsOfWarp;
     }
     if (left > 0) t.rows |= (uint32_t)(left < kRowsOfWarp ? left : kRowsOfWarp) << (8 * g);
   }
+#undef PAGED_EACH
+#undef PAGED_UNROLL
   return t;
 }
 
