@@ -255,6 +255,7 @@ class PagedCache:
         self.desc = PagedCacheDesc(_ptr(K), _ptr(V), k[0], k[1], k[2], v[0], v[1], v[2], _ptr(logw), _ptr(bounds), _ptr(w_max),
                                    self.n_pages, self.page_rows)
         self.ref = C.byref(self.desc)
+        self.kind = (self.n_kvh, self.d_h, self.dtype, self.device)
 
 
 PRUNE_STATIC_MAX_N = 65536
@@ -387,43 +388,25 @@ class Context:
         return Graph(self, h, images, self.ws)
 
     # ---- the paged cache ------------------------------------------------------------------
+    # (A call of a decoding step takes the GPU a few microseconds, and looking at nine tensors one function call each takes as long: the methods test
+    # everything in one expression and ask _explain only when it fails.)
     def _make_args(self):
         self._args = C.create_string_buffer(max(_PLAN.size, _NEW_ROWS.size, _QUERY.size))
         self._args_at = C.addressof(self._args)
+        self._kind = (self.n_kvh, self.d_h, self.in_dtype, self.device)
 
-    def _flat(self, t, dtype, n, what):
-        """Address of a contiguous tensor of n elements of this type on the context's device; 0 for None."""
-        if t is None:
-            return 0
-        if t.dtype is not dtype or t.numel() != n or t.get_device() != self.device or not t.is_contiguous():
-            raise PactError(f"{what}: a contiguous {dtype} tensor of {n} elements on cuda:{self.device} is wanted")
-        return t.data_ptr()
-
-    def _table(self, t):
-        """Address, requests and width of a block table."""
-        if t.dtype is not torch.int32 or t.ndim != 2 or t.get_device() != self.device or not t.is_contiguous():
-            raise PactError(f"block_table: a contiguous {torch.int32} tensor of shape [B, max_pages] on cuda:{self.device} is wanted")
-        B, W = t.shape
-        return t.data_ptr(), B, W
-
-    def _heads(self, t, dtype, heads, n, what):
-        """Address and strides of a [n, heads, d_h] tensor on the context's device (n None: any)."""
-        shape = t.shape
-        if t.dtype is not dtype or len(shape) != 3 or shape[1] != heads or shape[2] != self.d_h or t.get_device() != self.device or (n is not None and shape[0] != n):
-            raise PactError(f"{what}: a {dtype} tensor of shape [{'..' if n is None else n}, {heads}, {self.d_h}] on cuda:{self.device} is wanted")
-        s0, s1, s2 = t.stride()
-        if s2 != 1 and self.d_h > 1:
-            raise PactError(f"{what}: the last axis has to be contiguous")
-        if heads == 1:                      # the stride of an axis of one element is anything: the one that it would have if packed
-            s1 = self.d_h
-        if shape[0] == 1:
-            s0 = s1 * heads
-        return t.data_ptr(), s0, s1
-
-    def _cache(self, cache):
-        if cache.n_kvh != self.n_kvh or cache.d_h != self.d_h or cache.dtype is not self.in_dtype or cache.device != self.device:
+    def _explain(self, cache, *wanted):
+        """Raises for the first of these that is not what is wanted: (tensor or None, dtype, shape, what), dense or, for [.., heads, d_h], strided."""
+        if cache is not None and cache.kind != self._kind:
             raise PactError(f"the cache is not one of {self.n_kvh} key heads of {self.d_h} {self.in_dtype} on cuda:{self.device}")
-        return cache.ref
+        for t, dtype, shape, strided, what in wanted:
+            if t is None:
+                continue
+            if t.dtype != dtype or t.get_device() != self.device or t.ndim != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+                raise PactError(f"{what}: a {dtype} tensor of shape [{', '.join('..' if n is None else str(n) for n in shape)}] on cuda:{self.device} is wanted")
+            if not t.is_contiguous() if not strided else t.stride()[-1] != 1 and t.shape[-1] != 1:
+                raise PactError(f"{what}: {'a contiguous tensor is wanted' if not strided else 'the last axis has to be contiguous'}")
+        raise PactError("the arguments do not fit together")
 
     def _paged_workspace(self, B, max_pages):
         """Address and size of the workspace.  One that is outgrown is kept: a captured graph may hold its address."""
@@ -447,63 +430,107 @@ class Context:
         """Pages and slots of the rows that come next (pact_cache_plan in pact.h).  block_table [B, max_pages], length, length_out [B], n_new [B] (may be a
         strided view, such as the N_OUT column of the counters of a batch; negative: the request has ended), free_pages [n_pages], n_free, n_free_out
         [1], row_start [B + 1], all int32; slot [n_rows] int64; n_rows: rows that the caller has room for, where slot is not given."""
-        i32, flat = torch.int32, self._flat
-        table, B, W = self._table(block_table)
-        if n_new.dtype is not i32 or n_new.ndim != 1 or n_new.numel() != B or n_new.get_device() != self.device:
-            raise PactError(f"n_new: an int32 tensor of shape [{B}] on cuda:{self.device} is wanted")
+        i32, dev = torch.int32, self.device
+        B, W = block_table.shape if block_table.ndim == 2 else (-1, None)
         n_pages = free_pages.numel()
         if slot is not None:
-            if n_rows is not None and n_rows != slot.numel():
+            room = slot.numel()
+            if n_rows is not None and n_rows != room:
                 raise PactError("n_rows is the length of slot")
-            n_rows = slot.numel()
+            n_rows = room
         elif n_rows is None:
             raise PactError("slot or n_rows is wanted")
-        _PLAN.pack_into(self._args, 0, page_rows, n_pages, B, W, table, flat(length, i32, B, "length"), n_new.data_ptr(), n_new.stride()[0] if B > 1 else 1,
-                        flat(free_pages, i32, n_pages, "free_pages"), flat(n_free, i32, 1, "n_free"), flat(length_out, i32, B, "length_out"),
-                        flat(n_free_out, i32, 1, "n_free_out"), flat(row_start, i32, B + 1, "row_start"), flat(slot, torch.int64, n_rows, "slot"), n_rows, row_stride, 0,
-                        flat(status, i32, 1, "status"))
-        _check(self.handle, self._L.pact_cache_plan(self.handle, self._args_at, _stream()))
+        if not (block_table.dtype is i32 and block_table.get_device() == dev and block_table.is_contiguous()
+                and length.dtype is i32 and length.get_device() == dev and length.numel() == B and length.is_contiguous()
+                and n_new.dtype is i32 and n_new.get_device() == dev and n_new.numel() == B and n_new.ndim == 1
+                and free_pages.dtype is i32 and free_pages.get_device() == dev and free_pages.is_contiguous()
+                and n_free.dtype is i32 and n_free.get_device() == dev and n_free.numel() == 1
+                and length_out.dtype is i32 and length_out.get_device() == dev and length_out.numel() == B and length_out.is_contiguous()
+                and n_free_out.dtype is i32 and n_free_out.get_device() == dev and n_free_out.numel() == 1
+                and (row_start is None or row_start.dtype is i32 and row_start.get_device() == dev and row_start.numel() == B + 1 and row_start.is_contiguous())
+                and (slot is None or slot.dtype is torch.int64 and slot.get_device() == dev and slot.is_contiguous())
+                and (status is None or status.dtype is i32 and status.get_device() == dev and status.numel() == 1)):
+            self._explain(None, (block_table, i32, (None, None), False, "block_table"), (length, i32, (B,), False, "length"), (n_new, i32, (B,), True, "n_new"),
+                          (free_pages, i32, (None,), False, "free_pages"), (n_free, i32, (1,), False, "n_free"), (length_out, i32, (B,), False, "length_out"),
+                          (n_free_out, i32, (1,), False, "n_free_out"), (row_start, i32, (B + 1,), False, "row_start"), (slot, torch.int64, (None,), False, "slot"),
+                          (status, i32, (1,), False, "status"))
+        _PLAN.pack_into(self._args, 0, page_rows, n_pages, B, W, block_table.data_ptr(), length.data_ptr(), n_new.data_ptr(), n_new.stride()[0] if B > 1 else 1,
+                        free_pages.data_ptr(), n_free.data_ptr(), length_out.data_ptr(), n_free_out.data_ptr(), 0 if row_start is None else row_start.data_ptr(),
+                        0 if slot is None else slot.data_ptr(), n_rows, row_stride, 0, 0 if status is None else status.data_ptr())
+        r = self._L.pact_cache_plan(self.handle, self._args_at, _stream())
+        if r:
+            _check(self.handle, r)
 
     def pact_cache_write(self, cache: PagedCache, K_new, V_new, logw_new, slot, status=None):
         """Rows K_new, V_new [n, n_kvh, d_h] (alike in their strides) and logw_new [n] fp32 (None: 0) into slot [n] int64."""
-        ref = self._cache(cache)
-        k, ld_row, ld_head = self._heads(K_new, self.in_dtype, self.n_kvh, None, "K_new")
-        n = K_new.shape[0]
-        v, v_row, v_head = self._heads(V_new, self.in_dtype, self.n_kvh, n, "V_new")
-        if v_row != ld_row or v_head != ld_head:
-            raise PactError("K_new and V_new have the same strides")
-        _NEW_ROWS.pack_into(self._args, 0, k, v, ld_row, ld_head, self._flat(logw_new, torch.float32, n, "logw_new"), self._flat(slot, torch.int64, n, "slot"), n,
-                            self._flat(status, torch.int32, 1, "status"))
-        _check(self.handle, self._L.pact_cache_write(self.handle, ref, self._args_at, _stream()))
+        dtype, dev, heads, d_h = self.in_dtype, self.device, self.n_kvh, self.d_h
+        n = slot.numel()
+        shape = (n, heads, d_h)
+        strides = K_new.stride()
+        if not (cache.kind == self._kind and K_new.shape == shape and K_new.dtype is dtype and K_new.get_device() == dev
+                and V_new.shape == shape and V_new.dtype is dtype and V_new.get_device() == dev and V_new.stride() == strides and (strides[2] == 1 or d_h == 1)
+                and slot.dtype is torch.int64 and slot.get_device() == dev and slot.is_contiguous()
+                and (logw_new is None or logw_new.dtype is torch.float32 and logw_new.get_device() == dev and logw_new.numel() == n and logw_new.is_contiguous())
+                and (status is None or status.dtype is torch.int32 and status.get_device() == dev and status.numel() == 1)):
+            if V_new.shape == K_new.shape and V_new.stride() != strides:
+                raise PactError("K_new and V_new have the same strides")
+            self._explain(cache, (K_new, dtype, (None, heads, d_h), True, "K_new"), (V_new, dtype, K_new.shape, True, "V_new"),
+                          (slot, torch.int64, (K_new.shape[0],), False, "slot"), (logw_new, torch.float32, (n,), False, "logw_new"), (status, torch.int32, (1,), False, "status"))
+        # the stride of an axis of one element is anything: the one that it would have if packed
+        ld_head = strides[1] if heads > 1 else d_h
+        _NEW_ROWS.pack_into(self._args, 0, K_new.data_ptr(), V_new.data_ptr(), strides[0] if n > 1 else ld_head * heads, ld_head, 0 if logw_new is None else logw_new.data_ptr(),
+                            slot.data_ptr(), n, 0 if status is None else status.data_ptr())
+        r = self._L.pact_cache_write(self.handle, cache.ref, self._args_at, _stream())
+        if r:
+            _check(self.handle, r)
 
     def pact_page_select(self, cache: PagedCache, Q, block_table, length, selected, n_first=1, n_last=1, scale=None, status=None):
         """Places of the pages that each request's token attends to, into selected [B, n_kvh, n_select] int32.  Q [B, n_qh, d_h]; scale: 1 / sqrt(d_h) if not given."""
-        i32 = torch.int32
-        ref = self._cache(cache)
-        table, B, W = self._table(block_table)
-        q, ldq, ldqh = self._heads(Q, self.in_dtype, self.n_qh, B, "Q")
+        i32, dev, heads, d_h = torch.int32, self.device, self.n_qh, self.d_h
+        B, W = block_table.shape if block_table.ndim == 2 else (-1, None)
         n_select = selected.shape[-1]
+        q = Q.stride()
+        if not (cache.kind == self._kind and Q.shape == (B, heads, d_h) and Q.dtype is self.in_dtype and Q.get_device() == dev and (q[2] == 1 or d_h == 1)
+                and block_table.dtype is i32 and block_table.get_device() == dev and block_table.is_contiguous()
+                and length.dtype is i32 and length.get_device() == dev and length.numel() == B and length.is_contiguous()
+                and selected.dtype is i32 and selected.get_device() == dev and selected.shape == (B, self.n_kvh, n_select) and selected.is_contiguous()
+                and (status is None or status.dtype is i32 and status.get_device() == dev and status.numel() == 1)):
+            self._explain(cache, (block_table, i32, (None, None), False, "block_table"), (Q, self.in_dtype, (B, heads, d_h), True, "Q"), (length, i32, (B,), False, "length"),
+                          (selected, i32, (B, self.n_kvh, None), False, "selected"), (status, i32, (1,), False, "status"))
         w, n, _ = self._paged_workspace(B, W)
-        _QUERY.pack_into(self._args, 0, q, ldq, ldqh, table, self._flat(length, i32, B, "length"), B, W, self._flat(selected, i32, B * self.n_kvh * n_select, "selected"),
-                         n_select, n_first, n_last, self.d_h ** -0.5 if scale is None else scale, 0, 0, 0, 0, self._flat(status, i32, 1, "status"), w, n)
-        _check(self.handle, self._L.pact_page_select(self.handle, ref, self._args_at, _stream()))
+        qh = q[1] if heads > 1 else d_h
+        _QUERY.pack_into(self._args, 0, Q.data_ptr(), q[0] if B > 1 else qh * heads, qh, block_table.data_ptr(), length.data_ptr(), B, W, selected.data_ptr(), n_select, n_first, n_last,
+                         d_h ** -0.5 if scale is None else scale, 0, 0, 0, 0, 0 if status is None else status.data_ptr(), w, n)
+        r = self._L.pact_page_select(self.handle, cache.ref, self._args_at, _stream())
+        if r:
+            _check(self.handle, r)
 
     def pact_paged_attention(self, cache: PagedCache, Q, block_table, length, out, lse=None, selected=None, scale=None, status=None):
         """Attention of one token per request, Q [B, n_qh, d_h] -> out [B, n_qh, d_h] (the context's output type), lse [B, n_qh] fp32, over the cached rows or
         those of the pages in selected [B, n_kvh, n_select]; scale: 1 / sqrt(d_h) if not given."""
-        i32 = torch.int32
-        ref = self._cache(cache)
-        table, B, W = self._table(block_table)
-        q, ldq, ldqh = self._heads(Q, self.in_dtype, self.n_qh, B, "Q")
-        o, ldo, ldoh = self._heads(out, self.out_dtype, self.n_qh, B, "out")
-        n_select = sel = 0
-        if selected is not None:
-            n_select = selected.shape[-1]
-            sel = self._flat(selected, i32, B * self.n_kvh * n_select, "selected")
+        i32, dev, heads, d_h = torch.int32, self.device, self.n_qh, self.d_h
+        B, W = block_table.shape if block_table.ndim == 2 else (-1, None)
+        shape = (B, heads, d_h)
+        q, o = Q.stride(), out.stride()
+        if not (cache.kind == self._kind and Q.shape == shape and Q.dtype is self.in_dtype and Q.get_device() == dev and (q[2] == 1 or d_h == 1)
+                and out.shape == shape and out.dtype is self.out_dtype and out.get_device() == dev and (o[2] == 1 or d_h == 1)
+                and block_table.dtype is i32 and block_table.get_device() == dev and block_table.is_contiguous()
+                and length.dtype is i32 and length.get_device() == dev and length.numel() == B and length.is_contiguous()
+                and (lse is None or lse.dtype is torch.float32 and lse.get_device() == dev and lse.numel() == B * heads and lse.is_contiguous())
+                and (selected is None or selected.dtype is i32 and selected.get_device() == dev and selected.ndim == 3 and selected.shape[:2] == (B, self.n_kvh) and selected.is_contiguous())
+                and (status is None or status.dtype is i32 and status.get_device() == dev and status.numel() == 1)):
+            self._explain(cache, (block_table, i32, (None, None), False, "block_table"), (Q, self.in_dtype, shape, True, "Q"), (out, self.out_dtype, shape, True, "out"),
+                          (length, i32, (B,), False, "length"), (lse, torch.float32, (B, heads), False, "lse"), (selected, i32, (B, self.n_kvh, None), False, "selected"),
+                          (status, i32, (1,), False, "status"))
         w, n, _ = self._paged_ws[-1] if self._paged_ws else self._paged_workspace(1, 1)   # (any is large enough for the parts)
-        _QUERY.pack_into(self._args, 0, q, ldq, ldqh, table, self._flat(length, i32, B, "length"), B, W, sel, n_select, 0, 0, self.d_h ** -0.5 if scale is None else scale,
-                         o, ldo, ldoh, self._flat(lse, torch.float32, B * self.n_qh, "lse"), self._flat(status, i32, 1, "status"), w, n)
-        _check(self.handle, self._L.pact_paged_attention(self.handle, ref, self._args_at, _stream()))
+        qh, oh = (q[1], o[1]) if heads > 1 else (d_h, d_h)
+        q0, o0 = (q[0], o[0]) if B > 1 else (qh * heads, oh * heads)
+        _QUERY.pack_into(self._args, 0, Q.data_ptr(), q0, qh, block_table.data_ptr(), length.data_ptr(), B, W, 0 if selected is None else selected.data_ptr(),
+                         0 if selected is None else selected.shape[2], 0, 0, d_h ** -0.5 if scale is None else scale, out.data_ptr(), o0, oh,
+                         0 if lse is None else lse.data_ptr(), 0 if status is None else status.data_ptr(), w, n)
+        r = self._L.pact_paged_attention(self.handle, cache.ref, self._args_at, _stream())
+        if r:
+            _check(self.handle, r)
 
     def set_wait_limits(self, barrier_polls: int = 0, center_sweeps: int = 0):
         """Bounds of the device-side waits (0 = default); see pact_set_wait_limits in pact.h."""
