@@ -7,7 +7,8 @@
 // the scores are formed in fp32 with a bound of their error, and in double only those that the bound leaves in doubt, a few per request.
 //
 // One kernel, a cluster of CTAs per request and key head (one CTA where there are enough of them): all CTAs score pages, the first one has the scores in
-// its shared memory and selects.  (As two kernels: 22 us instead of 13 for 32 requests of 16384 rows, 16 instead of 12 for two of 131072.)
+// its shared memory and selects.  (As two kernels: 22.2 us against 18.3 for 32 requests of 16384 rows, 16.5 against 14.6 for two of 131072; now 16.6 and
+// 9.2, of which the scores take 7 and 3.7 and the selection, a chain of dependent steps in one CTA, 5.)
 // Scores, bf16: pages (16) by query heads (8) on mma.sync; rows are loaded 16 bytes per lane straight into operands (a dot product does not
 // mind the order of its columns, so keys and queries take the same convenient one).  fp32: fused multiply-adds, folded over the lanes.
 // Selection: the bin of the n-th largest score (histograms of ten bits from the first bit in which the scores differ), what lies near it in
@@ -548,7 +549,8 @@ cudaError_t select_pages_configure(int d_h, bool bf16) {
 }
 
 cudaError_t launch_page_select(const SelectArgs &a, bool bf16, int most_ctas, int sm_count, cudaStream_t st) {
-  // As many CTAs as give every SM two, no more than there are pages for.
+  // As many CTAs as give every SM one, no more than there are pages for.  (Two per SM, 32 requests of 8 key heads in clusters of 2: 16.6 -> 21 us, with CTAs of half
+  // the threads 17.0.)
   int size = 1;
   const int pages = bf16 ? kSelectPages : kSelectPages / 2;
   while (size * 2 <= most_ctas && size * 2 <= kMaxSelectCluster && (long long)a.B * a.n_kvh * size < sm_count && size * pages < a.width) size *= 2;

@@ -948,13 +948,13 @@ template <bool CLUSTER> AttendKernel attend_kernel(const PagedCfg &cfg, bool bf1
 constexpr size_t kSmSmem = 228 * 1024, kCtaReserve = 1024;   // shared memory of an SM, and what the system takes of it for each CTA
 
 // CTAs of a cluster per request and key head, 0: no clusters.  `n` tiles of one at most, `heads` of them.
-// Clusters leave SMs idle where there are few heads and give every request the time of the longest, the line of tiles costs a second kernel.  One request of 28 heads on
-// 4: 1000 rows 9.3 us in clusters against 11.4, 5000 12.2 / 14.3, 9000 15.1 / 14.4, 16000 19.9 / 16.0; eight of them (clusters of 8, two CTAs per SM):
-// 1000 9.6 / 15.3, 5000 16.7 / 21.8, 16000 48 / 54.  fp32, 2 heads on 2: 200 rows 8.3 / 9.1, 1000 10.1 / 9.9, 4000 14.4 / 11.1.
-int cluster_for(const PagedCfg &cfg, long long n, long long heads, bool bf16, int sm_count) {
+// Clusters leave SMs idle where there are few heads and give every request the time of the longest, the line of tiles costs a second kernel.  One request
+// of 28 heads on 4: 1000 rows 7.1 us in clusters against 10.3, 5000 10.1 / 13.2, 9000 12.8 / 13.4, 16000 17.7 / 15.0; eight of them (clusters of 8, two CTAs
+// per SM): 1000 9.5 / 13.2, 5000 16.8 / 19.6, 9000 31 / 35, but the longest of unequal ones counts.  fp32, 2 heads on 2: 200 rows 6.2 / 7.6, 4000 9.2 / 10.6, 9000 13.8 / 13.5.
+int cluster_for(const PagedCfg &cfg, long long n, long long heads, int sm_count) {
   for (int size = cfg.cluster; size >= 2; size /= 2) {
     const int i = size == 2 ? 0 : size == 4 ? 1 : size == 8 ? 2 : 3;
-    const int most = (bf16 ? 8 : 2) * (heads * size * 4 >= sm_count * 3 ? 2 : 1);   // tiles of a CTA
+    const int most = heads * size > sm_count ? 16 : 8;         // tiles of a CTA
     if (heads <= cfg.clusters[i] && n <= (long long)size * most) return size;
   }
   return 0;
@@ -1030,7 +1030,7 @@ cudaError_t launch_attend(AttendArgs a, const pact_paged_cache &cache, const Pag
   const int ctas = dev.sm_count * per_sm;
   // the most tiles that a request and key head can have
   const long long n = ((long long)(a.selected && a.n_select < a.width ? a.n_select : a.width) * a.page + kTile - 1) / kTile;
-  const int size = cluster_for(cfg, n, (long long)a.B * Hn, bf16, dev.sm_count);
+  const int size = cluster_for(cfg, n, (long long)a.B * Hn, dev.sm_count);
   const int B = size ? 1 : a.B;
   const size_t most = kSmSmem / per_sm - kCtaReserve;
   a.stages = kMaxAttendStages;
