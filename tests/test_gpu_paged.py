@@ -501,6 +501,103 @@ def test_offsets_past_32_bits(pb):
     assert ((out[0].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -15).all()
 
 
+@pytest.mark.parametrize("dtype,n_qh,H,D,page", [(BF, 28, 4, 128, 64), (BF, 4, 4, 64, 16), (BF, 16, 1, 256, 32), (F32, 2, 2, 64, 16), (F32, 12, 2, 128, 64)])
+@pytest.mark.parametrize("lens", [[1], [900], [64, 0, 65], [5000], [3000, 1]])
+def test_short_and_wide_tables_agree(pb, dtype, n_qh, H, D, page, lens):
+    """The same requests in a table as long as they need, where clusters of CTAs take them, and in one of 100000 rows, where all CTAs share them out."""
+    rng, g = np.random.default_rng(7), torch.Generator(device="cuda").manual_seed(7)
+    n_pages = sum(po.pages_for(n, page) for n in lens) + 1
+    K, V, w, _, _ = cache_tensors(g, n_pages, H, page, D, dtype, bounds=False)
+    short = tables(rng, lens, max(1, max(po.pages_for(n, page) for n in lens)), page, n_pages)
+    wide = np.full((len(lens), 100000 // page), -1, np.int32)
+    wide[:, :short.shape[1]] = short
+    Q = torch.randn(len(lens), n_qh, D, generator=g, device="cuda").to(dtype)
+    ctx, got = context(pb, n_qh, H, D, dtype, F32), []
+    for table in (short, wide):
+        out, lse, status = torch.full((len(lens), n_qh, D), -5.0, device="cuda"), torch.zeros(len(lens), n_qh, device="cuda"), i32([0])
+        ctx.pact_paged_attention(pb.PagedCache(K, V, w), Q, i32(table), i32(lens), out, lse, status=status)
+        assert status.item() == 0
+        got.append((f64(out), f64(lse)))
+    scale = float(np.float32(D ** -0.5))
+    ref, lse_ref, mag, big = po.attend(f64(Q), f64(K), f64(V), f64(w), short, lens, page, scale)
+    # the tolerance of attend_and_check
+    delta, steps = (D + 8) * 2.0 ** -23 * big, max(lens) / 64 + 20
+    for out, lse in got:
+        assert (np.abs(out - ref) <= mag * (2 * delta + 2.0 ** -16 + 2.0 ** -20 + steps * 2.0 ** -21)[..., None] + np.abs(ref) * 2.0 ** -24 + 1e-30).all()
+        none = lse_ref == -np.inf
+        assert np.array_equal(lse == -np.inf, none)
+        assert (np.abs(lse[~none] - lse_ref[~none]) <= (delta + 2.0 ** -20 + steps * 2.0 ** -21)[~none] + 2.0 ** -22 * np.abs(lse_ref[~none])).all()
+
+
+def test_most_requests(pb):
+    """As many requests as a call may have, most of them short, some empty."""
+    lens = [(i * 7) % 40 for i in range(4096)]
+    attend_and_check(pb, BF, F32, 2, 1, 64, 16, lens, seed=1)
+
+
+def test_a_row_for_one_request_and_none_for_the_others(pb):
+    attend_and_check(pb, BF, F32, 4, 2, 64, 16, [0, 0, 0, 1, 0, 0, 0, 0, 0, 0, 0, 0])
+    attend_and_check(pb, F32, F32, 4, 2, 64, 16, [0] * 300 + [1])
+
+
+def test_the_same_page_named_for_a_write_by_two_requests_is_not_needed(pb):
+    """A page that two requests share (a common beginning) is written once; what both read is the same."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    K, V, w, b, wm = cache_tensors(g, 8, 2, 16, 64, BF)
+    ctx, cache = context(pb, 4, 2, 64, BF, F32), pb.PagedCache(K, V, w, b, wm)
+    rows = torch.randn(16, 2, 64, generator=g, device="cuda").to(BF)
+    ctx.pact_cache_write(cache, rows, rows, None, torch.arange(32, 48, device="cuda"))
+    Q, out = torch.randn(1, 4, 64, device="cuda").to(BF).expand(2, 4, 64).contiguous(), torch.zeros(2, 4, 64, device="cuda")
+    ctx.pact_paged_attention(cache, Q, i32([[2, 5], [2, 5]]), i32([30, 30]), out)
+    assert torch.equal(out[0], out[1])
+
+
+def test_the_first_call_of_a_context_inside_a_capture(pb):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    K, V, w, b, wm = cache_tensors(g, 200, 2, 16, 64, BF)
+    cache = pb.PagedCache(K, V, w, b, wm)
+    T, L, Q = torch.randperm(200, device="cuda").int()[None], i32([3000]), torch.randn(1, 8, 64, device="cuda").to(BF)
+    want, out = torch.zeros(1, 8, 64, device="cuda"), torch.zeros(1, 8, 64, device="cuda")
+    sel_want, sel = torch.zeros(1, 2, 7, dtype=I32, device="cuda"), torch.zeros(1, 2, 7, dtype=I32, device="cuda")
+    old = context(pb, 8, 2, 64, BF, F32)
+    old.pact_page_select(cache, Q, T, L, sel_want)
+    old.pact_paged_attention(cache, Q, T, L, want)
+    fresh = pb.Context(512, 8, 2, 64, BF, F32)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fresh.pact_paged_attention(cache, Q, T, L, out)          # makes the workspace ...
+        fresh.pact_page_select(cache, Q, T, L, sel)
+    # ... which stays, although a later call with many pages outgrows it
+    wide = torch.full((64, 60000), -1, dtype=I32, device="cuda")
+    fresh.pact_page_select(cache, Q.expand(64, 8, 64).contiguous(), wide, torch.zeros(64, dtype=I32, device="cuda"), torch.zeros(64, 2, 7, dtype=I32, device="cuda"))
+    junk = [torch.full((1 << 20,), 7, dtype=torch.uint8, device="cuda") for _ in range(40)]
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(sel, sel_want) and all((x == 7).all() for x in junk)
+
+
+def test_selection_of_infinite_and_huge_bounds(pb):
+    """What fp32 cannot hold is decided in double: infinities, products beyond 1e38, many scores alike."""
+    D, page, n = 64, 16, 1200
+    for dtype in (F32, BF):
+        g = torch.Generator(device="cuda").manual_seed(11)
+        K, V, w, b, wm = cache_tensors(g, n, 2, page, D, dtype)
+        b[7, 0, 1, 3] = float("inf")
+        b[9, 1, 0] = float("-inf")
+        b[30:40] *= 1e30
+        b[600, :, 1, 5] = float("nan")
+        wm[5], wm[6], wm[8] = float("inf"), float("-inf"), float("nan")
+        Q = torch.randn(2, 6, D, generator=g, device="cuda").to(dtype) * 1e9
+        Q[1, 2, 4] = float("nan")
+        table = np.stack([np.random.default_rng(i).permutation(n).astype(np.int32) for i in range(2)])
+        lens = [n * page, 700 * page - 3]
+        sel = torch.zeros(2, 2, 50, dtype=I32, device="cuda")
+        context(pb, 6, 2, D, dtype).pact_page_select(pb.PagedCache(K, V, w, b, wm), Q, i32(table), i32(lens), sel, 1, 1, scale=0.5)
+        with np.errstate(invalid="ignore"):
+            want = po.select(f64(Q), f64(b), np.nan_to_num(f64(wm), nan=-np.inf, posinf=np.inf, neginf=-np.inf), table, lens, page, 0.5, 1, 1, 50)
+        assert np.array_equal(sel.cpu().numpy(), want)
+
+
 # ---- as a serving program uses them --------------------------------------------------------------------------------
 
 def test_captured_and_replayed_with_other_lengths_beside_eager_calls(pb):
