@@ -389,7 +389,8 @@ size_t pact_paged_workspace_bytes(const pact_ctx *ctx, int max_requests, int max
  * score is the largest of these over the heads (a sum that is not a number is left out), in the order of double precision.  Selected are the first
  * n_first and the last n_last pages of the request, then those with the largest scores, ties to the lower page, n_select in all.
  * selected: their places in ascending order, -1 behind the last.  n_first, n_last >= 0, n_first + n_last <= n_select; max_pages <= 65536.  Lengths
- * outside 0 .. max_pages * page_rows are clamped and page ids outside the cache score minus infinity; both set status to INVALID_ARG. */
+ * outside 0 .. max_pages * page_rows are clamped and page ids outside the cache score minus infinity; both set status to INVALID_ARG (ids only where
+ * scores decide: a request with no more pages than n_select has all of them selected and none looked at). */
 pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_query *q /*host*/, void *stream);
 
 /* Attention of the new token over its request's cached rows (Eq. 11): with s_p = scale * q.k_p + logw_p over the rows p in

@@ -5,6 +5,8 @@
 // neighbours in the call.  A CTA takes the runs of one key head that begin in its block of rows, all of their rows and no others, so that a page's bounds are one
 // CTA's, without atomics or a second kernel, from rows that it has just copied and finds in its L1.  Its warps share out the runs, or a run.
 // Minimum and maximum are exact in any order.
+// 16 prompts of 2948 rows at most, 4 key heads of 128, pages of 64, bf16 (119 MB): 27.5 us, without bounds 23 to 24.  Others: bounds from pieces of runs kept in
+// registers 44 to 51 us, a warp per run 32, bounds in registers on the way through the copy 29.
 #include "paged.cuh"
 
 namespace pact {

@@ -243,7 +243,7 @@ def tables(rng, lens, width, page, n_pages):
 
 @pytest.mark.parametrize("dtype,n_qh,H,D,page,lens,n_first,n_last,n_select", [
     (BF, 4, 2, 64, 16, [200, 0, 1, 16, 500], 1, 1, 5), (BF, 7, 1, 128, 16, [3000, 2999], 0, 0, 17), (BF, 16, 2, 128, 32, [4000, 33], 2, 3, 64), (BF, 2, 2, 80, 64, [5000], 0, 4, 4),
-    (BF, 12, 2, 256, 16, [700], 1, 1, 9), (BF, 3, 3, 8, 48, [9000], 1, 0, 2), (F32, 4, 2, 64, 16, [1500, 40], 1, 1, 20), (F32, 5, 1, 128, 16, [20000], 1, 1, 1000), (F32, 2, 1, 100, 16, [160, 176], 0, 0, 10),
+    (BF, 10, 2, 256, 16, [700], 1, 1, 9), (BF, 3, 3, 8, 48, [9000], 1, 0, 2), (F32, 4, 2, 64, 16, [1500, 40], 1, 1, 20), (F32, 5, 1, 128, 16, [20000], 1, 1, 1000), (F32, 2, 1, 100, 16, [160, 176], 0, 0, 10),
     (BF, 8, 1, 64, 16, [16 * 9000, 100], 1, 1, 700)])
 def test_select(pb, dtype, n_qh, H, D, page, lens, n_first, n_last, n_select):
     rng, g = np.random.default_rng(D), torch.Generator(device="cuda").manual_seed(D)
