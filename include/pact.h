@@ -310,7 +310,7 @@ typedef struct {
                            row that must not be seen; NULL: nothing is added                       */
   void *bounds;         /* [n_pages][n_kvh][2][d_h], element type `in`: smallest and largest value of each coordinate of the page's
                            keys (an element that is not a number gives way to one that is); NULL: not kept */
-  float *w_max;         /* [n_pages] largest logw of the page (0 where logw_new was NULL); given if and only if bounds is */
+  float *w_max;         /* [n_pages] largest logw of the page, 0 in a cache without logw; given if and only if bounds is */
   int32_t n_pages, page_rows;
 } pact_paged_cache;
 
@@ -352,7 +352,7 @@ pact_status pact_cache_plan(pact_ctx *ctx, const pact_plan *p /*host*/, void *st
 typedef struct {
   const void *K, *V;
   int64_t ld_row, ld_head;
-  const float *logw;          /* [n_rows]; NULL: 0                                                  */
+  const float *logw;          /* [n_rows]; NULL: 0; not read where the cache has no logw           */
   const int64_t *slot;        /* [n_rows]                                                           */
   int64_t n_rows;
   int32_t *status;

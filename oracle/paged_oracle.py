@@ -54,7 +54,7 @@ def write(K, V, logw, bounds, w_max, K_new, V_new, logw_new, slot, page):
             continue
         at, place = divmod(int(s), page)
         K[at, :, place], V[at, :, place] = K_new[r], V_new[r]
-        w = 0.0 if logw_new is None else logw_new[r]
+        w = 0.0 if logw_new is None or logw is None else logw_new[r]
         if logw is not None:
             logw[at, place] = w
         if bounds is not None:

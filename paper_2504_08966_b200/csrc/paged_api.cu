@@ -78,7 +78,7 @@ pact_status pact_cache_write(pact_ctx *ctx, const pact_paged_cache *cache, const
   if (r->n_rows > INT32_MAX) return PACT_ERR_UNSUPPORTED;
   if (!ctx->paged.blocks) return PACT_ERR_UNSUPPORTED;
   WriteArgs a;
-  a.Kn = r->K; a.Vn = r->V; a.ld_row = r->ld_row; a.ld_head = r->ld_head; a.logw_new = r->logw; a.slot = r->slot; a.n_rows = r->n_rows;
+  a.Kn = r->K; a.Vn = r->V; a.ld_row = r->ld_row; a.ld_head = r->ld_head; a.logw_new = cache->logw ? r->logw : nullptr; a.slot = r->slot; a.n_rows = r->n_rows;
   a.K = cache->K; a.V = cache->V; a.k_page = cache->k_page; a.k_head = cache->k_head; a.k_row = cache->k_row;
   a.v_page = cache->v_page; a.v_head = cache->v_head; a.v_row = cache->v_row;
   a.logw = cache->logw; a.bounds = cache->bounds; a.w_max = cache->w_max; a.status = r->status;

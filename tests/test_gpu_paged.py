@@ -218,6 +218,15 @@ def test_write_without_biases_and_with_bad_slots(pb):
     assert np.array_equal(f64(K), want[0])
 
 
+def test_a_cache_without_biases_takes_none(pb):
+    # the attention adds nothing then, so neither may the bound of a page: with biases below 0 it would fall below the logits
+    g = torch.Generator(device="cuda").manual_seed(8)
+    K, V, _, b, wm = cache_tensors(g, 4, 1, 16, 64, F32, logw=False)
+    rows, lw = torch.randn(40, 1, 64, generator=g, device="cuda"), -5 - torch.rand(40, generator=g, device="cuda")
+    context(pb, 1, 1, 64, F32).pact_cache_write(pb.PagedCache(K, V, None, b, wm), rows, rows, lw, torch.arange(40, device="cuda"))
+    assert wm.tolist() == [0, 0, 0, 0]
+
+
 def test_bounds_leave_out_what_is_not_a_number(pb):
     K, V, w, b, wm = cache_tensors(torch.Generator(device="cuda").manual_seed(4), 3, 1, 16, 64, F32)
     rows = torch.randn(6, 1, 64, device="cuda")
