@@ -399,6 +399,23 @@ def test_attention_of_few_and_many_requests(pb, dtype, n_qh, H, D, page, lens):
     attend_and_check(pb, dtype, F32, n_qh, H, D, page, lens, seed=len(lens))
 
 
+@pytest.mark.parametrize("n_qh,D", [(1, 64), (8, 128), (16, 256)])
+def test_fp32_results_of_bf16_rows_have_fp32_probabilities(pb, n_qh, D):
+    # Two rows with logits 0 and b (queries 0), values 0 and 1: out = x / (1 + x), x = exp(b), -1 <= b < 0.  In units of 2^-22 of it: the argument b log2 e is off by
+    # 2^-24 and 1.44 * 2^-25 at most, so x by 0.3; ex2 by 1; the terms of x, of which an instruction cuts each to 2^-23, by 1.5; 1 + x, its reciprocal and the product by
+    # 2^-24 each, 0.75.  In all less than 4: 2^-20.  Probabilities of two bf16 terms would be off by up to 2^-16.
+    B, page = 64, 16
+    K = torch.zeros(B, 1, page, D, dtype=BF, device="cuda")
+    V, w = K.clone(), torch.zeros(B, page, device="cuda")
+    V[:, :, 1] = 1
+    w[:, 1] = -torch.rand(B, generator=torch.Generator(device="cuda").manual_seed(D), device="cuda")
+    out = torch.empty(B, n_qh, D, device="cuda")
+    ctx = context(pb, n_qh, 1, D, BF, F32)
+    ctx.pact_paged_attention(pb.PagedCache(K, V, w), torch.zeros(B, n_qh, D, dtype=BF, device="cuda"), torch.arange(B, dtype=I32, device="cuda")[:, None], i32([2] * B), out)
+    x = np.exp(f64(w)[:, 1])[:, None, None]
+    assert np.abs(f64(out) / (x / (1 + x)) - 1).max() <= 2.0 ** -20
+
+
 def _mask_some(w, table):
     g = torch.Generator(device="cuda").manual_seed(1)
     w.masked_fill_(torch.rand(w.shape, generator=g, device="cuda") < 0.5, float("-inf"))
