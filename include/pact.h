@@ -398,8 +398,7 @@ pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache /*host
  * floor(j * n_kvh / n_qh).  With `selected` only the rows of those pages count: of the first min(n_select, pages of the request) entries,
  * those below 0 or beyond the request's pages are skipped, and a page named twice counts twice.  Rows with logw = minus infinity and
  * rows past the length have no effect, whatever their keys and values hold.  Without any row out is 0 and lse minus infinity.
- * Logits, softmax statistics and sums are fp32; bf16 probabilities are carried as two bf16 terms (error 2^-16), or
- * three (fp32 accuracy) where `out` is fp32.
+ * Logits, probabilities, softmax statistics and sums are fp32 (beside bf16 values probabilities are carried as three bf16 terms).
  * Lengths are clamped to 0 .. max_pages * page_rows and rows of pages outside
  * the cache are left out; both set status to INVALID_ARG. */
 pact_status pact_paged_attention(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_query *q /*host*/, void *stream);

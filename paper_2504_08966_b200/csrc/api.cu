@@ -223,7 +223,7 @@ pact_status pact_create(pact_ctx **out, int d, int n_qh, int n_kvh, int d_h, pac
     return PACT_ERR_CUDA;
   }
   c->umma = in == PACT_BF16 && umma_supported(c->d_k);
-  e = paged_configure(&c->paged, c->dev, n_qh, n_kvh, d_h, in == PACT_BF16, o == PACT_BF16);
+  e = paged_configure(&c->paged, c->dev, n_qh, n_kvh, d_h, in == PACT_BF16);
   if (e != cudaSuccess) {
     fail_cuda(ctx, e, "pact_create");
     delete c;

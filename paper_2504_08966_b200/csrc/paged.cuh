@@ -91,11 +91,10 @@ struct PagedCfg {
   int blocks = 0;                 // 128-byte blocks of a row; 0: no kernel for this head width
   int tile_heads = 0;             // query heads of a key head that a CTA takes at once
   int head_tiles = 0;
-  bool exact = false;             // probabilities to fp32: the results are fp32
   int cluster = 1;                // largest cluster of CTAs that can be launched
   int clusters[4] = {};           // clusters of 2, 4, 8 and 16 that fit the device at once
 };
-cudaError_t paged_configure(PagedCfg *cfg, const DeviceCfg &dev, int n_qh, int n_kvh, int d_h, bool bf16, bool out_bf16);
+cudaError_t paged_configure(PagedCfg *cfg, const DeviceCfg &dev, int n_qh, int n_kvh, int d_h, bool bf16);
 // bytes of workspace of a call; with `a` its slices are set too
 size_t attend_scratch(const PagedCfg &cfg, const DeviceCfg &dev, bool bf16, AttendArgs *a, char *base);
 cudaError_t launch_attend(AttendArgs a, const pact_paged_cache &cache, const PagedCfg &cfg, const DeviceCfg &dev, bool bf16, cudaStream_t st,

@@ -18,9 +18,8 @@
 //
 // bf16: logits as K (16 rows x 16) by q^T (16 x 8 heads) on mma.sync, so that eight heads are one operand; the output as V^T (16 columns x 16 rows)
 // by P^T (16 rows x 8 heads), also without padding.  tcgen05 would want 64 or 128 rows per instruction and its results through tensor memory,
-// where HBM delivers a tile every 1400 clocks of an SM and the warps need less.  Probabilities go in as two bf16 terms (p = hi + lo to
-// 2^-16) for bf16 results: one term would put an error of 2^-8 on every product, as large as the rounding of the result.  For fp32 results a third term makes up
-// fp32's 24 bits (EXACT; 48 requests of 4097 rows at most, 28 heads on 4: 52.1 -> 52.5 us; two rows, worst relative error of a result 5.8e-6 -> below 2^-20).
+// where HBM delivers a tile every 1400 clocks of an SM and the warps need less.  Probabilities go in as three bf16 terms, which hold all of fp32's 24 bits.  (Two are
+// off by 2^-17: two rows, worst relative error of a result 5.8e-6 against less than 2^-20, and one bf16 result in 3000 rounded the other way; the third costs 0.5 % of a call that HBM bounds.)
 // fp32: fused multiply-adds; for the logits a lane has one row and half of the columns, for the output four columns of all rows.
 #include "paged.cuh"
 #include "paged_tiles.h"
@@ -169,8 +168,6 @@ template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
   }
 
   // 16 rows, of which the first `rows` count: K from sk on, V from sv on, 128 bytes of each and `block` bytes to the next 128 of their columns
-  // EXACT: probabilities to fp32
-  template <bool EXACT>
   __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, uint32_t block, const float *bias, bool has_bias, int rows, float scale, int lane, float *) {
     float s[NT][4];
 #pragma unroll
@@ -245,7 +242,7 @@ template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
         const float x = p[2 * i] - __uint_as_float(h << 16), y = p[2 * i + 1] - __uint_as_float(h & 0xFFFF0000u);   // (exact)
         const uint32_t g = pack_bf16(x, y);
         lo[n][i] = transpose8(g);
-        if constexpr (EXACT) rest[n][i] = transpose8(pack_bf16(x - __uint_as_float(g << 16), y - __uint_as_float(g & 0xFFFF0000u)));
+        rest[n][i] = transpose8(pack_bf16(x - __uint_as_float(g << 16), y - __uint_as_float(g & 0xFFFF0000u)));
       }
     }
     // values of rows that do not count are cleared: zero times an infinity or a NaN would not be zero
@@ -274,7 +271,7 @@ template <int NB, int NT> struct Part<__nv_bfloat16, NB, NT> {
         for (int n = 0; n < NT; ++n) {
           mma_bf16(o[c][n], a, hi[n][0], hi[n][1]);
           mma_bf16(o[c][n], a, lo[n][0], lo[n][1]);
-          if constexpr (EXACT) mma_bf16(o[c][n], a, rest[n][0], rest[n][1]);
+          mma_bf16(o[c][n], a, rest[n][0], rest[n][1]);
         }
       }
     }
@@ -343,7 +340,6 @@ template <int NB, int NT> struct Part<float, NB, NT> {
   }
 
   // scratch: 16 rows of probabilities and a row of factors, this warp's
-  template <bool>
   __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, uint32_t block, const float *bias, bool has_bias, int rows, float scale, int lane, float *scratch) {
     const int r = lane & 15, half = lane >> 4, x = r & 7;
     float s[kHeads];
@@ -465,7 +461,7 @@ __device__ __forceinline__ void store4(const AttendArgs &a, int b, int head, int
 constexpr int attend_ctas(int blocks, int tiles_of_heads) { return blocks <= 2 && tiles_of_heads <= 1 ? 2 : 1; }   // of an SM
 
 // CLUSTER: CTA (rank, key head and head tile, request) has a share of that request's tiles alone.
-template <typename T, int NB, int NT, bool CLUSTER, bool EXACT>
+template <typename T, int NB, int NT, bool CLUSTER>
 __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
     k_attend(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttendArgs a) {
   using P = Part<T, NB, NT>;
@@ -695,7 +691,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
         const int rows = (int)(meta[st] >> (8 * warp) & 0xffu);
         if (rows > 0 && ok) {
           const uint32_t sk = smem_u32(sm + st * at.stage) + of_warp;
-          part.template step<EXACT>(sk, sk + NB * kBlockBytes, block, reinterpret_cast<const float *>(sm + at.bias) + st * kTile + warp * kRowsOfWarp, a.logw != nullptr, rows, a.scale, lane,
+          part.step(sk, sk + NB * kBlockBytes, block, reinterpret_cast<const float *>(sm + at.bias) + st * kTile + warp * kRowsOfWarp, a.logw != nullptr, rows, a.scale, lane,
                     slots + warp * kScratch<P::kHeads>);
         }
         __syncwarp();
@@ -938,24 +934,19 @@ bool encode_pages(const PagedCfg &cfg, CUtensorMap *map, void *base, bool bf16, 
 }
 
 using AttendKernel = void (*)(CUtensorMap, CUtensorMap, AttendArgs);
-template <bool CLUSTER, bool EXACT> AttendKernel attend_kernel_bf16(const PagedCfg &cfg) {
-  const bool wide = cfg.tile_heads == 16;
-  switch (cfg.blocks) {
-    case 1: return wide ? k_attend<__nv_bfloat16, 1, 2, CLUSTER, EXACT> : k_attend<__nv_bfloat16, 1, 1, CLUSTER, EXACT>;
-    case 2: return wide ? k_attend<__nv_bfloat16, 2, 2, CLUSTER, EXACT> : k_attend<__nv_bfloat16, 2, 1, CLUSTER, EXACT>;
-    case 3: return wide ? k_attend<__nv_bfloat16, 3, 2, CLUSTER, EXACT> : k_attend<__nv_bfloat16, 3, 1, CLUSTER, EXACT>;
-    case 4: return wide ? k_attend<__nv_bfloat16, 4, 2, CLUSTER, EXACT> : k_attend<__nv_bfloat16, 4, 1, CLUSTER, EXACT>;
-  }
-  return nullptr;
-}
 template <bool CLUSTER> AttendKernel attend_kernel(const PagedCfg &cfg, bool bf16) {
-  const bool few = cfg.tile_heads == 2;
-  if (bf16) return cfg.exact ? attend_kernel_bf16<CLUSTER, true>(cfg) : attend_kernel_bf16<CLUSTER, false>(cfg);
-  switch (cfg.blocks) {
-    case 1: return few ? k_attend<float, 1, 0, CLUSTER, false> : k_attend<float, 1, 1, CLUSTER, false>;
-    case 2: return few ? k_attend<float, 2, 0, CLUSTER, false> : k_attend<float, 2, 1, CLUSTER, false>;
-    case 3: return few ? k_attend<float, 3, 0, CLUSTER, false> : k_attend<float, 3, 1, CLUSTER, false>;
-    case 4: return few ? k_attend<float, 4, 0, CLUSTER, false> : k_attend<float, 4, 1, CLUSTER, false>;
+  const bool few = cfg.tile_heads == 2, wide = cfg.tile_heads == 16;
+  if (bf16) switch (cfg.blocks) {
+    case 1: return wide ? k_attend<__nv_bfloat16, 1, 2, CLUSTER> : k_attend<__nv_bfloat16, 1, 1, CLUSTER>;
+    case 2: return wide ? k_attend<__nv_bfloat16, 2, 2, CLUSTER> : k_attend<__nv_bfloat16, 2, 1, CLUSTER>;
+    case 3: return wide ? k_attend<__nv_bfloat16, 3, 2, CLUSTER> : k_attend<__nv_bfloat16, 3, 1, CLUSTER>;
+    case 4: return wide ? k_attend<__nv_bfloat16, 4, 2, CLUSTER> : k_attend<__nv_bfloat16, 4, 1, CLUSTER>;
+  }
+  else switch (cfg.blocks) {
+    case 1: return few ? k_attend<float, 1, 0, CLUSTER> : k_attend<float, 1, 1, CLUSTER>;
+    case 2: return few ? k_attend<float, 2, 0, CLUSTER> : k_attend<float, 2, 1, CLUSTER>;
+    case 3: return few ? k_attend<float, 3, 0, CLUSTER> : k_attend<float, 3, 1, CLUSTER>;
+    case 4: return few ? k_attend<float, 4, 0, CLUSTER> : k_attend<float, 4, 1, CLUSTER>;
   }
   return nullptr;
 }
@@ -977,7 +968,7 @@ int cluster_for(const PagedCfg &cfg, long long n, long long heads, int sm_count)
 
 }  // namespace
 
-cudaError_t paged_configure(PagedCfg *cfg, const DeviceCfg &dev, int n_qh, int n_kvh, int d_h, bool bf16, bool out_bf16) {
+cudaError_t paged_configure(PagedCfg *cfg, const DeviceCfg &dev, int n_qh, int n_kvh, int d_h, bool bf16) {
   void *fn = nullptr;
   cudaDriverEntryPointQueryResult qres;
   cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
@@ -990,7 +981,6 @@ cudaError_t paged_configure(PagedCfg *cfg, const DeviceCfg &dev, int n_qh, int n
   e = select_pages_configure(d_h, bf16);
   if (e != cudaSuccess) return e;
   cfg->blocks = blocks;
-  cfg->exact = !out_bf16;
   cfg->tile_heads = bf16 ? (group > 8 ? 16 : 8) : group > 2 ? 8 : 2;
   cfg->head_tiles = (group + cfg->tile_heads - 1) / cfg->tile_heads;
   e = cudaFuncSetAttribute(attend_kernel<false>(*cfg, bf16), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dev.smem_optin);

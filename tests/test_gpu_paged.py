@@ -416,6 +416,23 @@ def test_fp32_results_of_bf16_rows_have_fp32_probabilities(pb, n_qh, D):
     assert np.abs(f64(out) / (x / (1 + x)) - 1).max() <= 2.0 ** -20
 
 
+@pytest.mark.parametrize("B,n_qh,D,page", [(4096, 1, 64, 16), (64, 8, 256, 16), (1000, 16, 128, 32)])
+def test_bf16_results_are_rounded_once(pb, B, n_qh, D, page):
+    # Two rows with logits 0 and b (queries 0), values 0 and v: out = v x / (1 + x), x = exp(b), -1 <= b < 0.  In fp32 it is good to 2^-20, as above (v x is three products of eight
+    # bits by eight, exact each), so the result is off by half a bf16 step and 2^-20 at most.
+    g = torch.Generator(device="cuda").manual_seed(D)
+    K = torch.zeros(B, 1, page, D, dtype=BF, device="cuda")
+    V, w = K.clone(), torch.zeros(B, page, device="cuda")
+    V[:, 0, 1] = 1 + torch.rand(B, D, generator=g, device="cuda").to(BF)
+    w[:, 1] = -torch.rand(B, generator=g, device="cuda")
+    out = torch.empty(B, n_qh, D, dtype=BF, device="cuda")
+    context(pb, n_qh, 1, D, BF).pact_paged_attention(pb.PagedCache(K, V, w), torch.zeros(B, n_qh, D, dtype=BF, device="cuda"), torch.arange(B, dtype=I32, device="cuda")[:, None], i32([2] * B), out)
+    x = np.exp(f64(w)[:, 1])[:, None, None]
+    want = f64(V)[:, :, 1] * x / (1 + x)
+    half_step = 2.0 ** (np.floor(np.log2(want)) - 8)
+    assert (np.abs(f64(out) - want) <= half_step + 2.0 ** -20 * want).all()
+
+
 def _mask_some(w, table):
     g = torch.Generator(device="cuda").manual_seed(1)
     w.masked_fill_(torch.rand(w.shape, generator=g, device="cuda") < 0.5, float("-inf"))
