@@ -433,6 +433,25 @@ def test_bf16_results_are_rounded_once(pb, B, n_qh, D, page):
     assert (np.abs(f64(out) - want) <= half_step + 2.0 ** -20 * want).all()
 
 
+@pytest.mark.parametrize("n_qh,H,D,rows", [(32, 32, 64, 1 << 17), (64, 4, 64, 1 << 20), (8, 8, 256, 1 << 18)])
+def test_sums_over_many_rows_are_not_biased(pb, n_qh, H, D, rows):
+    # Values of one sign, thousands of rows of one running sum.  What a sum in fp32 may be off by grows as its roundings happen to fall, and their mean over heads and columns
+    # stays near 0; what is cut off towards 0 adds up.  Within 16 rows there are three instructions; each cuts its terms and its result to 2^-23 of them at most, which is 2^-21 in all.  The
+    # same p are in numerator and denominator, so their errors (2^-21 each) cancel but for those of independent rows.  2^-20 leaves as much again for the mean of the roundings: a
+    # sum of 500 steps is off by 2^-24 * sqrt(500) = 2^-19.5 (one standard deviation, at most), the mean over 2048 results and more by 2^-25; that of the denominators, one per head
+    # but of 32 lanes and thousands of parts each, by less than 2^-22.
+    P, page = 64, 64
+    g = torch.Generator(device="cuda").manual_seed(D)
+    K = torch.zeros(P, H, page, D, dtype=BF, device="cuda")
+    V, w = 1 + torch.rand(P, H, page, D, generator=g, device="cuda").to(BF), -torch.rand(P, page, generator=g, device="cuda")
+    out = torch.empty(1, n_qh, D, device="cuda")
+    table = torch.arange(rows // page, dtype=I32, device="cuda")[None] % P
+    context(pb, n_qh, H, D, BF, F32).pact_paged_attention(pb.PagedCache(K, V, w), torch.zeros(1, n_qh, D, dtype=BF, device="cuda"), table, i32([rows]), out)
+    p = torch.exp(w.double())
+    want = (torch.einsum("pr,phrc->hc", p, V.double()) / p.sum()).repeat_interleave(n_qh // H, 0)
+    assert abs(((out[0].double() - want) / want).mean().item()) <= 2.0 ** -20
+
+
 def _mask_some(w, table):
     g = torch.Generator(device="cuda").manual_seed(1)
     w.masked_fill_(torch.rand(w.shape, generator=g, device="cuda") < 0.5, float("-inf"))
