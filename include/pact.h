@@ -149,7 +149,9 @@ const char *pact_last_cuda_error(const pact_ctx *ctx);
  * tensor cores do not take, i.e. fp32, or bf16 whose width is no multiple of 64, unless it is small enough for one cluster).  When a bound is reached the
  * kernel stops waiting, writes PACT_ERR_TIMEOUT to counters[PACT_CNT_STATUS] of the image and carries on
  * within bounds; the call itself still returns PACT_OK and the outputs of that image are not valid.
- * barrier_polls: polls of the member-list barrier; center_sweeps: sweeps of the centre selection (rows that are
+ * The waits of pact_paged_attention for its copies are bounded too; there the status of the call becomes PACT_ERR_TIMEOUT.
+ * barrier_polls: polls of the member-list barrier, and of each wait of pact_paged_attention (default: as many as fit into a second);
+ * center_sweeps: sweeps of the centre selection (rows that are
  * still open are then decided without waiting, in at most one pass per surviving token; the same happens, with no
  * status, when no row has been removed for 512 sweeps); 0 restores the default (about a million).  Graphs recorded
  * earlier keep the limits they were recorded with. */

@@ -231,6 +231,7 @@ pact_status pact_create(pact_ctx **out, int d, int n_qh, int n_kvh, int d_h, pac
   }
   c->spin_limit = kSpinLimit;
   c->sweep_limit = kSpinLimit;
+  c->copy_polls = INT32_MAX;
   *out = c;
   return PACT_OK;
 }
@@ -269,6 +270,7 @@ pact_status pact_set_wait_limits(pact_ctx *ctx, int barrier_polls, int center_sw
   if (!ctx || barrier_polls < 0 || center_sweeps < 0) return PACT_ERR_INVALID_ARG;
   ctx->spin_limit = barrier_polls ? barrier_polls : kSpinLimit;
   ctx->sweep_limit = center_sweeps ? center_sweeps : kSpinLimit;
+  ctx->copy_polls = barrier_polls ? barrier_polls : INT32_MAX;
   return PACT_OK;
 }
 

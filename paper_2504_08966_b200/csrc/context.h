@@ -21,6 +21,7 @@ struct pact_ctx {
   long long launches;      // kernels launched by this context so far
   int spin_limit;          // polls the barrier of the member-list kernel makes before it raises PACT_ERR_TIMEOUT
   int sweep_limit;         // sweeps the centre selection makes before it raises PACT_ERR_TIMEOUT
+  int copy_polls;          // polls that a wait of the paged attention makes before it raises PACT_ERR_TIMEOUT, if a second has not passed before
   int prof_on;             // record an event after every stage of pact_reduce
   int prof_n;              // stages recorded by the last profiled call
   cudaEvent_t ev[kProfStages + 1];

@@ -81,6 +81,7 @@ struct AttendArgs {
   int n_kvh, group, d_h, head_tiles;
   int box_rows;          // rows of one copy: the largest of 64, 32, 16 that divides the page
   int stages;
+  int polls;             // of a wait for copies, or for a free stage
   bool whole_blocks;     // a row is a whole number of 128-byte blocks
   bool out_bf16;
 };

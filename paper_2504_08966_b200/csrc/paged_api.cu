@@ -142,6 +142,7 @@ pact_status pact_paged_attention(pact_ctx *ctx, const pact_paged_cache *cache, c
   a.out = q->out; a.ldO = q->ldO; a.ldOh = q->ldOh; a.lse = q->lse; a.status = q->status; a.scale = q->scale;
   a.B = q->n_requests; a.width = q->max_pages; a.page = cache->page_rows; a.n_pages = cache->n_pages; a.n_select = q->selected ? q->n_select : 0;
   a.n_kvh = ctx->n_kvh; a.group = ctx->n_qh / ctx->n_kvh; a.d_h = ctx->d_h; a.out_bf16 = ctx->out == PACT_BF16;
+  a.polls = ctx->copy_polls;
   int launches = 0;
   CK(launch_attend(a, *cache, ctx->paged, ctx->dev, ctx->in == PACT_BF16, (cudaStream_t)stream, &launches));
   ctx->launches += launches;

@@ -15,6 +15,8 @@
 // Pipeline.  One warp copies: each lane works out page ids and row counts of one tile, 32 tiles at a time, and tiles arrive as boxes of
 // 128-byte columns through the tensor-copy unit (swizzled, so that ldmatrix meets no bank conflicts) in a ring that runs on across requests.
 // Four warps compute; each has 16 rows of every tile and its own running maximum, sum and output, so they meet only at the end of a request.
+// A warp whose wait runs out gives up for its CTA: it gives no stage back any more, so that the copying warp fills none whose copies have not been waited for
+// and stops within a ring; all go on through the barriers, and the copies under way land before the CTA ends.
 //
 // bf16: logits as K (16 rows x 16) by q^T (16 x 8 heads) on mma.sync, so that eight heads are one operand; the output as V^T (16 columns x 16 rows)
 // by P^T (16 rows x 8 heads), also without padding.  tcgen05 would want 64 or 128 rows per instruction and its results through tensor memory,
@@ -65,7 +67,7 @@ __host__ __device__ inline AttendSmem attend_smem(int stages, int blocks, int he
   m.tiles = m.ml + kConsumers * heads * 8;
   m.bars = m.tiles + 32 * (int)sizeof(TilePlan);
   m.meta = m.bars + 2 * stages * 8;
-  m.pre = m.meta + stages * 4 + 4;
+  m.pre = m.meta + stages * 4 + 8;
   m.total = m.pre + (B + 1 + kAttendThreads / 32) * 4;
   return m;
 }
@@ -475,7 +477,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
   const AttendSmem at = attend_smem(a.stages, NB, P::kHeads, sizeof(T), CLUSTER ? 1 : a.B);
   uint64_t *full = reinterpret_cast<uint64_t *>(sm + at.bars), *empty = full + a.stages;
   uint32_t *meta = reinterpret_cast<uint32_t *>(sm + at.meta);
-  int *abort = reinterpret_cast<int *>(meta + a.stages);
+  int *abort = reinterpret_cast<int *>(meta + a.stages), *filled = abort + 1;   // tiles that the copying warp has asked for
   int *pre = reinterpret_cast<int *>(sm + at.pre), *w_sum = pre + (CLUSTER ? 1 : a.B) + 1;
   TilePlan *plan = reinterpret_cast<TilePlan *>(sm + at.tiles);
   if (tid < a.stages) {
@@ -584,6 +586,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
     // ---- the copying warp ----
     int st = 0;
     uint32_t ph = 0;
+    int tiles = 0;
     bool given_up = false;
     for (long long base = t0; base < t1 && !given_up; base += 32) {
       const int n = (int)min(32ll, t1 - base);
@@ -613,7 +616,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
       __syncwarp();
       for (int i = 0; i < n; ++i) {
         const uint32_t rows = plan[i].rows, place = plan[i].place;
-        if (!mbar_wait_warp(empty + st, ph ^ 1)) {
+        if (!mbar_wait_warp_polls(abort, empty + st, ph ^ 1, a.polls)) {
           given_up = true;
           if (lane == 0) {
             atomicExch(abort, 1);
@@ -621,6 +624,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
           }
           break;
         }
+        ++tiles;
         if (lane == 0) {
           meta[st] = rows;
           mbar_arrive_expect_tx(full + st, plan[i].bytes);
@@ -657,6 +661,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
       }
       __syncwarp();
     }
+    if (lane == 0) *filled = tiles;
   } else {
     // ---- the computing warps ----
     P part;
@@ -685,7 +690,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
     for (long long t = t0; t < t1;) {
       const int n = CLUSTER ? pre[1] : pre[b + 1] - pre[b], j1 = (int)min((long long)n, j + (t1 - t));
       for (int i = j; i < j1; ++i) {
-        if (ok && !mbar_wait_warp_unless(abort, full + st, ph)) {
+        if (ok && !mbar_wait_warp_polls(abort, full + st, ph, a.polls)) {
           ok = false;
           if (lane == 0) {
             atomicExch(abort, 1);
@@ -700,7 +705,7 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
                     slots + warp * kScratch<P::kHeads>);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(empty + st);
+        if (lane == 0 && ok) mbar_arrive(empty + st);          // (a warp that has given up keeps its stage)
         if (++st == a.stages) {
           st = 0;
           ph ^= 1;
@@ -803,7 +808,10 @@ __global__ void __launch_bounds__(kAttendThreads, attend_ctas(NB, NT))
   } else {
     __syncthreads();
   }
-  if (*abort) land_copies(full, a.stages);
+  if (*abort && tid < min(a.stages, *filled)) {              // each stage's last copies, which still write to this CTA's shared memory
+    const int rounds = (*filled - 1 - tid) / a.stages;
+    mbar_wait_slow(full + tid, rounds & 1);
+  }
 }
 
 // Parts of the requests and key heads that were cut.  Few parts (a batch): CTA i < `shares` has what was cut at the beginning of share i and not before it, a

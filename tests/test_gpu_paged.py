@@ -791,6 +791,35 @@ def test_refusals_on_the_device(pb):
         ctx.pact_paged_attention(pb.PagedCache(K, K), Q.cpu(), i32([[0]]), i32([3]), Q.clone())
 
 
+@pytest.mark.parametrize("dtype,n_qh,H,D,lens,wide", [(BF, 8, 2, 64, [3000], False), (BF, 8, 2, 128, [60000, 5, 0, 20000], True), (F32, 2, 2, 64, [212], False), (F32, 8, 1, 128, [30000, 7], True),
+                                                      (BF, 16, 1, 256, [9000] * 3, True), (BF, 4, 2, 64, [700, 300] * 12, False)])
+def test_waits_that_run_out(pb, dtype, n_qh, H, D, lens, wide):
+    """Waits of a few polls: the call ends with its status, wherever in the ring a warp gave up, nothing outside the result is touched, and the next call is right."""
+    rng, g, page = np.random.default_rng(0), torch.Generator(device="cuda").manual_seed(0), 16
+    n_pages = sum(po.pages_for(n, page) for n in lens) + 1
+    K, V, w, _, _ = cache_tensors(g, n_pages, H, page, D, dtype, bounds=False)
+    width = 100000 // page if wide else max(po.pages_for(n, page) for n in lens)
+    table = i32(tables(rng, lens, width, page, n_pages))
+    ctx, cache = pb.Context(n_qh * D, n_qh, H, D, dtype, F32), pb.PagedCache(K, V, w)
+    Q, L, B = torch.randn(len(lens), n_qh, D, generator=g, device="cuda").to(dtype), i32(lens), len(lens)
+    want, buf, status = torch.zeros(B, n_qh, D, device="cuda"), torch.full((B + 2, n_qh, D), -5.0, device="cuda"), i32([0])
+    copies = [x.clone() for x in (K, V, w)]
+    ctx.pact_paged_attention(cache, Q, table, L, want, status=status)
+    assert status.item() == 0
+    seen = set()
+    for polls in (1, 2, 1, 3, 5, 9, 20, 50, 100, 1, 0):
+        ctx.set_wait_limits(barrier_polls=polls)
+        buf.fill_(-5)
+        status.zero_()
+        ctx.pact_paged_attention(cache, Q, table, L, buf[1:-1], status=status)
+        seen.add(status.item())
+        assert status.item() in (0, -5) and (polls != 1 or status.item() == -5) and (polls or status.item() == 0)
+        assert (buf[0] == -5).all() and (buf[-1] == -5).all()
+        if status.item() == 0:
+            assert torch.equal(buf[1:-1], want)
+    assert seen == {0, -5} and all(torch.equal(x, y) for x, y in zip(copies, (K, V, w)))
+
+
 def test_two_calls_at_once_on_two_contexts(pb):
     """Contexts have workspaces of their own."""
     g = torch.Generator(device="cuda").manual_seed(6)
