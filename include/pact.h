@@ -387,7 +387,7 @@ typedef struct {
 size_t pact_paged_workspace_bytes(const pact_ctx *ctx, int max_requests, int max_pages);
 
 /* Pages that the new token should attend to.  For a page with bounds lo, hi and every query head j of a key head,
- * scale * sum_c (max(q_c, 0) hi_c + min(q_c, 0) lo_c) + w_max is at least every logit scale * q.k + logw of its rows (scale >= 0); the page's
+ * scale * sum_c (q_c hi_c where q_c > 0, q_c lo_c where q_c < 0) + w_max is at least every logit scale * q.k + logw of its rows that is a number (scale > 0); the page's
  * score is the largest of these over the heads (a sum that is not a number is left out), in the order of double precision.  Selected are the first
  * n_first and the last n_last pages of the request, then those with the largest scores, ties to the lower page, n_select in all.
  * selected: their places in ascending order, -1 behind the last.  n_first, n_last >= 0, n_first + n_last <= n_select; max_pages <= 65536.  Lengths

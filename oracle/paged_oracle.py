@@ -74,7 +74,8 @@ def page_scores(q, bounds, w_max, ids, scale):
         if not 0 <= at < len(bounds):
             out.append(-np.inf)
             continue
-        s = (np.maximum(q, 0) * bounds[at, 1] + np.minimum(q, 0) * bounds[at, 0]).sum(1) * scale
+        with np.errstate(invalid="ignore"):                # (infinities: 0 times one is no part of the sum, two of them may make a NaN)
+            s = (np.where(q == 0, 0.0, q * np.where(q > 0, bounds[at, 1], bounds[at, 0]))).sum(1) * scale
         s = s[~np.isnan(s)]
         out.append(max(s) + w_max[at] if len(s) else -np.inf)
     return np.array(out)

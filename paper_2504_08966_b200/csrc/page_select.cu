@@ -1,7 +1,8 @@
 // Pages that one new token should attend to (pact_page_select).
 //
-// For a page with key bounds lo, hi and a query q, the largest q.k over all k with lo <= k <= hi is sum_c (max(q_c, 0) hi_c + min(q_c, 0) lo_c), so
-// scale times it, plus the page's largest bias, bounds every logit of the page.  The order of the scores decides what is selected, and with
+// For a page with key bounds lo, hi and a query q, the largest q.k over all k with lo <= k <= hi is the sum of q_c hi_c where q_c > 0 and q_c lo_c where q_c < 0, so
+// scale times it, plus the page's largest bias, bounds every logit of the page.  (As max(q_c, 0) hi_c + min(q_c, 0) lo_c in the fp32 scores: the same but for
+// infinite bounds, where 0 times infinity has no place in the sum; those scores are formed again in double.)  The order of the scores decides what is selected, and with
 // thousands of pages two scores that differ by 1e-6 of themselves are common: the order is that of scores formed in double (products of bf16 or
 // fp32 numbers are exact there, sums good to 1e-15).  Doubles for all of them cost 12 times what the bytes do (82 us where HBM would need 7), so
 // the scores are formed in fp32 with a bound of their error, and in double only those that the bound leaves in doubt, a few per request.
@@ -232,12 +233,11 @@ template <typename T> __device__ __noinline__ double exact_score(const SelectArg
     double s[4] = {0.0, 0.0, 0.0, 0.0};
 #pragma unroll 1                              // (its code is cold: unrolled it takes 0.4 us more)
     for (int c = lane; c < a.d_h; c += 32) {
-      const double lo = (float)row[c], hi = (float)row[a.d_h + c];
+      const float lo = (float)row[c], hi = (float)row[a.d_h + c];
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
         const float q = h0 + h < a.group ? (float)Q[(h0 + h) * a.ldQh + c] : 0.f;
-        const double qp = q > 0.f ? q : q == q ? 0.f : q, qn = q < 0.f ? q : 0.f;
-        s[h] = fma(qp, hi, fma(qn, lo, s[h]));
+        s[h] = fma((double)q, (double)(q > 0.f ? hi : q < 0.f ? lo : q), s[h]);   // (0 and NaN by themselves)
       }
     }
 #pragma unroll

@@ -660,6 +660,29 @@ def test_selection_of_infinite_and_huge_bounds(pb):
         assert np.array_equal(sel.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("dtype,D,n", [(BF, 64, 12), (F32, 64, 12), (BF, 128, 900), (F32, 100, 300), (BF, 256, 40)])
+def test_a_key_with_an_infinite_coordinate_hides_no_other_row(pb, dtype, D, n):
+    """Pages written by the library; one page has the row with the largest logit and another row with an infinite key, whose own logit is minus infinity."""
+    page, H, g = 16, 1, torch.Generator(device="cuda").manual_seed(D + n)
+    K, V, w, b, wm = cache_tensors(g, n, H, page, D, dtype)
+    ctx, cache = context(pb, 2, H, D, dtype), pb.PagedCache(K, V, w, b, wm)
+    Q = torch.randn(1, 2, D, generator=g, device="cuda").to(dtype)
+    Q[0, :, 5], Q[0, :, 9] = -1, 0
+    rows = (torch.randn(n * page, H, D, generator=g, device="cuda") * 0.1).to(dtype)
+    target = n // 2
+    rows[target * page + 3, 0] = 0.5 * Q[0, 1]                # the largest logit of all
+    for bad in (float("inf"), float("-inf")):
+        rows[target * page + 8, 0, 9] = bad                    # 0 times it: the logit is not a number
+        rows[target * page + 9, 0, 5] = float("inf")
+        status, sel = i32([0]), torch.zeros(1, H, 3, dtype=I32, device="cuda")
+        ctx.pact_cache_write(cache, rows, rows, None, torch.arange(n * page, device="cuda"), status=status)
+        ctx.pact_page_select(cache, Q, torch.arange(n, dtype=I32, device="cuda")[None], i32([n * page]), sel, 0, 0, scale=0.2, status=status)
+        logits = torch.einsum("hc,nc->nh", Q[0].double(), rows[:, 0].double()).nan_to_num(nan=float("-inf")).amax(1)
+        assert logits.argmax().item() // page == target and logits.amax().isfinite()
+        assert status.item() == 0 and target in sel[0, 0].tolist()
+        assert np.array_equal(sel.cpu().numpy(), po.select(f64(Q), f64(b), f64(wm), np.arange(n)[None], [n * page], page, float(np.float32(0.2)), 0, 0, 3))
+
+
 # ---- as a serving program uses them --------------------------------------------------------------------------------
 
 def test_captured_and_replayed_with_other_lengths_beside_eager_calls(pb):

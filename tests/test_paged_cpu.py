@@ -387,3 +387,20 @@ def test_oracle_scores_bound_every_logit():
         s = po.page_scores(q[0, h * 3:h * 3 + 3], bounds[:, h], logw.max(1), range(40), 0.3)
         logits = np.einsum("gc,prc->pgr", q[0, h * 3:h * 3 + 3], K[:, h]) * 0.3 + logw[:, None]
         assert (s >= logits.max((1, 2)) - 1e-12).all()
+
+
+def test_oracle_scores_bound_every_logit_beside_infinities():
+    """A key with infinite coordinates: the page's other rows still have the logits that they have."""
+    rng = np.random.default_rng(1)
+    K, q = rng.normal(size=(60, 1, 16, 8)), rng.normal(size=(1, 5, 8))
+    q[0, :, 3] = 0
+    for page in range(60):
+        for _ in range(page % 4):
+            K[page, 0, rng.integers(16), rng.integers(8)] = rng.choice([np.inf, -np.inf])
+    K[7, 0, :, 2] = -np.inf                                   # in every row: what of this page is a number is an infinity
+    bounds = np.stack([K.min(2), K.max(2)], 2)
+    s = po.page_scores(q[0], bounds[:, 0], np.zeros(60), range(60), 0.3)
+    with np.errstate(invalid="ignore"):
+        logits = np.einsum("gc,prc->pgr", q[0], K[:, 0]) * 0.3
+    assert np.isnan(logits).any()
+    assert (s >= np.where(np.isnan(logits), -np.inf, logits).max((1, 2)) - 1e-12).all()
