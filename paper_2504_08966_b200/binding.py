@@ -409,7 +409,8 @@ class Context:
         raise PactError("the arguments do not fit together")
 
     def _paged_workspace(self, B, max_pages):
-        """Address and size of the workspace.  One that is outgrown is kept: a captured graph may hold its address."""
+        """Address and size of the workspace.  One that is outgrown is kept: a captured graph may hold its address.  (So that they are few, the next one is twice as
+        large, up to 64 MB; beyond that it is as large as needed.)"""
         need = self._paged_need.get((B, max_pages))
         if need is None:
             if len(self._paged_need) >= 4096:
@@ -417,7 +418,7 @@ class Context:
             need = self._paged_need[(B, max_pages)] = int(self._L.pact_paged_workspace_bytes(self.handle, B, max_pages))
         have = self._paged_ws[-1] if self._paged_ws else None
         if have is None or have[1] < need:
-            size = max(need, 2 * have[1] if have else 0)   # (never less than what the attention's parts need, which does not depend on B or max_pages)
+            size = max(need, min(2 * have[1], 64 << 20) if have else 0)   # (never less than what the attention's parts need, which does not depend on B or max_pages)
             ws = torch.empty(size, dtype=torch.uint8, device=self._cuda())
             self._paged_ws.append((ws.data_ptr(), size, ws))
         return self._paged_ws[-1]

@@ -250,7 +250,6 @@ template <typename T> __device__ __noinline__ double exact_score(const SelectArg
 }
 
 constexpr int kPickBits = 10;
-constexpr int kPickKeys = 8192;            // scores of a request and head that are kept in shared memory
 constexpr int kPickNear = 256;             // most scores near the n-th largest that are decided by comparing them with one another
 constexpr int kPickBin = 64;               // a bin of no more scores than this is not divided further
 

@@ -46,6 +46,7 @@ cudaError_t launch_cache_write(const WriteArgs &a, bool bf16, int sm_count, cuda
 // ---- page_select.cu ------------------------------------------------------------------------------------
 
 constexpr int kMaxSelectPages = 65536;
+constexpr int kPickKeys = 8192;            // scores of a request and head that are kept in shared memory
 struct SelectArgs {
   const void *Q;
   long long ldQ, ldQh;

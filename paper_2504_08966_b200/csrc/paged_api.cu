@@ -42,7 +42,8 @@ pact_status check_ws(void *ws, size_t have, size_t need) {
 
 size_t select_scores(const pact_ctx *c, int requests, int pages) { return (size_t)requests * c->n_kvh * pages; }
 size_t select_bytes(const pact_ctx *c, int requests, int pages) {
-  return (select_scores(c, requests, pages) * (sizeof(uint32_t) + sizeof(unsigned long long)) + kAlign - 1) / kAlign * kAlign;
+  const size_t of_score = sizeof(unsigned long long) + (pages > kPickKeys ? sizeof(uint32_t) : 0);
+  return (select_scores(c, requests, pages) * of_score + kAlign - 1) / kAlign * kAlign;
 }
 
 }  // namespace

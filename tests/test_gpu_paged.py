@@ -685,6 +685,14 @@ def test_a_key_with_an_infinite_coordinate_hides_no_other_row(pb, dtype, D, n):
 
 # ---- as a serving program uses them --------------------------------------------------------------------------------
 
+def test_workspace_of_a_selection(pb):
+    """Eight bytes per request, key head and page for scores in double, and four for those in fp32 only where a request may have more than shared memory holds."""
+    ctx = context(pb, 6, 2, 64)
+    parts = ctx._L.pact_paged_workspace_bytes(ctx.handle, 1, 1)
+    for B, pages, of_score in ((128, 8192, 8), (1, 60000, 12), (64, 8193, 12)):
+        assert ctx._L.pact_paged_workspace_bytes(ctx.handle, B, pages) == max(parts, (B * 2 * pages * of_score + 255) // 256 * 256)
+
+
 def test_captured_and_replayed_with_other_lengths_beside_eager_calls(pb):
     """Two captured graphs and eager calls of one context take turns on its workspace."""
     rng, g = np.random.default_rng(0), torch.Generator(device="cuda").manual_seed(0)

@@ -353,6 +353,17 @@ def test_workspaces_that_are_outgrown_are_kept(monkeypatch):
     assert len({a for a, _, _ in got}) == 3 and len(ctx._paged_ws) == 3
 
 
+def test_a_large_workspace_grows_to_what_is_needed(monkeypatch):
+    """Where two of them would not fit beside the outgrown one."""
+    ctx = _stub_context()
+    del ctx._paged_workspace
+    monkeypatch.setattr(type(ctx), "_cuda", lambda self: torch.device("meta"))
+    mb = 1 << 20
+    ctx._paged_need.update({(1, 1): 20 * mb, (2, 2): 21 * mb, (3, 3): 50 * mb, (4, 4): 800 * mb, (5, 5): 801 * mb})
+    got = [ctx._paged_workspace(i, i)[1] // mb for i in range(1, 6)]
+    assert got == [20, 40, 64, 800, 801] and len(ctx._paged_ws) == 5
+
+
 # ---- pins of the plain implementations ------------------------------------------------------------------------------
 
 def test_oracle_plan_by_hand():
