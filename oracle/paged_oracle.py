@@ -77,7 +77,9 @@ def page_scores(q, bounds, w_max, ids, scale):
         with np.errstate(invalid="ignore"):                # (infinities: 0 times one is no part of the sum, two of them may make a NaN)
             s = (np.where(q == 0, 0.0, q * np.where(q > 0, bounds[at, 1], bounds[at, 0]))).sum(1) * scale
         s = s[~np.isnan(s)]
-        out.append(max(s) + w_max[at] if len(s) else -np.inf)
+        with np.errstate(invalid="ignore"):
+            s = max(s) + w_max[at] if len(s) else -np.inf
+        out.append(-np.inf if np.isnan(s) else s)
     return np.array(out)
 
 

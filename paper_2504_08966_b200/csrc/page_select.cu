@@ -48,16 +48,21 @@ __device__ __forceinline__ int pages_of(const SelectArgs &a, int b, bool report)
 }
 
 // A page's score in fp32 as an integer, and a bound of its error.  `size` is the sum of the absolute products, the largest over the heads, times |scale|;
-// rel: what the additions are off by, as a part of it; the addition of w is off by 2^-24 of the result.  What fp32 cannot hold, infinities and
-// NaN get an unlimited error: they are decided in double.
+// rel: what the additions are off by, as a part of it; the addition of w is off by 2^-24 of the result.
+// What fp32 cannot hold is marked: the first CTA forms these scores in double.  (An unlimited error for all scores of the request instead, which decides every one of them in
+// double: one infinite key among 4096 pages 1.7 ms against 18 us, among 65536 pages 28 ms
+// against 0.26.)
+constexpr uint32_t kMarked = ~0u;              // in place of a score
+constexpr uint32_t kAnyMarked = 0x80000000u;   // beside the largest error
+constexpr uint32_t kUnlimited = 0x7f800000u;   // an error
 __device__ __forceinline__ uint32_t approx(float best, float size, float rel, float w, uint32_t &err) {
   if (w == -INFINITY) return order_key(-INFINITY);
   const float s = best + w, e = size * rel + (size + fabsf(w)) * (1.f / 4194304.f);
   if (!(e < 1e30f) || !(fabsf(s) < 1e30f)) {
-    err = 0x7f800000u;
-    return order_key(0.f);
+    err |= kAnyMarked;
+    return kMarked;
   }
-  err = max(err, __float_as_uint(e));
+  err = max(err & ~kAnyMarked, __float_as_uint(e)) | (err & kAnyMarked);
   return order_key(s);
 }
 
@@ -388,7 +393,7 @@ __global__ void __launch_bounds__(kSelectThreads, W * sizeof(T) <= 4 ? 2 : 1) k_
     }
     kmax = __reduce_max_sync(0xffffffffu, kmax);
     kmin = __reduce_min_sync(0xffffffffu, kmin);
-    err = __reduce_max_sync(0xffffffffu, err);
+    err = __reduce_max_sync(0xffffffffu, err & ~kAnyMarked) | __reduce_or_sync(0xffffffffu, err & kAnyMarked);
     if (lane < 3) st_cluster_u32(s.range[lane] + rank * kSelectWarps + warp, 0, lane == 0 ? kmax : lane == 1 ? kmin : err);
   }
   cluster_sync();
@@ -408,9 +413,55 @@ __global__ void __launch_bounds__(kSelectThreads, W * sizeof(T) <= 4 ? 2 : 1) k_
   kmax = __reduce_max_sync(0xffffffffu, kmax);
   kmin = __reduce_min_sync(0xffffffffu, kmin);
   err = __reduce_max_sync(0xffffffffu, err);
+  const auto key = [&](int i) { return kept ? s_keys[i] : apx[i]; };
+  if (err & kAnyMarked) {
+    err = 0;
+    for (int i = 0; i < ctas * kSelectWarps; ++i) err = max(err, s.range[2][i] & ~kAnyMarked);
+    kmax = 0;                                              // (a mark is above all scores)
+    if (tid == 0) s.n_near = 0;
+    __syncthreads();
+    for (int i = tid; i < np; i += kSelectThreads) {
+      const uint32_t k = key(i);
+      if (k != kMarked) {
+        kmax = max(kmax, k);
+      } else {
+        const int at = atomicAdd(&s.n_near, 1);
+        if (at < kPickNear) s.near_at[at] = i;
+      }
+    }
+    __syncthreads();
+    const int n = s.n_near;
+    if (n > kPickNear) err = kUnlimited;
+    for (int j = warp; j < min(n, kPickNear); j += kSelectWarps) {
+      const int p = s.near_at[j];
+      const double x = exact_score<T>(a, b, head, p);
+      uint32_t k;
+      if (fabs(x) < 1e30) {
+        k = order_key((float)x);
+        err = max(err, __float_as_uint((float)fabs(x) * (1.f / 8388608.f)));
+      } else {                                             // infinities (NaN as minus infinity) as they are; what is beyond fp32: all scores are decided in double
+        k = order_key(x == INFINITY ? INFINITY : x > -INFINITY ? 0.f : -INFINITY);
+        if (fabs(x) < INFINITY) err = kUnlimited;
+      }
+      kmax = max(kmax, k);
+      kmin = min(kmin, k);
+      if (lane == 0) {
+        if (kept) s_keys[p] = k;
+        else a.approx[row + p] = k;
+      }
+    }
+    kmax = __reduce_max_sync(0xffffffffu, kmax);
+    __syncthreads();                                       // (all have read the ranges of the cluster)
+    if (lane < 3) s.range[lane][warp] = lane == 0 ? kmax : lane == 1 ? kmin : err;
+    __syncthreads();
+    for (int w = 0; w < kSelectWarps; ++w) {
+      kmax = max(kmax, s.range[0][w]);
+      kmin = min(kmin, s.range[1][w]);
+      err = max(err, s.range[2][w]);
+    }
+  }
   if (tid == 0) s.n_near = s.n_sure = s.n_doubt = 0;
   __syncthreads();
-  const auto key = [&](int i) { return kept ? s_keys[i] : apx[i]; };
   const int words = (np + 31) / 32;
   // Of two scores whose fp32 values differ by more than twice the largest error the larger one is the larger one in double as well.  [low, high]: fp32
   // values that may lie on either side of the need-th largest; those above it are selected.
@@ -418,7 +469,7 @@ __global__ void __launch_bounds__(kSelectThreads, W * sizeof(T) <= 4 ? 2 : 1) k_
   const auto below = [&](uint32_t k) { return order_key(__fsub_rd(from_order_key(k), e2)); };
   const auto above = [&](uint32_t k) { return order_key(__fadd_ru(from_order_key(k), e2)); };
   uint32_t low = 0, high = ~0u;
-  if (err < 0x7f800000u) {
+  if (err < kUnlimited) {
     const Cut<uint32_t> cut = find_cut<uint32_t>(s, key, first, end, need, kmax, kmin, kPickBin);
     // the need-th largest agrees with the prefix
     const uint32_t least = cut.shift >= 32 ? 0u : cut.prefix << cut.shift, most = cut.shift >= 32 ? ~0u : least | ((1u << cut.shift) - 1u);
@@ -449,7 +500,7 @@ __global__ void __launch_bounds__(kSelectThreads, W * sizeof(T) <= 4 ? 2 : 1) k_
     // each against the others: `over` of them are larger whatever the errors, `maybe` may be (itself among them)
     int in = 0;
     for (int j = tid; j < near; j += kSelectThreads) {
-      const uint32_t k = s.near_key[j], up = err < 0x7f800000u ? above(k) : ~0u, down = err < 0x7f800000u ? below(k) : 0u;
+      const uint32_t k = s.near_key[j], up = err < kUnlimited ? above(k) : ~0u, down = err < kUnlimited ? below(k) : 0u;
       int over = 0, maybe = 0;
       for (int i = 0; i < near; ++i) {
         over += s.near_key[i] > up;

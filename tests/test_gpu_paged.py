@@ -683,6 +683,25 @@ def test_a_key_with_an_infinite_coordinate_hides_no_other_row(pb, dtype, D, n):
         assert np.array_equal(sel.cpu().numpy(), po.select(f64(Q), f64(b), f64(wm), np.arange(n)[None], [n * page], page, float(np.float32(0.2)), 0, 0, 3))
 
 
+@pytest.mark.parametrize("dtype,D,n,n_bad,n_select", [(BF, 64, 300, 1, 40), (BF, 128, 9000, 3, 500), (F32, 64, 2000, 700, 300), (F32, 128, 9000, 40, 64), (BF, 64, 2000, 2000, 30), (BF, 64, 1500, 5, 1499)])
+def test_pages_with_infinite_bounds_among_many(pb, dtype, D, n, n_bad, n_select):
+    """Only their scores are formed in double; the others keep the order that they have, and infinite scores tie to the lower page."""
+    rng, g, page = np.random.default_rng(n + n_bad), torch.Generator(device="cuda").manual_seed(n), 16
+    K, V, w, b, wm = cache_tensors(g, n, 1, page, D, dtype)
+    bad = rng.permutation(n)[:n_bad]
+    at = lambda x: torch.tensor(np.ascontiguousarray(x), device="cuda")   # noqa: E731
+    b[at(bad), 0, at(rng.integers(0, 2, n_bad)), at(rng.integers(0, D, n_bad))] = at(rng.choice([np.inf, -np.inf, np.nan], n_bad)).to(dtype)
+    wm[at(bad[1::7])] = float("-inf")
+    wm[at(bad[2::7])] = float("inf")
+    Q = torch.randn(2, 3, D, generator=g, device="cuda").to(dtype)
+    Q[1, :, ::2] = 0
+    table = np.stack([rng.permutation(n).astype(np.int32) for _ in range(2)])
+    lens, sel, status = [n * page, (n - 1) * page - 3], torch.zeros(2, 1, n_select, dtype=I32, device="cuda"), i32([0])
+    context(pb, 3, 1, D, dtype).pact_page_select(pb.PagedCache(K, V, w, b, wm), Q, i32(table), i32(lens), sel, 1, 1, scale=0.5, status=status)
+    want = po.select(f64(Q), f64(b), f64(wm), table, lens, page, 0.5, 1, 1, n_select)
+    assert status.item() == 0 and np.array_equal(sel.cpu().numpy(), want)
+
+
 # ---- as a serving program uses them --------------------------------------------------------------------------------
 
 def test_workspace_of_a_selection(pb):
