@@ -52,12 +52,15 @@ __device__ __forceinline__ int pages_of(const SelectArgs &a, int b, bool report)
 // What fp32 cannot hold is marked: the first CTA forms these scores in double.  (An unlimited error for all scores of the request instead, which decides every one of them in
 // double: one infinite key among 4096 pages 1.7 ms against 18 us, among 65536 pages 28 ms
 // against 0.26.)
+// Below the normal numbers errors are no part of the value: sums of products are off by a few hundred times 2^-126 at most (where tensor cores drop them), which is
+// less than any rel of kTiny, and everything else by steps of 2^-149 (kLast: seven of them).
+constexpr float kTiny = 1e-28f, kLast = 1e-44f;
 constexpr uint32_t kMarked = ~0u;              // in place of a score
 constexpr uint32_t kAnyMarked = 0x80000000u;   // beside the largest error
 constexpr uint32_t kUnlimited = 0x7f800000u;   // an error
 __device__ __forceinline__ uint32_t approx(float best, float size, float rel, float w, uint32_t &err) {
   if (w == -INFINITY) return order_key(-INFINITY);
-  const float s = best + w, e = size * rel + (size + fabsf(w)) * (1.f / 4194304.f);
+  const float s = best + w, e = size * rel + (size + fabsf(w)) * (1.f / 4194304.f) + kLast;
   if (!(e < 1e30f) || !(fabsf(s) < 1e30f)) {
     err |= kAnyMarked;
     return kMarked;
@@ -149,7 +152,7 @@ template <int ND, typename F> __device__ __forceinline__ void score_pages(const 
     size1 = max(size1, __shfl_xor_sync(0xffffffffu, size1, o));
   }
   const int p = p0 + r + 8 * c;                            // lane 4 r has page r, lane 4 r + 1 page r + 8
-  if (c < 2 && p < np) put(p, approx(c ? best1 : best0, fabsf(a.scale) * __uint_as_float(c ? size1 : size0), kRel, w, err));
+  if (c < 2 && p < np) put(p, approx(c ? best1 : best0, fabsf(a.scale) * (__uint_as_float(c ? size1 : size0) + kTiny), kRel, w, err));
 }
 
 constexpr int kHeadsAtOnce = 4;
@@ -224,7 +227,7 @@ template <int DL, typename F> __device__ __forceinline__ void score_pages_f32(co
     size = max(size, __shfl_xor_sync(0xffffffffu, size, o));
   }
   const int p = p0 + (lane >> 2);
-  if ((lane & 3) == 0 && p < np) put(p, approx(best, fabsf(a.scale) * __uint_as_float(size), kRel, w, err));
+  if ((lane & 3) == 0 && p < np) put(p, approx(best, fabsf(a.scale) * (__uint_as_float(size) + kTiny), kRel, w, err));
 }
 
 // The score of page p in double, by a warp.
@@ -438,7 +441,7 @@ __global__ void __launch_bounds__(kSelectThreads, W * sizeof(T) <= 4 ? 2 : 1) k_
       uint32_t k;
       if (fabs(x) < 1e30) {
         k = order_key((float)x);
-        err = max(err, __float_as_uint((float)fabs(x) * (1.f / 8388608.f)));
+        err = max(err, __float_as_uint((float)fabs(x) * (1.f / 8388608.f) + kLast));
       } else {                                             // infinities (NaN as minus infinity) as they are; what is beyond fp32: all scores are decided in double
         k = order_key(x == INFINITY ? INFINITY : x > -INFINITY ? 0.f : -INFINITY);
         if (fabs(x) < INFINITY) err = kUnlimited;

@@ -300,6 +300,18 @@ def test_scores_that_differ_beyond_32_bits(pb):
     assert sel[0, 0].tolist() == sorted(order.argsort(descending=True)[:100].tolist())
 
 
+@pytest.mark.parametrize("dtype,D,k_size,q_size,scale", [(F32, 64, 1e-22, 1e-20, 1.0), (BF, 64, 1e-22, 1e-20, 1.0), (BF, 128, 1e-20, 1e-18, 0.5), (F32, 128, 1.0, 1.0, 1e-43), (BF, 128, 1.0, 1.0, 1e-43), (F32, 100, 1e-25, 1e-20, 1e30)])
+def test_scores_below_the_normal_numbers_of_fp32(pb, dtype, D, k_size, q_size, scale):
+    """Products of about 1e-38 and far below, which fp32 holds in few bits or not at all."""
+    n, page, n_select, g = 700, 16, 90, torch.Generator(device="cuda").manual_seed(D)
+    b = (torch.randn(n, 1, 2, D, generator=g, device="cuda") * k_size).to(dtype).sort(2).values.contiguous()
+    Q, K, wm = (torch.randn(1, 3, D, generator=g, device="cuda") * q_size).to(dtype), torch.zeros(n, 1, page, D, dtype=dtype, device="cuda"), torch.zeros(n, device="cuda")
+    sel, table = torch.zeros(1, 1, n_select, dtype=I32, device="cuda"), torch.arange(n, device="cuda", dtype=I32)[None]
+    context(pb, 3, 1, D, dtype).pact_page_select(pb.PagedCache(K, K, None, b, wm), Q, table, i32([n * page]), sel, 1, 1, scale=scale)
+    want = po.select(f64(Q), f64(b), f64(wm), table.cpu().numpy(), [n * page], page, float(np.float32(scale)), 1, 1, n_select)
+    assert np.array_equal(sel.cpu().numpy(), want)
+
+
 def test_select_with_bad_pages_lengths_and_scores(pb):
     rng = np.random.default_rng(0)
     n_pages, page, D, width = 40, 16, 64, 12
