@@ -445,6 +445,41 @@ def test_bf16_results_are_rounded_once(pb, B, n_qh, D, page):
     assert (np.abs(f64(out) - want) <= half_step + 2.0 ** -20 * want).all()
 
 
+@pytest.mark.parametrize("dtype,n_qh,D", [(BF, 1, 64), (BF, 8, 128), (BF, 16, 256), (F32, 1, 64), (F32, 8, 128), (F32, 2, 100)])
+@pytest.mark.parametrize("wide", [False, True])
+def test_probabilities_are_fp32_on_every_route(pb, dtype, n_qh, D, wide):
+    # the two rows and the 2^-20 of test_fp32_results_of_bf16_rows_have_fp32_probabilities, in tables that clusters take and in wide ones, which all CTAs share out; fp32 rows
+    # have products of one rounding each, less than the three terms of bf16
+    B, page = 64, 16
+    g = torch.Generator(device="cuda").manual_seed(D)
+    K = torch.zeros(B, 1, page, D, dtype=dtype, device="cuda")
+    V, w = K.clone(), torch.zeros(B, page, device="cuda")
+    V[:, :, 1] = 1
+    w[:, 1] = -torch.rand(B, generator=g, device="cuda")
+    out, table = torch.empty(B, n_qh, D, device="cuda"), torch.full((B, 6000 if wide else 1), -1, dtype=I32, device="cuda")
+    table[:, 0] = torch.arange(B, dtype=I32, device="cuda")
+    context(pb, n_qh, 1, D, dtype, F32).pact_paged_attention(pb.PagedCache(K, V, w), torch.zeros(B, n_qh, D, dtype=dtype, device="cuda"), table, i32([2] * B), out)
+    x = np.exp(f64(w)[:, 1])[:, None, None]
+    assert np.abs(f64(out) / (x / (1 + x)) - 1).max() <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("dtype,n_qh,H,D,lens,wide", [(BF, 8, 2, 64, [1000, 3, 64], False), (BF, 28, 4, 128, [5000, 17], True), (BF, 16, 1, 256, [900], True), (F32, 2, 2, 64, [700, 1], False), (F32, 8, 1, 128, [4000], True)])
+def test_results_to_fp32(pb, dtype, n_qh, H, D, lens, wide):
+    # Logits from the biases alone (queries 0), values of both signs.  In units of 2^-22 of sum p |v|: p as above, 1.5 in the numerator and 1.5 in the denominator (fp32 rows: less); an
+    # instruction cuts its sum to 2^-23, six of them for a warp's 16 rows: 3; sums: a step per 64 rows and warp in an fp32 of its own, then three to join the warps, eight for the parts
+    # that meet, off by half a step, 2^-24, each.
+    rng, g, page = np.random.default_rng(D), torch.Generator(device="cuda").manual_seed(D), 16
+    n_pages = sum(po.pages_for(n, page) for n in lens) + 1
+    K, V, w, _, _ = cache_tensors(g, n_pages, H, page, D, dtype, bounds=False)
+    w = -torch.rand(n_pages, page, generator=g, device="cuda")
+    table = tables(rng, lens, 6000 if wide else max(po.pages_for(n, page) for n in lens), page, n_pages)
+    Q, out = torch.zeros(len(lens), n_qh, D, dtype=dtype, device="cuda"), torch.empty(len(lens), n_qh, D, device="cuda")
+    context(pb, n_qh, H, D, dtype, F32).pact_paged_attention(pb.PagedCache(K, V, w), Q, i32(table), i32(lens), out)
+    ref, _, mag, _ = po.attend(f64(Q), f64(K), f64(V), f64(w), table, lens, page, 1.0)
+    steps = np.array([n / 64 + 12 for n in lens])[:, None, None]
+    assert (np.abs(f64(out) - ref) <= mag * (6 * 2.0 ** -22 + 2 * steps * 2.0 ** -24)).all()
+
+
 @pytest.mark.parametrize("n_qh,H,D,rows", [(32, 32, 64, 1 << 17), (64, 4, 64, 1 << 20), (8, 8, 256, 1 << 18)])
 def test_sums_over_many_rows_are_not_biased(pb, n_qh, H, D, rows):
     # Values of one sign, thousands of rows of one running sum.  What a sum in fp32 may be off by grows as its roundings happen to fall, and their mean over heads and columns
