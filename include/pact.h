@@ -22,7 +22,8 @@
  *    alignment, workspace too small, parameter out of range) are reported before anything
  *    is launched.  Device-side problems (a bounded wait that ran out) set counters[PACT_CNT_STATUS]
  *    of the image; the library never traps, aborts or throws.
- *  - A context may be used from one host thread and one stream at a time.
+ *  - A context may be used from one host thread and one stream at a time (the replay of a captured call is a use as well: its
+ *    workspace is the one that it was captured with).
  *  - Same inputs give bitwise the same outputs, run after run.
  *
  * Readings of the paper that fix the semantics (the paper is silent on them)
@@ -320,7 +321,9 @@ typedef struct {
  * (0 or more) are to follow: a count array of its own, or the N_OUT counters of a batch that pact_reduce has just written
  * (stride PACT_N_COUNTERS).  A negative count ends the request: its pages go back and its length becomes 0.
  * free_pages is a stack of page ids, its top at free_pages[*n_free - 1].  Ended requests push their pages first, by ascending request and
- * ascending place; then the others take pages off the top in the same order.
+ * ascending place; then the others take pages off the top in the same order.  Page ids are taken as they are (the calls that read or write rows check them).
+ * The tables and the stack of a call name no page twice: one that two requests share (pact_paged_attention may read it for both) goes back once for each that ends, and is
+ * handed out as often.  A caller that shares pages ends these requests itself.
  * New rows are packed (row_stride 0: row i of request b is row_start[b] + i, and n_rows is what the caller has room for), or each request has
  * row_stride of them (row b * row_stride + i; n_rows = n_requests * row_stride).
  * A call that cannot be served as a whole changes nothing: length_out and n_free_out repeat the old values, row_start is 0, every
@@ -399,7 +402,8 @@ pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache /*host
  * 0 .. length[b] - 1, out = sum_p exp(s_p - lse) v_p and lse = log sum_p exp(s_p), for every query head, which reads key head
  * floor(j * n_kvh / n_qh).  With `selected` only the rows of those pages count: of the first min(n_select, pages of the request) entries,
  * those below 0 or beyond the request's pages are skipped, and a page named twice counts twice.  Rows with logw = minus infinity and
- * rows past the length have no effect, whatever their keys and values hold.  Without any row out is 0 and lse minus infinity.
+ * rows past the length have no effect, whatever their keys and values hold.  Without any row out is 0 and lse minus infinity.  Infinities and NaN in rows that count
+ * leave infinities or NaN in the results that they enter (an infinite value beside bf16 keys: NaN).  Keys and values are read once for every 16 query heads of a key head (fp32: 8).
  * Logits, probabilities, softmax statistics and sums are fp32 (beside bf16 values probabilities are carried as three bf16 terms).
  * Lengths are clamped to 0 .. max_pages * page_rows and rows of pages outside
  * the cache are left out; both set status to INVALID_ARG. */

@@ -3,7 +3,7 @@
 //   s_p = scale q.k_p + logw_p,   out = sum_p exp(s_p - m) v_p / sum_p exp(s_p - m),   m = max_p s_p
 //
 // Keys and values are read once and each is used by the few query heads of its key head, so HBM bounds it: 4 d_h bytes per row and key
-// head in bf16 against 4 d_h g operations for g query heads.
+// head in bf16 against 4 d_h g operations for g query heads.  (Once for up to 16 query heads of a key head, in fp32 8; wider groups are several tiles of heads, which read them once each.)
 //
 // Split.  The rows of all requests and key heads, in tiles of 64, form one line of T tiles that G CTAs share out evenly: CTA i takes tiles
 // [i T / G, (i + 1) T / G).  No length, batch or number of heads leaves SMs idle, at most G - 1 cuts are made in all, and k_attend_join puts
@@ -21,7 +21,8 @@
 // bf16: logits as K (16 rows x 16) by q^T (16 x 8 heads) on mma.sync, so that eight heads are one operand; the output as V^T (16 columns x 16 rows)
 // by P^T (16 rows x 8 heads), also without padding.  tcgen05 would want 64 or 128 rows per instruction and its results through tensor memory,
 // where HBM delivers a tile every 1400 clocks of an SM and the warps need less.  Probabilities go in as three bf16 terms, which hold all of fp32's 24 bits.  (Two are
-// off by 2^-17: two rows, worst relative error of a result 5.8e-6 against less than 2^-20, and one bf16 result in 3000 rounded the other way; the third costs 0.5 % of a call that HBM bounds.)
+// off by 2^-17: two rows, worst relative error of a result 5.8e-6 against less than 2^-20; of 28672 bf16 results over 2500 rows 28 were not the nearest number, with three 7.  The third costs 0.5 %
+// of a call that HBM bounds.)
 // The products of 16 rows are summed by themselves, the small terms first, and added with rounding: an instruction cuts its sum off towards 0, so that a running sum in its
 // accumulator loses some 2^-25 at each (values of one sign, 1048576 rows: the mean of the results 2.9e-5 too small, now below 2^-20; 128 requests of 8192 rows 408 -> 412 us).
 // fp32: fused multiply-adds; for the logits a lane has one row and half of the columns, for the output four columns of all rows.
@@ -969,7 +970,8 @@ constexpr size_t kSmSmem = 228 * 1024, kCtaReserve = 1024;   // shared memory of
 // CTAs of a cluster per request and key head, 0: no clusters.  `n` tiles of one at most, `heads` of them.
 // Clusters leave SMs idle where there are few heads and give every request the time of the longest, the line of tiles costs a second kernel.  One request
 // of 28 heads on 4: 1000 rows 7.1 us in clusters against 10.3, 5000 10.1 / 13.2, 9000 12.8 / 13.4, 16000 17.7 / 15.0; eight of them (clusters of 8, two CTAs
-// per SM): 1000 9.5 / 13.2, 5000 16.8 / 19.6, 9000 31 / 35, but the longest of unequal ones counts.  fp32, 2 heads on 2: 200 rows 6.2 / 7.6, 4000 9.2 / 10.6, 9000 13.8 / 13.5.
+// per SM): 1000 9.5 / 13.2, 5000 16.8 / 19.6, 9000 31.7 / 35.5, 16000 48.4 / 52.7 where all are as long, but of eight between 0 and 9000 the longest counts, 23.1 / 22.3, of 0 to 16000 39.0 / 36.5: no clusters
+// beyond 8192 rows.  fp32, 2 heads on 2: 200 rows 6.2 / 7.6, 4000 9.2 / 10.6, 9000 13.8 / 13.5.
 int cluster_for(const PagedCfg &cfg, long long n, long long heads, int sm_count) {
   for (int size = cfg.cluster; size >= 2; size /= 2) {
     const int i = size == 2 ? 0 : size == 4 ? 1 : size == 8 ? 2 : 3;
