@@ -409,6 +409,48 @@ pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache /*host
  * the cache are left out; both set status to INVALID_ARG. */
 pact_status pact_paged_attention(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_query *q /*host*/, void *stream);
 
+/* ---- several new tokens per request, and pages that several requests hold ------------------------------------------------ */
+
+/* What pact_chunk_attention takes: the rows of the new tokens lie as pact_cache_plan lays them out. */
+typedef struct {
+  const void *Q;              /* element [r][j][c] at r * ldQ + j * ldQh + c, type `in`; row r as row_start or row_stride say */
+  int64_t ldQ, ldQh;
+  const int32_t *block_table; /* [n_requests][max_pages]                                            */
+  const int32_t *length;      /* [n_requests] cached rows, those of the new tokens among them (the length_out of pact_cache_plan) */
+  const int32_t *n_new;       /* [n_requests] with stride n_new_stride >= 1: new tokens, the last of the cached rows; 0 or less: none */
+  int64_t n_new_stride;
+  const int32_t *row_start;   /* [n_requests]: token i of request b is row row_start[b] + i; NULL with a row_stride */
+  int64_t n_rows;             /* rows that Q, out and lse have                                      */
+  int32_t row_stride;         /* > 0: token i of request b is row b * row_stride + i, and n_rows = n_requests * row_stride */
+  int32_t n_requests, max_pages;
+  int32_t causal;             /* 1: a token sees the cached rows up to its own; 0: all rows of its request */
+  float scale;                /* of the logits; 1 / sqrt(d_h) as a rule                             */
+  int32_t reserved;
+  void *out;                  /* element [r][j][c] at r * ldO + j * ldOh + c, type `out` (pointer and strides: multiples of four elements) */
+  int64_t ldO, ldOh;
+  float *lse;                 /* [n_rows][n_qh]; may be NULL                                        */
+  int32_t *status;
+  void *ws;                   /* workspace, 256-byte aligned                                        */
+  size_t ws_bytes;
+} pact_chunk;
+
+/* Bytes of device workspace that pact_chunk_attention needs for at most max_requests requests.  It needs no initialisation and keeps nothing between calls;
+ * calls that may run at the same time have one each. */
+size_t pact_chunk_workspace_bytes(const pact_ctx *ctx, int max_requests);
+
+/* Attention of the new tokens of every request (a prompt, a further turn, drafted tokens) over its cached rows, their own among them (pact_cache_write comes first):
+ * with s_p = scale * q.k_p + logw_p (Eq. 11), out = sum_p exp(s_p - lse) v_p and lse = log sum_p exp(s_p) for every query head, which reads key head
+ * floor(j * n_kvh / n_qh).  Token i of request b is cached row length[b] - n_new[b] + i and sees the rows p up to that one (causal), or all rows 0 .. length[b] - 1 (text that
+ * looks at the states of an encoder, say).
+ * Rows with logw = minus infinity, rows past the length and rows that a token must not see have no effect on it, whatever their keys and values hold.  A token
+ * without any row gets 0, and lse minus infinity.  Infinities and NaN in rows that count leave infinities or NaN in the results that they enter (infinite values beside bf16 keys: NaN).
+ * Rows of Q, out and lse that belong to no token are not touched.
+ * Logits, softmax statistics and sums are fp32.  bf16 keys and values: probabilities are rounded to bf16 where results are bf16, and carried as
+ * three bf16 terms where they are fp32.
+ * Lengths outside 0 .. max_pages * page_rows are clamped, rows of pages outside the cache left out, tokens without a row of Q left out, and tokens before the first cached row (n_new above
+ * length) see nothing; each sets status to INVALID_ARG.  Heads as above; n_rows * (n_qh / n_kvh) below 2^31. */
+pact_status pact_chunk_attention(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_chunk *c /*host*/, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

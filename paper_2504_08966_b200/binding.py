@@ -28,7 +28,7 @@ EXPORTS = ["pact_create", "pact_destroy", "pact_workspace_bytes", "pact_status_s
            "pact_host_staging_bytes", "pact_launch_count", "pact_profile_enable", "pact_profile_read",
            "pact_profile_stage_name", "pact_graph_create", "pact_graph_launch", "pact_graph_destroy",
            "pact_key_spread", "pact_set_wait_limits", "pact_cache_plan", "pact_cache_write", "pact_page_select",
-           "pact_paged_attention", "pact_paged_workspace_bytes"]
+           "pact_paged_attention", "pact_paged_workspace_bytes", "pact_chunk_attention", "pact_chunk_workspace_bytes"]
 
 
 class Params(C.Structure):
@@ -52,10 +52,11 @@ class PagedCacheDesc(C.Structure):
                 ("bounds", C.c_void_p), ("w_max", C.c_void_p), ("n_pages", C.c_int32), ("page_rows", C.c_int32)]
 
 
-# pact_plan, pact_new_rows and pact_query of pact.h: packed into a buffer of the context, a tenth of the time of as many ctypes arguments
+# pact_plan, pact_new_rows, pact_query and pact_chunk of pact.h: packed into a buffer of the context, a tenth of the time of as many ctypes arguments
 _PLAN = struct.Struct("@4iPPPqPPPPPPqiiP")
 _NEW_ROWS = struct.Struct("@PPqqPPqP")
 _QUERY = struct.Struct("@PqqPPiiPiiifPqqPPPN")
+_CHUNK = struct.Struct("@PqqPPPqPqiiiifiPqqPPPN")
 
 _lib = None
 
@@ -105,6 +106,9 @@ def lib():
         L.pact_paged_attention.argtypes = [vp, pc, vp, vp]
         L.pact_paged_workspace_bytes.argtypes = [vp, i32, i32]
         L.pact_paged_workspace_bytes.restype = sz
+        L.pact_chunk_attention.argtypes = [vp, pc, vp, vp]
+        L.pact_chunk_workspace_bytes.argtypes = [vp, i32]
+        L.pact_chunk_workspace_bytes.restype = sz
         for name in EXPORTS:
             if getattr(L, name).restype is C.c_int:
                 getattr(L, name).restype = C.c_int
@@ -282,6 +286,7 @@ class Context:
         self.device = torch.cuda.current_device()
         self._paged_ws = []                  # workspaces of the paged cache's calls: address, size, tensor; the last one is in use
         self._paged_need = {}
+        self._chunk_ws, self._chunk_need = [], {}   # the same of pact_chunk_attention
         self._make_args()
 
     def close(self):
@@ -391,7 +396,7 @@ class Context:
     # (A call of a decoding step takes the GPU a few microseconds, and looking at nine tensors one function call each takes as long: the methods test
     # everything in one expression and ask _explain only when it fails.)
     def _make_args(self):
-        self._args = C.create_string_buffer(max(_PLAN.size, _NEW_ROWS.size, _QUERY.size))
+        self._args = C.create_string_buffer(max(_PLAN.size, _NEW_ROWS.size, _QUERY.size, _CHUNK.size))
         self._args_at = C.addressof(self._args)
         self._kind = (self.n_kvh, self.d_h, self.in_dtype, self.device)
 
@@ -530,6 +535,49 @@ class Context:
                          0 if selected is None else selected.shape[2], 0, 0, d_h ** -0.5 if scale is None else scale, out.data_ptr(), o0, oh,
                          0 if lse is None else lse.data_ptr(), 0 if status is None else status.data_ptr(), w, n)
         r = self._L.pact_paged_attention(self.handle, cache.ref, self._args_at, _stream())
+        if r:
+            _check(self.handle, r)
+
+    # ---- several new tokens per request ---------------------------------------------------
+    def _chunk_workspace(self, B):
+        """Address and size; as with _paged_workspace one that is outgrown is kept.  (Parts of items take most of it, whatever B is.)"""
+        need = self._chunk_need.get(B)
+        if need is None:
+            need = self._chunk_need[B] = int(self._L.pact_chunk_workspace_bytes(self.handle, B))
+        have = self._chunk_ws[-1] if self._chunk_ws else None
+        if have is None or have[1] < need:
+            ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self._cuda())
+            self._chunk_ws.append((ws.data_ptr(), ws.numel(), ws))
+        return self._chunk_ws[-1]
+
+    def pact_chunk_attention(self, cache: PagedCache, Q, block_table, length, n_new, out, row_start=None, row_stride=0, lse=None, causal=True, scale=None,
+                             status=None):
+        """Attention of the new tokens of every request over its cached rows (pact_chunk_attention in pact.h): Q [n_rows, n_qh, d_h] -> out [n_rows, n_qh, d_h]
+        (the context's output type), lse [n_rows, n_qh] fp32.  block_table [B, max_pages], length, n_new [B] (n_new may be a strided view) int32; the rows are
+        packed (row_start [B] or [B + 1] int32) or row_stride per request; scale: 1 / sqrt(d_h) if not given."""
+        i32, dev, heads, d_h = torch.int32, self.device, self.n_qh, self.d_h
+        B, W = block_table.shape if block_table.ndim == 2 else (-1, None)
+        n = Q.shape[0]
+        shape = (n, heads, d_h)
+        q, o = Q.stride(), out.stride()
+        if not (cache.kind == self._kind and Q.shape == shape and Q.dtype is self.in_dtype and Q.get_device() == dev and (q[2] == 1 or d_h == 1)
+                and out.shape == shape and out.dtype is self.out_dtype and out.get_device() == dev and (o[2] == 1 or d_h == 1)
+                and block_table.dtype is i32 and block_table.get_device() == dev and block_table.is_contiguous()
+                and length.dtype is i32 and length.get_device() == dev and length.numel() == B and length.is_contiguous()
+                and n_new.dtype is i32 and n_new.get_device() == dev and n_new.numel() == B and n_new.ndim == 1
+                and (row_start is None or row_start.dtype is i32 and row_start.get_device() == dev and B <= row_start.numel() <= B + 1 and row_start.is_contiguous())
+                and (lse is None or lse.dtype is torch.float32 and lse.get_device() == dev and lse.numel() == n * heads and lse.is_contiguous())
+                and (status is None or status.dtype is i32 and status.get_device() == dev and status.numel() == 1)):
+            self._explain(cache, (block_table, i32, (None, None), False, "block_table"), (Q, self.in_dtype, (None, heads, d_h), True, "Q"),
+                          (out, self.out_dtype, shape, True, "out"), (length, i32, (B,), False, "length"), (n_new, i32, (B,), True, "n_new"),
+                          (row_start, i32, (None,), False, "row_start"), (lse, torch.float32, (n, heads), False, "lse"), (status, i32, (1,), False, "status"))
+        w, size, _ = self._chunk_workspace(B)
+        qh, oh = (q[1], o[1]) if heads > 1 else (d_h, d_h)
+        q0, o0 = (q[0], o[0]) if n > 1 else (qh * heads, oh * heads)
+        _CHUNK.pack_into(self._args, 0, Q.data_ptr(), q0, qh, block_table.data_ptr(), length.data_ptr(), n_new.data_ptr(), n_new.stride()[0] if B > 1 else 1,
+                         0 if row_start is None else row_start.data_ptr(), n, row_stride, B, W, 1 if causal else 0, d_h ** -0.5 if scale is None else scale, 0,
+                         out.data_ptr(), o0, oh, 0 if lse is None else lse.data_ptr(), 0 if status is None else status.data_ptr(), w, size)
+        r = self._L.pact_chunk_attention(self.handle, cache.ref, self._args_at, _stream())
         if r:
             _check(self.handle, r)
 

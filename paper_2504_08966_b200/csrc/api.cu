@@ -224,6 +224,7 @@ pact_status pact_create(pact_ctx **out, int d, int n_qh, int n_kvh, int d_h, pac
   }
   c->umma = in == PACT_BF16 && umma_supported(c->d_k);
   e = paged_configure(&c->paged, c->dev, n_qh, n_kvh, d_h, in == PACT_BF16);
+  if (e == cudaSuccess) e = chunk_configure(&c->chunk, c->dev, d_h, in == PACT_BF16, c->out == PACT_BF16);
   if (e != cudaSuccess) {
     fail_cuda(ctx, e, "pact_create");
     delete c;

@@ -1,0 +1,823 @@
+// Attention of several new tokens per request over a paged cache of bf16 rows (pact_chunk_attention): Eq. 11 of the paper for prompts and further turns.
+//
+//   s_ip = scale q_i.k_p + logw_p  (p up to the token's own row, or all),   out_i = sum_p exp(s_ip - m) v_p / sum_p exp(s_ip - m)
+//
+// Work.  The query heads of a key head read the same rows, so an item is 256 rows (token, head) of one key head: two blocks of 128, a tensor-memory lane
+// per row, against tiles of 128 cached rows that arrive once for both.  Per tile and SM 4 x 512 clocks of tcgen05 (128 x 128 x 128, logits and values, two
+// blocks), 2048 clocks of exponentials (16 a clock) and 64 KB from the L2: the three balance, and the two blocks take turns at the
+// first two.  Items of up to 128 rows (a few tokens: HBM bounds them) have one block; its even and odd tiles then take the place of the two blocks, each with a running
+// maximum and sums of its own.
+// Above 128 columns there is one block (tensor memory has room for one result), with tiles of 64.
+//
+// Warps: two groups of four have a row per lane (softmax, results), one copies pages through the tensor-copy unit, one issues the products, one looks
+// after the values: where a tile has rows that some token must not see, zero times an infinity or a NaN would not be zero, so rows that do not count are
+// cleared and other values that are not finite are replaced by zero; their columns and first rows are noted, and the tokens that see them get NaN at the end.
+// Logits lie in tensor memory, probabilities take their place there, and results stay in it until the end.  The maximum that logits are taken from lags behind
+// the true one by at most 2^8 of a probability, so that results are rescaled a few times per item only.
+//
+// Rounding: probabilities go into the products with bf16 values as one bf16 term where results are bf16: unbiased errors of 2^-8 at most in the weights, which together are no
+// larger than the one rounding of the result that follows.  For fp32 results as three terms, which hold all of fp32's 24 bits, and the products of two tiles at a
+// time are added with rounding, since the tensor cores cut their running sums off towards 0 (some 2^-25 at each of 16 rows).  Sums of probabilities are taken before the rounding.
+#include "chunk_row.cuh"
+
+namespace pact {
+namespace {
+
+constexpr int kSoftmaxWarps = 8;
+constexpr int kCopyWarp = 8, kMmaWarp = 9, kValueWarp = 10;
+constexpr int kChunkThreads = 12 * 32;      // (the last warp has no part: registers are shared out by fours of warps)
+// Registers of a thread: a row of logits and what is made of it take more than the 168 that 384 threads may have each, the other warps need fewer.
+constexpr int kRowRegs = 208, kOtherRegs = 88;
+static_assert(kSoftmaxWarps * 32 * kRowRegs + (kChunkThreads - kSoftmaxWarps * 32) * kOtherRegs <= kChunkThreads * 168, "what the CTA is launched with");
+constexpr float kLag = 8.f;                // of the reference behind the maximum, in powers of two
+constexpr size_t kChunkSmem = 227 * 1024;
+
+template <int NB, bool WIDE> struct ChunkShape {
+  static constexpr int kBlocks = NB <= 2 ? 2 : 1;                    // of 128 rows in an item
+  static constexpr int kRows = kBlocks * 128;
+  static constexpr int kTileRows = NB <= 2 && !WIDE ? 128 : 64;
+  static constexpr int kGroups = kTileRows / 16;
+  static constexpr int kQBytes = NB * 128 * 128;                     // of a block
+  static constexpr int kStage = NB * kTileRows * 128;                // K or V of a tile
+  static constexpr int kFit = (int)((kChunkSmem - kBlocks * kQBytes - 4096) / kStage);
+  static constexpr int kStages = NB == 2 && !WIDE ? 5 : kFit > 10 ? 10 : kFit;   // (five of 32 KB leave 3 KB for everything else)
+  static constexpr int kRing = kStages <= 5 ? 4 : 8;                 // biases of tiles: the copies run ahead by fewer
+  static constexpr int kTerms = WIDE ? 3 : 1;
+  static constexpr int kRegion = WIDE ? 96 : kTileRows;              // columns of tensor memory for logits, then probabilities
+  static constexpr int kO = kBlocks * kRegion;                       // first column of the results
+  static constexpr int kWidth = NB * 64;
+  static_assert(kO + kBlocks * kWidth <= 512 && 2 * kRing - 3 >= kStages, "");
+};
+
+template <int NB, bool WIDE> struct ChunkShared {
+  using C = ChunkShape<NB, WIDE>;
+  char q[C::kBlocks][C::kQBytes];
+  char stage[C::kStages][C::kStage];
+  float bias[C::kRing][C::kTileRows];
+  uint64_t full[C::kStages], empty[C::kStages];
+  uint64_t b_full[C::kRing], b_ready[C::kRing], clean[C::kRing];
+  uint64_t q_full[2], s_full[2], p_ready[2], o_full[2], drained;
+  int flags[C::kRing];                     // 1: biases count, 2: some are minus infinity
+  int poison[2 * C::kRing];                // a tile had values that are not finite beside rows that some token must not see
+  int abort, issued;
+  uint32_t tmem;
+  ChunkLineKept line;
+};
+
+__device__ __forceinline__ void chunk_load_4d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y, int z, int w) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+               ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void chunk_copy16(void *dst, const void *src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void chunk_arrive_after_copies(uint64_t *bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accum) {   // A from tensor memory
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accum) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// An operand whose rows are the summed index (values: columns contiguous): 128-byte blocks of columns `block` bytes apart, 8 rows 1024 bytes.
+__device__ __forceinline__ uint64_t smem_desc_rows(uint32_t addr, uint32_t block) {
+  return smem_desc(addr) & ~((uint64_t)0x3FFF << 16) | ((uint64_t)(block >> 4) << 16);
+}
+
+__device__ __forceinline__ unsigned long long pair_of(float x, float y) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void unpair(unsigned long long v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ unsigned long long of_pair(uint32_t x, uint32_t y) {   // the same of bits
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(x), "r"(y));
+  return r;
+}
+__device__ __forceinline__ void to_pair(uint32_t &x, uint32_t &y, unsigned long long v) { asm("mov.b64 {%0, %1}, %2;" : "=r"(x), "=r"(y) : "l"(v)); }
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+// The order in which the tiles of a segment of n are asked for: with one tile ahead K0 V0 K1 V1 .., with two K0 K1 V0 K2 V1 ..; load x of 2 n.
+struct LoadAt {
+  bool v;
+  int j;
+};
+__device__ __forceinline__ LoadAt chunk_load_at(int x, int n, int ahead) {
+  if (ahead == 1) return {(x & 1) != 0, x >> 1};
+  if (x == 2 * n - 1) return {true, n - 1};
+  if (x == 0 || (x & 1)) return {false, (x + 1) >> 1};
+  return {true, (x - 2) >> 1};
+}
+__device__ __forceinline__ int chunk_k_load(int j, int ahead) { return ahead == 1 ? 2 * j : j == 0 ? 0 : 2 * j - 1; }
+__device__ __forceinline__ int chunk_v_load(int j, int n, int ahead) { return ahead == 1 ? 2 * j + 1 : min(2 * j + 2, 2 * n - 1); }
+
+// A warp's bounded wait: false once kWaitNs or `polls` have run out, or another warp has given up.  Without a call: a kernel that moves registers from one group of
+// warps to another cannot have any there.
+__device__ __forceinline__ bool chunk_wait(int *abort, uint64_t *bar, uint32_t parity, int polls, int32_t *status) {
+  int ok = 1;
+  if ((threadIdx.x & 31) == 0) {
+    ok = polls == INT32_MAX ? mbar_try_wait(bar, parity) : mbar_test(bar, parity);
+    if (!ok) {
+      const unsigned long long t0 = global_ns();
+      for (int i = 1; i < polls && !*const_cast<volatile int *>(abort); ++i) {
+        if ((ok = mbar_try_wait(bar, parity)) || ((i & 63) == 63 && global_ns() - t0 > kWaitNs)) break;
+      }
+      if (!ok) {
+        atomicExch(abort, 1);
+        if (status) atomicMin(status, (int)PACT_ERR_TIMEOUT);
+      }
+    }
+  }
+  return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+
+template <int NB, bool WIDE>
+__global__ void __launch_bounds__(kChunkThreads, 1)
+    k_chunk(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ ChunkArgs a) {
+  using C = ChunkShape<NB, WIDE>;
+  constexpr int N = C::kTileRows, S = C::kStages, R = C::kRing;
+  extern __shared__ __align__(1024) char smem_raw[];
+  ChunkShared<NB, WIDE> &sh = *reinterpret_cast<ChunkShared<NB, WIDE> *>(smem_raw);
+  static_assert(sizeof(sh) <= kChunkSmem && sizeof(ChunkLineSetup) <= C::kStage, "");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid < S) {
+    mbar_init(sh.full + tid, 1);
+    mbar_init(sh.empty + tid, 1);
+  }
+  if (tid < R) {
+    mbar_init(sh.clean + tid, 1);
+    mbar_init(sh.b_full + tid, 33);
+    mbar_init(sh.b_ready + tid, 1);
+  }
+  if (tid < 2) {
+    mbar_init(sh.q_full + tid, 4);
+    mbar_init(sh.s_full + tid, 1);
+    mbar_init(sh.p_ready + tid, 4);
+    mbar_init(sh.o_full + tid, 1);
+  }
+  if (tid == 0) {
+    mbar_init(&sh.drained, 1);
+    sh.abort = sh.issued = 0;
+  }
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  if (warp == kMmaWarp) tmem_alloc(&sh.tmem, 512);
+  tc_fence_before();
+  pdl_wait();
+  pdl_trigger();
+  ChunkLine line = chunk_line<kChunkThreads>(a, C::kRows, N, sh.line, *reinterpret_cast<ChunkLineSetup *>(sh.stage[0]));
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // (the set-up's words lie where copies will land)
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem;
+  const auto wait = [&](uint64_t *bar, uint32_t parity) { return chunk_wait(&sh.abort, bar, parity & 1, a.polls, a.status); };
+  ChunkSegment s;
+  bool ok = true;
+
+  if (warp < kSoftmaxWarps) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRowRegs));
+    // ---- rows: softmax and results ----
+    const int t = warp >> 2, row = tid & 127;                        // of the block
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+    const uint32_t my_s = tmem + t * C::kRegion + lanes, my_o = tmem + C::kO + t * C::kWidth + lanes;
+    const int d16 = (a.d_h + 15) / 16 * 16;
+    float4 *flush = reinterpret_cast<float4 *>(a.flush) + ((long long)blockIdx.x * C::kBlocks + t) * (C::kWidth / 4) * 128 + row;
+    const float scale = a.scale;
+    const unsigned long long scale2 = pair_of(scale, scale), log2e2 = pair_of(kChunkLog2e, kChunkLog2e);
+    uint32_t s_phase = 0, o_phase = 0;
+    int tiles = 0, segment = 0;
+    while (line.next(a, C::kRows, N, s)) {
+      const int n = s.j1 - s.j0;
+      const bool split = C::kBlocks == 2 && s.rows <= 128;
+      const int my_first = split ? t : 0, step = split ? 2 : 1;
+      const bool active = t < C::kBlocks && my_first < n;
+      const int r = (split ? 0 : t * 128) + row;                     // of the item
+      const int at_row = s.first + r, token = at_row / a.group, head = s.kv * a.group + at_row - token * a.group;
+      const bool there = r < s.rows;
+      const int limit = there ? s.limit(token, a.causal) : 0;
+      if (t < C::kBlocks && (!split || t == 0) && ok) {
+        // this warp's 32 rows of Q, a row per half warp (or less), swizzled as the copies of K are
+        const long long my_at = (s.row0 + token) * a.ldQ + head * a.ldQh;
+        constexpr int kLanes = NB == 1 ? 8 : NB == 2 ? 16 : 32, kAtOnce = 32 / kLanes;
+        const int c = lane % kLanes;
+        char *to = sh.q[t] + c / 8 * (128 * 128);
+#pragma unroll 8
+        for (int i = 0; i < 32; i += kAtOnce) {
+          const int src = i + lane / kLanes;
+          const long long at = __shfl_sync(0xffffffffu, my_at, src);
+          const bool row_there = __shfl_sync(0xffffffffu, there ? 1 : 0, src) != 0;
+          const int rr = (warp & 3) * 32 + src;
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (row_there && c * 8 < a.d_h) v = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.Q) + at + c * 8));
+          if (c < NB * 8) *reinterpret_cast<uint4 *>(to + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sh.q_full + t);
+      }
+      float m = -INFINITY, l = 0.f, f_flush = 1.f;
+      bool poisoned = false, flushed = false;
+      if (active)
+        for (int j = my_first; j < n && ok; j += step) {
+          const int tile = tiles + j, at = tile % R, row0 = (s.j0 + j) * N, nth = split ? j >> 1 : j;
+          ok = wait(sh.s_full + t, s_phase++) && wait(sh.b_ready + at, tile / R);
+          if (!ok) break;
+          tc_fence_after();
+          const int flags = sh.flags[at];
+          if (nth > 0) poisoned = poisoned || sh.poison[(tile - step) % (2 * R)];   // (the products before this tile's are done)
+          uint32_t x[N / 32][32];                                    // logits; 32 registers each, as they are loaded
+#pragma unroll
+          for (int i = 0; i < N / 32; ++i) tmem_ld32(my_s + i * 32, x[i]);
+          tmem_ld_wait();
+          const int valid = min(max(limit - row0, 0), N);
+          const bool edge = __any_sync(0xffffffffu, valid < N) || (flags & 2);
+          const float4 *bias = reinterpret_cast<const float4 *>(sh.bias[at]);
+          float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c = 0; c < N / 32; ++c) {
+            if (!(flags & 1)) {
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) to_pair(x[c][i], x[c][i + 1], mul2(of_pair(x[c][i], x[c][i + 1]), scale2));
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                const float4 b = bias[c * 8 + i / 4];
+                to_pair(x[c][i], x[c][i + 1], fma2(of_pair(x[c][i], x[c][i + 1]), scale2, pair_of(b.x, b.y)));
+                to_pair(x[c][i + 2], x[c][i + 3], fma2(of_pair(x[c][i + 2], x[c][i + 3]), scale2, pair_of(b.z, b.w)));
+              }
+            }
+            if (edge) {
+              // rows that the token does not see; hidden ones by their bias, since their keys may be anything
+              constexpr uint32_t kNone = 0xFF800000u;                // minus infinity
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (flags & 2) b = bias[c * 8 + i / 4];
+                if (c * 32 + i >= valid || b.x == -INFINITY) x[c][i] = kNone;
+                if (c * 32 + i + 1 >= valid || b.y == -INFINITY) x[c][i + 1] = kNone;
+                if (c * 32 + i + 2 >= valid || b.z == -INFINITY) x[c][i + 2] = kNone;
+                if (c * 32 + i + 3 >= valid || b.w == -INFINITY) x[c][i + 3] = kNone;
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 32; i += 8)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) tops[k] = max3(tops[k], __uint_as_float(x[c][i + 2 * k]), __uint_as_float(x[c][i + 2 * k + 1]));
+          }
+          const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+          if (WIDE && nth > 0 && nth % 2 == 0) {                     // the results of two tiles, added with rounding
+#pragma unroll 1
+            for (int c0 = 0; c0 < d16; c0 += 32) {
+              uint32_t v[32];
+              tmem_ld32(my_o + c0, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; i += 4)
+                if (c0 + i < d16) {
+                  float4 y = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+                  float4 *p = flush + (c0 + i) / 4 * 128;
+                  if (flushed) {
+                    const float4 z = *p;
+                    y = make_float4(fmaf(z.x, f_flush, y.x), fmaf(z.y, f_flush, y.y), fmaf(z.z, f_flush, y.z), fmaf(z.w, f_flush, y.w));
+                  }
+                  *p = y;
+                }
+            }
+            flushed = true;
+            f_flush = 1.f;
+          }
+          if (nth == 0) {
+            m = top;
+          } else if (__any_sync(0xffffffffu, top > m && (m == -INFINITY || (top - m) * kChunkLog2e > kLag))) {
+            const float to = fmaxf(m, top), f = part_weight(m, to);
+            m = to;
+            l *= f;
+            f_flush *= f;
+            if (!WIDE || nth % 2 != 0) {
+#pragma unroll 1
+              for (int c0 = 0; c0 < d16; c0 += 32) {
+                uint32_t v[32];
+                tmem_ld32(my_o + c0, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+                tmem_st32(my_o + c0, v);
+              }
+            }
+          }
+          const float ref = m == -INFINITY ? 0.f : m;
+          const unsigned long long ref2 = pair_of(-ref, -ref);
+          unsigned long long sums[4] = {0ull, 0ull, 0ull, 0ull};
+          if constexpr (!WIDE) {
+#pragma unroll
+            for (int c = 0; c < N / 32; ++c) {
+              uint32_t p[16];
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) {
+                float u, w;
+                unpair(mul2(add2(of_pair(x[c][i], x[c][i + 1]), ref2), log2e2), u, w);
+                u = ex2_approx(u);
+                w = ex2_approx(w);
+                sums[i / 2 % 4] = add2(sums[i / 2 % 4], pair_of(u, w));
+                p[i / 2] = bf16_pair(u, w);
+              }
+              tmem_st16(my_s + c * 16, p);
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < N / 32; ++c) {
+              uint32_t p[3][16];
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) {
+                float u, w;
+                unpair(mul2(add2(of_pair(x[c][i], x[c][i + 1]), ref2), log2e2), u, w);
+                u = ex2_approx(u);
+                w = ex2_approx(w);
+                sums[i / 2 % 4] = add2(sums[i / 2 % 4], pair_of(u, w));
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                  const uint32_t h = bf16_pair(u, w);
+                  p[k][i / 2] = h;
+                  u -= __uint_as_float(h << 16);                     // (exact)
+                  w -= __uint_as_float(h & 0xFFFF0000u);
+                }
+              }
+#pragma unroll
+              for (int k = 0; k < 3; ++k) tmem_st16(my_s + k * (N / 2) + c * 16, p[k]);
+            }
+          }
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(sh.p_ready + t);
+          float u[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) unpair(sums[k], u[2 * k], u[2 * k + 1]);
+          l += ((u[0] + u[1]) + (u[2] + u[3])) + ((u[4] + u[5]) + (u[6] + u[7]));
+        }
+      // ---- results ----
+      if (active && ok) {
+        ok = wait(sh.o_full + t, o_phase++);
+        tc_fence_after();
+        const int last = my_first + (n - 1 - my_first) / step * step;
+        poisoned = poisoned || sh.poison[(tiles + last) % (2 * R)];
+      }
+      const int *poison = a.poison + ((long long)blockIdx.x * kChunkPoison + segment % kChunkPoison) * kChunkMaxWidth;
+      // columns c0 .. c0 + 31 of this row's results, all tiles so far
+      const auto results = [&](uint32_t from, const float4 *kept, bool has_kept, float f_kept, int c0, float (&o)[32]) {
+        uint32_t v[32];
+        tmem_ld32(from + c0, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(v[i]);
+        if (WIDE && has_kept) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)
+            if (c0 + i < d16) {
+              const float4 z = kept[(c0 + i) / 4 * 128];
+              o[i] = fmaf(z.x, f_kept, o[i]);
+              o[i + 1] = fmaf(z.y, f_kept, o[i + 1]);
+              o[i + 2] = fmaf(z.z, f_kept, o[i + 2]);
+              o[i + 3] = fmaf(z.w, f_kept, o[i + 3]);
+            }
+        }
+      };
+      float f_flush1 = 1.f;
+      bool flushed1 = false;
+      float m1 = -INFINITY, l1 = 0.f, f0 = 1.f, f1 = 0.f;
+      if (split) {
+        // The odd tiles' results lie in the same lanes of tensor memory: the first group reads them there, with the reference and sum that the second leaves.
+        if (t == 1 && ok) {
+          const uint32_t v[16] = {__float_as_uint(m), __float_as_uint(l), __float_as_uint(f_flush), (flushed ? 1u : 0u) | (poisoned ? 2u : 0u)};
+          tmem_st16(my_s, v);
+          tmem_st_wait();
+          tc_fence_before();
+        }
+        asm volatile("bar.sync 1, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
+        if (t == 0 && ok) {
+          tc_fence_after();
+          uint32_t v[32];
+          tmem_ld32(my_s + C::kRegion, v);
+          tmem_ld_wait();
+          m1 = __uint_as_float(v[0]);
+          l1 = __uint_as_float(v[1]);
+          const float to = fmaxf(m, m1);
+          f0 = part_weight(m, to);
+          f1 = part_weight(m1, to);
+          f_flush1 = __uint_as_float(v[2]);
+          flushed1 = v[3] & 1u;
+          poisoned = poisoned || (v[3] & 2u);
+          m = to;
+          l = l * f0 + l1 * f1;
+        }
+      }
+      if (active && ok && (!split || t == 0)) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const long long out_at = (s.row0 + token) * a.ldO + head * a.ldOh;
+#pragma unroll 1
+        for (int c0 = 0; c0 < d16; c0 += 32) {
+          float o[32];
+          results(my_o, flush, flushed, f_flush, c0, o);
+          if (split && __any_sync(0xffffffffu, l1 != 0.f)) {
+            float o1[32];
+            results(my_o + C::kWidth, flush + (C::kWidth / 4) * 128, flushed1, f_flush1, c0, o1);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = l1 != 0.f ? o[i] * f0 + o1[i] * f1 : o[i] * f0;
+          }
+          if (poisoned) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (c0 + i < a.d_h && __ldcg(poison + c0 + i) < limit) o[i] = __int_as_float(0x7fffffff);
+          }
+          if (there && s.slot >= 0) {
+            float4 *p = reinterpret_cast<float4 *>(a.part_o) + ((long long)s.slot * (C::kWidth / 4) + c0 / 4) * C::kRows + r;
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+              if (c0 + i < d16) p[i / 4 * C::kRows] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+          } else if (there) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] *= inv;
+#pragma unroll
+            for (int i = 0; i < 32; i += 8)
+              if (c0 + i < a.d_h) store8(a, out_at + c0 + i, o + i);
+          }
+          __syncwarp();
+        }
+        if (there) {
+          if (s.slot >= 0) a.part_ml[(long long)s.slot * C::kRows + r] = make_float2(m, l);
+          else if (a.lse) a.lse[(s.row0 + token) * (a.n_kvh * a.group) + head] = l == 0.f ? -INFINITY : m + logf(l);
+        }
+      }
+      tc_fence_before();
+      tiles += n;
+      ++segment;
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == kCopyWarp) {
+      // ---- pages ----
+      constexpr int kAtOnce = 32 / C::kGroups;                         // tiles whose pages the lanes hold: 16 rows each
+      const int per_box = a.box_rows / 16, boxes = N / a.box_rows, my_box = lane / NB, my_nb = lane % NB;
+      struct {
+        int at, id, off;
+        uint32_t bad;
+      } win[2] = {{-1, -1, 0, 0u}, {-1, -1, 0, 0u}};                   // of K and of V
+      int loads = 0, tiles = 0;
+      while (ok && line.next(a, C::kRows, N, s)) {
+        const int n = s.j1 - s.j0, ahead = C::kBlocks == 2 && s.rows <= 128 ? 2 : 1;
+        win[0].at = win[1].at = -1;
+        for (int x = 0; x < 2 * n; ++x, ++loads) {
+          const LoadAt l = chunk_load_at(x, n, ahead);
+          const int j = s.j0 + l.j, w = j / kAtOnce, in = j % kAtOnce;
+          auto &pages = win[l.v];
+          if (pages.at != w) {                                         // page and place of 16 rows per lane
+            const long long pos = ((long long)w * 32 + lane) * 16;
+            pages.at = w;
+            pages.id = -1;
+            bool bad = false;
+            if (pos < s.len) {
+              const int place = (int)pos / a.page;
+              pages.off = (int)pos - place * a.page;
+              pages.id = a.table[(long long)s.b * a.width + place];
+              bad = pages.id < 0 || pages.id >= a.n_pages;
+              if (bad) {
+                pages.id = -1;
+                if (a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
+              }
+            }
+            pages.bad = __ballot_sync(0xffffffffu, bad);
+          }
+          const int from = in * C::kGroups + my_box * per_box;
+          const int id = __shfl_sync(0xffffffffu, pages.id, from & 31), off = __shfl_sync(0xffffffffu, pages.off, from & 31);
+          const bool mine = my_box < boxes && id >= 0;
+          const uint32_t n_boxes = __popc(__ballot_sync(0xffffffffu, mine));
+          const int st = loads % S;
+          ok = wait(sh.empty + st, loads / S + 1);
+          if (!ok) break;
+          if (lane == 0) mbar_arrive_expect_tx(sh.full + st, n_boxes * a.box_rows * 128);
+          __syncwarp();
+          if (mine)
+            chunk_load_4d(sh.stage[st] + (my_nb * N + my_box * a.box_rows) * 128, l.v ? &map_v : &map_k, sh.full + st, my_nb * 64, off, s.kv, id);
+          if (!l.v) {                                                  // the biases come with the keys
+            const int at = (tiles + l.j) % R;
+            const bool counts = a.logw || (pages.bad >> (in * C::kGroups) & ((1u << C::kGroups) - 1u));
+            const int g = in * C::kGroups + lane / 4, bid = __shfl_sync(0xffffffffu, pages.id, g & 31), boff = __shfl_sync(0xffffffffu, pages.off, g & 31);
+            if (counts && lane < N / 4) {
+              float *to = sh.bias[at] + lane * 4;
+              if (bid < 0) *reinterpret_cast<float4 *>(to) = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+              else if (a.logw) chunk_copy16(to, a.logw + (long long)bid * a.page + boff + (lane & 3) * 4);
+              else *reinterpret_cast<float4 *>(to) = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            chunk_arrive_after_copies(sh.b_full + at);
+            if (lane == 0) sh.flags[at] = counts;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sh.b_full + at);
+          }
+        }
+        tiles += n;
+      }
+      if (lane == 0) sh.issued = loads;
+    } else if (warp == kMmaWarp) {
+      // ---- products ----
+      const int d16 = (a.d_h + 15) / 16 * 16, steps = d16 / 16;
+      constexpr uint32_t kTypes = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);
+      constexpr uint32_t kLogits = kTypes | ((uint32_t)(N >> 3) << 17);
+      const uint32_t values = kTypes | (1u << 16) | ((uint32_t)(d16 >> 3) << 17);
+      int loads = 0, tiles = 0;
+      uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+      const auto logits = [&](int t, int q, int st) {
+        if (lane == 0) {
+          const uint64_t da = smem_desc(smem_u32(sh.q[q])), db = smem_desc(smem_u32(sh.stage[st]));
+          for (int k = 0; k < steps; ++k)
+            umma_bf16(tmem + t * C::kRegion, desc_at(da, k / 4 * (128 * 128) + k % 4 * 32), desc_at(db, k / 4 * (N * 128) + k % 4 * 32), kLogits, k != 0);
+          umma_commit(sh.s_full + t);
+        }
+        __syncwarp();
+      };
+      const auto add_values = [&](int t, int st, bool accumulate) {
+        if (lane == 0) {
+          const uint64_t db = smem_desc_rows(smem_u32(sh.stage[st]), N * 128);
+  #pragma unroll
+          for (int term = C::kTerms - 1; term >= 0; --term)            // the small terms first
+  #pragma unroll
+            for (int k = 0; k < N / 16; ++k)
+              umma_bf16_ta(tmem + C::kO + t * C::kWidth, tmem + t * C::kRegion + term * (N / 2) + k * 8, desc_at(db, k * 2048), values, accumulate || k != 0 || term != C::kTerms - 1);
+        }
+        __syncwarp();
+      };
+      const auto commit = [&](uint64_t *bar) {
+        if (lane == 0) umma_commit(bar);
+        __syncwarp();
+      };
+      while (ok && line.next(a, C::kRows, N, s)) {
+        const int n = s.j1 - s.j0;
+        const bool split = C::kBlocks == 2 && s.rows <= 128;           // even and odd tiles
+        const int blocks = split ? 1 : C::kBlocks, ahead = split ? 2 : 1;
+        const auto stage_of = [&](int x) { return (loads + x) % S; };
+        const auto phase_of = [&](int x) { return (uint32_t)((loads + x) / S); };
+        for (int t = 0; t < blocks && ok; ++t) ok = wait(sh.q_full + t, q_phase[t]++);
+        for (int j = 0; j < min(ahead, n) && ok; ++j) {
+          const int x = chunk_k_load(j, ahead), st = stage_of(x);
+          ok = wait(sh.full + st, phase_of(x));
+          if (!ok) break;
+          tc_fence_after();
+          if (split) logits(j, 0, st);
+          else
+            for (int t = 0; t < blocks; ++t) logits(t, t, st);
+          commit(sh.empty + st);
+        }
+        for (int j = 0; j < n && ok; ++j) {
+          const int xv = chunk_v_load(j, n, ahead), sv = stage_of(xv), xk = chunk_k_load(j + ahead, ahead), sk = stage_of(xk);
+          const bool more = j + ahead < n;
+          ok = wait(sh.full + sv, phase_of(xv)) && wait(sh.clean + (tiles + j) % R, (tiles + j) / R) && (!more || wait(sh.full + sk, phase_of(xk)));
+          for (int i = 0; i < blocks && ok; ++i) {
+            const int t = split ? j & 1 : i, nth = split ? j >> 1 : j;
+            ok = wait(sh.p_ready + t, p_phase[t]++);
+            if (!ok) break;
+            tc_fence_after();
+            add_values(t, sv, WIDE ? (nth & 1) != 0 : nth > 0);
+            if (more) logits(t, split ? 0 : t, sk);
+            else commit(sh.o_full + t);
+          }
+          if (!ok) break;
+          commit(sh.empty + sv);
+          if (more) commit(sh.empty + sk);
+        }
+        loads += 2 * n;
+        tiles += n;
+      }
+      commit(&sh.drained);
+    } else if (warp == kValueWarp) {
+      // ---- values beside rows that must not be seen ----
+      int loads = 0, tiles = 0, segment = 0;
+      while (ok && line.next(a, C::kRows, N, s)) {
+        const int n = s.j1 - s.j0, ahead = C::kBlocks == 2 && s.rows <= 128 ? 2 : 1;
+        const int seen = s.limit(s.first / a.group, a.causal);         // by all tokens of the item
+        int *poison = a.poison + ((long long)blockIdx.x * kChunkPoison + segment % kChunkPoison) * kChunkMaxWidth;
+        bool poisoned = false;
+        for (int j = 0; j < n; ++j) {
+          const int tile = tiles + j, at = tile % R, row0 = (s.j0 + j) * N;
+          ok = wait(sh.b_full + at, tile / R);
+          if (!ok) break;
+          const bool counts = sh.flags[at] & 1;
+          float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (counts && lane < N / 4) b = *reinterpret_cast<const float4 *>(sh.bias[at] + lane * 4);
+          const float bs[4] = {b.x, b.y, b.z, b.w};
+          const int left = s.len - row0 - lane * 4;
+          uint32_t live[4];                                            // bit l of live[i]: row 4 l + i
+          bool hidden = false;
+  #pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            hidden = hidden || bs[i] == -INFINITY;
+            live[i] = __ballot_sync(0xffffffffu, i < left && bs[i] != -INFINITY);
+          }
+          hidden = __any_sync(0xffffffffu, hidden);
+          __syncwarp();
+          if (lane == 0) {
+            sh.flags[at] = (counts ? 1 : 0) | (hidden ? 2 : 0);
+            mbar_arrive(sh.b_ready + at);
+          }
+          const int x = loads + chunk_v_load(j, n, ahead), st = x % S;
+          ok = wait(sh.full + st, x / S);
+          if (!ok) break;
+          bool found = false;
+          if (hidden || row0 + N > seen) {
+            const int c = lane & 7;
+            for (int nb = 0; nb < NB; ++nb)
+  #pragma unroll 8
+              for (int r0 = 0; r0 < N; r0 += 4) {
+                const int r = r0 + (lane >> 3);
+                uint4 *p = reinterpret_cast<uint4 *>(sh.stage[st] + (nb * N + r) * 128 + c * 16);
+                const uint32_t mine = (r & 2) ? ((r & 1) ? live[3] : live[2]) : ((r & 1) ? live[1] : live[0]);
+                if (mine >> (r >> 2) & 1u) {
+                  const uint4 v = *p;
+                  const uint32_t m = 0x7FFF7FFFu;
+                  const uint32_t top = __vmaxu2(__vmaxu2(v.x & m, v.y & m), __vmaxu2(v.z & m, v.w & m));
+                  found = found || (top & 0xFFFFu) >= 0x7F80u || (top >> 16) >= 0x7F80u;
+                } else {
+                  *p = make_uint4(0, 0, 0, 0);
+                }
+              }
+            __syncwarp();
+            found = __any_sync(0xffffffffu, found);
+            if (found) {                                               // (rare)
+              if (!poisoned)
+                for (int i = lane; i < kChunkMaxWidth; i += 32) poison[i] = INT32_MAX;
+              poisoned = true;
+              __syncwarp();
+              for (int nb = 0; nb < NB; ++nb)
+                for (int r0 = 0; r0 < N; r0 += 4) {
+                  const int r = r0 + (lane >> 3);
+                  __nv_bfloat16 *p = reinterpret_cast<__nv_bfloat16 *>(sh.stage[st] + (nb * N + r) * 128 + c * 16);
+                  for (int e = 0; e < 8; ++e) {
+                    const uint16_t bits = *reinterpret_cast<const uint16_t *>(p + e);
+                    if ((bits & 0x7FFFu) >= 0x7F80u) {
+                      *reinterpret_cast<uint16_t *>(p + e) = 0;
+                      atomicMin(poison + nb * 64 + (c ^ (r & 7)) * 8 + e, row0 + r);
+                    }
+                  }
+                }
+              __threadfence();
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          }
+          if (lane == 0) sh.poison[tile % (2 * R)] = found;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(sh.clean + at);
+        }
+        loads += 2 * n;
+        tiles += n;
+        ++segment;
+      }
+    }
+  }
+  if (warp == kCopyWarp) asm volatile("cp.async.wait_all;" ::: "memory");
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) mbar_wait_slow(&sh.drained, 0);
+  if (sh.abort && tid < min(S, sh.issued)) mbar_wait_slow(sh.full + tid, (sh.issued - 1 - tid) / S & 1);   // copies under way still write to this CTA's shared memory
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+}
+
+// ---- host side -----------------------------------------------------------------------------------
+
+typedef CUresult (*ChunkEncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// Pages as [page][head][row][column], boxes of box_rows rows and 128 bytes (zeros past d_h).
+bool encode_chunk_pages(const ChunkCfg &cfg, CUtensorMap *map, void *base, const ChunkArgs &a, long long ld_page, long long ld_head, long long ld_row) {
+  const cuuint64_t dims[4] = {(cuuint64_t)a.d_h, (cuuint64_t)a.page, (cuuint64_t)a.n_kvh, (cuuint64_t)a.n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)ld_row * 2, (cuuint64_t)ld_head * 2, (cuuint64_t)ld_page * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)a.box_rows, 1, 1}, estr[4] = {1, 1, 1, 1};
+  return reinterpret_cast<ChunkEncodeFn>(cfg.encode_tiled)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+using ChunkKernel = void (*)(CUtensorMap, CUtensorMap, ChunkArgs);
+struct ChunkForm {
+  ChunkKernel kernel;
+  int rows, tile, smem;
+};
+template <int NB, bool WIDE> ChunkForm form() {
+  return {k_chunk<NB, WIDE>, ChunkShape<NB, WIDE>::kRows, ChunkShape<NB, WIDE>::kTileRows, (int)sizeof(ChunkShared<NB, WIDE>)};
+}
+ChunkForm form_of(const ChunkCfg &cfg) {
+  switch (cfg.blocks) {
+    case 1: return cfg.wide ? form<1, true>() : form<1, false>();
+    case 2: return cfg.wide ? form<2, true>() : form<2, false>();
+    case 3: return cfg.wide ? form<3, true>() : form<3, false>();
+    case 4: return cfg.wide ? form<4, true>() : form<4, false>();
+  }
+  return {nullptr, 0, 0, 0};
+}
+
+size_t round256(size_t x) { return (x + 255) / 256 * 256; }
+
+}  // namespace
+
+cudaError_t chunk_configure(ChunkCfg *cfg, const DeviceCfg &dev, int d_h, bool bf16, bool out_bf16) {
+  const int blocks = (d_h * (bf16 ? 2 : 4) + 127) / 128;
+  if (blocks > 4 || dev.sm_count > kChunkMaxSms) return cudaSuccess;
+  cfg->bf16 = bf16;
+  cfg->blocks = blocks;
+  cfg->ctas = dev.sm_count;
+  if (!bf16) {
+    const ChunkFormF32 f = chunk_form_f32();
+    cfg->rows = f.rows;
+    cfg->tile = f.tile;
+    cfg->width = f.width;
+    return chunk_configure_f32(*cfg, d_h);
+  }
+  void *fn = nullptr;
+  cudaDriverEntryPointQueryResult qres;
+  cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+  if (e != cudaSuccess) return e;
+  if (qres != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
+  cfg->encode_tiled = fn;
+  cfg->wide = !out_bf16;
+  const ChunkForm f = form_of(*cfg);
+  cfg->rows = f.rows;
+  cfg->tile = f.tile;
+  cfg->width = blocks * 64;
+  return cudaFuncSetAttribute(f.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, f.smem);
+}
+
+size_t chunk_scratch(const ChunkCfg &cfg, int requests, ChunkArgs *a, char *base) {
+  if (!cfg.blocks) return 0;
+  const size_t G = cfg.ctas, parts = 4 * G * cfg.rows;
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    char *p = base + at;
+    at += round256(bytes);
+    return p;
+  };
+  char *o = take(parts * cfg.width * sizeof(float)), *ml = take(parts * sizeof(float2)), *flush = take(cfg.wide ? G * cfg.rows * cfg.width * sizeof(float) : 0),
+       *cut = take(2 * G * sizeof(ChunkCut)), *tail = take(G * sizeof(int)), *head = take(G * G * sizeof(int)),
+       *pre = take(requests < kChunkPreInSmem ? 0 : G * ((size_t)requests + 1) * sizeof(int)), *poison = take(G * kChunkPoison * kChunkMaxWidth * sizeof(int));
+  if (a) {
+    a->part_o = reinterpret_cast<float *>(o);
+    a->part_ml = reinterpret_cast<float2 *>(ml);
+    a->flush = reinterpret_cast<float *>(flush);
+    a->cut = reinterpret_cast<ChunkCut *>(cut);
+    a->tail = reinterpret_cast<int *>(tail);
+    a->head = reinterpret_cast<int *>(head);
+    a->pre = reinterpret_cast<int *>(pre);
+    a->poison = reinterpret_cast<int *>(poison);
+  }
+  return at;
+}
+
+cudaError_t launch_chunk(ChunkArgs a, const pact_paged_cache &cache, const ChunkCfg &cfg, cudaStream_t st, int *launches) {
+  *launches = 2;
+  if (!cfg.bf16) {
+    const cudaError_t e = launch_chunk_f32(a, cache, cfg, st);
+    return e != cudaSuccess ? e : launch_chunk_join(a, cfg, st);
+  }
+  a.box_rows = 16;
+  while (a.box_rows < cfg.tile && a.page % (2 * a.box_rows) == 0) a.box_rows *= 2;
+  CUtensorMap mk, mv;
+  if (!encode_chunk_pages(cfg, &mk, cache.K, a, cache.k_page, cache.k_head, cache.k_row) ||
+      !encode_chunk_pages(cfg, &mv, cache.V, a, cache.v_page, cache.v_head, cache.v_row))
+    return cudaErrorInvalidValue;
+  const ChunkForm f = form_of(cfg);
+  const cudaError_t e = launch_k(f.kernel, dim3((unsigned)cfg.ctas), dim3(kChunkThreads), (size_t)f.smem, st, true, mk, mv, a);
+  if (e != cudaSuccess) return e;
+  return launch_chunk_join(a, cfg, st);
+}
+
+}  // namespace pact

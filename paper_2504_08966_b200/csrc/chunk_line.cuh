@@ -1,0 +1,265 @@
+// The shares of the attention of several new tokens per request: every CTA works out, from lengths that are known on the device only, which items and
+// which of their tiles are its own.
+//
+// Items lie in a line: request, key head, place.  As long as there are two for every CTA, CTA c takes items c, c + G, .. as a whole: CTAs that run side by side
+// then read the same keys and values at about the same time.  The last G to 2 G items even out what the CTAs have: CTA c takes the beginning
+// of the c-th of them, as many tiles as it may still have, and what is left of them all is a line of tiles that the CTAs with room share.  A CTA that shares a
+// head with others so begins at its first rows, as they do.  The join puts together what was cut.
+#pragma once
+#include "chunk.cuh"
+#include "chunk_tiles.h"
+
+namespace pact {
+
+struct ChunkRequest : ChunkLengths {
+  long long row0;                          // its first row of Q and out
+  bool bad;
+};
+__device__ __forceinline__ ChunkRequest chunk_request(const ChunkArgs &a, int b) {
+  ChunkRequest q;
+  const long long room = (long long)a.width * a.page;
+  const int len = a.length[b], want = a.n_new[b * a.n_new_stride];
+  q.len = len < 0 ? 0 : len > room ? (int)room : len;
+  q.want = max(0, want);
+  long long have = a.row_stride;
+  q.row0 = b * (long long)a.row_stride;
+  if (!a.row_stride) {
+    q.row0 = a.row_start[b];
+    have = q.row0 < 0 || q.row0 > a.n_rows ? 0 : a.n_rows - q.row0;
+  }
+  q.n = (int)min((long long)q.want, have);
+  q.bad = q.len != len || q.n != q.want || q.want > q.len;
+  return q;
+}
+
+// Tiles [j0, j1) of an item of k tiles.
+struct ChunkSegment : ChunkRequest {
+  int b, kv, rows, first;                  // rows of the item, its first row among the request's (token row / group, head row % group)
+  int k, j0, j1;
+  int slot;                                // of its part, -1: the whole item
+  __device__ __forceinline__ int limit(int token, bool causal) const { return causal ? min(len, len - want + token + 1) : len; }   // rows that a token sees
+};
+
+struct ChunkLine {
+  const int *pre, *head;
+  int rounds, last, r;                     // rounds of whole items, the first item after them, how many there are
+  int q, off, tail;                        // where this CTA's part of the rests begins, and its tiles
+  // walking through the segments
+  int done, stage;
+  __device__ __forceinline__ void item(const ChunkArgs &a, int x, int rows, int tile, ChunkSegment &s) const {
+    int lo = 0, hi = a.B;
+    const int H = a.n_kvh;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (pre[mid] * H <= x) lo = mid;
+      else hi = mid;
+    }
+    static_cast<ChunkRequest &>(s) = chunk_request(a, lo);
+    const int n = pre[lo + 1] - pre[lo], at = x - pre[lo] * H;
+    s.b = lo;
+    s.kv = at / n;
+    const int i = at - s.kv * n;
+    s.first = i * rows;
+    s.rows = min(rows, s.n * a.group - s.first);
+    s.k = chunk_tiles(s, i, a.group, rows, tile, a.causal);
+  }
+  __device__ __forceinline__ bool next(const ChunkArgs &a, int rows, int tile, ChunkSegment &s) {
+    const int G = gridDim.x, me = blockIdx.x;
+    if (done < rounds) {
+      item(a, me + done++ * G, rows, tile, s);
+      s.j0 = 0;
+      s.j1 = s.k;
+      s.slot = -1;
+      return true;
+    }
+    if (stage == 0) {
+      stage = 1;
+      if (me < r && head[me] > 0) {
+        item(a, last + me, rows, tile, s);
+        s.j0 = 0;
+        s.j1 = head[me];
+        s.slot = s.j1 == s.k ? -1 : me;
+        return true;
+      }
+    }
+    while (tail > 0) {
+      item(a, last + q, rows, tile, s);
+      s.j0 = (q < G ? head[q] : 0) + off;
+      s.j1 = min(s.k, s.j0 + tail);
+      s.slot = s.j0 == 0 && s.j1 == s.k ? -1 : G + q + me;
+      ++q;
+      off = 0;
+      if (s.j1 <= s.j0) continue;
+      tail -= s.j1 - s.j0;
+      return true;
+    }
+    return false;
+  }
+};
+
+constexpr int kChunkPreInSmem = 128;       // entries of `pre` that are kept in shared memory
+
+// Shared memory of the set-up: kept (`pre`, where the rests begin) and passing (for the set-up alone).
+struct ChunkLineKept {
+  int pre[kChunkPreInSmem];
+  int q, off;
+};
+struct ChunkLineSetup {
+  unsigned long long tiles;
+  int warp[32];
+  int dp[kChunkMaxSms];                    // tiles of the whole items of each CTA
+  int lp[2 * kChunkMaxSms + 1];            // rests before each item of the last round
+  int tp[kChunkMaxSms + 1];                // tiles that the CTAs before have room for
+};
+
+// Exclusive sums of a value per thread; ends with a barrier.
+template <int THREADS> __device__ __forceinline__ int chunk_scan(int v, int *warp_sums, int *total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 31) warp_sums[warp] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int w = 0; w < THREADS / 32; ++w) {
+    if (w < warp) before += warp_sums[w];
+    all += warp_sums[w];
+  }
+  *total = all;
+  return before + x - v;
+}
+
+// Called by all threads of the CTA, at least as many as the grid has CTAs.
+template <int THREADS> __device__ __forceinline__ ChunkLine chunk_line(const ChunkArgs &a, int rows, int tile, ChunkLineKept &kept, ChunkLineSetup &set) {
+  static_assert(THREADS >= kChunkMaxSms, "");
+  constexpr int PER = (2 * kChunkMaxSms + THREADS - 1) / THREADS;    // items of the last round that a thread looks at
+  const int tid = threadIdx.x, G = gridDim.x, me = blockIdx.x;
+  int *pre = a.B < kChunkPreInSmem ? kept.pre : a.pre + (long long)me * (a.B + 1), *head = a.head + me * G;
+  ChunkLine line;
+  line.pre = pre;
+  line.head = head;
+  line.done = line.stage = 0;
+  if (tid == 0) {
+    set.tiles = 0;
+    kept.q = kept.off = 0;
+  }
+  __syncthreads();
+  {
+    const int per = (a.B + THREADS - 1) / THREADS, b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
+    int mine = 0, total;
+    unsigned long long tiles = 0;
+    for (int b = b0; b < b1; ++b) {
+      const ChunkRequest q = chunk_request(a, b);
+      if (q.bad && me == 0 && a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
+      pre[b] = mine;
+      mine += chunk_items(q, a.group, rows);
+      tiles += chunk_tiles_of_head(q, a.group, rows, tile, a.causal);
+    }
+    if (tiles) atomicAdd(&set.tiles, tiles);
+    const int before = chunk_scan<THREADS>(mine, set.warp, &total);
+    for (int b = b0; b < b1; ++b) pre[b] += before;
+    if (tid == 0) pre[a.B] = total;
+  }
+  __syncthreads();
+  const int items = pre[a.B] * a.n_kvh;
+  const long long T = (long long)set.tiles * a.n_kvh;
+  line.rounds = items >= 2 * G ? items / G - 1 : 0;
+  line.last = line.rounds * G;
+  line.r = items - line.last;
+  ChunkSegment s;
+  if (tid < G) {
+    int mine = 0;
+    for (int w = 0; w < line.rounds; ++w) {
+      line.item(a, tid + w * G, rows, tile, s);
+      mine += s.k;
+    }
+    set.dp[tid] = mine;
+  }
+  __syncthreads();
+  // tiles that a CTA may have: those with more already are left out of the mean
+  int most = (int)((T + G - 1) / G);
+  if (line.rounds > 0)
+    for (int round = 0; round < 4; ++round) {
+      long long over = 0;
+      int n = 0;
+      for (int c = 0; c < G; ++c)
+        if (set.dp[c] > most) {
+          over += set.dp[c];
+          ++n;
+        }
+      if (n == 0 || n == G) break;
+      most = (int)((T - over + G - n - 1) / (G - n));
+    }
+  int begins[PER], rest[PER], room[PER], sum_rest = 0, sum_room = 0, all, rests;
+  for (int k = 0; k < PER; ++k) {
+    const int q = tid * PER + k;
+    begins[k] = rest[k] = room[k] = 0;
+    if (q < G) room[k] = max(0, most - set.dp[q]);
+    if (q < line.r) {
+      line.item(a, line.last + q, rows, tile, s);
+      begins[k] = min(s.k, room[k]);
+      rest[k] = s.k - begins[k];
+    }
+    if (q < G) head[q] = begins[k];
+    room[k] -= begins[k];
+    sum_rest += rest[k];
+    sum_room += room[k];
+  }
+  int lp = chunk_scan<THREADS>(sum_rest, set.warp, &rests), tp = chunk_scan<THREADS>(sum_room, set.warp, &all);
+  for (int k = 0; k < PER; ++k) {
+    const int q = tid * PER + k;
+    if (q < line.r) set.lp[q] = lp;
+    if (q < G) set.tp[q] = min(tp, rests);
+    lp += rest[k];
+    tp += room[k];
+  }
+  if (tid == 0) {
+    set.lp[line.r] = rests;
+    set.tp[G] = rests;                     // (the last CTA has whatever is left)
+  }
+  __syncthreads();
+  const int t0 = set.tp[me];
+  line.tail = set.tp[me + 1] - t0;
+  if (me == 0 && tid < G) a.tail[tid] = set.tp[tid + 1] - set.tp[tid];
+  for (int k = 0; k < PER; ++k) {
+    const int q = tid * PER + k;
+    const int from = q < line.r ? set.lp[q] : 0;
+    if (q < line.r && from <= t0 && t0 < from + rest[k]) {
+      kept.q = q;
+      kept.off = t0 - from;
+    }
+    if (q < 2 * G && q % G == me) {
+      ChunkCut cut = {0, begins[k] > 0, 0, -1, 0, 0, 0, 0, 0};
+      if (q < line.r && rest[k] > 0) {
+        const auto owner = [&](int t) {    // the CTA that has tile t of the rests: the last one that begins at or before it
+          int lo = 0, hi = G;
+          while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (set.tp[mid] <= t) lo = mid;
+            else hi = mid;
+          }
+          return lo;
+        };
+        cut.first = owner(from);
+        cut.last = owner(from + rest[k] - 1);
+        cut.cut = begins[k] > 0 || cut.first != cut.last;
+        line.item(a, line.last + q, rows, tile, s);
+        cut.kv = s.kv;
+        cut.rows = s.rows;
+        cut.first_row = s.first;
+        cut.row0 = s.row0;
+      }
+      a.cut[q] = cut;
+    }
+  }
+  __syncthreads();
+  line.q = kept.q;
+  line.off = kept.off;
+  return line;
+}
+
+}  // namespace pact

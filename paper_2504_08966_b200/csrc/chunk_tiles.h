@@ -1,0 +1,57 @@
+// How the attention of several new tokens per request shares out its work: items (256 or 128 rows of one key head of a request) and their tiles of cached
+// rows.  Plain functions, so that they can be run on the host as well.
+#pragma once
+#include <stdint.h>
+
+#include "paged_tiles.h"
+
+namespace pact {
+
+// sum of floor((a i + b) / m) over i = 0 .. n - 1: whole multiples of m leave a and b, what is left counts lattice points below a line, and counting them
+// along the other axis gives a shorter sum of the same kind (the steps of Euclid's algorithm).
+PAGED_HD unsigned long long floor_sum(unsigned long long n, unsigned long long m, unsigned long long a, unsigned long long b) {
+  unsigned long long sum = 0;
+  while (n) {
+    if (a >= m) {
+      sum += (n & 1 ? n * ((n - 1) / 2) : n / 2 * (n - 1)) * (a / m);
+      a %= m;
+    }
+    if (b >= m) {
+      sum += n * (b / m);
+      b %= m;
+    }
+    const unsigned long long top = a * n + b;
+    if (top < m) break;
+    n = top / m;
+    b = top % m;
+    const unsigned long long t = m;
+    m = a;
+    a = t;
+  }
+  return sum;
+}
+
+// One request of a chunk: `n` new tokens that are served out of `want`, the last of `len` cached rows.
+struct ChunkLengths {
+  int n, want, len;
+};
+PAGED_HD int chunk_before(const ChunkLengths &q) { return q.len > q.want ? q.len - q.want : 0; }   // rows cached before the new ones
+PAGED_HD int chunk_items(const ChunkLengths &q, int group, int rows) { return (int)(((long long)q.n * group + rows - 1) / rows); }
+// Tiles of `tile` rows that item i of a key head meets.  Its last row is of token ceil(min(n g, (i + 1) rows) / g) - 1.
+PAGED_HD int chunk_tiles(const ChunkLengths &q, int i, int group, int rows, int tile, bool causal) {
+  if (!causal) return q.len > tile ? (int)(((unsigned)q.len + tile - 1u) / (unsigned)tile) : 1;
+  const long long all = (long long)q.n * group, end = (long long)(i + 1) * rows;
+  const int tokens = end < all ? (int)((end + group - 1) / group) : q.n;
+  return (int)(((unsigned)chunk_before(q) + (unsigned)tokens + tile - 1u) / (unsigned)tile);
+}
+// The same over all items of a key head (a division by g and one by the tile in turn round up like one by their product).
+PAGED_HD unsigned long long chunk_tiles_of_head(const ChunkLengths &q, int group, int rows, int tile, bool causal) {
+  const int items = chunk_items(q, group, rows);
+  if (items == 0) return 0;
+  const int last = chunk_tiles(q, items - 1, group, rows, tile, causal);
+  if (!causal) return (unsigned long long)items * last;
+  const unsigned long long m = (unsigned long long)group * tile;
+  return floor_sum((unsigned long long)items - 1, m, rows, (unsigned long long)chunk_before(q) * group + rows + m - 1) + last;
+}
+
+}  // namespace pact

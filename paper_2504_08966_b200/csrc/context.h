@@ -4,6 +4,7 @@
 
 #include <atomic>
 
+#include "chunk.cuh"
 #include "kernels.cuh"
 #include "paged.cuh"
 
@@ -16,6 +17,7 @@ struct pact_ctx {
   pact::DeviceCfg dev;     // of the device the context was created on
   bool umma;               // bf16 keys of a width the tcgen05 tile kernels take
   pact::PagedCfg paged;    // the paged cache's kernels for these heads
+  pact::ChunkCfg chunk;    // the attention of several new tokens per request for them
   int device;
   char err[256];
   long long launches;      // kernels launched by this context so far
