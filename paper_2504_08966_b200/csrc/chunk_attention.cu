@@ -18,6 +18,8 @@
 // Rounding: probabilities go into the products with bf16 values as one bf16 term where results are bf16: unbiased errors of 2^-8 at most in the weights, which together are no
 // larger than the one rounding of the result that follows.  For fp32 results as three terms, which hold all of fp32's 24 bits, and the products of two tiles at a
 // time are added with rounding, since the tensor cores cut their running sums off towards 0 (some 2^-25 at each of 16 rows).  Sums of probabilities are taken before the rounding.
+#include <float.h>
+
 #include "chunk_row.cuh"
 
 namespace pact {
@@ -81,6 +83,15 @@ __device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, u
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accum) : "memory");
 }
+// After the wait for loads from tensor memory: what was loaded is used from here on.  The loads are asynchronous and the wait names no registers, so nothing else keeps the
+// compiler from using them, and then others in their place, before they have been written.
+__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[32]) {
+  asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                    "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                    "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                    "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :: "memory");
+}
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
@@ -130,7 +141,16 @@ __device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigne
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float4 lds_here(uint32_t at) {            // (in this place of the program: asked for well before it is used)
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at));
+  return v;
+}
 // The order in which the tiles of a segment of n are asked for: with one tile ahead K0 V0 K1 V1 .., with two K0 K1 V0 K2 V1 ..; load x of 2 n.
 struct LoadAt {
   bool v;
@@ -147,23 +167,32 @@ __device__ __forceinline__ int chunk_v_load(int j, int n, int ahead) { return ah
 
 // A warp's bounded wait: false once kWaitNs or `polls` have run out, or another warp has given up.  Without a call: a kernel that moves registers from one group of
 // warps to another cannot have any there.
-__device__ __forceinline__ bool chunk_wait(int *abort, uint64_t *bar, uint32_t parity, int polls, int32_t *status) {
-  int ok = 1;
-  if ((threadIdx.x & 31) == 0) {
-    ok = polls == INT32_MAX ? mbar_try_wait(bar, parity) : mbar_test(bar, parity);
+struct ChunkWait {
+  int *abort;
+  int32_t *status;
+  int polls;
+  __device__ __forceinline__ bool first(uint64_t *bar, uint32_t parity) const { return polls == INT32_MAX ? mbar_try_wait(bar, parity & 1) : mbar_test(bar, parity & 1); }
+  __device__ __forceinline__ bool more(uint64_t *bar, uint32_t parity) const {
+    const unsigned long long t0 = global_ns();
+    bool ok = false;
+    for (int i = 1; i < polls && !*const_cast<volatile int *>(abort); ++i)
+      if ((ok = mbar_try_wait(bar, parity & 1)) || ((i & 63) == 63 && global_ns() - t0 > kWaitNs)) break;
     if (!ok) {
-      const unsigned long long t0 = global_ns();
-      for (int i = 1; i < polls && !*const_cast<volatile int *>(abort); ++i) {
-        if ((ok = mbar_try_wait(bar, parity)) || ((i & 63) == 63 && global_ns() - t0 > kWaitNs)) break;
-      }
-      if (!ok) {
-        atomicExch(abort, 1);
-        if (status) atomicMin(status, (int)PACT_ERR_TIMEOUT);
-      }
+      atomicExch(abort, 1);
+      if (status) atomicMin(status, (int)PACT_ERR_TIMEOUT);
     }
+    return ok;
   }
-  return __shfl_sync(0xffffffffu, ok, 0) != 0;
-}
+  __device__ __forceinline__ bool operator()(uint64_t *bar, uint32_t parity) const {
+    int ok = first(bar, parity) ? 1 : 0;
+    if (!__all_sync(0xffffffffu, ok)) {
+      if ((threadIdx.x & 31) == 0) ok = more(bar, parity) ? 1 : 0;
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+    }
+    __syncwarp();
+    return ok != 0;
+  }
+};
 
 template <int NB, bool WIDE>
 __global__ void __launch_bounds__(kChunkThreads, 1)
@@ -201,9 +230,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   ChunkLine line = chunk_line<kChunkThreads>(a, C::kRows, N, sh.line, *reinterpret_cast<ChunkLineSetup *>(sh.stage[0]));
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // (the set-up's words lie where copies will land)
   __syncthreads();
+  __syncwarp();                                                      // (one thread has had more to do; what follows asks for whole warps)
   tc_fence_after();
   const uint32_t tmem = sh.tmem;
-  const auto wait = [&](uint64_t *bar, uint32_t parity) { return chunk_wait(&sh.abort, bar, parity & 1, a.polls, a.status); };
+  const ChunkWait wait = {&sh.abort, a.status, a.polls};
   ChunkSegment s;
   bool ok = true;
 
@@ -215,7 +245,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     const uint32_t my_s = tmem + t * C::kRegion + lanes, my_o = tmem + C::kO + t * C::kWidth + lanes;
     const int d16 = (a.d_h + 15) / 16 * 16;
     float4 *flush = reinterpret_cast<float4 *>(a.flush) + ((long long)blockIdx.x * C::kBlocks + t) * (C::kWidth / 4) * 128 + row;
-    const float scale = a.scale;
+    // Logits of bf16 results are kept in powers of two, a multiplication less; those of fp32 results in natural units, which round once less.
+    constexpr float kTwos = WIDE ? kChunkLog2e : 1.f;
+    const float scale = WIDE ? a.scale : a.scale * kChunkLog2e;
+    const auto weight = [](float m, float to) { return m == -INFINITY ? 0.f : m == to ? 1.f : ex2_approx((m - to) * kTwos); };   // as part_weight
     const unsigned long long scale2 = pair_of(scale, scale), log2e2 = pair_of(kChunkLog2e, kChunkLog2e);
     uint32_t s_phase = 0, o_phase = 0;
     int tiles = 0, segment = 0;
@@ -229,21 +262,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       const bool there = r < s.rows;
       const int limit = there ? s.limit(token, a.causal) : 0;
       if (t < C::kBlocks && (!split || t == 0) && ok) {
-        // this warp's 32 rows of Q, a row per half warp (or less), swizzled as the copies of K are
+        // this warp's 32 rows of Q, swizzled as the copies of K are; zeros past d_h and the last row
         const long long my_at = (s.row0 + token) * a.ldQ + head * a.ldQh;
         constexpr int kLanes = NB == 1 ? 8 : NB == 2 ? 16 : 32, kAtOnce = 32 / kLanes;
         const int c = lane % kLanes;
-        char *to = sh.q[t] + c / 8 * (128 * 128);
-#pragma unroll 8
+        const uint32_t to = smem_u32(sh.q[t]) + c / 8 * (128 * 128);
+#pragma unroll
         for (int i = 0; i < 32; i += kAtOnce) {
-          const int src = i + lane / kLanes;
+          const int src = i + lane / kLanes, rr = (warp & 3) * 32 + src;
           const long long at = __shfl_sync(0xffffffffu, my_at, src);
-          const bool row_there = __shfl_sync(0xffffffffu, there ? 1 : 0, src) != 0;
-          const int rr = (warp & 3) * 32 + src;
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (row_there && c * 8 < a.d_h) v = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.Q) + at + c * 8));
-          if (c < NB * 8) *reinterpret_cast<uint4 *>(to + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)) = v;
+          const bool row_there = __shfl_sync(0xffffffffu, there ? 1 : 0, src) != 0 && c * 8 < a.d_h;
+          const __nv_bfloat16 *from = static_cast<const __nv_bfloat16 *>(a.Q) + (row_there ? at + c * 8 : 0);
+          if (c < NB * 8)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)), "l"(from), "r"(row_there ? 16 : 0) : "memory");
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(sh.q_full + t);
@@ -262,48 +295,57 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll
           for (int i = 0; i < N / 32; ++i) tmem_ld32(my_s + i * 32, x[i]);
           tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < N / 32; ++i) tmem_arrived(x[i]);
           const int valid = min(max(limit - row0, 0), N);
           const bool edge = __any_sync(0xffffffffu, valid < N) || (flags & 2);
-          const float4 *bias = reinterpret_cast<const float4 *>(sh.bias[at]);
+          const uint32_t bias = smem_u32(sh.bias[at]);
           float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          if (flags & 1) {
+            float4 b[2][4];
 #pragma unroll
-          for (int c = 0; c < N / 32; ++c) {
-            if (!(flags & 1)) {
+            for (int k = 0; k < 4; ++k) b[0][k] = lds_here(bias + k * 16);
 #pragma unroll
-              for (int i = 0; i < 32; i += 2) to_pair(x[c][i], x[c][i + 1], mul2(of_pair(x[c][i], x[c][i + 1]), scale2));
-            } else {
+            for (int g = 0; g < N / 16; ++g) {
+              if (g + 1 < N / 16)
 #pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                const float4 b = bias[c * 8 + i / 4];
-                to_pair(x[c][i], x[c][i + 1], fma2(of_pair(x[c][i], x[c][i + 1]), scale2, pair_of(b.x, b.y)));
-                to_pair(x[c][i + 2], x[c][i + 3], fma2(of_pair(x[c][i + 2], x[c][i + 3]), scale2, pair_of(b.z, b.w)));
+                for (int k = 0; k < 4; ++k) b[(g + 1) & 1][k] = lds_here(bias + (g + 1) * 64 + k * 16);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                uint32_t *y = x[g / 2] + g % 2 * 16 + k * 4;
+                const float4 w = b[g & 1][k];
+                to_pair(y[0], y[1], fma2(of_pair(y[0], y[1]), scale2, pair_of(w.x, w.y)));
+                to_pair(y[2], y[3], fma2(of_pair(y[2], y[3]), scale2, pair_of(w.z, w.w)));
               }
             }
-            if (edge) {
-              // rows that the token does not see; hidden ones by their bias, since their keys may be anything
-              constexpr uint32_t kNone = 0xFF800000u;                // minus infinity
-#pragma unroll
-              for (int i = 0; i < 32; i += 4) {
-                float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (flags & 2) b = bias[c * 8 + i / 4];
-                if (c * 32 + i >= valid || b.x == -INFINITY) x[c][i] = kNone;
-                if (c * 32 + i + 1 >= valid || b.y == -INFINITY) x[c][i + 1] = kNone;
-                if (c * 32 + i + 2 >= valid || b.z == -INFINITY) x[c][i + 2] = kNone;
-                if (c * 32 + i + 3 >= valid || b.w == -INFINITY) x[c][i + 3] = kNone;
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < 32; i += 8)
-#pragma unroll
-              for (int k = 0; k < 4; ++k) tops[k] = max3(tops[k], __uint_as_float(x[c][i + 2 * k]), __uint_as_float(x[c][i + 2 * k + 1]));
           }
-          const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+          if (edge) {
+            // rows that the token does not see; hidden ones by their bias, since their keys may be anything
+            constexpr uint32_t kNone = 0xFF800000u;                  // minus infinity
+#pragma unroll
+            for (int i = 0; i < N; i += 4) {
+              float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (flags & 2) w = lds_here(bias + i * 4);
+              uint32_t *y = x[i / 32] + i % 32;
+              if (i >= valid || w.x == -INFINITY) y[0] = kNone;
+              if (i + 1 >= valid || w.y == -INFINITY) y[1] = kNone;
+              if (i + 2 >= valid || w.z == -INFINITY) y[2] = kNone;
+              if (i + 3 >= valid || w.w == -INFINITY) y[3] = kNone;
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < N; i += 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) tops[k] = max3(tops[k], __uint_as_float(x[i / 32][i % 32 + 2 * k]), __uint_as_float(x[i / 32][i % 32 + 2 * k + 1]));
+          // (without biases x are still products of queries and keys, and the scale, which is positive then, comes with the exponent)
+          const float unit = flags & 1 ? 1.f : scale, top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * unit;
           if (WIDE && nth > 0 && nth % 2 == 0) {                     // the results of two tiles, added with rounding
 #pragma unroll 1
             for (int c0 = 0; c0 < d16; c0 += 32) {
               uint32_t v[32];
               tmem_ld32(my_o + c0, v);
               tmem_ld_wait();
+              tmem_arrived(v);
 #pragma unroll
               for (int i = 0; i < 32; i += 4)
                 if (c0 + i < d16) {
@@ -321,8 +363,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           }
           if (nth == 0) {
             m = top;
-          } else if (__any_sync(0xffffffffu, top > m && (m == -INFINITY || (top - m) * kChunkLog2e > kLag))) {
-            const float to = fmaxf(m, top), f = part_weight(m, to);
+          } else if (__any_sync(0xffffffffu, top > m && (m == -INFINITY || (top - m) * kTwos > kLag))) {
+            const float to = fmaxf(m, top), f = weight(m, to);
             m = to;
             l *= f;
             f_flush *= f;
@@ -332,6 +374,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 uint32_t v[32];
                 tmem_ld32(my_o + c0, v);
                 tmem_ld_wait();
+                tmem_arrived(v);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
                 tmem_st32(my_o + c0, v);
@@ -339,7 +382,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             }
           }
           const float ref = m == -INFINITY ? 0.f : m;
-          const unsigned long long ref2 = pair_of(-ref, -ref);
+          const unsigned long long ref2 = pair_of(-ref, -ref), unit2 = pair_of(unit, unit);
           unsigned long long sums[4] = {0ull, 0ull, 0ull, 0ull};
           if constexpr (!WIDE) {
 #pragma unroll
@@ -348,7 +391,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll
               for (int i = 0; i < 32; i += 2) {
                 float u, w;
-                unpair(mul2(add2(of_pair(x[c][i], x[c][i + 1]), ref2), log2e2), u, w);
+                unpair(fma2(of_pair(x[c][i], x[c][i + 1]), unit2, ref2), u, w);
                 u = ex2_approx(u);
                 w = ex2_approx(w);
                 sums[i / 2 % 4] = add2(sums[i / 2 % 4], pair_of(u, w));
@@ -363,7 +406,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll
               for (int i = 0; i < 32; i += 2) {
                 float u, w;
-                unpair(mul2(add2(of_pair(x[c][i], x[c][i + 1]), ref2), log2e2), u, w);
+                unpair(mul2(fma2(of_pair(x[c][i], x[c][i + 1]), unit2, ref2), log2e2), u, w);
                 u = ex2_approx(u);
                 w = ex2_approx(w);
                 sums[i / 2 % 4] = add2(sums[i / 2 % 4], pair_of(u, w));
@@ -401,6 +444,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         uint32_t v[32];
         tmem_ld32(from + c0, v);
         tmem_ld_wait();
+        tmem_arrived(v);
 #pragma unroll
         for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(v[i]);
         if (WIDE && has_kept) {
@@ -432,11 +476,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           uint32_t v[32];
           tmem_ld32(my_s + C::kRegion, v);
           tmem_ld_wait();
+          tmem_arrived(v);
           m1 = __uint_as_float(v[0]);
           l1 = __uint_as_float(v[1]);
           const float to = fmaxf(m, m1);
-          f0 = part_weight(m, to);
-          f1 = part_weight(m1, to);
+          f0 = weight(m, to);
+          f1 = weight(m1, to);
           f_flush1 = __uint_as_float(v[2]);
           flushed1 = v[3] & 1u;
           poisoned = poisoned || (v[3] & 2u);
@@ -444,6 +489,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           l = l * f0 + l1 * f1;
         }
       }
+      if (!WIDE) m = m < -2.3e38f ? m : m * 0.6931471805599453f;     // (the lowest float stands for itself)
       if (active && ok && (!split || t == 0)) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const long long out_at = (s.row0 + token) * a.ldO + head * a.ldOh;
@@ -533,7 +579,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             chunk_load_4d(sh.stage[st] + (my_nb * N + my_box * a.box_rows) * 128, l.v ? &map_v : &map_k, sh.full + st, my_nb * 64, off, s.kv, id);
           if (!l.v) {                                                  // the biases come with the keys
             const int at = (tiles + l.j) % R;
-            const bool counts = a.logw || (pages.bad >> (in * C::kGroups) & ((1u << C::kGroups) - 1u));
+            const bool counts = a.logw || !(a.scale > 0.f) || (pages.bad >> (in * C::kGroups) & ((1u << C::kGroups) - 1u));
             const int g = in * C::kGroups + lane / 4, bid = __shfl_sync(0xffffffffu, pages.id, g & 31), boff = __shfl_sync(0xffffffffu, pages.off, g & 31);
             if (counts && lane < N / 4) {
               float *to = sh.bias[at] + lane * 4;
@@ -551,30 +597,39 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       }
       if (lane == 0) sh.issued = loads;
     } else if (warp == kMmaWarp) {
-      // ---- products ----
+      // ---- products: the warp goes through the tiles together, its first thread asks for them ----
       const int d16 = (a.d_h + 15) / 16 * 16, steps = d16 / 16;
       constexpr uint32_t kTypes = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);
       constexpr uint32_t kLogits = kTypes | ((uint32_t)(N >> 3) << 17);
       const uint32_t values = kTypes | (1u << 16) | ((uint32_t)(d16 >> 3) << 17);
+      // (descriptors of the first blocks, from which the others are an addition away: forming them for every product took twice the time of the products)
+      const uint64_t q0 = smem_desc(smem_u32(sh.q[0])), k0 = smem_desc(smem_u32(sh.stage[0])), v0 = smem_desc_rows(smem_u32(sh.stage[0]), N * 128);
       int loads = 0, tiles = 0;
-      uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+      uint32_t q_phase = 0, p_phase = 0;                             // a bit for each block
       const auto logits = [&](int t, int q, int st) {
+        const uint64_t da = desc_at(q0, q * C::kQBytes), db = desc_at(k0, st * C::kStage);
+        const uint32_t to = tmem + t * C::kRegion;
         if (lane == 0) {
-          const uint64_t da = smem_desc(smem_u32(sh.q[q])), db = smem_desc(smem_u32(sh.stage[st]));
-          for (int k = 0; k < steps; ++k)
-            umma_bf16(tmem + t * C::kRegion, desc_at(da, k / 4 * (128 * 128) + k % 4 * 32), desc_at(db, k / 4 * (N * 128) + k % 4 * 32), kLogits, k != 0);
+          if (steps == NB * 4) {
+#pragma unroll
+            for (int k = 0; k < NB * 4; ++k) umma_bf16(to, desc_at(da, k / 4 * (128 * 128) + k % 4 * 32), desc_at(db, k / 4 * (N * 128) + k % 4 * 32), kLogits, k != 0);
+          } else {
+#pragma unroll 1
+            for (int k = 0; k < steps; ++k) umma_bf16(to, desc_at(da, k / 4 * (128 * 128) + k % 4 * 32), desc_at(db, k / 4 * (N * 128) + k % 4 * 32), kLogits, k != 0);
+          }
           umma_commit(sh.s_full + t);
         }
         __syncwarp();
       };
       const auto add_values = [&](int t, int st, bool accumulate) {
+        const uint64_t db = desc_at(v0, st * C::kStage);
+        const uint32_t to = tmem + C::kO + t * C::kWidth, from = tmem + t * C::kRegion;
         if (lane == 0) {
-          const uint64_t db = smem_desc_rows(smem_u32(sh.stage[st]), N * 128);
-  #pragma unroll
-          for (int term = C::kTerms - 1; term >= 0; --term)            // the small terms first
-  #pragma unroll
+#pragma unroll
+          for (int term = C::kTerms - 1; term >= 0; --term)          // the small terms first
+#pragma unroll
             for (int k = 0; k < N / 16; ++k)
-              umma_bf16_ta(tmem + C::kO + t * C::kWidth, tmem + t * C::kRegion + term * (N / 2) + k * 8, desc_at(db, k * 2048), values, accumulate || k != 0 || term != C::kTerms - 1);
+              umma_bf16_ta(to, from + term * (N / 2) + k * 8, desc_at(db, k * 2048), values, k != 0 || term != C::kTerms - 1 ? 1 : accumulate);
         }
         __syncwarp();
       };
@@ -584,11 +639,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       };
       while (ok && line.next(a, C::kRows, N, s)) {
         const int n = s.j1 - s.j0;
-        const bool split = C::kBlocks == 2 && s.rows <= 128;           // even and odd tiles
+        const bool split = C::kBlocks == 2 && s.rows <= 128;         // even and odd tiles
         const int blocks = split ? 1 : C::kBlocks, ahead = split ? 2 : 1;
         const auto stage_of = [&](int x) { return (loads + x) % S; };
         const auto phase_of = [&](int x) { return (uint32_t)((loads + x) / S); };
-        for (int t = 0; t < blocks && ok; ++t) ok = wait(sh.q_full + t, q_phase[t]++);
+        for (int t = 0; t < blocks && ok; ++t) {
+          ok = wait(sh.q_full + t, q_phase >> t);
+          q_phase ^= 1u << t;
+        }
         for (int j = 0; j < min(ahead, n) && ok; ++j) {
           const int x = chunk_k_load(j, ahead), st = stage_of(x);
           ok = wait(sh.full + st, phase_of(x));
@@ -605,7 +663,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           ok = wait(sh.full + sv, phase_of(xv)) && wait(sh.clean + (tiles + j) % R, (tiles + j) / R) && (!more || wait(sh.full + sk, phase_of(xk)));
           for (int i = 0; i < blocks && ok; ++i) {
             const int t = split ? j & 1 : i, nth = split ? j >> 1 : j;
-            ok = wait(sh.p_ready + t, p_phase[t]++);
+            ok = wait(sh.p_ready + t, p_phase >> t);
+            p_phase ^= 1u << t;
             if (!ok) break;
             tc_fence_after();
             add_values(t, sv, WIDE ? (nth & 1) != 0 : nth > 0);
@@ -645,6 +704,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             live[i] = __ballot_sync(0xffffffffu, i < left && bs[i] != -INFINITY);
           }
           hidden = __any_sync(0xffffffffu, hidden);
+          __syncwarp();
+          if (!WIDE && counts && lane < N / 4) {                       // in powers of two; finite ones stay finite
+            const auto in_twos = [](float x) { return isinf(x) ? x : fminf(fmaxf(x * kChunkLog2e, -FLT_MAX), FLT_MAX); };
+            *reinterpret_cast<float4 *>(sh.bias[at] + lane * 4) = make_float4(in_twos(b.x), in_twos(b.y), in_twos(b.z), in_twos(b.w));
+          }
           __syncwarp();
           if (lane == 0) {
             sh.flags[at] = (counts ? 1 : 0) | (hidden ? 2 : 0);

@@ -256,6 +256,7 @@ template <int THREADS> __device__ __forceinline__ ChunkLine chunk_line(const Chu
       a.cut[q] = cut;
     }
   }
+  __syncwarp();
   __syncthreads();
   line.q = kept.q;
   line.off = kept.off;

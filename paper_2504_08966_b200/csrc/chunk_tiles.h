@@ -36,12 +36,12 @@ struct ChunkLengths {
   int n, want, len;
 };
 PAGED_HD int chunk_before(const ChunkLengths &q) { return q.len > q.want ? q.len - q.want : 0; }   // rows cached before the new ones
-PAGED_HD int chunk_items(const ChunkLengths &q, int group, int rows) { return (int)(((long long)q.n * group + rows - 1) / rows); }
+PAGED_HD int chunk_items(const ChunkLengths &q, int group, int rows) { return (int)(((unsigned)q.n * (unsigned)group + (unsigned)rows - 1u) / (unsigned)rows); }   // (n g < 2^31)
 // Tiles of `tile` rows that item i of a key head meets.  Its last row is of token ceil(min(n g, (i + 1) rows) / g) - 1.
 PAGED_HD int chunk_tiles(const ChunkLengths &q, int i, int group, int rows, int tile, bool causal) {
   if (!causal) return q.len > tile ? (int)(((unsigned)q.len + tile - 1u) / (unsigned)tile) : 1;
-  const long long all = (long long)q.n * group, end = (long long)(i + 1) * rows;
-  const int tokens = end < all ? (int)((end + group - 1) / group) : q.n;
+  const unsigned all = (unsigned)q.n * (unsigned)group, end = (unsigned)(i + 1) * (unsigned)rows;
+  const int tokens = end < all ? (int)((end + (unsigned)group - 1u) / (unsigned)group) : q.n;
   return (int)(((unsigned)chunk_before(q) + (unsigned)tokens + tile - 1u) / (unsigned)tile);
 }
 // The same over all items of a key head (a division by g and one by the tile in turn round up like one by their product).
@@ -50,6 +50,11 @@ PAGED_HD unsigned long long chunk_tiles_of_head(const ChunkLengths &q, int group
   if (items == 0) return 0;
   const int last = chunk_tiles(q, items - 1, group, rows, tile, causal);
   if (!causal) return (unsigned long long)items * last;
+  if (items <= 8) {                        // (fewer steps than those of the sum)
+    unsigned long long sum = last;
+    for (int i = 0; i + 1 < items; ++i) sum += chunk_tiles(q, i, group, rows, tile, true);
+    return sum;
+  }
   const unsigned long long m = (unsigned long long)group * tile;
   return floor_sum((unsigned long long)items - 1, m, rows, (unsigned long long)chunk_before(q) * group + rows + m - 1) + last;
 }
