@@ -42,7 +42,8 @@ struct ChunkArgs {
   int n_kvh, group, d_h;
   int box_rows;          // rows of one copy: the largest of 128, 64, 32, 16 that divides the page and is at most a tile
   int polls;             // of a wait
-  bool causal, out_bf16, wide_stores;
+  int store_bytes;       // rows of out lie at multiples of: 8 (bf16), 16 or 32
+  bool causal, out_bf16;
 };
 
 // What a context knows about these kernels for its heads; filled by chunk_configure.

@@ -42,7 +42,8 @@ pact_status pact_chunk_attention(pact_ctx *ctx, const pact_paged_cache *cache, c
   a.out = c->out; a.ldO = c->ldO; a.ldOh = c->ldOh; a.lse = c->lse; a.status = c->status; a.scale = c->scale;
   a.B = c->n_requests; a.width = c->max_pages; a.page = cache->page_rows; a.n_pages = cache->n_pages;
   a.n_kvh = ctx->n_kvh; a.group = group; a.d_h = ctx->d_h; a.causal = c->causal != 0; a.out_bf16 = ctx->out == PACT_BF16;
-  a.wide_stores = aligned16(c->out) && c->ldO * oe % 16 == 0 && c->ldOh * oe % 16 == 0;
+  const uint64_t at = reinterpret_cast<uintptr_t>(c->out) | (uint64_t)c->ldO * oe | (uint64_t)c->ldOh * oe;
+  a.store_bytes = at % 32 == 0 ? 32 : at % 16 == 0 ? 16 : 8;
   a.polls = ctx->copy_polls;
   int launches = 0;
   CK(launch_chunk(a, *cache, ctx->chunk, (cudaStream_t)stream, &launches));

@@ -26,8 +26,8 @@ namespace pact {
 namespace {
 
 constexpr int kSoftmaxWarps = 8;
-constexpr int kCopyWarp = 8, kMmaWarp = 9, kValueWarp = 10;
-constexpr int kChunkThreads = 12 * 32;      // (the last warp has no part: registers are shared out by fours of warps)
+constexpr int kCopyWarp = 8, kMmaWarp = 9, kValueWarp = 10, kCutWarp = 11;
+constexpr int kChunkThreads = 12 * 32;
 // Registers of a thread: a row of logits and what is made of it take more than the 168 that 384 threads may have each, the other warps need fewer.
 constexpr int kRowRegs = 208, kOtherRegs = 88;
 static_assert(kSoftmaxWarps * 32 * kRowRegs + (kChunkThreads - kSoftmaxWarps * 32) * kOtherRegs <= kChunkThreads * 168, "what the CTA is launched with");
@@ -58,7 +58,7 @@ template <int NB, bool WIDE> struct ChunkShared {
   float bias[C::kRing][C::kTileRows];
   uint64_t full[C::kStages], empty[C::kStages];
   uint64_t b_full[C::kRing], b_ready[C::kRing], clean[C::kRing];
-  uint64_t q_full[2], s_full[2], p_ready[2], o_full[2], drained;
+  uint64_t q_full[2], s_full[2], p_half[2], p_ready[2], o_full[2], drained;
   int flags[C::kRing];                     // 1: biases count, 2: some are minus infinity
   int poison[2 * C::kRing];                // a tile had values that are not finite beside rows that some token must not see
   int abort, issued;
@@ -76,12 +76,24 @@ __device__ __forceinline__ void chunk_copy16(void *dst, const void *src) {
 __device__ __forceinline__ void chunk_arrive_after_copies(uint64_t *bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accum) {   // A from tensor memory
+// Products whose operands are given by the lower words of their descriptors; the upper ones are the same for all (rows of 128 bytes swizzled, groups of 8 rows 1024 bytes apart).
+constexpr uint32_t kDescUpper = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint32_t a_desc, uint32_t b_desc, uint32_t idesc, uint32_t accum) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accum) : "memory");
+      "mov.b64 x, {%1, %5};\n\t"
+      "mov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_desc), "r"(b_desc), "r"(idesc), "r"(accum), "n"(kDescUpper) : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_desc, uint32_t idesc, uint32_t accum) {   // A from tensor memory
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_desc), "r"(idesc), "r"(accum), "n"(kDescUpper) : "memory");
 }
 // After the wait for loads from tensor memory: what was loaded is used from here on.  The loads are asynchronous and the wait names no registers, so nothing else keeps the
 // compiler from using them, and then others in their place, before they have been written.
@@ -162,7 +174,6 @@ __device__ __forceinline__ LoadAt chunk_load_at(int x, int n, int ahead) {
   if (x == 0 || (x & 1)) return {false, (x + 1) >> 1};
   return {true, (x - 2) >> 1};
 }
-__device__ __forceinline__ int chunk_k_load(int j, int ahead) { return ahead == 1 ? 2 * j : j == 0 ? 0 : 2 * j - 1; }
 __device__ __forceinline__ int chunk_v_load(int j, int n, int ahead) { return ahead == 1 ? 2 * j + 1 : min(2 * j + 2, 2 * n - 1); }
 
 // A warp's bounded wait: false once kWaitNs or `polls` have run out, or another warp has given up.  Without a call: a kernel that moves registers from one group of
@@ -183,6 +194,7 @@ struct ChunkWait {
     }
     return ok;
   }
+  __device__ __forceinline__ bool alone(uint64_t *bar, uint32_t parity) const { return first(bar, parity) || more(bar, parity); }   // one thread
   __device__ __forceinline__ bool operator()(uint64_t *bar, uint32_t parity) const {
     int ok = first(bar, parity) ? 1 : 0;
     if (!__all_sync(0xffffffffu, ok)) {
@@ -215,6 +227,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   if (tid < 2) {
     mbar_init(sh.q_full + tid, 4);
     mbar_init(sh.s_full + tid, 1);
+    mbar_init(sh.p_half + tid, 4);
     mbar_init(sh.p_ready + tid, 4);
     mbar_init(sh.o_full + tid, 1);
   }
@@ -227,7 +240,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   tc_fence_before();
   pdl_wait();
   pdl_trigger();
-  ChunkLine line = chunk_line<kChunkThreads>(a, C::kRows, N, sh.line, *reinterpret_cast<ChunkLineSetup *>(sh.stage[0]));
+  ChunkCuts cuts;
+  ChunkLine line = chunk_line<kChunkThreads>(a, C::kRows, N, sh.line, *reinterpret_cast<ChunkLineSetup *>(sh.stage[0]), cuts);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // (the set-up's words lie where copies will land)
   __syncthreads();
   __syncwarp();                                                      // (one thread has had more to do; what follows asks for whole warps)
@@ -252,35 +266,48 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     const unsigned long long scale2 = pair_of(scale, scale), log2e2 = pair_of(kChunkLog2e, kChunkLog2e);
     uint32_t s_phase = 0, o_phase = 0;
     int tiles = 0, segment = 0;
-    while (line.next(a, C::kRows, N, s)) {
+    const auto is_split = [](const ChunkSegment &x) { return C::kBlocks == 2 && x.rows <= 128; };
+    const auto fills_q = [&](const ChunkSegment &x) { return t < C::kBlocks && (t == 0 || !is_split(x)); };
+    // This warp's 32 rows of Q, swizzled as the copies of K are; zeros past d_h and the last row.
+    const auto ask_for_q = [&](const ChunkSegment &x) {
+      const int r = t * 128 + row, at_row = x.first + r, token = at_row / a.group, head = x.kv * a.group + at_row - token * a.group;
+      const bool there = r < x.rows;
+      const long long my_at = (x.row0 + token) * a.ldQ + head * a.ldQh;
+      constexpr int kLanes = NB == 1 ? 8 : NB == 2 ? 16 : 32, kAtOnce = 32 / kLanes;
+      const int c = lane % kLanes;
+      const uint32_t to = smem_u32(sh.q[t]) + c / 8 * (128 * 128);
+#pragma unroll
+      for (int i = 0; i < 32; i += kAtOnce) {
+        const int src = i + lane / kLanes, rr = (warp & 3) * 32 + src;
+        const long long at = __shfl_sync(0xffffffffu, my_at, src);
+        const bool row_there = __shfl_sync(0xffffffffu, there ? 1 : 0, src) != 0 && c * 8 < a.d_h;
+        const __nv_bfloat16 *from = static_cast<const __nv_bfloat16 *>(a.Q) + (row_there ? at + c * 8 : 0);
+        if (c < NB * 8)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)), "l"(from), "r"(row_there ? 16 : 0) : "memory");
+      }
+    };
+    const auto give_q = [&] {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(sh.q_full + t);
+    };
+    bool have = line.next(a, C::kRows, N, s), being_read = false;
+    if (have && fills_q(s)) {
+      ask_for_q(s);
+      give_q();
+    }
+    while (have) {
       const int n = s.j1 - s.j0;
-      const bool split = C::kBlocks == 2 && s.rows <= 128;
+      const bool split = is_split(s);
       const int my_first = split ? t : 0, step = split ? 2 : 1;
       const bool active = t < C::kBlocks && my_first < n;
       const int r = (split ? 0 : t * 128) + row;                     // of the item
       const int at_row = s.first + r, token = at_row / a.group, head = s.kv * a.group + at_row - token * a.group;
       const bool there = r < s.rows;
       const int limit = there ? s.limit(token, a.causal) : 0;
-      if (t < C::kBlocks && (!split || t == 0) && ok) {
-        // this warp's 32 rows of Q, swizzled as the copies of K are; zeros past d_h and the last row
-        const long long my_at = (s.row0 + token) * a.ldQ + head * a.ldQh;
-        constexpr int kLanes = NB == 1 ? 8 : NB == 2 ? 16 : 32, kAtOnce = 32 / kLanes;
-        const int c = lane % kLanes;
-        const uint32_t to = smem_u32(sh.q[t]) + c / 8 * (128 * 128);
-#pragma unroll
-        for (int i = 0; i < 32; i += kAtOnce) {
-          const int src = i + lane / kLanes, rr = (warp & 3) * 32 + src;
-          const long long at = __shfl_sync(0xffffffffu, my_at, src);
-          const bool row_there = __shfl_sync(0xffffffffu, there ? 1 : 0, src) != 0 && c * 8 < a.d_h;
-          const __nv_bfloat16 *from = static_cast<const __nv_bfloat16 *>(a.Q) + (row_there ? at + c * 8 : 0);
-          if (c < NB * 8)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)), "l"(from), "r"(row_there ? 16 : 0) : "memory");
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sh.q_full + t);
-      }
+      if (being_read) asm volatile("bar.sync 2, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");   // (the first group has read this one's results)
+      being_read = false;
       float m = -INFINITY, l = 0.f, f_flush = 1.f;
       bool poisoned = false, flushed = false;
       if (active)
@@ -398,6 +425,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 p[i / 2] = bf16_pair(u, w);
               }
               tmem_st16(my_s + c * 16, p);
+              if (c == N / 64 - 1) {                                 // products with the first half of the rows may begin
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sh.p_half + t);
+              }
             }
           } else {
 #pragma unroll
@@ -432,12 +465,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           l += ((u[0] + u[1]) + (u[2] + u[3])) + ((u[4] + u[5]) + (u[6] + u[7]));
         }
       // ---- results ----
+      // The next segment's queries come meanwhile: once this block's logits are done with these (where both groups have the same ones, once all products are).
+      ChunkSegment next;
+      const bool more = line.next(a, C::kRows, N, next), fills = more && fills_q(next);
+      if (fills && ok && !split) ask_for_q(next);
       if (active && ok) {
         ok = wait(sh.o_full + t, o_phase++);
         tc_fence_after();
         const int last = my_first + (n - 1 - my_first) / step * step;
         poisoned = poisoned || sh.poison[(tiles + last) % (2 * R)];
       }
+      if (fills && ok && split) ask_for_q(next);
+      if (fills && ok && !split) give_q();
       const int *poison = a.poison + ((long long)blockIdx.x * kChunkPoison + segment % kChunkPoison) * kChunkMaxWidth;
       // columns c0 .. c0 + 31 of this row's results, all tiles so far
       const auto results = [&](uint32_t from, const float4 *kept, bool has_kept, float f_kept, int c0, float (&o)[32]) {
@@ -488,6 +527,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           m = to;
           l = l * f0 + l1 * f1;
         }
+        if (fills && ok) give_q();                                   // (the next logits take the place of what has just been read)
       }
       if (!WIDE) m = m < -2.3e38f ? m : m * 0.6931471805599453f;     // (the lowest float stands for itself)
       if (active && ok && (!split || t == 0)) {
@@ -517,8 +557,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] *= inv;
 #pragma unroll
-            for (int i = 0; i < 32; i += 8)
-              if (c0 + i < a.d_h) store8(a, out_at + c0 + i, o + i);
+            for (int i = 0; i < 32; i += 16) {
+              if (c0 + i + 16 <= a.d_h) store16(a, out_at + c0 + i, o + i);
+              else if (c0 + i < a.d_h) store8(a, out_at + c0 + i, o + i);
+            }
           }
           __syncwarp();
         }
@@ -528,9 +570,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         }
       }
       tc_fence_before();
+      if (split) {
+        if (t == 0) asm volatile("bar.arrive 2, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
+        else being_read = true;
+      }
       tiles += n;
       ++segment;
+      have = more;
+      s = next;
     }
+    if (being_read) asm volatile("bar.sync 2, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kCopyWarp) {
@@ -596,89 +645,99 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         tiles += n;
       }
       if (lane == 0) sh.issued = loads;
+    } else if (warp == kCutWarp) {
+      cuts.write(a, line, C::kRows, N);
     } else if (warp == kMmaWarp) {
-      // ---- products: the warp goes through the tiles together, its first thread asks for them ----
-      const int d16 = (a.d_h + 15) / 16 * 16, steps = d16 / 16;
-      constexpr uint32_t kTypes = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);
-      constexpr uint32_t kLogits = kTypes | ((uint32_t)(N >> 3) << 17);
-      const uint32_t values = kTypes | (1u << 16) | ((uint32_t)(d16 >> 3) << 17);
-      // (descriptors of the first blocks, from which the others are an addition away: forming them for every product took twice the time of the products)
-      const uint64_t q0 = smem_desc(smem_u32(sh.q[0])), k0 = smem_desc(smem_u32(sh.stage[0])), v0 = smem_desc_rows(smem_u32(sh.stage[0]), N * 128);
-      int loads = 0, tiles = 0;
-      uint32_t q_phase = 0, p_phase = 0;                             // a bit for each block
-      const auto logits = [&](int t, int q, int st) {
-        const uint64_t da = desc_at(q0, q * C::kQBytes), db = desc_at(k0, st * C::kStage);
-        const uint32_t to = tmem + t * C::kRegion;
-        if (lane == 0) {
+      // ---- products, all by one thread: what it does between two of them is time in which none is under way ----
+      if (lane == 0) {
+        const int d16 = (a.d_h + 15) / 16 * 16, steps = d16 / 16;
+        constexpr uint32_t kTypes = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);
+        constexpr uint32_t kLogits = kTypes | ((uint32_t)(N >> 3) << 17);
+        const uint32_t values = kTypes | (1u << 16) | ((uint32_t)(d16 >> 3) << 17);
+        // (lower words of the descriptors of the first blocks, from which the others are an addition away)
+        const uint32_t q0 = (uint32_t)smem_desc(smem_u32(sh.q[0])), k0 = (uint32_t)smem_desc(smem_u32(sh.stage[0])), v0 = (uint32_t)smem_desc_rows(smem_u32(sh.stage[0]), N * 128);
+        int tiles = 0, stage = 0;
+        uint32_t phase = 0, q_phase = 0, p_phase = 0;                // (of the ring; a bit for each block)
+        const auto logits = [&](int t, int q, int st) {
+          const uint32_t da = q0 + q * (C::kQBytes / 16), db = k0 + st * (C::kStage / 16), to = tmem + t * C::kRegion;
           if (steps == NB * 4) {
 #pragma unroll
-            for (int k = 0; k < NB * 4; ++k) umma_bf16(to, desc_at(da, k / 4 * (128 * 128) + k % 4 * 32), desc_at(db, k / 4 * (N * 128) + k % 4 * 32), kLogits, k != 0);
+            for (int k = 0; k < NB * 4; ++k) umma_ss(to, da + (k / 4 * (128 * 128) + k % 4 * 32) / 16, db + (k / 4 * (N * 128) + k % 4 * 32) / 16, kLogits, k != 0);
           } else {
 #pragma unroll 1
-            for (int k = 0; k < steps; ++k) umma_bf16(to, desc_at(da, k / 4 * (128 * 128) + k % 4 * 32), desc_at(db, k / 4 * (N * 128) + k % 4 * 32), kLogits, k != 0);
+            for (int k = 0; k < steps; ++k) umma_ss(to, da + (k / 4 * (128 * 128) + k % 4 * 32) / 16, db + (k / 4 * (N * 128) + k % 4 * 32) / 16, kLogits, k != 0);
           }
           umma_commit(sh.s_full + t);
-        }
-        __syncwarp();
-      };
-      const auto add_values = [&](int t, int st, bool accumulate) {
-        const uint64_t db = desc_at(v0, st * C::kStage);
-        const uint32_t to = tmem + C::kO + t * C::kWidth, from = tmem + t * C::kRegion;
-        if (lane == 0) {
+        };
+        // rows [half N / 2, (half + 1) N / 2) of a tile, or all of them
+        const auto add_values = [&](int t, int st, int half, bool accumulate) {
+          const uint32_t db = v0 + st * (C::kStage / 16) + half * (N / 32) * (2048 / 16), to = tmem + C::kO + t * C::kWidth, from = tmem + t * C::kRegion + half * (N / 32) * 8;
 #pragma unroll
           for (int term = C::kTerms - 1; term >= 0; --term)          // the small terms first
 #pragma unroll
-            for (int k = 0; k < N / 16; ++k)
-              umma_bf16_ta(to, from + term * (N / 2) + k * 8, desc_at(db, k * 2048), values, k != 0 || term != C::kTerms - 1 ? 1 : accumulate);
-        }
-        __syncwarp();
-      };
-      const auto commit = [&](uint64_t *bar) {
-        if (lane == 0) umma_commit(bar);
-        __syncwarp();
-      };
-      while (ok && line.next(a, C::kRows, N, s)) {
-        const int n = s.j1 - s.j0;
-        const bool split = C::kBlocks == 2 && s.rows <= 128;         // even and odd tiles
-        const int blocks = split ? 1 : C::kBlocks, ahead = split ? 2 : 1;
-        const auto stage_of = [&](int x) { return (loads + x) % S; };
-        const auto phase_of = [&](int x) { return (uint32_t)((loads + x) / S); };
-        for (int t = 0; t < blocks && ok; ++t) {
-          ok = wait(sh.q_full + t, q_phase >> t);
-          q_phase ^= 1u << t;
-        }
-        for (int j = 0; j < min(ahead, n) && ok; ++j) {
-          const int x = chunk_k_load(j, ahead), st = stage_of(x);
-          ok = wait(sh.full + st, phase_of(x));
-          if (!ok) break;
-          tc_fence_after();
-          if (split) logits(j, 0, st);
-          else
-            for (int t = 0; t < blocks; ++t) logits(t, t, st);
-          commit(sh.empty + st);
-        }
-        for (int j = 0; j < n && ok; ++j) {
-          const int xv = chunk_v_load(j, n, ahead), sv = stage_of(xv), xk = chunk_k_load(j + ahead, ahead), sk = stage_of(xk);
-          const bool more = j + ahead < n;
-          ok = wait(sh.full + sv, phase_of(xv)) && wait(sh.clean + (tiles + j) % R, (tiles + j) / R) && (!more || wait(sh.full + sk, phase_of(xk)));
-          for (int i = 0; i < blocks && ok; ++i) {
-            const int t = split ? j & 1 : i, nth = split ? j >> 1 : j;
-            ok = wait(sh.p_ready + t, p_phase >> t);
-            p_phase ^= 1u << t;
+            for (int k = 0; k < (WIDE ? N / 16 : N / 32); ++k)
+              umma_ts(to, from + term * (N / 2) + k * 8, db + k * (2048 / 16), values, k != 0 || term != C::kTerms - 1 ? 1 : accumulate);
+        };
+        // the stage of the next load in the order in which they were asked for, and its phase
+        const auto take = [&](uint32_t &ph) {
+          const int st = stage;
+          ph = phase;
+          if (++stage == S) {
+            stage = 0;
+            phase ^= 1;
+          }
+          return st;
+        };
+        while (ok && line.next(a, C::kRows, N, s)) {
+          const int n = s.j1 - s.j0;
+          const bool split = C::kBlocks == 2 && s.rows <= 128;       // even and odd tiles
+          const int blocks = split ? 1 : C::kBlocks, ahead = split ? 2 : 1;
+          uint32_t ph;
+          for (int t = 0; t < blocks && ok; ++t) {
+            ok = wait.alone(sh.q_full + t, q_phase >> t);
+            q_phase ^= 1u << t;
+          }
+          for (int j = 0; j < min(ahead, n) && ok; ++j) {
+            const int st = take(ph);
+            ok = wait.alone(sh.full + st, ph);
             if (!ok) break;
             tc_fence_after();
-            add_values(t, sv, WIDE ? (nth & 1) != 0 : nth > 0);
-            if (more) logits(t, split ? 0 : t, sk);
-            else commit(sh.o_full + t);
+            if (split) logits(j, 0, st);
+            else
+              for (int t = 0; t < blocks; ++t) logits(t, t, st);
+            umma_commit(sh.empty + st);
           }
-          if (!ok) break;
-          commit(sh.empty + sv);
-          if (more) commit(sh.empty + sk);
+          for (int j = 0; j < n && ok; ++j) {
+            const bool more = j + ahead < n;
+            uint32_t ph_k = 0;
+            const int sv = take(ph), sk = more ? take(ph_k) : 0;
+            ok = wait.alone(sh.clean + (tiles + j) % R, (tiles + j) / R) && (!more || wait.alone(sh.full + sk, ph_k));   // (values that are clean have arrived)
+            for (int i = 0; i < blocks && ok; ++i) {
+              const int t = split ? j & 1 : i, nth = split ? j >> 1 : j;
+              if (!WIDE) {
+                ok = wait.alone(sh.p_half + t, p_phase >> t);
+                if (!ok) break;
+                tc_fence_after();
+                add_values(t, sv, 0, nth > 0);
+              }
+              ok = wait.alone(sh.p_ready + t, p_phase >> t);
+              p_phase ^= 1u << t;
+              if (!ok) break;
+              tc_fence_after();
+              if (WIDE) add_values(t, sv, 0, (nth & 1) != 0);
+              else add_values(t, sv, 1, true);
+              if (more) logits(t, split ? 0 : t, sk);
+              else umma_commit(sh.o_full + t);
+            }
+            if (!ok) break;
+            umma_commit(sh.empty + sv);
+            if (more) umma_commit(sh.empty + sk);
+          }
+          tiles += n;
         }
-        loads += 2 * n;
-        tiles += n;
+        umma_commit(&sh.drained);
       }
-      commit(&sh.drained);
+      __syncwarp();
     } else if (warp == kValueWarp) {
       // ---- values beside rows that must not be seen ----
       int loads = 0, tiles = 0, segment = 0;

@@ -39,7 +39,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_f32(const __grid_constant
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   pdl_wait();
   pdl_trigger();
-  ChunkLine line = chunk_line<kThreads>(a, kRows, kTileF, sh.line, *reinterpret_cast<ChunkLineSetup *>(sh.k[0]));
+  ChunkCuts cuts;
+  ChunkLine line = chunk_line<kThreads>(a, kRows, kTileF, sh.line, *reinterpret_cast<ChunkLineSetup *>(sh.k[0]), cuts);
+  if (tid < 32) cuts.write(a, line, kRows, kTileF);
   ChunkSegment s = {};
   const int chunks = a.d_h / 4;
   // rows [row0, row0 + 64) of a request, those it has; each thread a quarter of a row

@@ -12,8 +12,8 @@
 namespace pact {
 
 struct ChunkRequest : ChunkLengths {
-  long long row0;                          // its first row of Q and out
   bool bad;
+  long long row0;                          // its first row of Q and out
 };
 __device__ __forceinline__ ChunkRequest chunk_request(const ChunkArgs &a, int b) {
   ChunkRequest q;
@@ -40,8 +40,12 @@ struct ChunkSegment : ChunkRequest {
   __device__ __forceinline__ int limit(int token, bool causal) const { return causal ? min(len, len - want + token + 1) : len; }   // rows that a token sees
 };
 
+constexpr int kChunkPreInSmem = 33;        // entries of `pre` that are kept in shared memory
+constexpr int kChunkKept = 8;              // requests that are
+
 struct ChunkLine {
   const int *pre, *head;
+  const ChunkRequest *kept;                // the requests where there are no more than kChunkKept
   int rounds, last, r;                     // rounds of whole items, the first item after them, how many there are
   int q, off, tail;                        // where this CTA's part of the rests begins, and its tiles
   // walking through the segments
@@ -54,7 +58,7 @@ struct ChunkLine {
       if (pre[mid] * H <= x) lo = mid;
       else hi = mid;
     }
-    static_cast<ChunkRequest &>(s) = chunk_request(a, lo);
+    static_cast<ChunkRequest &>(s) = a.B <= kChunkKept ? kept[lo] : chunk_request(a, lo);
     const int n = pre[lo + 1] - pre[lo], at = x - pre[lo] * H;
     s.b = lo;
     s.kv = at / n;
@@ -97,10 +101,9 @@ struct ChunkLine {
   }
 };
 
-constexpr int kChunkPreInSmem = 128;       // entries of `pre` that are kept in shared memory
-
 // Shared memory of the set-up: kept (`pre`, where the rests begin) and passing (for the set-up alone).
 struct ChunkLineKept {
+  ChunkRequest request[kChunkKept];
   int pre[kChunkPreInSmem];
   int q, off;
 };
@@ -133,8 +136,55 @@ template <int THREADS> __device__ __forceinline__ int chunk_scan(int v, int *war
   return before + x - v;
 }
 
+// What the join has to know about items `me` and `me + G` of the last round; written by one warp while the others go on, from what all warps took before the set-up's
+// shared memory was given to the copies.
+struct ChunkCuts {
+  static constexpr int kWords = (kChunkMaxSms + 31) / 32;
+  int tp[kWords];                          // set.tp[32 i + lane], INT32_MAX past the last
+  int from[2], to[2];                      // set.lp of the two items and of the ones after them
+  __device__ __forceinline__ void take(const ChunkLine &line, const ChunkLineSetup &set, int G, int me) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const int c = i * 32 + (threadIdx.x & 31);
+      tp[i] = c < G ? set.tp[c] : INT32_MAX;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int q = me + k * G;
+      from[k] = q < line.r ? set.lp[q] : 0;
+      to[k] = q < line.r ? set.lp[q + 1] : 0;
+    }
+  }
+  __device__ __forceinline__ int owner(int t) const {                // the CTA that has tile t of the rests: the last one that begins at or before it
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) n += __popc(__ballot_sync(0xffffffffu, tp[i] <= t));
+    return n - 1;
+  }
+  __device__ __forceinline__ void write(const ChunkArgs &a, const ChunkLine &line, int rows, int tile) const {   // a whole warp
+    const int G = gridDim.x, me = blockIdx.x;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int q = me + k * G;
+      ChunkCut cut = {0, q < G && q < line.r && line.head[q] > 0, 0, -1, 0, 0, 0, 0, 0};
+      if (to[k] > from[k]) {
+        cut.first = owner(from[k]);
+        cut.last = owner(to[k] - 1);
+        cut.cut = cut.head || cut.first != cut.last;
+        ChunkSegment s;
+        line.item(a, line.last + q, rows, tile, s);
+        cut.kv = s.kv;
+        cut.rows = s.rows;
+        cut.first_row = s.first;
+        cut.row0 = s.row0;
+      }
+      if ((threadIdx.x & 31) == 0) a.cut[q] = cut;
+    }
+  }
+};
+
 // Called by all threads of the CTA, at least as many as the grid has CTAs.
-template <int THREADS> __device__ __forceinline__ ChunkLine chunk_line(const ChunkArgs &a, int rows, int tile, ChunkLineKept &kept, ChunkLineSetup &set) {
+template <int THREADS> __device__ __forceinline__ ChunkLine chunk_line(const ChunkArgs &a, int rows, int tile, ChunkLineKept &kept, ChunkLineSetup &set, ChunkCuts &cuts) {
   static_assert(THREADS >= kChunkMaxSms, "");
   constexpr int PER = (2 * kChunkMaxSms + THREADS - 1) / THREADS;    // items of the last round that a thread looks at
   const int tid = threadIdx.x, G = gridDim.x, me = blockIdx.x;
@@ -142,6 +192,7 @@ template <int THREADS> __device__ __forceinline__ ChunkLine chunk_line(const Chu
   ChunkLine line;
   line.pre = pre;
   line.head = head;
+  line.kept = kept.request;
   line.done = line.stage = 0;
   if (tid == 0) {
     set.tiles = 0;
@@ -154,6 +205,7 @@ template <int THREADS> __device__ __forceinline__ ChunkLine chunk_line(const Chu
     unsigned long long tiles = 0;
     for (int b = b0; b < b1; ++b) {
       const ChunkRequest q = chunk_request(a, b);
+      if (a.B <= kChunkKept) kept.request[b] = q;
       if (q.bad && me == 0 && a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
       pre[b] = mine;
       mine += chunk_items(q, a.group, rows);
@@ -227,35 +279,12 @@ template <int THREADS> __device__ __forceinline__ ChunkLine chunk_line(const Chu
   if (me == 0 && tid < G) a.tail[tid] = set.tp[tid + 1] - set.tp[tid];
   for (int k = 0; k < PER; ++k) {
     const int q = tid * PER + k;
-    const int from = q < line.r ? set.lp[q] : 0;
-    if (q < line.r && from <= t0 && t0 < from + rest[k]) {
+    if (q < line.r && set.lp[q] <= t0 && t0 < set.lp[q] + rest[k]) {
       kept.q = q;
-      kept.off = t0 - from;
-    }
-    if (q < 2 * G && q % G == me) {
-      ChunkCut cut = {0, begins[k] > 0, 0, -1, 0, 0, 0, 0, 0};
-      if (q < line.r && rest[k] > 0) {
-        const auto owner = [&](int t) {    // the CTA that has tile t of the rests: the last one that begins at or before it
-          int lo = 0, hi = G;
-          while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (set.tp[mid] <= t) lo = mid;
-            else hi = mid;
-          }
-          return lo;
-        };
-        cut.first = owner(from);
-        cut.last = owner(from + rest[k] - 1);
-        cut.cut = begins[k] > 0 || cut.first != cut.last;
-        line.item(a, line.last + q, rows, tile, s);
-        cut.kv = s.kv;
-        cut.rows = s.rows;
-        cut.first_row = s.first;
-        cut.row0 = s.row0;
-      }
-      a.cut[q] = cut;
+      kept.off = t0 - set.lp[q];
     }
   }
+  cuts.take(line, set, G, me);
   __syncwarp();
   __syncthreads();
   line.q = kept.q;
