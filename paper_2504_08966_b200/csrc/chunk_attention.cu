@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   pdl_wait();
   pdl_trigger();
   ChunkCuts cuts;
-  ChunkLine line = chunk_line<kChunkThreads>(a, C::kRows, N, sh.line, *reinterpret_cast<ChunkLineSetup *>(sh.stage[0]), cuts);
+  ChunkLine line = chunk_line<kChunkThreads, C::kRows, N>(a, sh.line, *reinterpret_cast<ChunkLineSetup *>(sh.stage[0]), cuts);
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // (the set-up's words lie where copies will land)
   __syncthreads();
   __syncwarp();                                                      // (one thread has had more to do; what follows asks for whole warps)
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(sh.q_full + t);
     };
-    bool have = line.next(a, C::kRows, N, s), being_read = false;
+    bool have = line.next<C::kRows, N>(a, s), being_read = false;
     if (have && fills_q(s)) {
       ask_for_q(s);
       give_q();
@@ -305,7 +305,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       const int r = (split ? 0 : t * 128) + row;                     // of the item
       const int at_row = s.first + r, token = at_row / a.group, head = s.kv * a.group + at_row - token * a.group;
       const bool there = r < s.rows;
-      const int limit = there ? s.limit(token, a.causal) : 0;
+      // (rows that are not there take part as if they were of the last token, so that no tile is treated as an edge for their sake; a warp of such rows alone only keeps step)
+      const int limit = s.limit(there ? token : (s.first + s.rows - 1) / a.group, a.causal);
+      const bool idle = !__any_sync(0xffffffffu, there);
       if (being_read) asm volatile("bar.sync 2, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");   // (the first group has read this one's results)
       being_read = false;
       float m = -INFINITY, l = 0.f, f_flush = 1.f;
@@ -316,6 +318,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           ok = wait(sh.s_full + t, s_phase++) && wait(sh.b_ready + at, tile / R);
           if (!ok) break;
           tc_fence_after();
+          if (idle) {
+            if (lane == 0) {
+              if (!WIDE) mbar_arrive(sh.p_half + t);
+              mbar_arrive(sh.p_ready + t);
+            }
+            continue;
+          }
           const int flags = sh.flags[at];
           if (nth > 0) poisoned = poisoned || sh.poison[(tile - step) % (2 * R)];   // (the products before this tile's are done)
           uint32_t x[N / 32][32];                                    // logits; 32 registers each, as they are loaded
@@ -325,7 +334,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll
           for (int i = 0; i < N / 32; ++i) tmem_arrived(x[i]);
           const int valid = min(max(limit - row0, 0), N);
-          const bool edge = __any_sync(0xffffffffu, valid < N) || (flags & 2);
           const uint32_t bias = smem_u32(sh.bias[at]);
           float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
           if (flags & 1) {
@@ -346,19 +354,22 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
               }
             }
           }
-          if (edge) {
-            // rows that the token does not see; hidden ones by their bias, since their keys may be anything
-            constexpr uint32_t kNone = 0xFF800000u;                  // minus infinity
+          constexpr uint32_t kNone = 0xFF800000u;                    // minus infinity
+          if (flags & 2) {                                           // hidden rows, whose keys may be anything
 #pragma unroll
             for (int i = 0; i < N; i += 4) {
-              float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (flags & 2) w = lds_here(bias + i * 4);
+              const float4 w = lds_here(bias + i * 4);
               uint32_t *y = x[i / 32] + i % 32;
-              if (i >= valid || w.x == -INFINITY) y[0] = kNone;
-              if (i + 1 >= valid || w.y == -INFINITY) y[1] = kNone;
-              if (i + 2 >= valid || w.z == -INFINITY) y[2] = kNone;
-              if (i + 3 >= valid || w.w == -INFINITY) y[3] = kNone;
+              if (w.x == -INFINITY) y[0] = kNone;
+              if (w.y == -INFINITY) y[1] = kNone;
+              if (w.z == -INFINITY) y[2] = kNone;
+              if (w.w == -INFINITY) y[3] = kNone;
             }
+          }
+          if (__any_sync(0xffffffffu, valid < N)) {                  // rows that the token does not see
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+              if (i >= valid) x[i / 32][i % 32] = kNone;
           }
 #pragma unroll
           for (int i = 0; i < N; i += 8)
@@ -467,7 +478,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       // ---- results ----
       // The next segment's queries come meanwhile: once this block's logits are done with these (where both groups have the same ones, once all products are).
       ChunkSegment next;
-      const bool more = line.next(a, C::kRows, N, next), fills = more && fills_q(next);
+      const bool more = line.next<C::kRows, N>(a, next), fills = more && fills_q(next);
       if (fills && ok && !split) ask_for_q(next);
       if (active && ok) {
         ok = wait(sh.o_full + t, o_phase++);
@@ -591,7 +602,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         uint32_t bad;
       } win[2] = {{-1, -1, 0, 0u}, {-1, -1, 0, 0u}};                   // of K and of V
       int loads = 0, tiles = 0;
-      while (ok && line.next(a, C::kRows, N, s)) {
+      while (ok && line.next<C::kRows, N>(a, s)) {
         const int n = s.j1 - s.j0, ahead = C::kBlocks == 2 && s.rows <= 128 ? 2 : 1;
         win[0].at = win[1].at = -1;
         for (int x = 0; x < 2 * n; ++x, ++loads) {
@@ -646,7 +657,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       }
       if (lane == 0) sh.issued = loads;
     } else if (warp == kCutWarp) {
-      cuts.write(a, line, C::kRows, N);
+      cuts.write<C::kRows, N>(a, line);
     } else if (warp == kMmaWarp) {
       // ---- products, all by one thread: what it does between two of them is time in which none is under way ----
       if (lane == 0) {
@@ -688,7 +699,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           }
           return st;
         };
-        while (ok && line.next(a, C::kRows, N, s)) {
+        while (ok && line.next<C::kRows, N>(a, s)) {
           const int n = s.j1 - s.j0;
           const bool split = C::kBlocks == 2 && s.rows <= 128;       // even and odd tiles
           const int blocks = split ? 1 : C::kBlocks, ahead = split ? 2 : 1;
@@ -741,7 +752,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     } else if (warp == kValueWarp) {
       // ---- values beside rows that must not be seen ----
       int loads = 0, tiles = 0, segment = 0;
-      while (ok && line.next(a, C::kRows, N, s)) {
+      while (ok && line.next<C::kRows, N>(a, s)) {
         const int n = s.j1 - s.j0, ahead = C::kBlocks == 2 && s.rows <= 128 ? 2 : 1;
         const int seen = s.limit(s.first / a.group, a.causal);         // by all tokens of the item
         int *poison = a.poison + ((long long)blockIdx.x * kChunkPoison + segment % kChunkPoison) * kChunkMaxWidth;
@@ -757,7 +768,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           const int left = s.len - row0 - lane * 4;
           uint32_t live[4];                                            // bit l of live[i]: row 4 l + i
           bool hidden = false;
-  #pragma unroll
+#pragma unroll
           for (int i = 0; i < 4; ++i) {
             hidden = hidden || bs[i] == -INFINITY;
             live[i] = __ballot_sync(0xffffffffu, i < left && bs[i] != -INFINITY);
@@ -778,22 +789,32 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           if (!ok) break;
           bool found = false;
           if (hidden || row0 + N > seen) {
-            const int c = lane & 7;
-            for (int nb = 0; nb < NB; ++nb)
-  #pragma unroll 8
-              for (int r0 = 0; r0 < N; r0 += 4) {
-                const int r = r0 + (lane >> 3);
-                uint4 *p = reinterpret_cast<uint4 *>(sh.stage[st] + (nb * N + r) * 128 + c * 16);
-                const uint32_t mine = (r & 2) ? ((r & 1) ? live[3] : live[2]) : ((r & 1) ? live[1] : live[0]);
-                if (mine >> (r >> 2) & 1u) {
-                  const uint4 v = *p;
-                  const uint32_t m = 0x7FFF7FFFu;
-                  const uint32_t top = __vmaxu2(__vmaxu2(v.x & m, v.y & m), __vmaxu2(v.z & m, v.w & m));
-                  found = found || (top & 0xFFFFu) >= 0x7F80u || (top >> 16) >= 0x7F80u;
-                } else {
-                  *p = make_uint4(0, 0, 0, 0);
+            // (rows that every token of the item sees may hold what they like)
+            const int c = lane & 7, from = hidden ? 0 : max(0, seen - row0) & ~3;
+            constexpr uint32_t kAll = N == 128 ? 0xffffffffu : (1u << (N / 4 % 32)) - 1u;
+            const bool all_live = (live[0] & live[1] & live[2] & live[3] & kAll) == kAll;
+            const auto is_live = [&](int r) { return (((r & 2) ? ((r & 1) ? live[3] : live[2]) : ((r & 1) ? live[1] : live[0])) >> (r >> 2) & 1u) != 0; };
+            for (int nb = 0; nb < NB; ++nb) {
+              char *base = sh.stage[st] + nb * N * 128 + c * 16;
+              uint32_t top = 0;
+              for (int r0 = from; r0 < N; r0 += 32) {                // eight rows of a lane at a time
+                uint4 v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  const int r = r0 + 4 * k + (lane >> 3);
+                  v[k] = r < N ? *reinterpret_cast<const uint4 *>(base + r * 128) : make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  const uint32_t m = 0x7FFF7FFFu, most = __vmaxu2(__vmaxu2(v[k].x & m, v[k].y & m), __vmaxu2(v[k].z & m, v[k].w & m));
+                  if (all_live || is_live(r0 + 4 * k + (lane >> 3))) top = __vmaxu2(top, most);
                 }
               }
+              found = found || (top & 0xFFFFu) >= 0x7F80u || (top >> 16) >= 0x7F80u;
+              if (!all_live)
+                for (int r = from + (lane >> 3); r < N; r += 4)
+                  if (!is_live(r)) *reinterpret_cast<uint4 *>(base + r * 128) = make_uint4(0, 0, 0, 0);
+            }
             __syncwarp();
             found = __any_sync(0xffffffffu, found);
             if (found) {                                               // (rare)
@@ -802,7 +823,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
               poisoned = true;
               __syncwarp();
               for (int nb = 0; nb < NB; ++nb)
-                for (int r0 = 0; r0 < N; r0 += 4) {
+                for (int r0 = from; r0 < N; r0 += 4) {
                   const int r = r0 + (lane >> 3);
                   __nv_bfloat16 *p = reinterpret_cast<__nv_bfloat16 *>(sh.stage[st] + (nb * N + r) * 128 + c * 16);
                   for (int e = 0; e < 8; ++e) {

@@ -40,8 +40,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_f32(const __grid_constant
   pdl_wait();
   pdl_trigger();
   ChunkCuts cuts;
-  ChunkLine line = chunk_line<kThreads>(a, kRows, kTileF, sh.line, *reinterpret_cast<ChunkLineSetup *>(sh.k[0]), cuts);
-  if (tid < 32) cuts.write(a, line, kRows, kTileF);
+  ChunkLine line = chunk_line<kThreads, kRows, kTileF>(a, sh.line, *reinterpret_cast<ChunkLineSetup *>(sh.k[0]), cuts);
+  if (tid < 32) cuts.write<kRows, kTileF>(a, line);
   ChunkSegment s = {};
   const int chunks = a.d_h / 4;
   // rows [row0, row0 + 64) of a request, those it has; each thread a quarter of a row
@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_f32(const __grid_constant
     if ((tid & 3) == 0) sh.bias[buf][row] = id < 0 ? -INFINITY : a.logw ? a.logw[(long long)id * a.page + off] : 0.f;
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  while (line.next(a, kRows, kTileF, s)) {
+  while (line.next<kRows, kTileF>(a, s)) {
     const int n = s.j1 - s.j0;
     __syncthreads();                                                 // (the segment before is done with the shared memory)
     load(s.j0, 0);

@@ -41,7 +41,7 @@ struct ChunkSegment : ChunkRequest {
 };
 
 constexpr int kChunkPreInSmem = 33;        // entries of `pre` that are kept in shared memory
-constexpr int kChunkKept = 8;              // requests that are
+constexpr int kChunkKept = 16;             // requests that are
 
 struct ChunkLine {
   const int *pre, *head;
@@ -50,7 +50,7 @@ struct ChunkLine {
   int q, off, tail;                        // where this CTA's part of the rests begins, and its tiles
   // walking through the segments
   int done, stage;
-  __device__ __forceinline__ void item(const ChunkArgs &a, int x, int rows, int tile, ChunkSegment &s) const {
+  template <int ROWS, int TILE> __device__ __forceinline__ void item(const ChunkArgs &a, int x, ChunkSegment &s) const {
     int lo = 0, hi = a.B;
     const int H = a.n_kvh;
     while (hi - lo > 1) {
@@ -63,14 +63,14 @@ struct ChunkLine {
     s.b = lo;
     s.kv = at / n;
     const int i = at - s.kv * n;
-    s.first = i * rows;
-    s.rows = min(rows, s.n * a.group - s.first);
-    s.k = chunk_tiles(s, i, a.group, rows, tile, a.causal);
+    s.first = i * ROWS;
+    s.rows = min(ROWS, s.n * a.group - s.first);
+    s.k = chunk_tiles(s, i, a.group, ROWS, TILE, a.causal);
   }
-  __device__ __forceinline__ bool next(const ChunkArgs &a, int rows, int tile, ChunkSegment &s) {
+  template <int ROWS, int TILE> __device__ __forceinline__ bool next(const ChunkArgs &a, ChunkSegment &s) {
     const int G = gridDim.x, me = blockIdx.x;
     if (done < rounds) {
-      item(a, me + done++ * G, rows, tile, s);
+      item<ROWS, TILE>(a, me + done++ * G, s);
       s.j0 = 0;
       s.j1 = s.k;
       s.slot = -1;
@@ -79,7 +79,7 @@ struct ChunkLine {
     if (stage == 0) {
       stage = 1;
       if (me < r && head[me] > 0) {
-        item(a, last + me, rows, tile, s);
+        item<ROWS, TILE>(a, last + me, s);
         s.j0 = 0;
         s.j1 = head[me];
         s.slot = s.j1 == s.k ? -1 : me;
@@ -87,7 +87,7 @@ struct ChunkLine {
       }
     }
     while (tail > 0) {
-      item(a, last + q, rows, tile, s);
+      item<ROWS, TILE>(a, last + q, s);
       s.j0 = (q < G ? head[q] : 0) + off;
       s.j1 = min(s.k, s.j0 + tail);
       s.slot = s.j0 == 0 && s.j1 == s.k ? -1 : G + q + me;
@@ -161,7 +161,7 @@ struct ChunkCuts {
     for (int i = 0; i < kWords; ++i) n += __popc(__ballot_sync(0xffffffffu, tp[i] <= t));
     return n - 1;
   }
-  __device__ __forceinline__ void write(const ChunkArgs &a, const ChunkLine &line, int rows, int tile) const {   // a whole warp
+  template <int ROWS, int TILE> __device__ __forceinline__ void write(const ChunkArgs &a, const ChunkLine &line) const {   // a whole warp
     const int G = gridDim.x, me = blockIdx.x;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -172,7 +172,7 @@ struct ChunkCuts {
         cut.last = owner(to[k] - 1);
         cut.cut = cut.head || cut.first != cut.last;
         ChunkSegment s;
-        line.item(a, line.last + q, rows, tile, s);
+        line.item<ROWS, TILE>(a, line.last + q, s);
         cut.kv = s.kv;
         cut.rows = s.rows;
         cut.first_row = s.first;
@@ -184,7 +184,7 @@ struct ChunkCuts {
 };
 
 // Called by all threads of the CTA, at least as many as the grid has CTAs.
-template <int THREADS> __device__ __forceinline__ ChunkLine chunk_line(const ChunkArgs &a, int rows, int tile, ChunkLineKept &kept, ChunkLineSetup &set, ChunkCuts &cuts) {
+template <int THREADS, int ROWS, int TILE> __device__ __forceinline__ ChunkLine chunk_line(const ChunkArgs &a, ChunkLineKept &kept, ChunkLineSetup &set, ChunkCuts &cuts) {
   static_assert(THREADS >= kChunkMaxSms, "");
   constexpr int PER = (2 * kChunkMaxSms + THREADS - 1) / THREADS;    // items of the last round that a thread looks at
   const int tid = threadIdx.x, G = gridDim.x, me = blockIdx.x;
@@ -208,8 +208,8 @@ template <int THREADS> __device__ __forceinline__ ChunkLine chunk_line(const Chu
       if (a.B <= kChunkKept) kept.request[b] = q;
       if (q.bad && me == 0 && a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
       pre[b] = mine;
-      mine += chunk_items(q, a.group, rows);
-      tiles += chunk_tiles_of_head(q, a.group, rows, tile, a.causal);
+      mine += chunk_items(q, a.group, ROWS);
+      tiles += chunk_tiles_of_head(q, a.group, ROWS, TILE, a.causal);
     }
     if (tiles) atomicAdd(&set.tiles, tiles);
     const int before = chunk_scan<THREADS>(mine, set.warp, &total);
@@ -223,26 +223,21 @@ template <int THREADS> __device__ __forceinline__ ChunkLine chunk_line(const Chu
   line.last = line.rounds * G;
   line.r = items - line.last;
   ChunkSegment s;
-  if (tid < G) {
-    int mine = 0;
-    for (int w = 0; w < line.rounds; ++w) {
-      line.item(a, tid + w * G, rows, tile, s);
-      mine += s.k;
-    }
-    set.dp[tid] = mine;
+  if (tid < G) set.dp[tid] = 0;
+  __syncthreads();
+  for (int x = tid; x < line.last; x += THREADS) {
+    line.item<ROWS, TILE>(a, x, s);
+    atomicAdd(&set.dp[x % G], s.k);
   }
   __syncthreads();
   // tiles that a CTA may have: those with more already are left out of the mean
   int most = (int)((T + G - 1) / G);
   if (line.rounds > 0)
     for (int round = 0; round < 4; ++round) {
-      long long over = 0;
-      int n = 0;
-      for (int c = 0; c < G; ++c)
-        if (set.dp[c] > most) {
-          over += set.dp[c];
-          ++n;
-        }
+      const int mine = tid < G && set.dp[tid] > most ? set.dp[tid] : 0;
+      int over, n;
+      (void)chunk_scan<THREADS>(mine, set.warp, &over);
+      n = __syncthreads_count(mine > 0);
       if (n == 0 || n == G) break;
       most = (int)((T - over + G - n - 1) / (G - n));
     }
@@ -252,7 +247,7 @@ template <int THREADS> __device__ __forceinline__ ChunkLine chunk_line(const Chu
     begins[k] = rest[k] = room[k] = 0;
     if (q < G) room[k] = max(0, most - set.dp[q]);
     if (q < line.r) {
-      line.item(a, line.last + q, rows, tile, s);
+      line.item<ROWS, TILE>(a, line.last + q, s);
       begins[k] = min(s.k, room[k]);
       rest[k] = s.k - begins[k];
     }

@@ -9,26 +9,32 @@ namespace pact {
 
 // sum of floor((a i + b) / m) over i = 0 .. n - 1: whole multiples of m leave a and b, what is left counts lattice points below a line, and counting them
 // along the other axis gives a shorter sum of the same kind (the steps of Euclid's algorithm).
-PAGED_HD unsigned long long floor_sum(unsigned long long n, unsigned long long m, unsigned long long a, unsigned long long b) {
+// (In 32 bits where they are enough: a division in 64 takes as long as the rest of the set-up of a call with few requests.)
+template <typename I> PAGED_HD unsigned long long floor_sum_in(I n, I m, I a, I b) {
   unsigned long long sum = 0;
   while (n) {
     if (a >= m) {
-      sum += (n & 1 ? n * ((n - 1) / 2) : n / 2 * (n - 1)) * (a / m);
+      sum += (unsigned long long)(n & 1 ? (unsigned long long)n * ((n - 1) / 2) : (unsigned long long)(n / 2) * (n - 1)) * (a / m);
       a %= m;
     }
     if (b >= m) {
-      sum += n * (b / m);
+      sum += (unsigned long long)n * (b / m);
       b %= m;
     }
-    const unsigned long long top = a * n + b;
+    const I top = a * n + b;
     if (top < m) break;
     n = top / m;
     b = top % m;
-    const unsigned long long t = m;
+    const I t = m;
     m = a;
     a = t;
   }
   return sum;
+}
+PAGED_HD unsigned long long floor_sum(unsigned long long n, unsigned long long m, unsigned long long a, unsigned long long b) {
+  // (a and b fall below m in the first step and m never grows, so a n + b stays below m (n + 1))
+  if (n < (1u << 31) && m < (1u << 31) && a < (1u << 31) && b < (1ull << 32) && m * (n + 1) < (1ull << 32)) return floor_sum_in<unsigned>((unsigned)n, (unsigned)m, (unsigned)a, (unsigned)b);
+  return floor_sum_in<unsigned long long>(n, m, a, b);
 }
 
 // One request of a chunk: `n` new tokens that are served out of `want`, the last of `len` cached rows.
