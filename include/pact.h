@@ -451,6 +451,75 @@ size_t pact_chunk_workspace_bytes(const pact_ctx *ctx, int max_requests);
  * length) see nothing; each sets status to INVALID_ARG.  Heads as above; n_rows * (n_qh / n_kvh) below 2^31. */
 pact_status pact_chunk_attention(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_chunk *c /*host*/, void *stream);
 
+/* Pages that several requests hold: answers to one prompt, beams, prompts kept for requests to come.  `shared` (device int32[n_pages]) counts the holders of a page beside the first:
+ * 0 for a page that one request holds, as pact_cache_plan hands them out, and for a free one.  A program whose requests share pages ends them with pact_cache_fork (source -1), not with
+ * pact_cache_plan, and counts a hold of its own (a prompt that it keeps) there itself.
+ *
+ * pact_cache_fork: request b goes on with the first rows[b] rows of what request source[b] has before the call; source[b] = b keeps (or cuts) its own, -1 ends it, and a request that was empty may get
+ * another's.  Whole pages are shared.  A page that the last rows fill in part is kept by the first request that ends in it if nobody else holds it afterwards; every other such
+ * request gets a page of its own, off the top of the free stack, and an entry {from, to, rows} in `copies`, which pact_page_copy carries out for every layer (in the order of the requests).  Pages that
+ * nobody holds any more are pushed on the stack first, in the order of the first places (request, then place) that named them.
+ * A call that cannot be served as a whole leaves everything as it is: the tables, lengths, counts, stack and n_free_out repeat the old ones, there are no copies, and status becomes PACT_ERR_NO_PAGES or
+ * PACT_ERR_INVALID_ARG (a length outside 0 .. max_pages * page_rows, a source that is none, rows outside 0 .. the source's length, a page id outside the cache, n_free outside 0 .. n_pages, a page named
+ * by more requests than it has holders). */
+typedef struct {
+  int32_t page_rows, n_pages, n_requests, max_pages;
+  const int32_t *block_table;   /* [n_requests][max_pages]                                          */
+  const int32_t *length;        /* [n_requests]                                                     */
+  const int32_t *source;        /* [n_requests]                                                     */
+  const int32_t *rows;          /* [n_requests]; NULL: all of the source's                          */
+  const int32_t *shared;        /* [n_pages]                                                        */
+  const int32_t *free_pages;    /* [n_pages], a stack as in pact_plan                               */
+  const int32_t *n_free;        /* [1]                                                              */
+  int32_t *block_table_out;     /* [n_requests][max_pages], another buffer than block_table; entries behind a request's last page are left alone */
+  int32_t *length_out;          /* [n_requests], another buffer than length                         */
+  int32_t *shared_out;          /* [n_pages]; may be shared                                         */
+  int32_t *free_out;            /* [n_pages]; may be free_pages; entries above the new top are left alone */
+  int32_t *n_free_out;          /* [1]; may be n_free                                               */
+  int32_t *copies;              /* [n_requests][3]; -1, -1, 0 behind the last                       */
+  int32_t *n_copies;            /* [1]                                                              */
+  int32_t *status;
+  void *ws;                     /* workspace, 256-byte aligned                                      */
+  size_t ws_bytes;
+} pact_fork;
+pact_status pact_cache_fork(pact_ctx *ctx, const pact_fork *f /*host*/, void *stream);
+
+/* pact_cache_compact: the pages in use to the lowest ids, so that the rest of a cache may be given back or used otherwise.  With n_used = n_pages - n_free, the k-th (by id) used page from id n_used
+ * on moves to the k-th free one below; tables and counts follow, the stack becomes n_pages - 1, .., n_used (the lowest on top), and `copies` lists the moves for pact_page_copy, which no page appears
+ * in twice.  moved_to[p] is where page p is now, for holders that are not in these tables.  Every page that is not on the stack counts as used.
+ * A stack that names a page twice, or one outside the cache, or n_free outside 0 .. n_pages: nothing moves, and status becomes INVALID_ARG.  Lengths are clamped, entries outside the cache repeated; both set
+ * status. */
+typedef struct {
+  int32_t page_rows, n_pages, n_requests, max_pages;
+  const int32_t *block_table, *length, *shared, *free_pages, *n_free;   /* as above */
+  int32_t *block_table_out;     /* may be block_table; entries behind a request's last page are left alone */
+  int32_t *shared_out;          /* may be shared                                                    */
+  int32_t *free_out;            /* [n_pages]; may be free_pages; the first n_free are written       */
+  int32_t *moved_to;            /* [n_pages]                                                        */
+  int32_t *copies;              /* [n_list][3]; -1, -1, 0 behind the last                           */
+  int32_t n_list;               /* at least n_pages / 2                                             */
+  int32_t reserved;
+  int32_t *n_copies;            /* [1]                                                              */
+  int32_t *status;
+  void *ws;
+  size_t ws_bytes;
+} pact_compact;
+pact_status pact_cache_compact(pact_ctx *ctx, const pact_compact *c /*host*/, void *stream);
+
+/* Bytes of device workspace that the two calls need; no initialisation, nothing kept between calls. */
+size_t pact_share_workspace_bytes(const pact_ctx *ctx, int max_requests, int max_pages, int n_pages);
+
+/* Copies of one layer: the first `rows` rows of page `from` to page `to`, keys, values and biases; where the cache keeps bounds, those of the page (of more rows than are copied, perhaps: bounds still) and
+ * its w_max.  Entries with from < 0 or rows <= 0 are skipped; one with a page outside the cache, more rows than a page has, or twice the same page is skipped and sets status to INVALID_ARG.
+ * No page is written twice, or both read and written. */
+typedef struct {
+  const int32_t *copies;        /* [n_list][3]                                                      */
+  const int32_t *n_copies;      /* [1], how many count; NULL: all                                   */
+  int32_t *status;
+  int32_t n_list, reserved;
+} pact_copies;
+pact_status pact_page_copy(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_copies *c /*host*/, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

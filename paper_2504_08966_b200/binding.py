@@ -28,7 +28,8 @@ EXPORTS = ["pact_create", "pact_destroy", "pact_workspace_bytes", "pact_status_s
            "pact_host_staging_bytes", "pact_launch_count", "pact_profile_enable", "pact_profile_read",
            "pact_profile_stage_name", "pact_graph_create", "pact_graph_launch", "pact_graph_destroy",
            "pact_key_spread", "pact_set_wait_limits", "pact_cache_plan", "pact_cache_write", "pact_page_select",
-           "pact_paged_attention", "pact_paged_workspace_bytes", "pact_chunk_attention", "pact_chunk_workspace_bytes"]
+           "pact_paged_attention", "pact_paged_workspace_bytes", "pact_chunk_attention", "pact_chunk_workspace_bytes", "pact_cache_fork",
+           "pact_cache_compact", "pact_page_copy", "pact_share_workspace_bytes"]
 
 
 class Params(C.Structure):
@@ -52,11 +53,14 @@ class PagedCacheDesc(C.Structure):
                 ("bounds", C.c_void_p), ("w_max", C.c_void_p), ("n_pages", C.c_int32), ("page_rows", C.c_int32)]
 
 
-# pact_plan, pact_new_rows, pact_query and pact_chunk of pact.h: packed into a buffer of the context, a tenth of the time of as many ctypes arguments
+# pact_plan, pact_new_rows, pact_query, pact_chunk, pact_fork, pact_compact and pact_copies of pact.h: packed into a buffer of the context, a tenth of the time of as many ctypes arguments
 _PLAN = struct.Struct("@4iPPPqPPPPPPqiiP")
 _NEW_ROWS = struct.Struct("@PPqqPPqP")
 _QUERY = struct.Struct("@PqqPPiiPiiifPqqPPPN")
 _CHUNK = struct.Struct("@PqqPPPqPqiiiifiPqqPPPN")
+_FORK = struct.Struct("@4i16PN")
+_COMPACT = struct.Struct("@4i10Pii3PN")
+_COPIES = struct.Struct("@PPPii")
 
 _lib = None
 
@@ -109,6 +113,11 @@ def lib():
         L.pact_chunk_attention.argtypes = [vp, pc, vp, vp]
         L.pact_chunk_workspace_bytes.argtypes = [vp, i32]
         L.pact_chunk_workspace_bytes.restype = sz
+        L.pact_cache_fork.argtypes = [vp, vp, vp]
+        L.pact_cache_compact.argtypes = [vp, vp, vp]
+        L.pact_page_copy.argtypes = [vp, pc, vp, vp]
+        L.pact_share_workspace_bytes.argtypes = [vp, i32, i32, i32]
+        L.pact_share_workspace_bytes.restype = sz
         for name in EXPORTS:
             if getattr(L, name).restype is C.c_int:
                 getattr(L, name).restype = C.c_int
@@ -287,6 +296,7 @@ class Context:
         self._paged_ws = []                  # workspaces of the paged cache's calls: address, size, tensor; the last one is in use
         self._paged_need = {}
         self._chunk_ws, self._chunk_need = [], {}   # the same of pact_chunk_attention
+        self._share_ws, self._share_need = [], {}   # and of pact_cache_fork and pact_cache_compact
         self._make_args()
 
     def close(self):
@@ -396,7 +406,7 @@ class Context:
     # (A call of a decoding step takes the GPU a few microseconds, and looking at nine tensors one function call each takes as long: the methods test
     # everything in one expression and ask _explain only when it fails.)
     def _make_args(self):
-        self._args = C.create_string_buffer(max(_PLAN.size, _NEW_ROWS.size, _QUERY.size, _CHUNK.size))
+        self._args = C.create_string_buffer(max(x.size for x in (_PLAN, _NEW_ROWS, _QUERY, _CHUNK, _FORK, _COMPACT, _COPIES)))
         self._args_at = C.addressof(self._args)
         self._kind = (self.n_kvh, self.d_h, self.in_dtype, self.device)
 
@@ -578,6 +588,76 @@ class Context:
                          0 if row_start is None else row_start.data_ptr(), n, row_stride, B, W, 1 if causal else 0, d_h ** -0.5 if scale is None else scale, 0,
                          out.data_ptr(), o0, oh, 0 if lse is None else lse.data_ptr(), 0 if status is None else status.data_ptr(), w, size)
         r = self._L.pact_chunk_attention(self.handle, cache.ref, self._args_at, _stream())
+        if r:
+            _check(self.handle, r)
+
+    # ---- pages that several requests hold ---------------------------------------------------
+    def _share_workspace(self, B, max_pages, n_pages):
+        need = self._share_need.get((B, max_pages, n_pages))
+        if need is None:
+            if len(self._share_need) >= 4096:
+                self._share_need.clear()
+            need = self._share_need[(B, max_pages, n_pages)] = int(self._L.pact_share_workspace_bytes(self.handle, B, max_pages, n_pages))
+        have = self._share_ws[-1] if self._share_ws else None
+        if have is None or have[1] < need:   # (one that is outgrown is kept, as with _paged_workspace)
+            size = max(need, min(2 * have[1], 64 << 20) if have else 256)
+            ws = torch.empty(size, dtype=torch.uint8, device=self._cuda())
+            self._share_ws.append((ws.data_ptr(), size, ws))
+        return self._share_ws[-1]
+
+    def _words(self, *wanted):
+        """Whether all of these (tensor or None, number of elements) are dense int32 tensors of the context's device."""
+        i32, dev = torch.int32, self.device
+        return all(t is None or t.dtype is i32 and t.get_device() == dev and t.numel() == n and t.is_contiguous() for t, n in wanted)
+
+    def pact_cache_fork(self, page_rows, block_table, length, source, shared, free_pages, n_free, block_table_out, length_out, shared_out, free_out, n_free_out, copies,
+                        n_copies, rows=None, status=None):
+        """Requests that go on with the rows of others (pact_cache_fork in pact.h): block_table, block_table_out [B, max_pages], length, source, length_out, rows [B]
+        (None: all rows), shared, shared_out, free_pages, free_out [n_pages], n_free, n_free_out, n_copies [1], copies [B, 3], all int32."""
+        i32 = torch.int32
+        B, W = block_table.shape if block_table.ndim == 2 else (-1, -1)
+        P = free_pages.numel()
+        if block_table.ndim != 2 or not self._words((block_table, B * W), (block_table_out, B * W), (length, B), (length_out, B), (source, B), (rows, B), (shared, P), (shared_out, P),
+                                                    (free_pages, P), (free_out, P), (n_free, 1), (n_free_out, 1), (copies, 3 * B), (n_copies, 1), (status, 1)):
+            self._explain(None, (block_table, i32, (None, None), False, "block_table"), (block_table_out, i32, (B, W), False, "block_table_out"), (length, i32, (B,), False, "length"),
+                          (length_out, i32, (B,), False, "length_out"), (source, i32, (B,), False, "source"), (rows, i32, (B,), False, "rows"), (free_pages, i32, (None,), False, "free_pages"),
+                          (shared, i32, (P,), False, "shared"), (shared_out, i32, (P,), False, "shared_out"), (free_out, i32, (P,), False, "free_out"), (n_free, i32, (1,), False, "n_free"),
+                          (n_free_out, i32, (1,), False, "n_free_out"), (copies, i32, (B, 3), False, "copies"), (n_copies, i32, (1,), False, "n_copies"), (status, i32, (1,), False, "status"))
+        w, size, _ = self._share_workspace(B, W, P)
+        _FORK.pack_into(self._args, 0, page_rows, P, B, W, block_table.data_ptr(), length.data_ptr(), source.data_ptr(), 0 if rows is None else rows.data_ptr(), shared.data_ptr(),
+                        free_pages.data_ptr(), n_free.data_ptr(), block_table_out.data_ptr(), length_out.data_ptr(), shared_out.data_ptr(), free_out.data_ptr(), n_free_out.data_ptr(),
+                        copies.data_ptr(), n_copies.data_ptr(), 0 if status is None else status.data_ptr(), w, size)
+        r = self._L.pact_cache_fork(self.handle, self._args_at, _stream())
+        if r:
+            _check(self.handle, r)
+
+    def pact_cache_compact(self, page_rows, block_table, length, shared, free_pages, n_free, block_table_out, shared_out, free_out, moved_to, copies, n_copies, status=None):
+        """The pages in use to the lowest ids (pact_cache_compact in pact.h): block_table, block_table_out [B, max_pages], length [B], shared, shared_out, free_pages, free_out,
+        moved_to [n_pages], n_free, n_copies [1], copies [at least n_pages // 2, 3], all int32."""
+        i32 = torch.int32
+        B, W = block_table.shape if block_table.ndim == 2 else (-1, -1)
+        P, room = free_pages.numel(), copies.shape[0]
+        if block_table.ndim != 2 or not self._words((block_table, B * W), (block_table_out, B * W), (length, B), (shared, P), (shared_out, P), (free_pages, P), (free_out, P),
+                                                    (moved_to, P), (n_free, 1), (copies, 3 * room), (n_copies, 1), (status, 1)):
+            self._explain(None, (block_table, i32, (None, None), False, "block_table"), (block_table_out, i32, (B, W), False, "block_table_out"), (length, i32, (B,), False, "length"),
+                          (free_pages, i32, (None,), False, "free_pages"), (shared, i32, (P,), False, "shared"), (shared_out, i32, (P,), False, "shared_out"),
+                          (free_out, i32, (P,), False, "free_out"), (moved_to, i32, (P,), False, "moved_to"), (n_free, i32, (1,), False, "n_free"), (copies, i32, (None, 3), False, "copies"),
+                          (n_copies, i32, (1,), False, "n_copies"), (status, i32, (1,), False, "status"))
+        w, size, _ = self._share_workspace(B, W, P)
+        _COMPACT.pack_into(self._args, 0, page_rows, P, B, W, block_table.data_ptr(), length.data_ptr(), shared.data_ptr(), free_pages.data_ptr(), n_free.data_ptr(),
+                           block_table_out.data_ptr(), shared_out.data_ptr(), free_out.data_ptr(), moved_to.data_ptr(), copies.data_ptr(), room, 0, n_copies.data_ptr(),
+                           0 if status is None else status.data_ptr(), w, size)
+        r = self._L.pact_cache_compact(self.handle, self._args_at, _stream())
+        if r:
+            _check(self.handle, r)
+
+    def pact_page_copy(self, cache: PagedCache, copies, n_copies=None, status=None):
+        """Copies of one layer's rows from page to page: copies [n, 3] int32 (from, to, rows), of which the first n_copies [1] count (None: all)."""
+        n = copies.shape[0]
+        if cache.kind != self._kind or copies.ndim != 2 or not self._words((copies, 3 * n), (n_copies, 1), (status, 1)):
+            self._explain(cache, (copies, torch.int32, (None, 3), False, "copies"), (n_copies, torch.int32, (1,), False, "n_copies"), (status, torch.int32, (1,), False, "status"))
+        _COPIES.pack_into(self._args, 0, copies.data_ptr(), 0 if n_copies is None else n_copies.data_ptr(), 0 if status is None else status.data_ptr(), n, 0)
+        r = self._L.pact_page_copy(self.handle, cache.ref, self._args_at, _stream())
         if r:
             _check(self.handle, r)
 

@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpact.so")
 LIB_TIMELINE = os.path.join(HERE, "libpact_timeline.so")   # instrumented build (per-CTA timestamps), see timeline.py
 SOURCES = ["api.cu", "euti.cu", "cluster.cu", "gram_umma.cu", "merge.cu", "small.cu", "prune_static.cu", "cache_plan.cu", "cache_write.cu",
-           "page_select.cu", "paged_attention.cu", "paged_api.cu", "chunk_attention.cu", "chunk_f32.cu", "chunk_join.cu", "chunk_api.cu"]
+           "page_select.cu", "paged_attention.cu", "paged_api.cu", "chunk_attention.cu", "chunk_f32.cu", "chunk_join.cu", "chunk_api.cu", "cache_share.cu", "page_copy.cu",
+           "share_api.cu"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 
