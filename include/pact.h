@@ -151,7 +151,7 @@ const char *pact_last_cuda_error(const pact_ctx *ctx);
  * kernel stops waiting, writes PACT_ERR_TIMEOUT to counters[PACT_CNT_STATUS] of the image and carries on
  * within bounds; the call itself still returns PACT_OK and the outputs of that image are not valid.
  * The waits of pact_paged_attention for its copies are bounded too; there the status of the call becomes PACT_ERR_TIMEOUT.
- * barrier_polls: polls of the member-list barrier, and of each wait of pact_paged_attention (default: as many as fit into a second);
+ * barrier_polls: polls of the member-list barrier, and of each wait of pact_paged_attention and pact_chunk_attention (default: as many as fit into a second);
  * center_sweeps: sweeps of the centre selection (rows that are
  * still open are then decided without waiting, in at most one pass per surviving token; the same happens, with no
  * status, when no row has been removed for 512 sweeps); 0 restores the default (about a million).  Graphs recorded
@@ -419,7 +419,7 @@ typedef struct {
   const int32_t *length;      /* [n_requests] cached rows, those of the new tokens among them (the length_out of pact_cache_plan) */
   const int32_t *n_new;       /* [n_requests] with stride n_new_stride >= 1: new tokens, the last of the cached rows; 0 or less: none */
   int64_t n_new_stride;
-  const int32_t *row_start;   /* [n_requests]: token i of request b is row row_start[b] + i; NULL with a row_stride */
+  const int32_t *row_start;   /* [n_requests]: token i of request b is row row_start[b] + i (none of them where row_start[b] < 0); NULL with a row_stride */
   int64_t n_rows;             /* rows that Q, out and lse have                                      */
   int32_t row_stride;         /* > 0: token i of request b is row b * row_stride + i, and n_rows = n_requests * row_stride */
   int32_t n_requests, max_pages;
@@ -446,8 +446,8 @@ size_t pact_chunk_workspace_bytes(const pact_ctx *ctx, int max_requests);
  * without any row gets 0, and lse minus infinity.  Infinities and NaN in rows that count leave infinities or NaN in the results that they enter (infinite values beside bf16 keys: NaN).
  * Rows of Q, out and lse that belong to no token are not touched.
  * Logits, softmax statistics and sums are fp32.  bf16 keys and values: probabilities are rounded to bf16 where results are bf16, and carried as
- * three bf16 terms where they are fp32.
- * Lengths outside 0 .. max_pages * page_rows are clamped, rows of pages outside the cache left out, tokens without a row of Q left out, and tokens before the first cached row (n_new above
+ * three bf16 terms where they are fp32; bf16 results take logits in powers of two, so that finite biases beyond 2.35e38 in magnitude count as the largest number.
+ * Lengths outside 0 .. max_pages * page_rows are clamped, rows of pages outside the cache left out, tokens without a row of Q (beyond n_rows or the row_stride) left out, and tokens before the first cached row (n_new above
  * length) see nothing; each sets status to INVALID_ARG.  Heads as above; n_rows * (n_qh / n_kvh) below 2^31. */
 pact_status pact_chunk_attention(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_chunk *c /*host*/, void *stream);
 

@@ -62,6 +62,8 @@ _FORK = struct.Struct("@4i16PN")
 _COMPACT = struct.Struct("@4i10Pii3PN")
 _COPIES = struct.Struct("@PPPii")
 
+MAX_REQUESTS = 4096   # PACT_MAX_REQUESTS of pact.h
+
 _lib = None
 
 
@@ -295,7 +297,7 @@ class Context:
         self.device = torch.cuda.current_device()
         self._paged_ws = []                  # workspaces of the paged cache's calls: address, size, tensor; the last one is in use
         self._paged_need = {}
-        self._chunk_ws, self._chunk_need = [], {}   # the same of pact_chunk_attention
+        self._chunk_ws = None                       # the workspace of pact_chunk_attention
         self._share_ws, self._share_need = [], {}   # and of pact_cache_fork and pact_cache_compact
         self._make_args()
 
@@ -411,7 +413,7 @@ class Context:
         self._kind = (self.n_kvh, self.d_h, self.in_dtype, self.device)
 
     def _explain(self, cache, *wanted):
-        """Raises for the first of these that is not what is wanted: (tensor or None, dtype, shape, what), dense or, for [.., heads, d_h], strided."""
+        """Raises for the first of these that is not what is wanted: (tensor or None, dtype, shape, strided, what), dense or, where strided, with a dense last axis (of several)."""
         if cache is not None and cache.kind != self._kind:
             raise PactError(f"the cache is not one of {self.n_kvh} key heads of {self.d_h} {self.in_dtype} on cuda:{self.device}")
         for t, dtype, shape, strided, what in wanted:
@@ -419,7 +421,7 @@ class Context:
                 continue
             if t.dtype != dtype or t.get_device() != self.device or t.ndim != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
                 raise PactError(f"{what}: a {dtype} tensor of shape [{', '.join('..' if n is None else str(n) for n in shape)}] on cuda:{self.device} is wanted")
-            if not t.is_contiguous() if not strided else t.stride()[-1] != 1 and t.shape[-1] != 1:
+            if not t.is_contiguous() if not strided else t.ndim > 1 and t.stride()[-1] != 1 and t.shape[-1] != 1:
                 raise PactError(f"{what}: {'a contiguous tensor is wanted' if not strided else 'the last axis has to be contiguous'}")
         raise PactError("the arguments do not fit together")
 
@@ -549,16 +551,12 @@ class Context:
             _check(self.handle, r)
 
     # ---- several new tokens per request ---------------------------------------------------
-    def _chunk_workspace(self, B):
-        """Address and size; as with _paged_workspace one that is outgrown is kept.  (Parts of items take most of it, whatever B is.)"""
-        need = self._chunk_need.get(B)
-        if need is None:
-            need = self._chunk_need[B] = int(self._L.pact_chunk_workspace_bytes(self.handle, B))
-        have = self._chunk_ws[-1] if self._chunk_ws else None
-        if have is None or have[1] < need:
-            ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self._cuda())
-            self._chunk_ws.append((ws.data_ptr(), ws.numel(), ws))
-        return self._chunk_ws[-1]
+    def _chunk_workspace(self):
+        """Address and size: one for any number of requests (parts of items take most of it), so that none is ever outgrown."""
+        if self._chunk_ws is None:
+            ws = torch.empty(max(256, int(self._L.pact_chunk_workspace_bytes(self.handle, MAX_REQUESTS))), dtype=torch.uint8, device=self._cuda())
+            self._chunk_ws = (ws.data_ptr(), ws.numel(), ws)
+        return self._chunk_ws
 
     def pact_chunk_attention(self, cache: PagedCache, Q, block_table, length, n_new, out, row_start=None, row_stride=0, lse=None, causal=True, scale=None,
                              status=None):
@@ -580,8 +578,8 @@ class Context:
                 and (status is None or status.dtype is i32 and status.get_device() == dev and status.numel() == 1)):
             self._explain(cache, (block_table, i32, (None, None), False, "block_table"), (Q, self.in_dtype, (None, heads, d_h), True, "Q"),
                           (out, self.out_dtype, shape, True, "out"), (length, i32, (B,), False, "length"), (n_new, i32, (B,), True, "n_new"),
-                          (row_start, i32, (None,), False, "row_start"), (lse, torch.float32, (n, heads), False, "lse"), (status, i32, (1,), False, "status"))
-        w, size, _ = self._chunk_workspace(B)
+                          (row_start, i32, (B if row_start is None or row_start.numel() <= B else B + 1,), False, "row_start"), (lse, torch.float32, (n, heads), False, "lse"), (status, i32, (1,), False, "status"))
+        w, size, _ = self._chunk_workspace()
         qh, oh = (q[1], o[1]) if heads > 1 else (d_h, d_h)
         q0, o0 = (q[0], o[0]) if n > 1 else (qh * heads, oh * heads)
         _CHUNK.pack_into(self._args, 0, Q.data_ptr(), q0, qh, block_table.data_ptr(), length.data_ptr(), n_new.data_ptr(), n_new.stride()[0] if B > 1 else 1,

@@ -20,8 +20,8 @@ pact_status pact_chunk_attention(pact_ctx *ctx, const pact_paged_cache *cache, c
   if (s == PACT_OK) s = check_cache(ctx, cache);
   if (s != PACT_OK) return s;
   const size_t oe = ctx->out == PACT_BF16 ? 2 : 4;
-  if (!c->Q || !aligned16(c->Q) || !stride_ok(ctx, c->ldQ) || !stride_ok(ctx, c->ldQh) || !isfinite(c->scale)) return PACT_ERR_INVALID_ARG;
-  if (!c->out || reinterpret_cast<uintptr_t>(c->out) % (4 * oe) != 0) return PACT_ERR_INVALID_ARG;
+  if ((!c->Q && c->n_rows) || !aligned16(c->Q) || !stride_ok(ctx, c->ldQ) || !stride_ok(ctx, c->ldQh) || !isfinite(c->scale)) return PACT_ERR_INVALID_ARG;
+  if ((!c->out && c->n_rows) || reinterpret_cast<uintptr_t>(c->out) % (4 * oe) != 0) return PACT_ERR_INVALID_ARG;
   if (c->ldO < ctx->d_h || c->ldOh < ctx->d_h || c->ldO % 4 != 0 || c->ldOh % 4 != 0) return PACT_ERR_INVALID_ARG;
   if (!c->n_new || c->n_new_stride < 1 || c->n_rows < 0 || c->row_stride < 0 || (c->causal != 0 && c->causal != 1)) return PACT_ERR_INVALID_ARG;
   if (c->row_stride ? c->row_start || c->n_rows != (int64_t)c->n_requests * c->row_stride : !c->row_start) return PACT_ERR_INVALID_ARG;
@@ -33,7 +33,6 @@ pact_status pact_chunk_attention(pact_ctx *ctx, const pact_paged_cache *cache, c
   if (c->n_rows > INT32_MAX / group || items > INT32_MAX / 2 || items > INT32_MAX / tiles) return PACT_ERR_UNSUPPORTED;
   s = check_ws(c->ws, c->ws_bytes, chunk_scratch(ctx->chunk, c->n_requests, nullptr, nullptr));
   if (s != PACT_OK) return s;
-  if (c->n_rows == 0) return PACT_OK;
   ChunkArgs a;
   memset(&a, 0, sizeof(a));
   chunk_scratch(ctx->chunk, c->n_requests, &a, (char *)c->ws);

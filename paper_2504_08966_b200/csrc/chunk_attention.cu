@@ -776,7 +776,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           hidden = __any_sync(0xffffffffu, hidden);
           __syncwarp();
           if (!WIDE && counts && lane < N / 4) {                       // in powers of two; finite ones stay finite
-            const auto in_twos = [](float x) { return isinf(x) ? x : fminf(fmaxf(x * kChunkLog2e, -FLT_MAX), FLT_MAX); };
+            const auto in_twos = [](float x) { return isfinite(x) ? fminf(fmaxf(x * kChunkLog2e, -FLT_MAX), FLT_MAX) : x; };
             *reinterpret_cast<float4 *>(sh.bias[at] + lane * 4) = make_float4(in_twos(b.x), in_twos(b.y), in_twos(b.z), in_twos(b.w));
           }
           __syncwarp();
@@ -848,7 +848,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       }
     }
   }
-  if (warp == kCopyWarp) asm volatile("cp.async.wait_all;" ::: "memory");
+  asm volatile("cp.async.wait_all;" ::: "memory");                   // (queries and biases asked for before a wait ran out)
   tc_fence_before();
   __syncthreads();
   if (warp == kMmaWarp) mbar_wait_slow(&sh.drained, 0);

@@ -31,7 +31,7 @@ __device__ __forceinline__ void store8(const ChunkArgs &a, long long at, const f
   }
 }
 
-// sixteen: 32 bytes at a time where they lie so (a lane has a row, and every store of a warp takes as long as it has rows, whatever its width: 12 prompts 5 % of the time)
+// sixteen: 32 bytes at a time where they lie so (a lane has a row, and a store of a warp takes as long as it has rows, whatever its width)
 __device__ __forceinline__ void store16(const ChunkArgs &a, long long at, const float *x) {
   if (a.store_bytes < 32) {
     store8(a, at, x);
