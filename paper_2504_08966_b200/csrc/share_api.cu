@@ -15,6 +15,8 @@ pact_status check_share(const pact_ctx *ctx, int page_rows, int n_pages, int n_r
   return (int64_t)n_requests * max_pages > INT32_MAX ? PACT_ERR_UNSUPPORTED : PACT_OK;   // (places are counted in 32 bits)
 }
 
+uint64_t page_mul_of(int page) { return ((1ull << 33) + page / 16 - 1) / (page / 16); }
+
 }  // namespace
 
 extern "C" {
@@ -40,7 +42,7 @@ pact_status pact_cache_fork(pact_ctx *ctx, const pact_fork *f, void *stream) {
   a.table = f->block_table; a.length = f->length; a.source = f->source; a.rows = f->rows; a.shared = f->shared; a.free_pages = f->free_pages; a.n_free = f->n_free;
   a.table_out = f->block_table_out; a.length_out = f->length_out; a.shared_out = f->shared_out; a.free_out = f->free_out; a.n_free_out = f->n_free_out;
   a.copies = f->copies; a.n_copies = f->n_copies; a.status = f->status;
-  a.B = f->n_requests; a.width = f->max_pages; a.page = f->page_rows; a.n_pages = f->n_pages; a.n_list = f->n_requests;
+  a.B = f->n_requests; a.width = f->max_pages; a.page = f->page_rows; a.n_pages = f->n_pages; a.n_list = f->n_requests; a.page_mul = page_mul_of(a.page);
   CK(launch_cache_fork(a, (cudaStream_t)stream));
   ctx->launches += 1;
   CK(cudaGetLastError());
@@ -60,7 +62,7 @@ pact_status pact_cache_compact(pact_ctx *ctx, const pact_compact *c, void *strea
   compact_scratch(c->n_pages, &a, (char *)c->ws);
   a.table = c->block_table; a.length = c->length; a.shared = c->shared; a.free_pages = c->free_pages; a.n_free = c->n_free;
   a.table_out = c->block_table_out; a.shared_out = c->shared_out; a.free_out = c->free_out; a.moved_to = c->moved_to; a.copies = c->copies; a.n_copies = c->n_copies; a.status = c->status;
-  a.B = c->n_requests; a.width = c->max_pages; a.page = c->page_rows; a.n_pages = c->n_pages; a.n_list = c->n_list;
+  a.B = c->n_requests; a.width = c->max_pages; a.page = c->page_rows; a.n_pages = c->n_pages; a.n_list = c->n_list; a.page_mul = page_mul_of(a.page);
   CK(launch_cache_compact(a, (cudaStream_t)stream));
   ctx->launches += 1;
   CK(cudaGetLastError());

@@ -173,6 +173,11 @@ int main() {
   if (pact_share_workspace_bytes(nullptr, 1, 1, 1) || pact_share_workspace_bytes(&ctx, 0, 1, 1) || pact_share_workspace_bytes(&ctx, 1, 0, 1) || pact_share_workspace_bytes(&ctx, 1, 1, 0) ||
       pact_share_workspace_bytes(&ctx, PACT_MAX_REQUESTS + 1, 1, 1) || pact_share_workspace_bytes(&ctx, 1, 1, 1) != 4096)
     return 1;
+  // n / page by a multiplication, up to the ends of its range
+  for (int page = 16; page <= 1024; page += 16)
+    for (unsigned k = 0; k <= ((1u << 31) + 1024) / page; k += k < 3000 ? 1 : 977)
+      for (unsigned n : {k * page, k * page + page / 2, k * page + page - 1, (1u << 31) - 1 - k, (1u << 31) + 1023 - k % 1024})
+        if (n < (1u << 31) + 1024 && page_of(page_mul_of(page), n) != (int)(n / page)) { printf("%u / %d\n", n, page); return 1; }
   const auto with_cache = [&] {
     REFUSED(x.ctx = nullptr) REFUSED(x.cache_null = true) REFUSED(x.c.K = nullptr) REFUSED(x.c.V = nullptr) REFUSED(x.c.K = buf + 8) REFUSED(x.c.k_row = 120) REFUSED(x.c.k_row = 129)
     REFUSED(x.c.v_head = 0) REFUSED(x.c.v_page = -4096) UNSUPPORTED(x.c.k_page = 1ll << 40) REFUSED(x.c.logw = (float *)(buf + 4)) REFUSED(x.c.bounds = nullptr) REFUSED(x.c.n_pages = 0)
