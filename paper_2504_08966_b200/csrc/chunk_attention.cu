@@ -104,6 +104,16 @@ __device__ __forceinline__ void tmem_arrived(uint32_t (&r)[32]) {
                     "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
                :: "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                 "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_arrived(uint32_t (&r)[16]) {
+  asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                    "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :: "memory");
+}
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
@@ -270,21 +280,25 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     const auto fills_q = [&](const ChunkSegment &x) { return t < C::kBlocks && (t == 0 || !is_split(x)); };
     // This warp's 32 rows of Q, swizzled as the copies of K are; zeros past d_h and the last row.
     const auto ask_for_q = [&](const ChunkSegment &x) {
-      const int r = t * 128 + row, at_row = x.first + r, token = at_row / a.group, head = x.kv * a.group + at_row - token * a.group;
-      const bool there = r < x.rows;
-      const long long my_at = (x.row0 + token) * a.ldQ + head * a.ldQh;
       constexpr int kLanes = NB == 1 ? 8 : NB == 2 ? 16 : 32, kAtOnce = 32 / kLanes;
-      const int c = lane % kLanes;
-      const uint32_t to = smem_u32(sh.q[t]) + c / 8 * (128 * 128);
-#pragma unroll
-      for (int i = 0; i < 32; i += kAtOnce) {
-        const int src = i + lane / kLanes, rr = (warp & 3) * 32 + src;
-        const long long at = __shfl_sync(0xffffffffu, my_at, src);
-        const bool row_there = __shfl_sync(0xffffffffu, there ? 1 : 0, src) != 0 && c * 8 < a.d_h;
-        const __nv_bfloat16 *from = static_cast<const __nv_bfloat16 *>(a.Q) + (row_there ? at + c * 8 : 0);
-        if (c < NB * 8)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)), "l"(from), "r"(row_there ? 16 : 0) : "memory");
-      }
+      const int c = lane % kLanes, rr = (warp & 3) * 32 + lane / kLanes, at_row = x.first + t * 128 + rr, token = at_row / a.group;
+      const int tokens = kAtOnce / a.group, heads = kAtOnce - tokens * a.group;   // from one row of this lane to the next
+      const long long step = tokens * a.ldQ + heads * a.ldQh, over = a.ldQ - a.group * a.ldQh;   // over: where the heads of a token end in between
+      int head = at_row - token * a.group, left = c * 8 < a.d_h ? x.rows - t * 128 - rr : 0;
+      const __nv_bfloat16 *from = static_cast<const __nv_bfloat16 *>(a.Q) + (x.row0 + token) * a.ldQ + (x.kv * a.group + head) * a.ldQh + c * 8;
+      uint32_t to = smem_u32(sh.q[t]) + c / 8 * (128 * 128) + rr * 128;
+      if (c < NB * 8)
+#pragma unroll 4                                                     // (executed once per item: code that is fetched for it costs more than the loop)
+        for (int i = 0; i < 32; i += kAtOnce) {
+          const bool there = left > i;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + i * 128 + (((c & 7) ^ ((rr + i) & 7)) << 4)), "l"(there ? from : a.Q), "r"(there ? 16 : 0) : "memory");
+          from += step;
+          head += heads;
+          if (head >= a.group) {
+            head -= a.group;
+            from += over;
+          }
+        }
     };
     const auto give_q = [&] {
       asm volatile("cp.async.wait_all;" ::: "memory");
@@ -489,26 +503,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       if (fills && ok && split) ask_for_q(next);
       if (fills && ok && !split) give_q();
       const int *poison = a.poison + ((long long)blockIdx.x * kChunkPoison + segment % kChunkPoison) * kChunkMaxWidth;
-      // columns c0 .. c0 + 31 of this row's results, all tiles so far
-      const auto results = [&](uint32_t from, const float4 *kept, bool has_kept, float f_kept, int c0, float (&o)[32]) {
-        uint32_t v[32];
-        tmem_ld32(from + c0, v);
-        tmem_ld_wait();
-        tmem_arrived(v);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(v[i]);
-        if (WIDE && has_kept) {
-#pragma unroll
-          for (int i = 0; i < 32; i += 4)
-            if (c0 + i < d16) {
-              const float4 z = kept[(c0 + i) / 4 * 128];
-              o[i] = fmaf(z.x, f_kept, o[i]);
-              o[i + 1] = fmaf(z.y, f_kept, o[i + 1]);
-              o[i + 2] = fmaf(z.z, f_kept, o[i + 2]);
-              o[i + 3] = fmaf(z.w, f_kept, o[i + 3]);
-            }
-        }
-      };
       float f_flush1 = 1.f;
       bool flushed1 = false;
       float m1 = -INFINITY, l1 = 0.f, f0 = 1.f, f1 = 0.f;
@@ -541,37 +535,55 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         if (fills && ok) give_q();                                   // (the next logits take the place of what has just been read)
       }
       if (!WIDE) m = m < -2.3e38f ? m : m * 0.6931471805599453f;     // (the lowest float stands for itself)
-      if (active && ok && (!split || t == 0)) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+      if (active && ok && (!split || t == 0) && !idle) {
+        const bool both = split && __any_sync(0xffffffffu, l1 != 0.f);
+        const float inv = s.slot >= 0 ? 1.f : l == 0.f ? 0.f : 1.f / l;
         const long long out_at = (s.row0 + token) * a.ldO + head * a.ldOh;
-#pragma unroll 1
-        for (int c0 = 0; c0 < d16; c0 += 32) {
-          float o[32];
-          results(my_o, flush, flushed, f_flush, c0, o);
-          if (split && __any_sync(0xffffffffu, l1 != 0.f)) {
-            float o1[32];
-            results(my_o + C::kWidth, flush + (C::kWidth / 4) * 128, flushed1, f_flush1, c0, o1);
+        f0 *= inv;
+        f1 *= inv;
+        // sixteen columns at a time: the code of a larger step takes longer to fetch than it saves
+        const auto columns = [&](uint32_t from, const float4 *kept, bool has_kept, float f_kept, float (&o)[16]) {
+          uint32_t v[16];
+          tmem_ld16(from, v);
+          tmem_ld_wait();
+          tmem_arrived(v);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = l1 != 0.f ? o[i] * f0 + o1[i] * f1 : o[i] * f0;
+          for (int i = 0; i < 16; ++i) o[i] = __uint_as_float(v[i]);
+          if (WIDE && has_kept) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+              const float4 z = kept[i / 4 * 128];
+              o[i] = fmaf(z.x, f_kept, o[i]);
+              o[i + 1] = fmaf(z.y, f_kept, o[i + 1]);
+              o[i + 2] = fmaf(z.z, f_kept, o[i + 2]);
+              o[i + 3] = fmaf(z.w, f_kept, o[i + 3]);
+            }
+          }
+        };
+#pragma unroll 1
+        for (int c0 = 0; c0 < d16; c0 += 16) {
+          float o[16];
+          columns(my_o + c0, flush + c0 / 4 * 128, flushed, f_flush, o);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[i] *= f0;
+          if (both) {
+            float o1[16];
+            columns(my_o + C::kWidth + c0, flush + (C::kWidth / 4 + c0 / 4) * 128, flushed1, f_flush1, o1);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = l1 != 0.f ? fmaf(o1[i], f1, o[i]) : o[i];
           }
           if (poisoned) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
+            for (int i = 0; i < 16; ++i)
               if (c0 + i < a.d_h && __ldcg(poison + c0 + i) < limit) o[i] = __int_as_float(0x7fffffff);
           }
           if (there && s.slot >= 0) {
             float4 *p = reinterpret_cast<float4 *>(a.part_o) + ((long long)s.slot * (C::kWidth / 4) + c0 / 4) * C::kRows + r;
 #pragma unroll
-            for (int i = 0; i < 32; i += 4)
-              if (c0 + i < d16) p[i / 4 * C::kRows] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+            for (int i = 0; i < 16; i += 4) p[i / 4 * C::kRows] = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
           } else if (there) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] *= inv;
-#pragma unroll
-            for (int i = 0; i < 32; i += 16) {
-              if (c0 + i + 16 <= a.d_h) store16(a, out_at + c0 + i, o + i);
-              else if (c0 + i < a.d_h) store8(a, out_at + c0 + i, o + i);
-            }
+            if (c0 + 16 <= a.d_h) store16(a, out_at + c0, o);
+            else store8(a, out_at + c0, o);
           }
           __syncwarp();
         }
