@@ -394,21 +394,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           if (WIDE && nth > 0 && nth % 2 == 0) {                     // the results of two tiles, added with rounding
 #pragma unroll 1
             for (int c0 = 0; c0 < d16; c0 += 32) {
+              float4 *p = flush + c0 / 4 * 128, z[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {                            // (all of them before the first store: one trip to the L2 instead of eight)
+                z[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (flushed && c0 + 4 * i < d16) z[i] = p[i * 128];
+              }
               uint32_t v[32];
               tmem_ld32(my_o + c0, v);
               tmem_ld_wait();
               tmem_arrived(v);
 #pragma unroll
-              for (int i = 0; i < 32; i += 4)
-                if (c0 + i < d16) {
-                  float4 y = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
-                  float4 *p = flush + (c0 + i) / 4 * 128;
-                  if (flushed) {
-                    const float4 z = *p;
-                    y = make_float4(fmaf(z.x, f_flush, y.x), fmaf(z.y, f_flush, y.y), fmaf(z.z, f_flush, y.z), fmaf(z.w, f_flush, y.w));
-                  }
-                  *p = y;
-                }
+              for (int i = 0; i < 8; ++i)
+                if (c0 + 4 * i < d16)
+                  p[i * 128] = make_float4(fmaf(z[i].x, f_flush, __uint_as_float(v[4 * i])), fmaf(z[i].y, f_flush, __uint_as_float(v[4 * i + 1])),
+                                           fmaf(z[i].z, f_flush, __uint_as_float(v[4 * i + 2])), fmaf(z[i].w, f_flush, __uint_as_float(v[4 * i + 3])));
             }
             flushed = true;
             f_flush = 1.f;
