@@ -323,7 +323,7 @@ typedef struct {
  * free_pages is a stack of page ids, its top at free_pages[*n_free - 1].  Ended requests push their pages first, by ascending request and
  * ascending place; then the others take pages off the top in the same order.  Page ids are taken as they are (the calls that read or write rows check them).
  * The tables and the stack of a call name no page twice: one that two requests share (pact_paged_attention may read it for both) goes back once for each that ends, and is
- * handed out as often.  A caller that shares pages ends these requests itself.
+ * handed out as often.  Requests that share pages are ended with pact_cache_fork instead, which counts holders.
  * New rows are packed (row_stride 0: row i of request b is row_start[b] + i, and n_rows is what the caller has room for), or each request has
  * row_stride of them (row b * row_stride + i; n_rows = n_requests * row_stride).
  * A call that cannot be served as a whole changes nothing: length_out and n_free_out repeat the old values, row_start is 0, every
