@@ -7,7 +7,7 @@
 namespace pact {
 
 constexpr int kChunkMaxSms = 176;          // most CTAs of a call
-constexpr int kChunkPoison = 4;            // segments whose columns with infinite values are remembered at a time
+constexpr int kChunkPoison = 8;            // segments whose columns with infinite values are remembered at a time
 constexpr int kChunkMaxWidth = 256;
 
 // What the join finds about an item of the last round: whether it was cut; whether a CTA began it; the first and the last of the CTAs that share the rest; its

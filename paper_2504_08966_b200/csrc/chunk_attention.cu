@@ -54,6 +54,8 @@ template <int NB, bool WIDE> struct ChunkShape {
   static constexpr int kO = kBlocks * kRegion;                       // first column of the results
   static constexpr int kWidth = NB * 64;
   static_assert(kO + kBlocks * kWidth <= 512 && 2 * kRing - 3 >= kStages, "");
+  // Where every segment has one tile, half of the stages hold values of as many segments, all after the one whose results are being written.
+  static_assert(kStages / 2 + 1 <= kChunkPoison, "");
 };
 
 template <int NB, bool WIDE> struct ChunkShared {

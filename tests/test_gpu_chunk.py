@@ -232,6 +232,28 @@ def test_what_is_not_finite_shows_to_the_tokens_that_see_it_only(pb, dtype, out,
         assert got[first:].isnan().all() and not torch.isfinite(lse[first:]).any() and torch.equal(got[:first], clean[:first]) and torch.isfinite(lse[:first]).all()
 
 
+@pytest.mark.parametrize("dtype,out,D", [(BF, BF, 64), (BF, F32, 64), (BF, BF, 128), (BF, F32, 200), (F32, F32, 64)])
+def test_what_is_not_finite_in_many_short_requests(pb, dtype, out, D):
+    """A tile each, every one with an infinity of its own among the new tokens' values: each shows in its request, its column and the tokens that see it, although values are looked at ahead."""
+    B, H, n_qh, page = 1500, 2, 4, 32
+    g, rng = torch.Generator(device="cuda").manual_seed(D), np.random.default_rng(D)
+    K, V, w = cache_of(g, B, H, page, D, dtype)
+    lens, new = rng.integers(8, page + 1, B), rng.integers(3, 8, B)
+    starts, row, col, head = np.concatenate([[0], np.cumsum(new)[:-1]]), np.array([n - m + rng.integers(0, m) for n, m in zip(lens, new)]), rng.integers(0, D, B), rng.integers(0, H, B)
+    Q = torch.randn(int(new.sum()), n_qh, D, generator=g, device="cuda").to(dtype)
+    clean, got, status = torch.zeros(len(Q), n_qh, D, dtype=out, device="cuda"), torch.zeros(len(Q), n_qh, D, dtype=out, device="cuda"), i32([0])
+    ctx, args = context(pb, n_qh, H, D, dtype, out), (i32(np.arange(B)[:, None]), i32(lens), i32(new))
+    ctx.pact_chunk_attention(pb.PagedCache(K, V, w), Q, *args, clean, row_start=i32(starts), status=status)
+    at = torch.arange(B, device="cuda")
+    V[at, torch.tensor(head, device="cuda"), torch.tensor(row, device="cuda"), torch.tensor(col, device="cuda")] = float("inf")
+    ctx.pact_chunk_attention(pb.PagedCache(K, V, w), Q, *args, got, row_start=i32(starts), status=status)
+    hit = np.zeros((len(Q), n_qh, D), bool)
+    for b in range(B):
+        hit[starts[b] + row[b] - (lens[b] - new[b]):starts[b] + new[b], head[b] * 2:head[b] * 2 + 2, col[b]] = True
+    hit = torch.tensor(hit, device="cuda")
+    assert status.item() == 0 and torch.equal(~torch.isfinite(got), hit) and torch.equal(got[~hit], clean[~hit])
+
+
 @pytest.mark.parametrize("dtype,out", [(BF, BF), (BF, F32), (F32, F32)])
 def test_masks_of_the_lowest_value_and_large_logits(pb, dtype, out):
     """The lowest float as a bias is a number: where all rows have it, they share the attention; beside others it is nothing."""
