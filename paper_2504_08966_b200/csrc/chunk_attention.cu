@@ -17,8 +17,8 @@
 //
 // Measured: 1,024 tokens of 32 heads of 128 on 8 key heads over 65,536 rows 1.14 ms, 960 TFLOP/s (a tile 4,500 clocks: 1,000 for the maximum, 1,500 for probabilities, 300 to hand them on, 1,650
 // until the next logits are there); 12 prompts of up to 2,948 rows 0.71 ms, 490 TFLOP/s of what the mask leaves (nine tiles an item, then 7,000 clocks for results and the next queries);
-// 32 requests of five tokens over up to 8,192 rows 165 us, 4.1 TB/s; with fp32 results eight times 256 tokens over up to 2,916 rows 277 us (adding up the results of two tiles takes 4,700 of
-// their 13,500 clocks).  What is done once per item is mostly fetching of its code: results 32 columns at a time took 3 % longer, the queries' loop unrolled 1 %.
+// 32 requests of five tokens over up to 8,192 rows 165 us, 4.1 TB/s; with fp32 results eight times 256 tokens over up to 2,916 rows 270 us (adding up the results of two tiles took 4,700 of
+// their 13,500 clocks with all sums in the L2; 64 columns in shared memory: 277 -> 270 us there, 1,154 -> 1,045 us for 30 times 879 tokens, 406 -> 382 us with heads of 64, all of whose columns fit).  What is done once per item is mostly fetching of its code: results 32 columns at a time took 3 % longer, the queries' loop unrolled 1 %.
 //
 // Rounding: probabilities go into the products with bf16 values as one bf16 term where results are bf16: unbiased errors of 2^-8 at most in the weights, which together are no
 // larger than the one rounding of the result that follows (relative error of the results 0.0020, with exact probabilities 0.0017).  For fp32 results as three terms, which hold all of fp32's 24 bits, and the products of two tiles at a
@@ -46,7 +46,10 @@ template <int NB, bool WIDE> struct ChunkShape {
   static constexpr int kGroups = kTileRows / 16;
   static constexpr int kQBytes = NB * 128 * 128;                     // of a block
   static constexpr int kStage = NB * kTileRows * 128;                // K or V of a tile
-  static constexpr int kFit = (int)((kChunkSmem - kBlocks * kQBytes - 4096) / kStage);
+  // Columns of the sums of earlier tiles (fp32 results) that stay in shared memory; the others go to the L2.
+  static constexpr int kKept = WIDE && NB <= 2 ? 64 : 0;
+  static constexpr int kKeptBytes = kBlocks * kKept * 128 * 4;
+  static constexpr int kFit = (int)((kChunkSmem - kBlocks * kQBytes - kKeptBytes - 4096) / kStage);
   static constexpr int kStages = NB == 2 && !WIDE ? 5 : kFit > 10 ? 10 : kFit;   // (five of 32 KB leave 3 KB for everything else)
   static constexpr int kRing = kStages <= 5 ? 4 : 8;                 // biases of tiles: the copies run ahead by fewer
   static constexpr int kTerms = WIDE ? 3 : 1;
@@ -62,6 +65,7 @@ template <int NB, bool WIDE> struct ChunkShared {
   using C = ChunkShape<NB, WIDE>;
   char q[C::kBlocks][C::kQBytes];
   char stage[C::kStages][C::kStage];
+  float4 kept[C::kKept ? C::kBlocks : 1][C::kKept ? C::kKept / 4 : 1][C::kKept ? 128 : 1];
   float bias[C::kRing][C::kTileRows];
   uint64_t full[C::kStages], empty[C::kStages];
   uint64_t b_full[C::kRing], b_ready[C::kRing], clean[C::kRing];
@@ -275,7 +279,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;
     const uint32_t my_s = tmem + t * C::kRegion + lanes, my_o = tmem + C::kO + t * C::kWidth + lanes;
     const int d16 = (a.d_h + 15) / 16 * 16;
-    float4 *flush = reinterpret_cast<float4 *>(a.flush) + ((long long)blockIdx.x * C::kBlocks + t) * (C::kWidth / 4) * 128 + row;
+    // sums of earlier tiles: columns c0 .. c0 + 3 of this row, the next four 128 vectors on (32 columns lie in one place)
+    const auto kept_at = [&](int block, int c0) {
+      if (C::kKept && c0 < C::kKept) return &sh.kept[block][c0 / 4][row];
+      return reinterpret_cast<float4 *>(a.flush) + (((long long)blockIdx.x * C::kBlocks + block) * (C::kWidth / 4) + c0 / 4) * 128 + row;
+    };
     // Logits of bf16 results are kept in powers of two, a multiplication less; those of fp32 results in natural units, which round once less.
     constexpr float kTwos = WIDE ? kChunkLog2e : 1.f;
     const float scale = WIDE ? a.scale : a.scale * kChunkLog2e;
@@ -401,7 +409,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           if (WIDE && nth > 0 && nth % 2 == 0) {                     // the results of two tiles, added with rounding
 #pragma unroll 1
             for (int c0 = 0; c0 < d16; c0 += 32) {
-              float4 *p = flush + c0 / 4 * 128, z[8];
+              float4 *p = kept_at(t, c0), z[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) {                            // (all of them before the first store: one trip to the L2 instead of eight)
                 z[i] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -570,12 +578,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll 1
         for (int c0 = 0; c0 < d16; c0 += 16) {
           float o[16];
-          columns(my_o + c0, flush + c0 / 4 * 128, flushed, f_flush, o);
+          columns(my_o + c0, kept_at(t, c0), flushed, f_flush, o);
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[i] *= f0;
           if (both) {
             float o1[16];
-            columns(my_o + C::kWidth + c0, flush + (C::kWidth / 4 + c0 / 4) * 128, flushed1, f_flush1, o1);
+            columns(my_o + C::kWidth + c0, kept_at(C::kBlocks - 1, c0), flushed1, f_flush1, o1);
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[i] = l1 != 0.f ? fmaf(o1[i], f1, o[i]) : o[i];
           }
@@ -949,7 +957,8 @@ size_t chunk_scratch(const ChunkCfg &cfg, int requests, ChunkArgs *a, char *base
     at += round256(bytes);
     return p;
   };
-  char *o = take(parts * cfg.width * sizeof(float)), *ml = take(parts * sizeof(float2)), *flush = take(cfg.wide ? G * cfg.rows * cfg.width * sizeof(float) : 0),
+  const bool kept = cfg.wide && cfg.blocks > 1;                       // (64 columns wide: sums of earlier tiles stay in shared memory)
+  char *o = take(parts * cfg.width * sizeof(float)), *ml = take(parts * sizeof(float2)), *flush = take(kept ? G * cfg.rows * cfg.width * sizeof(float) : 0),
        *cut = take(2 * G * sizeof(ChunkCut)), *tail = take(G * sizeof(int)), *head = take(G * G * sizeof(int)),
        *pre = take(requests < kChunkPreInSmem ? 0 : G * ((size_t)requests + 1) * sizeof(int)), *poison = take(G * kChunkPoison * kChunkMaxWidth * sizeof(int));
   if (a) {
