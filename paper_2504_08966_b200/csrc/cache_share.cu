@@ -91,11 +91,15 @@ template <typename F> __device__ __forceinline__ void each_chunk(const int *chun
     f(lo, (c - chunk[lo]) * kShareChunk, c);
   }
 }
-// f(request, place) for every entry of this thread
-template <typename F> __device__ __forceinline__ void each_entry(const int *chunk, int B, int rank, F f) {
+// f(request, place, what is there) for every entry of this thread: the first count(b) of row(b) of the table.  (Both are loaded before f, whose stores the compiler cannot tell from them.)
+template <typename N, typename R, typename F>
+__device__ __forceinline__ void each_entry(const int32_t *table, long long width, const int *chunk, int B, int rank, N count, R row, F f) {
   each_chunk(chunk, B, rank, [&](int b, int j0, int) {
-    f(b, j0 + (int)(threadIdx.x & 31));
-    f(b, j0 + 32 + (int)(threadIdx.x & 31));
+    const int n = count(b), j = j0 + (int)(threadIdx.x & 31);
+    const int32_t *at = table + row(b) * width + j;
+    const int p = j < n ? at[0] : -1, q = j + 32 < n ? at[32] : -1;
+    if (j < n) f(b, j, p);
+    if (j + 32 < n) f(b, j + 32, q);
   });
 }
 
@@ -128,6 +132,12 @@ __global__ void __launch_bounds__(kShareThreads) k_cache_fork(const __grid_const
   const auto pages_of = [&](unsigned n) { return page_of(a.page_mul, n); };
   const auto old_at = [&](int b, int j) { return a.table[(long long)b * a.width + j]; };
   const auto is_page = [&](int p) { return p >= 0 && p < a.n_pages; };
+  const auto old_entries = [&](auto f) {
+    each_entry(a.table, a.width, sh.old_chunk, a.B, rank, [&](int b) { return sh.pages[b]; }, [](int b) { return b; }, f);
+  };
+  const auto new_entries = [&](auto f) {                             // whole pages of the request after the call
+    each_entry(a.table, a.width, sh.new_chunk, a.B, rank, [&](int b) { return pages_of(sh.rows[b]); }, [&](int b) { return sh.source[b]; }, f);
+  };
   // 1: what is asked for, checked; the words of all pages named cleared
   {
     const int room = a.width * a.page, per = (a.B + kShareThreads - 1) / kShareThreads, b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
@@ -157,9 +167,7 @@ __global__ void __launch_bounds__(kShareThreads) k_cache_fork(const __grid_const
     __syncthreads();
   }
   const int first_b = share_of(a.B, rank), my_b = share_of(a.B, rank + 1) - first_b;   // this CTA's requests
-  each_entry(sh.old_chunk, a.B, rank, [&](int b, int j) {
-    if (j >= sh.pages[b]) return;
-    const int p = old_at(b, j);
+  old_entries([&](int, int, int p) {
     if (is_page(p)) *reinterpret_cast<int4 *>(a.pages + p) = make_int4(0, 0, INT32_MAX, INT32_MAX);
     else sh.bad = PACT_ERR_INVALID_ARG;
   });
@@ -171,16 +179,12 @@ __global__ void __launch_bounds__(kShareThreads) k_cache_fork(const __grid_const
     for (int p = me; p < a.n_pages; p += kAll) a.shared_out[p] = a.shared[p];
   cluster_sync();
   // 2: holders before and after
-  each_entry(sh.old_chunk, a.B, rank, [&](int b, int j) {
-    if (j >= sh.pages[b]) return;
-    const int p = old_at(b, j);
+  old_entries([&](int b, int j, int p) {
     if (!is_page(p)) return;
     atomicAdd(&a.pages[p].held, 1);
     atomicMin(&a.pages[p].first, b * a.width + j);
   });
-  each_entry(sh.new_chunk, a.B, rank, [&](int b, int j) {
-    if (j >= pages_of(sh.rows[b])) return;
-    const int p = old_at(sh.source[b], j);
+  new_entries([&](int, int, int p) {
     if (is_page(p)) atomicAdd(&a.pages[p].full, 1);
   });
   for (int i = tid; i < my_b; i += kShareThreads)
@@ -189,21 +193,17 @@ __global__ void __launch_bounds__(kShareThreads) k_cache_fork(const __grid_const
   // 3: pages that go back and requests that copy, counted in their order within the CTA
   each_chunk(sh.old_chunk, a.B, rank, [&](int b, int j0, int c) {
     uint64_t firsts = 0, gones = 0;
+    const int j = j0 + lane, n = sh.pages[b];
+    int p[2];
 #pragma unroll
-    for (int i = 0; i < kShareChunk; i += 32) {
-      const int j = j0 + i + lane;
-      bool first = false, gone = false;
-      if (j < sh.pages[b]) {
-        const int p = old_at(b, j);
-        if (is_page(p)) {
-          const ForkPage page(a, p);
-          first = page.first == b * a.width + j;
-          gone = first && page.now == 0;
-          if (page.shared < 0 || page.outside < 0) sh.bad = PACT_ERR_INVALID_ARG;
-        }
-      }
-      firsts |= (uint64_t)__ballot_sync(0xffffffffu, first) << i;
-      gones |= (uint64_t)__ballot_sync(0xffffffffu, gone) << i;
+    for (int i = 0; i < 2; ++i) p[i] = j + 32 * i < n ? old_at(b, j + 32 * i) : -1;
+    ForkPage page[2] = {ForkPage(a, is_page(p[0]) ? p[0] : 0), ForkPage(a, is_page(p[1]) ? p[1] : 0)};   // (page 0 in place of none: looked at, not used)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const bool first = is_page(p[i]) && page[i].first == b * a.width + j + 32 * i, gone = first && page[i].now == 0;
+      if (is_page(p[i]) && (page[i].shared < 0 || page[i].outside < 0)) sh.bad = PACT_ERR_INVALID_ARG;
+      firsts |= (uint64_t)__ballot_sync(0xffffffffu, first) << (32 * i);
+      gones |= (uint64_t)__ballot_sync(0xffffffffu, gone) << (32 * i);
     }
     if (lane == 0) {
       a.chunk_first[c] = firsts;
@@ -237,30 +237,30 @@ __global__ void __launch_bounds__(kShareThreads) k_cache_fork(const __grid_const
   if (have < 0 || have > a.n_pages || (!bad && freed > a.n_pages - have)) bad = PACT_ERR_INVALID_ARG;
   if (!bad && left < 0) bad = PACT_ERR_NO_PAGES;
   if (bad) {
-    each_entry(sh.old_chunk, a.B, rank, [&](int b, int j) {
-      if (j < sh.pages[b]) a.table_out[(long long)b * a.width + j] = old_at(b, j);
-    });
+    old_entries([&](int b, int j, int p) { a.table_out[(long long)b * a.width + j] = p; });
     for (int b = me; b < a.B; b += kAll) a.length_out[b] = a.length[b];
     if (me == 0 && a.status) atomicMin(a.status, bad);
   } else {
     each_chunk(sh.old_chunk, a.B, rank, [&](int b, int j0, int c) {
       const uint64_t firsts = a.chunk_first[c], gones = a.chunk_gone[c];
       const int at = sums.a_before + a.chunk_freed[c];
+      int p[2], now[2];
 #pragma unroll
-      for (int i = lane; i < kShareChunk; i += 32) {
-        if (!(firsts >> i & 1)) continue;
-        const int p = old_at(b, j0 + i);
-        a.shared_out[p] = max(ForkPage(a, p).now - 1, 0);            // (each page that was named is settled at its first place)
+      for (int h = 0; h < 2; ++h) p[h] = firsts >> (lane + 32 * h) & 1 ? old_at(b, j0 + lane + 32 * h) : -1;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) now[h] = ForkPage(a, max(p[h], 0)).now;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int i = lane + 32 * h;
+        if (p[h] >= 0) a.shared_out[p[h]] = max(now[h] - 1, 0);      // (each page that was named is settled at its first place)
         if (gones >> i & 1) {
           const int k = at + __popcll(gones & ((1ull << i) - 1));
-          a.freed[k] = p;
-          if (have + k < left) a.free_out[have + k] = p;
+          a.freed[k] = p[h];
+          if (have + k < left) a.free_out[have + k] = p[h];
         }
       }
     });
-    each_entry(sh.new_chunk, a.B, rank, [&](int b, int j) {
-      if (j < pages_of(sh.rows[b])) a.table_out[(long long)b * a.width + j] = old_at(sh.source[b], j);
-    });
+    new_entries([&](int b, int j, int p) { a.table_out[(long long)b * a.width + j] = p; });
     for (int b = me; b < a.B; b += kAll) a.length_out[b] = sh.rows[b];
   }
   if (a.free_out != a.free_pages)
@@ -393,13 +393,10 @@ __global__ void __launch_bounds__(kShareThreads) k_cache_compact(const __grid_co
   }
   cluster_sync();
   // 6: the tables
-  each_entry(sh.old_chunk, a.B, rank, [&](int b, int j) {
-    if (j >= sh.pages[b]) return;
-    const long long at = (long long)b * a.width + j;
-    const int p = a.table[at];
+  each_entry(a.table, a.width, sh.old_chunk, a.B, rank, [&](int b) { return sh.pages[b]; }, [](int b) { return b; }, [&](int b, int j, int p) {
     const bool there = p >= 0 && p < a.n_pages;
     if (!there && a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
-    a.table_out[at] = there ? a.moved_to[p] : p;
+    a.table_out[(long long)b * a.width + j] = there ? a.moved_to[p] : p;
   });
 }
 
