@@ -3,7 +3,7 @@
 // Both are bookkeeping over block tables, bound by latency: a chain of steps in which every entry has to be known to all before the next begins.  One cluster of CTAs walks through them with
 // barriers between, a launch instead of five; counts go to global memory by integer atomics, whose order does not show.  A warp looks at 64 entries of a table at a time.
 // Each instruction runs a few times only, so that fetching code is a good part of the time: what is needed of a request is worked out once, and steps are written once where they can be.
-// Measured: 128 requests in groups of four, 24,000 entries: 18.9 us; eight that go on with one of 131,072 rows: 13.9 us; a compaction of 2,048 pages 10.5 us, of 65,536 17.5 us.  Eight CTAs
+// Measured: 128 requests in groups of four, 24,000 entries: 17.6 us; eight that go on with one of 131,072 rows: 12.0 us; a compaction of 2,048 pages 10.3 us, of 65,536 17.3 us.  Eight CTAs
 // instead of 16: 34, 24, 13 and 27 us (before lengths and sources were kept in shared memory; 16 then: 27, 24, 13, 21); the counts of a page in four arrays instead of one word of 16 bytes: 47 us for the first.
 #include "share.cuh"
 

@@ -16,7 +16,7 @@
 // the true one by at most 2^8 of a probability, so that results are rescaled a few times per item only.
 //
 // Measured: 1,024 tokens of 32 heads of 128 on 8 key heads over 65,536 rows 1.14 ms, 960 TFLOP/s (a tile 4,500 clocks: 1,000 for the maximum, 1,500 for probabilities, 300 to hand them on, 1,650
-// until the next logits are there); 12 prompts of up to 2,948 rows 0.71 ms, 490 TFLOP/s of what the mask leaves (nine tiles an item, then 7,000 clocks for results and the next queries);
+// until the next logits are there); 12 prompts of up to 2,948 rows 0.70 ms, 500 TFLOP/s of what the mask leaves (nine tiles an item, then 7,000 clocks for results and the next queries);
 // 32 requests of five tokens over up to 8,192 rows 165 us, 4.1 TB/s; with fp32 results eight times 256 tokens over up to 2,916 rows 270 us (adding up the results of two tiles took 4,700 of
 // their 13,500 clocks with all sums in the L2; 64 columns in shared memory: 277 -> 270 us there, 1,154 -> 1,045 us for 30 times 879 tokens, 406 -> 382 us with heads of 64, all of whose columns fit).  What is done once per item is mostly fetching of its code: results 32 columns at a time took 3 % longer, the queries' loop unrolled 1 %.
 //
