@@ -445,8 +445,8 @@ size_t pact_chunk_workspace_bytes(const pact_ctx *ctx, int max_requests);
  * Rows with logw = minus infinity, rows past the length and rows that a token must not see have no effect on it, whatever their keys and values hold.  A token
  * without any row gets 0, and lse minus infinity.  Infinities and NaN in rows that count leave infinities or NaN in the results that they enter (infinite values beside bf16 keys: NaN).
  * Rows of Q, out and lse that belong to no token are not touched.
- * Logits, softmax statistics and sums are fp32.  bf16 keys and values: probabilities are rounded to bf16 where results are bf16, and carried as
- * three bf16 terms where they are fp32; bf16 results take logits in powers of two, so that finite biases beyond 2.35e38 in magnitude count as the largest number.
+ * Logits, softmax statistics and sums are fp32.  bf16 keys and values: probabilities are carried as two bf16 terms (off by 2^-17 at most) where results are bf16, and as
+ * three where they are fp32; bf16 results take logits in powers of two, so that finite biases beyond 2.35e38 in magnitude count as the largest number.
  * Lengths outside 0 .. max_pages * page_rows are clamped, rows of pages outside the cache left out, tokens without a row of Q (beyond n_rows or the row_stride) left out, and tokens before the first cached row (n_new above
  * length) see nothing; each sets status to INVALID_ARG.  Heads as above; n_rows * (n_qh / n_kvh) below 2^31. */
 pact_status pact_chunk_attention(pact_ctx *ctx, const pact_paged_cache *cache /*host*/, const pact_chunk *c /*host*/, void *stream);

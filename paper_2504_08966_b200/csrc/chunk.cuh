@@ -29,9 +29,8 @@ struct ChunkArgs {
   float *lse;
   int32_t *status;
   // workspace
-  float *part_o;         // [4 CTAs][width / 4][rows of an item][4] sums of the parts of items that several CTAs share
+  float *part_o;         // [4 CTAs][width / 4][rows of an item][4] sums of the parts of items that several CTAs share, and sums of earlier tiles while a part (or a whole item) is worked on
   float2 *part_ml;       // [4 CTAs][rows of an item] their reference logit and sum
-  float *flush;          // [CTAs][rows of an item][width] fp32 results of bf16 rows: sums of the tiles so far, where they do not stay in shared memory
   ChunkCut *cut;         // [2 CTAs]
   int *tail;             // [CTAs] tiles that each CTA has of the line of rests
   int *head;             // [CTAs][CTAs] tiles at the beginning of an item that its CTA takes; a copy for each CTA

@@ -20,9 +20,12 @@
 // 32 requests of five tokens over up to 8,192 rows 165 us, 4.1 TB/s; with fp32 results eight times 256 tokens over up to 2,916 rows 270 us (adding up the results of two tiles took 4,700 of
 // their 13,500 clocks with all sums in the L2; 64 columns in shared memory: 277 -> 270 us there, 1,154 -> 1,045 us for 30 times 879 tokens, 406 -> 382 us with heads of 64, all of whose columns fit).  What is done once per item is mostly fetching of its code: results 32 columns at a time took 3 % longer, the queries' loop unrolled 1 %.
 //
-// Rounding: probabilities go into the products with bf16 values as one bf16 term where results are bf16: unbiased errors of 2^-8 at most in the weights, which together are no
-// larger than the one rounding of the result that follows (relative error of the results 0.0020, with exact probabilities 0.0017).  For fp32 results as three terms, which hold all of fp32's 24 bits, and the products of two tiles at a
-// time are added with rounding, since the tensor cores cut their running sums off towards 0 (some 2^-25 at each of 16 rows).  Sums of probabilities are taken before the rounding.
+// Rounding: probabilities go into the products with bf16 values as two bf16 terms where results are bf16 (off by 2^-17 of a weight at most: 2 to 4 of
+// 1,000 results differ from those of fp32 probabilities; with one term 240 to 370 did), as three, which hold all of fp32's 24 bits, where they are fp32.  The tensor cores cut their running sums
+// off towards 0 (some 2^-25 at each of 16 rows and terms), so the products of 32 tiles (fp32 results: of two) at a time are added with rounding: 512 cuts of sums that grow from nothing, 2^-16 in the mean.
+// Sums of probabilities are taken before the rounding.
+// The second term took the long case from 1.14 to 1.50 ms, the prompts from 0.70 to 0.73 and left the drafts as they were, with the loops over a tile rolled: each is 32 columns of code, logits go back to tensor memory with their
+// biases.  All of a tile's columns in registers and straight code for them, as one term had it, took 1.99, 1.02 and 0.26 ms: the warps waited for instructions (1.4 warps per one that was issued, instead of 0.5).
 #include <float.h>
 
 #include "chunk_row.cuh"
@@ -46,17 +49,20 @@ template <int NB, bool WIDE> struct ChunkShape {
   static constexpr int kGroups = kTileRows / 16;
   static constexpr int kQBytes = NB * 128 * 128;                     // of a block
   static constexpr int kStage = NB * kTileRows * 128;                // K or V of a tile
-  // Columns of the sums of earlier tiles (fp32 results) that stay in shared memory; the others go to the L2.
+  // Columns of the sums of earlier tiles that stay in shared memory where there are many (fp32 results); the others go to the L2.
   static constexpr int kKept = WIDE && NB <= 2 ? 64 : 0;
   static constexpr int kKeptBytes = kBlocks * kKept * 128 * 4;
   static constexpr int kFit = (int)((kChunkSmem - kBlocks * kQBytes - kKeptBytes - 4096) / kStage);
   static constexpr int kStages = NB == 2 && !WIDE ? 5 : kFit > 10 ? 10 : kFit;   // (five of 32 KB leave 3 KB for everything else)
   static constexpr int kRing = kStages <= 5 ? 4 : 8;                 // biases of tiles: the copies run ahead by fewer
-  static constexpr int kTerms = WIDE ? 3 : 1;
-  static constexpr int kRegion = WIDE ? 96 : kTileRows;              // columns of tensor memory for logits, then probabilities
+  static constexpr int kTerms = WIDE ? 3 : 2;                        // of a probability
+  static constexpr int kSummed = WIDE ? 2 : 32;                      // tiles whose products are summed by the tensor cores before they are added to the earlier ones with rounding
+  static constexpr int kRegion = WIDE ? 96 : kTileRows;              // columns of tensor memory for logits, then the terms of probabilities
+  // First column of a term of the probabilities of rows 32 c ..: 16 columns, where logits have been read already (a third term begins behind the logits).
+  __host__ __device__ static constexpr int term_at(int c, int term) { return ((WIDE ? kTileRows : 0) + (c * kTerms + term) * 16) % kRegion; }
   static constexpr int kO = kBlocks * kRegion;                       // first column of the results
   static constexpr int kWidth = NB * 64;
-  static_assert(kO + kBlocks * kWidth <= 512 && 2 * kRing - 3 >= kStages, "");
+  static_assert(kO + kBlocks * kWidth <= 512 && kTerms * kTileRows / 2 <= kRegion && 2 * kRing - 3 >= kStages, "");
   // Where every segment has one tile, half of the stages hold values of as many segments, all after the one whose results are being written.
   static_assert(kStages / 2 + 1 <= kChunkPoison, "");
 };
@@ -279,10 +285,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;
     const uint32_t my_s = tmem + t * C::kRegion + lanes, my_o = tmem + C::kO + t * C::kWidth + lanes;
     const int d16 = (a.d_h + 15) / 16 * 16;
-    // sums of earlier tiles: columns c0 .. c0 + 3 of this row, the next four 128 vectors on (32 columns lie in one place)
+    // Sums of earlier tiles: columns c0 .. c0 + 3 of this row, the next four kept_step(c0) vectors on (32 columns lie in one memory).  Those in the L2 take the place of the segment's part, which
+    // the same thread puts there in the end.
+    const auto kept_step = [](int c0) { return C::kKept && c0 < C::kKept ? 128 : C::kRows; };
     const auto kept_at = [&](int block, int c0) {
       if (C::kKept && c0 < C::kKept) return &sh.kept[block][c0 / 4][row];
-      return reinterpret_cast<float4 *>(a.flush) + (((long long)blockIdx.x * C::kBlocks + block) * (C::kWidth / 4) + c0 / 4) * 128 + row;
+      return reinterpret_cast<float4 *>(a.part_o) + ((long long)s.place * (C::kWidth / 4) + c0 / 4) * C::kRows + block * 128 + row;
     };
     // Logits of bf16 results are kept in powers of two, a multiplication less; those of fp32 results in natural units, which round once less.
     constexpr float kTwos = WIDE ? kChunkLog2e : 1.f;
@@ -341,6 +349,30 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       being_read = false;
       float m = -INFINITY, l = 0.f, f_flush = 1.f;
       bool poisoned = false, flushed = false;
+      // The results of kSummed tiles to those of the earlier ones, with rounding.
+      const auto keep = [&] {
+#pragma unroll 1
+        for (int c0 = 0; c0 < d16; c0 += 32) {
+          float4 *p = kept_at(t, c0), z[8];
+          const int at = kept_step(c0);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {                                // (all of them before the first store: one trip to the L2 instead of eight)
+            z[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (flushed && c0 + 4 * i < d16) z[i] = p[i * at];
+          }
+          uint32_t v[32];
+          tmem_ld32(my_o + c0, v);
+          tmem_ld_wait();
+          tmem_arrived(v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (c0 + 4 * i < d16)
+              p[i * at] = make_float4(fmaf(z[i].x, f_flush, __uint_as_float(v[4 * i])), fmaf(z[i].y, f_flush, __uint_as_float(v[4 * i + 1])),
+                                      fmaf(z[i].z, f_flush, __uint_as_float(v[4 * i + 2])), fmaf(z[i].w, f_flush, __uint_as_float(v[4 * i + 3])));
+        }
+        flushed = true;
+        f_flush = 1.f;
+      };
       if (active)
         for (int j = my_first; j < n && ok; j += step) {
           const int tile = tiles + j, at = tile % R, row0 = (s.j0 + j) * N, nth = split ? j >> 1 : j;
@@ -356,78 +388,66 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           }
           const int flags = sh.flags[at];
           if (nth > 0) poisoned = poisoned || sh.poison[(tile - step) % (2 * R)];   // (the products before this tile's are done)
-          uint32_t x[N / 32][32];                                    // logits; 32 registers each, as they are loaded
-#pragma unroll
-          for (int i = 0; i < N / 32; ++i) tmem_ld32(my_s + i * 32, x[i]);
-          tmem_ld_wait();
-#pragma unroll
-          for (int i = 0; i < N / 32; ++i) tmem_arrived(x[i]);
+          if (nth > 0 && nth % C::kSummed == 0) keep();
           const int valid = min(max(limit - row0, 0), N);
           const uint32_t bias = smem_u32(sh.bias[at]);
-          float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          if (flags & 1) {
-            float4 b[2][4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) b[0][k] = lds_here(bias + k * 16);
-#pragma unroll
-            for (int g = 0; g < N / 16; ++g) {
-              if (g + 1 < N / 16)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) b[(g + 1) & 1][k] = lds_here(bias + (g + 1) * 64 + k * 16);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                uint32_t *y = x[g / 2] + g % 2 * 16 + k * 4;
-                const float4 w = b[g & 1][k];
-                to_pair(y[0], y[1], fma2(of_pair(y[0], y[1]), scale2, pair_of(w.x, w.y)));
-                to_pair(y[2], y[3], fma2(of_pair(y[2], y[3]), scale2, pair_of(w.z, w.w)));
-              }
-            }
-          }
+          const bool edge = __any_sync(0xffffffffu, valid < N);
           constexpr uint32_t kNone = 0xFF800000u;                    // minus infinity
-          if (flags & 2) {                                           // hidden rows, whose keys may be anything
+          // 32 logits, as they are loaded, with biases
+          const auto biased = [&](int c, uint32_t (&x)[32]) {
+            float4 w[8];
 #pragma unroll
-            for (int i = 0; i < N; i += 4) {
-              const float4 w = lds_here(bias + i * 4);
-              uint32_t *y = x[i / 32] + i % 32;
-              if (w.x == -INFINITY) y[0] = kNone;
-              if (w.y == -INFINITY) y[1] = kNone;
-              if (w.z == -INFINITY) y[2] = kNone;
-              if (w.w == -INFINITY) y[3] = kNone;
+            for (int k = 0; k < 8; ++k) w[k] = lds_here(bias + c * 128 + k * 16);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              uint32_t *y = x + k * 4;
+              to_pair(y[0], y[1], fma2(of_pair(y[0], y[1]), scale2, pair_of(w[k].x, w[k].y)));
+              to_pair(y[2], y[3], fma2(of_pair(y[2], y[3]), scale2, pair_of(w[k].z, w[k].w)));
             }
+          };
+          bool plain = (flags & 1) != 0;                             // biases are still to come
+          if (edge || (flags & 2)) {                                 // (a pass of its own: code that is seldom executed slows down the loop that it lies in)
+#pragma unroll 1
+            for (int c = 0; c < N / 32; ++c) {
+              uint32_t x[32];
+              tmem_ld32(my_s + c * 32, x);
+              tmem_ld_wait();
+              tmem_arrived(x);
+              if (flags & 1) biased(c, x);
+              const int left = valid - c * 32;                       // rows that the token sees
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                float4 w = make_float4(0.f, 0.f, 0.f, 0.f);          // hidden rows, whose keys may be anything
+                if (flags & 2) w = lds_here(bias + c * 128 + i * 4);
+                if (i >= left || w.x == -INFINITY) x[i] = kNone;
+                if (i + 1 >= left || w.y == -INFINITY) x[i + 1] = kNone;
+                if (i + 2 >= left || w.z == -INFINITY) x[i + 2] = kNone;
+                if (i + 3 >= left || w.w == -INFINITY) x[i + 3] = kNone;
+              }
+              tmem_st32(my_s + c * 32, x);
+            }
+            tmem_st_wait();
+            plain = false;
           }
-          if (__any_sync(0xffffffffu, valid < N)) {                  // rows that the token does not see
+          float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+          for (int c = 0; c < N / 32; ++c) {                         // (32 at a time: the code of a larger step takes longer to fetch than it saves)
+            uint32_t x[32];
+            tmem_ld32(my_s + c * 32, x);
+            tmem_ld_wait();
+            tmem_arrived(x);
+            if (plain) {
+              biased(c, x);
+              tmem_st32(my_s + c * 32, x);
+            }
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-              if (i >= valid) x[i / 32][i % 32] = kNone;
+            for (int i = 0; i < 32; i += 8)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) tops[k] = max3(tops[k], __uint_as_float(x[i + 2 * k]), __uint_as_float(x[i + 2 * k + 1]));
           }
-#pragma unroll
-          for (int i = 0; i < N; i += 8)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) tops[k] = max3(tops[k], __uint_as_float(x[i / 32][i % 32 + 2 * k]), __uint_as_float(x[i / 32][i % 32 + 2 * k + 1]));
+          tmem_st_wait();
           // (without biases x are still products of queries and keys, and the scale, which is positive then, comes with the exponent)
           const float unit = flags & 1 ? 1.f : scale, top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * unit;
-          if (WIDE && nth > 0 && nth % 2 == 0) {                     // the results of two tiles, added with rounding
-#pragma unroll 1
-            for (int c0 = 0; c0 < d16; c0 += 32) {
-              float4 *p = kept_at(t, c0), z[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {                            // (all of them before the first store: one trip to the L2 instead of eight)
-                z[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (flushed && c0 + 4 * i < d16) z[i] = p[i * 128];
-              }
-              uint32_t v[32];
-              tmem_ld32(my_o + c0, v);
-              tmem_ld_wait();
-              tmem_arrived(v);
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (c0 + 4 * i < d16)
-                  p[i * 128] = make_float4(fmaf(z[i].x, f_flush, __uint_as_float(v[4 * i])), fmaf(z[i].y, f_flush, __uint_as_float(v[4 * i + 1])),
-                                           fmaf(z[i].z, f_flush, __uint_as_float(v[4 * i + 2])), fmaf(z[i].w, f_flush, __uint_as_float(v[4 * i + 3])));
-            }
-            flushed = true;
-            f_flush = 1.f;
-          }
           if (nth == 0) {
             m = top;
           } else if (__any_sync(0xffffffffu, top > m && (m == -INFINITY || (top - m) * kTwos > kLag))) {
@@ -435,7 +455,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             m = to;
             l *= f;
             f_flush *= f;
-            if (!WIDE || nth % 2 != 0) {
+            if (nth % C::kSummed != 0) {                             // (otherwise they are among the earlier ones, and begin anew)
 #pragma unroll 1
               for (int c0 = 0; c0 < d16; c0 += 32) {
                 uint32_t v[32];
@@ -449,50 +469,37 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             }
           }
           const float ref = m == -INFINITY ? 0.f : m;
-          const unsigned long long ref2 = pair_of(-ref, -ref), unit2 = pair_of(unit, unit);
+          const unsigned long long ref2 = pair_of(-ref, -ref), unit2 = pair_of(unit, unit), minus2 = pair_of(-1.f, -1.f);
           unsigned long long sums[4] = {0ull, 0ull, 0ull, 0ull};
-          if constexpr (!WIDE) {
+#pragma unroll 1
+          for (int c = 0; c < N / 32; ++c) {
+            uint32_t x[32], p[C::kTerms][16];
+            tmem_ld32(my_s + c * 32, x);
+            tmem_ld_wait();
+            tmem_arrived(x);
 #pragma unroll
-            for (int c = 0; c < N / 32; ++c) {
-              uint32_t p[16];
+            for (int i = 0; i < 32; i += 2) {
+              float u, w;
+              unsigned long long y = fma2(of_pair(x[i], x[i + 1]), unit2, ref2);
+              if (WIDE) y = mul2(y, log2e2);
+              unpair(y, u, w);
+              y = pair_of(ex2_approx(u), ex2_approx(w));
+              sums[i / 2 % 4] = add2(sums[i / 2 % 4], y);
 #pragma unroll
-              for (int i = 0; i < 32; i += 2) {
-                float u, w;
-                unpair(fma2(of_pair(x[c][i], x[c][i + 1]), unit2, ref2), u, w);
-                u = ex2_approx(u);
-                w = ex2_approx(w);
-                sums[i / 2 % 4] = add2(sums[i / 2 % 4], pair_of(u, w));
-                p[i / 2] = bf16_pair(u, w);
-              }
-              tmem_st16(my_s + c * 16, p);
-              if (c == N / 64 - 1) {                                 // products with the first half of the rows may begin
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(sh.p_half + t);
+              for (int k = 0; k < C::kTerms; ++k) {
+                unpair(y, u, w);
+                const uint32_t h = bf16_pair(u, w);
+                p[k][i / 2] = h;
+                y = fma2(of_pair(h << 16, h & 0xFFFF0000u), minus2, y);   // (exact)
               }
             }
-          } else {
 #pragma unroll
-            for (int c = 0; c < N / 32; ++c) {
-              uint32_t p[3][16];
-#pragma unroll
-              for (int i = 0; i < 32; i += 2) {
-                float u, w;
-                unpair(mul2(fma2(of_pair(x[c][i], x[c][i + 1]), unit2, ref2), log2e2), u, w);
-                u = ex2_approx(u);
-                w = ex2_approx(w);
-                sums[i / 2 % 4] = add2(sums[i / 2 % 4], pair_of(u, w));
-#pragma unroll
-                for (int k = 0; k < 3; ++k) {
-                  const uint32_t h = bf16_pair(u, w);
-                  p[k][i / 2] = h;
-                  u -= __uint_as_float(h << 16);                     // (exact)
-                  w -= __uint_as_float(h & 0xFFFF0000u);
-                }
-              }
-#pragma unroll
-              for (int k = 0; k < 3; ++k) tmem_st16(my_s + k * (N / 2) + c * 16, p[k]);
+            for (int k = 0; k < C::kTerms; ++k) tmem_st16(my_s + C::term_at(c, k), p[k]);
+            if (!WIDE && c == N / 64 - 1) {                          // products with the first half of the rows may begin
+              tmem_st_wait();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(sh.p_half + t);
             }
           }
           tmem_st_wait();
@@ -557,17 +564,17 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         f0 *= inv;
         f1 *= inv;
         // sixteen columns at a time: the code of a larger step takes longer to fetch than it saves
-        const auto columns = [&](uint32_t from, const float4 *kept, bool has_kept, float f_kept, float (&o)[16]) {
+        const auto columns = [&](uint32_t from, const float4 *kept, int at, bool has_kept, float f_kept, float (&o)[16]) {
           uint32_t v[16];
           tmem_ld16(from, v);
           tmem_ld_wait();
           tmem_arrived(v);
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[i] = __uint_as_float(v[i]);
-          if (WIDE && has_kept) {
+          if (has_kept) {
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-              const float4 z = kept[i / 4 * 128];
+              const float4 z = kept[i / 4 * at];
               o[i] = fmaf(z.x, f_kept, o[i]);
               o[i + 1] = fmaf(z.y, f_kept, o[i + 1]);
               o[i + 2] = fmaf(z.z, f_kept, o[i + 2]);
@@ -578,12 +585,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll 1
         for (int c0 = 0; c0 < d16; c0 += 16) {
           float o[16];
-          columns(my_o + c0, kept_at(t, c0), flushed, f_flush, o);
+          columns(my_o + c0, kept_at(t, c0), kept_step(c0), flushed, f_flush, o);
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[i] *= f0;
           if (both) {
             float o1[16];
-            columns(my_o + C::kWidth + c0, kept_at(C::kBlocks - 1, c0), flushed1, f_flush1, o1);
+            columns(my_o + C::kWidth + c0, kept_at(C::kBlocks - 1, c0), kept_step(c0), flushed1, f_flush1, o1);
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[i] = l1 != 0.f ? fmaf(o1[i], f1, o[i]) : o[i];
           }
@@ -709,12 +716,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         };
         // rows [half N / 2, (half + 1) N / 2) of a tile, or all of them
         const auto add_values = [&](int t, int st, int half, bool accumulate) {
-          const uint32_t db = v0 + st * (C::kStage / 16) + half * (N / 32) * (2048 / 16), to = tmem + C::kO + t * C::kWidth, from = tmem + t * C::kRegion + half * (N / 32) * 8;
+          const uint32_t db = v0 + st * (C::kStage / 16) + half * (N / 32) * (2048 / 16), to = tmem + C::kO + t * C::kWidth, from = tmem + t * C::kRegion;
 #pragma unroll
           for (int term = C::kTerms - 1; term >= 0; --term)          // the small terms first
 #pragma unroll
             for (int k = 0; k < (WIDE ? N / 16 : N / 32); ++k)
-              umma_ts(to, from + term * (N / 2) + k * 8, db + k * (2048 / 16), values, k != 0 || term != C::kTerms - 1 ? 1 : accumulate);
+              umma_ts(to, from + C::term_at((half * (N / 32) + k) / 2, term) + k % 2 * 8, db + k * (2048 / 16), values, k != 0 || term != C::kTerms - 1 ? 1 : accumulate);
         };
         // the stage of the next load in the order in which they were asked for, and its phase
         const auto take = [&](uint32_t &ph) {
@@ -756,13 +763,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 ok = wait.alone(sh.p_half + t, p_phase >> t);
                 if (!ok) break;
                 tc_fence_after();
-                add_values(t, sv, 0, nth > 0);
+                add_values(t, sv, 0, nth % C::kSummed != 0);
               }
               ok = wait.alone(sh.p_ready + t, p_phase >> t);
               p_phase ^= 1u << t;
               if (!ok) break;
               tc_fence_after();
-              if (WIDE) add_values(t, sv, 0, (nth & 1) != 0);
+              if (WIDE) add_values(t, sv, 0, nth % C::kSummed != 0);
               else add_values(t, sv, 1, true);
               if (more) logits(t, split ? 0 : t, sk);
               else umma_commit(sh.o_full + t);
@@ -957,14 +964,12 @@ size_t chunk_scratch(const ChunkCfg &cfg, int requests, ChunkArgs *a, char *base
     at += round256(bytes);
     return p;
   };
-  const bool kept = cfg.wide && cfg.blocks > 1;                       // (64 columns wide: sums of earlier tiles stay in shared memory)
-  char *o = take(parts * cfg.width * sizeof(float)), *ml = take(parts * sizeof(float2)), *flush = take(kept ? G * cfg.rows * cfg.width * sizeof(float) : 0),
+  char *o = take(parts * cfg.width * sizeof(float)), *ml = take(parts * sizeof(float2)),
        *cut = take(2 * G * sizeof(ChunkCut)), *tail = take(G * sizeof(int)), *head = take(G * G * sizeof(int)),
        *pre = take(requests < kChunkPreInSmem ? 0 : G * ((size_t)requests + 1) * sizeof(int)), *poison = take(G * kChunkPoison * kChunkMaxWidth * sizeof(int));
   if (a) {
     a->part_o = reinterpret_cast<float *>(o);
     a->part_ml = reinterpret_cast<float2 *>(ml);
-    a->flush = reinterpret_cast<float *>(flush);
     a->cut = reinterpret_cast<ChunkCut *>(cut);
     a->tail = reinterpret_cast<int *>(tail);
     a->head = reinterpret_cast<int *>(head);

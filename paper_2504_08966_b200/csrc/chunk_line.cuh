@@ -37,6 +37,7 @@ struct ChunkSegment : ChunkRequest {
   int b, kv, rows, first;                  // rows of the item, its first row among the request's (token row / group, head row % group)
   int k, j0, j1;
   int slot;                                // of its part, -1: the whole item
+  int place;                               // the slot that it may use meanwhile, its own in any case
   __device__ __forceinline__ int limit(int token, bool causal) const { return causal ? min(len, len - want + token + 1) : len; }   // rows that a token sees
 };
 
@@ -74,6 +75,7 @@ struct ChunkLine {
       s.j0 = 0;
       s.j1 = s.k;
       s.slot = -1;
+      s.place = me;                        // (the CTA's beginning of an item comes later)
       return true;
     }
     if (stage == 0) {
@@ -83,6 +85,7 @@ struct ChunkLine {
         s.j0 = 0;
         s.j1 = head[me];
         s.slot = s.j1 == s.k ? -1 : me;
+        s.place = me;
         return true;
       }
     }
@@ -90,7 +93,8 @@ struct ChunkLine {
       item<ROWS, TILE>(a, last + q, s);
       s.j0 = (q < G ? head[q] : 0) + off;
       s.j1 = min(s.k, s.j0 + tail);
-      s.slot = s.j0 == 0 && s.j1 == s.k ? -1 : G + q + me;
+      s.place = G + q + me;
+      s.slot = s.j0 == 0 && s.j1 == s.k ? -1 : s.place;
       ++q;
       off = 0;
       if (s.j1 <= s.j0) continue;
