@@ -112,7 +112,7 @@ struct ChunkLineKept {
   int q, off;
 };
 struct ChunkLineSetup {
-  unsigned long long tiles;
+  unsigned long long tiles, rows;
   int warp[32];
   int dp[kChunkMaxSms];                    // tiles of the whole items of each CTA
   int lp[2 * kChunkMaxSms + 1];            // rests before each item of the last round
@@ -199,30 +199,36 @@ template <int THREADS, int ROWS, int TILE> __device__ __forceinline__ ChunkLine 
   line.kept = kept.request;
   line.done = line.stage = 0;
   if (tid == 0) {
-    set.tiles = 0;
+    set.tiles = set.rows = 0;
     kept.q = kept.off = 0;
   }
   __syncthreads();
   {
     const int per = (a.B + THREADS - 1) / THREADS, b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
     int mine = 0, total;
-    unsigned long long tiles = 0;
+    unsigned long long tiles = 0, rows = 0;
     for (int b = b0; b < b1; ++b) {
       const ChunkRequest q = chunk_request(a, b);
       if (a.B <= kChunkKept) kept.request[b] = q;
       if (q.bad && me == 0 && a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
       pre[b] = mine;
       mine += chunk_items(q, a.group, ROWS);
+      rows += q.n;
       tiles += chunk_tiles_of_head(q, a.group, ROWS, TILE, a.causal);
     }
-    if (tiles) atomicAdd(&set.tiles, tiles);
+    if (tiles) {
+      atomicAdd(&set.tiles, tiles);
+      atomicAdd(&set.rows, rows);
+    }
     const int before = chunk_scan<THREADS>(mine, set.warp, &total);
     for (int b = b0; b < b1; ++b) pre[b] += before;
     if (tid == 0) pre[a.B] = total;
   }
   __syncthreads();
-  const int items = pre[a.B] * a.n_kvh;
-  const long long T = (long long)set.tiles * a.n_kvh;
+  const bool fits = chunk_rows_fit(set.rows, a.n_rows);
+  if (!fits && me == 0 && tid == 0 && a.status) atomicMin(a.status, (int)PACT_ERR_INVALID_ARG);
+  const int items = fits ? pre[a.B] * a.n_kvh : 0;                   // (of nothing else is there more than was checked)
+  const long long T = fits ? (long long)set.tiles * a.n_kvh : 0;
   line.rounds = items >= 2 * G ? items / G - 1 : 0;
   line.last = line.rounds * G;
   line.r = items - line.last;

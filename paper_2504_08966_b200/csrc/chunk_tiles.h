@@ -37,6 +37,10 @@ PAGED_HD unsigned long long floor_sum(unsigned long long n, unsigned long long m
   return floor_sum_in<unsigned long long>(n, m, a, b);
 }
 
+// Requests whose rows overlap may be served more rows in all than there are, and their items and tiles go beyond the 32 bits that the host has checked for n_rows of them.  (`rows` of at most
+// PACT_MAX_REQUESTS requests, each below 2^31.)
+PAGED_HD bool chunk_rows_fit(unsigned long long rows, long long n_rows) { return rows <= (unsigned long long)n_rows; }
+
 // One request of a chunk: `n` new tokens that are served out of `want`, the last of `len` cached rows.
 struct ChunkLengths {
   int n, want, len;
