@@ -788,7 +788,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       int loads = 0, tiles = 0, segment = 0;
       while (ok && line.next<C::kRows, N>(a, s)) {
         const int n = s.j1 - s.j0, ahead = C::kBlocks == 2 && s.rows <= 128 ? 2 : 1;
-        const int seen = s.limit(s.first / a.group, a.causal);         // by all tokens of the item
+        const int seen = max(0, s.limit(s.first / a.group, a.causal)); // by all tokens of the item
         int *poison = a.poison + ((long long)blockIdx.x * kChunkPoison + segment % kChunkPoison) * kChunkMaxWidth;
         bool poisoned = false;
         for (int j = 0; j < n; ++j) {
@@ -822,7 +822,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           ok = wait(sh.full + st, x / S);
           if (!ok) break;
           bool found = false;
-          if (hidden || row0 + N > seen) {
+          if (hidden || chunk_edge(row0, N, seen)) {
             // (rows that every token of the item sees may hold what they like)
             const int c = lane & 7, from = hidden ? 0 : max(0, seen - row0) & ~3;
             constexpr uint32_t kAll = N == 128 ? 0xffffffffu : (1u << (N / 4 % 32)) - 1u;

@@ -46,6 +46,8 @@ struct ChunkLengths {
   int n, want, len;
 };
 PAGED_HD int chunk_before(const ChunkLengths &q) { return q.len > q.want ? q.len - q.want : 0; }   // rows cached before the new ones
+// Whether a tile from row0 on has rows beyond `seen` (which is not negative: row0 + tile may be 2^31).
+PAGED_HD bool chunk_edge(int row0, int tile, int seen) { return seen - row0 < tile; }
 PAGED_HD int chunk_items(const ChunkLengths &q, int group, int rows) { return (int)(((unsigned)q.n * (unsigned)group + (unsigned)rows - 1u) / (unsigned)rows); }   // (n g < 2^31)
 // Tiles of `tile` rows that item i of a key head meets.  Its last row is of token ceil(min(n g, (i + 1) rows) / g) - 1.
 PAGED_HD int chunk_tiles(const ChunkLengths &q, int i, int group, int rows, int tile, bool causal) {

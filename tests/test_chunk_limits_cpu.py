@@ -44,3 +44,27 @@ int main() {
   if (!chunk_rows_fit(0, 0) || chunk_rows_fit(1, 0) || !chunk_rows_fit(INT32_MAX, INT32_MAX) || chunk_rows_fit(4096ull * INT32_MAX, INT32_MAX)) return 1;
   return 0;
 }""", ["g++", "-O2", "-std=c++17", "-I", CSRC])
+
+
+def test_edges_at_the_largest_lengths(tmp_path):
+    """Whether a tile has rows that some token does not see, against 64 bits: lengths up to 2^31 - 1."""
+    _run(tmp_path, r"""
+#include <stdio.h>
+#include <initializer_list>
+#include "chunk_tiles.h"
+using namespace pact;
+int main() {
+  const int ends[] = {0, 1, 2, 63, 64, 127, 128, 129, 1000, 1 << 30, INT32_MAX - 200, INT32_MAX - 128, INT32_MAX - 127, INT32_MAX - 126, INT32_MAX - 64, INT32_MAX - 15, INT32_MAX - 1, INT32_MAX};
+  int past = 0;
+  for (int seen : ends)
+    for (int tile : {64, 128})
+      for (int at : ends)
+        for (int back = 0; back < 3; ++back) {
+          const long long row0 = ((long long)at / tile - back) * tile;
+          if (row0 < 0) continue;
+          const bool edge = row0 + tile > seen;
+          past += row0 + tile > INT32_MAX;
+          if (chunk_edge((int)row0, tile, seen) != edge) { printf("row %lld, tile %d, seen %d\n", row0, tile, seen); return 1; }
+        }
+  return past > 100 ? 0 : 1;
+}""", ["g++", "-O2", "-std=c++17", "-fsanitize=undefined", "-fno-sanitize-recover", "-I", CSRC])

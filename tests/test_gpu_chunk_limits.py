@@ -26,3 +26,23 @@ def test_requests_that_share_rows_of_q(pb, dtype, out, B, n_rows):
     m = n_rows // B
     ctx.pact_chunk_attention(cache, Q, table, length, i32([m] * B), got, row_start=i32([m * b for b in range(B)]), lse=lse, status=status)
     assert status.item() == 0 and torch.isfinite(got[:m * B]).all() and (got[:m * B] != -5).any(2).all() and (got[m * B:] == -5).all() and (lse[m * B:] == -5).all()
+
+
+@pytest.mark.parametrize("dtype,out,page,n", [(BF, BF, 64, (1 << 31) - 64 - 10), (BF, F32, 64, (1 << 31) - 64 - 10), (BF, BF, 16, (1 << 31) - 16 - 3)])
+def test_the_longest_requests(pb, dtype, out, page, n):
+    """2^31 rows, but for the last few, of pages that lie in the table many times: what the last page holds behind them does not matter."""
+    if torch.cuda.mem_get_info()[0] < 4 << 30:
+        pytest.skip("not enough memory")
+    D, width = 64, n // page + 1
+    K, V = torch.zeros(2, 1, page, D, dtype=dtype, device="cuda"), torch.ones(2, 1, page, D, dtype=dtype, device="cuda")
+    V[:, :, :, 1] = -2
+    V[1, :, n % page:], K[1, :, n % page:] = float("nan"), float("inf")
+    table = torch.zeros(1, width, dtype=I32, device="cuda")
+    table[0, -1] = 1
+    got, lse, status = torch.zeros(3, 1, D, dtype=out, device="cuda"), torch.zeros(3, 1, device="cuda"), i32([0])
+    context(pb, 1, 1, D, dtype, out).pact_chunk_attention(pb.PagedCache(K, V), torch.ones(3, 1, D, dtype=dtype, device="cuda"), table, i32([n]), i32([3]), got, row_start=i32([0]), lse=lse,
+                                                          status=status)
+    # equal weights: exact sums are the values.  A CTA adds up 2^24 / 148 tiles (fp32 results: twice as many of half the size) in sums that grow from nothing, with rounding: 2^18 / 2 * 2^-24 at most
+    # for the weights and as much for the results
+    assert status.item() == 0 and ((got.double()[..., [0, 1]] - torch.tensor([1.0, -2.0], device="cuda")).abs() <= 2.0 ** -6).all()
+    assert (got[..., 2:] == got[..., :1]).all() and ((lse.double() - torch.log(torch.tensor(float(n)))).abs() <= 2.0 ** -6).all()
