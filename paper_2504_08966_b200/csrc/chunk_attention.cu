@@ -788,7 +788,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       int loads = 0, tiles = 0, segment = 0;
       while (ok && line.next<C::kRows, N>(a, s)) {
         const int n = s.j1 - s.j0, ahead = C::kBlocks == 2 && s.rows <= 128 ? 2 : 1;
-        const int seen = max(0, s.limit(s.first / a.group, a.causal)); // by all tokens of the item
+        const int seen = s.limit(s.first / a.group, a.causal);         // by all tokens of the item
         int *poison = a.poison + ((long long)blockIdx.x * kChunkPoison + segment % kChunkPoison) * kChunkMaxWidth;
         bool poisoned = false;
         for (int j = 0; j < n; ++j) {

@@ -38,7 +38,7 @@ struct ChunkSegment : ChunkRequest {
   int k, j0, j1;
   int slot;                                // of its part, -1: the whole item
   int place;                               // the slot that it may use meanwhile, its own in any case
-  __device__ __forceinline__ int limit(int token, bool causal) const { return causal ? min(len, len - want + token + 1) : len; }   // rows that a token sees
+  __device__ __forceinline__ int limit(int token, bool causal) const { return chunk_seen(*this, token, causal); }   // rows that a token sees
 };
 
 constexpr int kChunkPreInSmem = 33;        // entries of `pre` that are kept in shared memory

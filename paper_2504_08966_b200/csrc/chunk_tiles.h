@@ -46,6 +46,11 @@ struct ChunkLengths {
   int n, want, len;
 };
 PAGED_HD int chunk_before(const ChunkLengths &q) { return q.len > q.want ? q.len - q.want : 0; }   // rows cached before the new ones
+// Rows that a token sees: none where there are more new tokens than rows and it comes before the first (by up to 2^31 - 2 rows, so that nothing could be taken from a negative number).
+PAGED_HD int chunk_seen(const ChunkLengths &q, int token, bool causal) {
+  const int seen = causal ? q.len - q.want + token + 1 : q.len;
+  return seen < 0 ? 0 : seen < q.len ? seen : q.len;
+}
 // Whether a tile from row0 on has rows beyond `seen` (which is not negative: row0 + tile may be 2^31).
 PAGED_HD bool chunk_edge(int row0, int tile, int seen) { return seen - row0 < tile; }
 PAGED_HD int chunk_items(const ChunkLengths &q, int group, int rows) { return (int)(((unsigned)q.n * (unsigned)group + (unsigned)rows - 1u) / (unsigned)rows); }   // (n g < 2^31)

@@ -68,3 +68,27 @@ int main() {
         }
   return past > 100 ? 0 : 1;
 }""", ["g++", "-O2", "-std=c++17", "-fsanitize=undefined", "-fno-sanitize-recover", "-I", CSRC])
+
+
+def test_what_a_token_sees_beside_the_largest_counts(tmp_path):
+    """Against 64 bits: lengths up to 2^31 - 1, and up to as many more new tokens than rows."""
+    _run(tmp_path, r"""
+#include <stdio.h>
+#include "chunk_tiles.h"
+using namespace pact;
+int main() {
+  const int ends[] = {0, 1, 2, 63, 64, 127, 128, 129, 1000, 1 << 30, INT32_MAX - 200, INT32_MAX - 128, INT32_MAX - 127, INT32_MAX - 126, INT32_MAX - 64, INT32_MAX - 15, INT32_MAX - 1, INT32_MAX};
+  int none = 0;
+  for (int len : ends)
+    for (int want : ends)
+      for (int token : ends)
+        for (int causal = 0; causal < 2; ++causal) {
+          if (token >= want) continue;
+          const ChunkLengths q = {want, want, len};
+          long long sees = causal ? (long long)len - want + token + 1 : len;
+          sees = sees < 0 ? 0 : sees > len ? len : sees;
+          none += sees == 0 && len > 0;
+          if (chunk_seen(q, token, causal) != sees) { printf("%d rows, %d new, token %d: %d instead of %lld\n", len, want, token, chunk_seen(q, token, causal), sees); return 1; }
+        }
+  return none > 100 ? 0 : 1;
+}""", ["g++", "-O2", "-std=c++17", "-fsanitize=undefined", "-fno-sanitize-recover", "-I", CSRC])

@@ -46,3 +46,21 @@ def test_the_longest_requests(pb, dtype, out, page, n):
     # for the weights and as much for the results
     assert status.item() == 0 and ((got.double()[..., [0, 1]] - torch.tensor([1.0, -2.0], device="cuda")).abs() <= 2.0 ** -6).all()
     assert (got[..., 2:] == got[..., :1]).all() and ((lse.double() - torch.log(torch.tensor(float(n)))).abs() <= 2.0 ** -6).all()
+
+
+@pytest.mark.parametrize("dtype,out", [(BF, BF), (BF, F32), (F32, F32)])
+def test_many_more_new_tokens_than_rows(pb, dtype, out):
+    """Up to 2^31 - 1 new tokens of a request of 50 rows, of which 300 have a row: none of these sees anything, whatever lay in the places of their tiles before."""
+    g, D, page = torch.Generator(device="cuda").manual_seed(0), 64, 16
+    K, V, _ = cache_of(g, 300, 1, page, D, dtype)
+    V[4:] = float("inf")
+    K[4:] = float("nan")
+    ctx, cache = context(pb, 1, 1, D, dtype, out), pb.PagedCache(K, V)
+    table = torch.arange(4, 300, dtype=I32, device="cuda")[None].repeat(3, 1)
+    table[1, :4] = torch.arange(4, dtype=I32, device="cuda")
+    Q, got, lse, status = torch.randn(600, 1, D, generator=g, device="cuda").to(dtype), torch.full((600, 1, D), -5.0, dtype=out, device="cuda"), torch.full((600, 1), -5.0, device="cuda"), i32([0])
+    for want in ((1 << 31) - 1, (1 << 31) - 200, 1 << 30, 1000):
+        ctx.pact_chunk_attention(cache, Q, table[:1], i32([296 * page]), i32([300]), got, row_start=i32([0]))     # (infinities and NaN in all the tiles that shared memory holds)
+        ctx.pact_chunk_attention(cache, Q, table[1:2], i32([50]), i32([want]), got, row_start=i32([300]), lse=lse, status=status)
+        assert status.item() == po.INVALID and not got[300:].any() and (lse[300:] == -torch.inf).all(), want
+        status.zero_()
