@@ -446,7 +446,7 @@ size_t pact_chunk_workspace_bytes(const pact_ctx *ctx, int max_requests);
  * without any row gets 0, and lse minus infinity.  Infinities and NaN in rows that count leave infinities or NaN in the results that they enter (infinite values beside bf16 keys: NaN).
  * Rows of Q, out and lse that belong to no token are not touched.
  * Logits, softmax statistics and sums are fp32.  bf16 keys and values: probabilities are carried as two bf16 terms (off by 2^-17 at most) where results are bf16, and as
- * three where they are fp32; bf16 results take logits in powers of two, so that finite biases beyond 2.35e38 in magnitude count as the largest number.
+ * three where they are fp32.
  * Lengths outside 0 .. max_pages * page_rows are clamped, rows of pages outside the cache left out, tokens without a row of Q (beyond n_rows or the row_stride) left out, and tokens before the first cached row (n_new above
  * length) see nothing; each sets status to INVALID_ARG.  Rows of Q and out belong to one request each: a call whose requests together name more rows than n_rows (their row_starts overlap) serves
  * nothing and sets it too.  Heads as above; n_rows * (n_qh / n_kvh) below 2^31. */

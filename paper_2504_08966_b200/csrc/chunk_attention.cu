@@ -26,8 +26,6 @@
 // Sums of probabilities are taken before the rounding.
 // The second term took the long case from 1.14 to 1.50 ms, the prompts from 0.70 to 0.73 and left the drafts as they were, with the loops over a tile rolled: each is 32 columns of code, logits go back to tensor memory with their
 // biases.  All of a tile's columns in registers and straight code for them, as one term had it, took 1.99, 1.02 and 0.26 ms: the warps waited for instructions (1.4 warps per one that was issued, instead of 0.5).
-#include <float.h>
-
 #include "chunk_row.cuh"
 
 namespace pact {
@@ -292,10 +290,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       if (C::kKept && c0 < C::kKept) return &sh.kept[block][c0 / 4][row];
       return reinterpret_cast<float4 *>(a.part_o) + ((long long)s.place * (C::kWidth / 4) + c0 / 4) * C::kRows + block * 128 + row;
     };
-    // Logits of bf16 results are kept in powers of two, a multiplication less; those of fp32 results in natural units, which round once less.
-    constexpr float kTwos = WIDE ? kChunkLog2e : 1.f;
-    const float scale = WIDE ? a.scale : a.scale * kChunkLog2e;
-    const auto weight = [](float m, float to) { return m == -INFINITY ? 0.f : m == to ? 1.f : ex2_approx((m - to) * kTwos); };   // as part_weight
+    const float scale = a.scale;                                     // (logits stay in natural units, a multiplication more than powers of two: a bias may be any float)
     const unsigned long long scale2 = pair_of(scale, scale), log2e2 = pair_of(kChunkLog2e, kChunkLog2e);
     uint32_t s_phase = 0, o_phase = 0;
     int tiles = 0, segment = 0;
@@ -450,8 +445,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           const float unit = flags & 1 ? 1.f : scale, top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * unit;
           if (nth == 0) {
             m = top;
-          } else if (__any_sync(0xffffffffu, top > m && (m == -INFINITY || (top - m) * kTwos > kLag))) {
-            const float to = fmaxf(m, top), f = weight(m, to);
+          } else if (__any_sync(0xffffffffu, top > m && (m == -INFINITY || (top - m) * kChunkLog2e > kLag))) {
+            const float to = fmaxf(m, top), f = part_weight(m, to);
             m = to;
             l *= f;
             f_flush *= f;
@@ -480,10 +475,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
               float u, w;
-              unsigned long long y = fma2(of_pair(x[i], x[i + 1]), unit2, ref2);
-              if (WIDE) y = mul2(y, log2e2);
-              unpair(y, u, w);
-              y = pair_of(ex2_approx(u), ex2_approx(w));
+              unpair(mul2(fma2(of_pair(x[i], x[i + 1]), unit2, ref2), log2e2), u, w);
+              unsigned long long y = pair_of(ex2_approx(u), ex2_approx(w));
               sums[i / 2 % 4] = add2(sums[i / 2 % 4], y);
 #pragma unroll
               for (int k = 0; k < C::kTerms; ++k) {
@@ -546,8 +539,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           m1 = __uint_as_float(v[0]);
           l1 = __uint_as_float(v[1]);
           const float to = fmaxf(m, m1);
-          f0 = weight(m, to);
-          f1 = weight(m1, to);
+          f0 = part_weight(m, to);
+          f1 = part_weight(m1, to);
           f_flush1 = __uint_as_float(v[2]);
           flushed1 = v[3] & 1u;
           poisoned = poisoned || (v[3] & 2u);
@@ -556,7 +549,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         }
         if (fills && ok) give_q();                                   // (the next logits take the place of what has just been read)
       }
-      if (!WIDE) m = m < -2.3e38f ? m : m * 0.6931471805599453f;     // (the lowest float stands for itself)
       if (active && ok && (!split || t == 0) && !idle) {
         const bool both = split && __any_sync(0xffffffffu, l1 != 0.f);
         const float inv = s.slot >= 0 ? 1.f : l == 0.f ? 0.f : 1.f / l;
@@ -808,11 +800,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             live[i] = __ballot_sync(0xffffffffu, i < left && bs[i] != -INFINITY);
           }
           hidden = __any_sync(0xffffffffu, hidden);
-          __syncwarp();
-          if (!WIDE && counts && lane < N / 4) {                       // in powers of two; finite ones stay finite
-            const auto in_twos = [](float x) { return isfinite(x) ? fminf(fmaxf(x * kChunkLog2e, -FLT_MAX), FLT_MAX) : x; };
-            *reinterpret_cast<float4 *>(sh.bias[at] + lane * 4) = make_float4(in_twos(b.x), in_twos(b.y), in_twos(b.z), in_twos(b.w));
-          }
           __syncwarp();
           if (lane == 0) {
             sh.flags[at] = (counts ? 1 : 0) | (hidden ? 2 : 0);

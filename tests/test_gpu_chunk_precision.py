@@ -48,3 +48,55 @@ def test_bf16_results_of_long_sums_are_not_cut_off(pb, m, D):
     want = (torch.einsum("pr,phrc->hc", p, V.double()) / p.sum()).cpu().numpy()
     tol = 2.0 ** -17 + 2.0 ** -15 + 264 * 2.0 ** -24 + 2.0 ** -20
     assert (np.abs(f64(out) - want) <= half_step(want) + tol * want).all()
+
+
+LOWEST = torch.finfo(F32).min
+
+
+@pytest.mark.parametrize("dtype,out", [(BF, BF), (BF, F32), (F32, F32), (F32, BF)])
+@pytest.mark.parametrize("n_qh,H,D,lens,new", [(8, 2, 64, [3000], [300]), (2, 1, 128, [2000, 700], [3, 2]), (2, 2, 64, [300] * 200, [150] * 200), (1, 1, 64, [20] * 500, [2] * 500)])
+def test_biases_as_large_as_floats_get(pb, dtype, out, n_qh, H, D, lens, new):
+    """Where all rows have the same large bias, logits are lost in its last place: they share the attention, and the bias is the log-sum-exp.  In items that several CTAs share, in whole ones, in
+    those of few rows and of one tile; beside rows without a bias such rows are nothing, or everything."""
+    # equal weights are exact, in one term; values of both signs: fp32 sums of up to 3,000, 24 instructions that cut 2^-23 each at every 128 rows, or 8 of them at every 128 of 4,096, and a rounding
+    # per row (fp32 rows) in sums that grow from nothing: less than 2^-12 of the mean of |v|
+    g, page, B = torch.Generator(device="cuda").manual_seed(len(lens)), 16, len(lens)
+    pages = [(n + page - 1) // page for n in lens]
+    first = np.concatenate([[0], np.cumsum(pages)])
+    K, V = (torch.randn(int(first[-1]), H, page, D, generator=g, device="cuda").to(dtype) for _ in range(2))
+    table = np.full((B, max(pages)), -1, np.int32)
+    for b in range(B):
+        table[b, :pages[b]] = np.arange(first[b], first[b + 1])
+    starts, rows = np.concatenate([[0], np.cumsum(new)]), sum(new)
+    Q, got, lse = torch.randn(rows, n_qh, D, generator=g, device="cuda").to(dtype), torch.zeros(rows, n_qh, D, dtype=out, device="cuda"), torch.zeros(rows, n_qh, device="cuda")
+    w = torch.zeros(int(first[-1]), page, device="cuda")
+    call = lambda: context(pb, n_qh, H, D, dtype, out).pact_chunk_attention(pb.PagedCache(K, V, w), Q, i32(table), i32(lens), i32(new), got, row_start=i32(starts), lse=lse)   # noqa: E731
+    means = []
+    for b in range(0, B, max(1, B // 4)):
+        v = V[first[b]:first[b + 1]].double().transpose(1, 2).reshape(-1, H, D)[:lens[b]]
+        n = torch.arange(lens[b] - new[b] + 1, lens[b] + 1, device="cuda")[:, None, None]
+        means.append((b, (v.cumsum(0)[lens[b] - new[b]:] / n).repeat_interleave(n_qh // H, 1), (v.abs().cumsum(0)[lens[b] - new[b]:] / n).repeat_interleave(n_qh // H, 1)))
+    for bias in (LOWEST, -3e38, -2.3e38, -2e38, -1.6e38, -1e30, 1e30, 1.6e38, 2.4e38, 3e38, -LOWEST):
+        w.fill_(bias)
+        call()
+        assert (lse == w[0, 0]).all(), bias
+        for b, mean, size in means:
+            assert ((got[starts[b]:starts[b + 1]].double() - mean).abs() <= size * 2.0 ** -12 + mean.abs() * torch.finfo(out).eps / 2).all(), bias
+    # every third row has the bias, the others none: what is left without it, and what it leaves
+    plain = torch.arange(page, device="cuda") % 3 != 0
+    w[:] = torch.where(plain, 0.0, -torch.inf)
+    call()
+    want, want_lse = got.clone(), lse.clone()
+    for bias in (LOWEST, -2e38, -1.6e38):
+        w[:] = torch.where(plain, 0.0, bias)
+        call()
+        seen = torch.isfinite(want_lse)
+        assert torch.equal(got[seen], want[seen]) and torch.equal(lse[seen], want_lse[seen])
+    for bias in (2e38, 3e38):
+        w[:] = torch.where(plain, 0.0, bias)
+        call()
+        assert (lse == torch.tensor(bias, device="cuda")).all()
+        w[:] = torch.where(plain, -torch.inf, bias)
+        want = got.clone()
+        call()
+        assert torch.equal(got, want)
