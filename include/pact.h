@@ -403,7 +403,7 @@ pact_status pact_page_select(pact_ctx *ctx, const pact_paged_cache *cache /*host
  * floor(j * n_kvh / n_qh).  With `selected` only the rows of those pages count: of the first min(n_select, pages of the request) entries,
  * those below 0 or beyond the request's pages are skipped, and a page named twice counts twice.  Rows with logw = minus infinity and
  * rows past the length have no effect, whatever their keys and values hold.  Without any row out is 0 and lse minus infinity.  Infinities and NaN in rows that count
- * leave infinities or NaN in the results that they enter (an infinite value beside bf16 keys: NaN).  Keys and values are read once for every 16 query heads of a key head (fp32: 8).
+ * leave infinities or NaN in the results that they enter (an infinite value beside bf16 keys: that infinity or NaN, as the terms of its probability have it).  Keys and values are read once for every 16 query heads of a key head (fp32: 8).
  * Logits, probabilities, softmax statistics and sums are fp32 (beside bf16 values probabilities are carried as three bf16 terms).
  * Lengths are clamped to 0 .. max_pages * page_rows and rows of pages outside
  * the cache are left out; both set status to INVALID_ARG. */
@@ -443,7 +443,8 @@ size_t pact_chunk_workspace_bytes(const pact_ctx *ctx, int max_requests);
  * floor(j * n_kvh / n_qh).  Token i of request b is cached row length[b] - n_new[b] + i and sees the rows p up to that one (causal), or all rows 0 .. length[b] - 1 (text that
  * looks at the states of an encoder, say).
  * Rows with logw = minus infinity, rows past the length and rows that a token must not see have no effect on it, whatever their keys and values hold.  A token
- * without any row gets 0, and lse minus infinity.  Infinities and NaN in rows that count leave infinities or NaN in the results that they enter (infinite values beside bf16 keys: NaN).
+ * without any row gets 0, and lse minus infinity.  Infinities and NaN in rows that count leave infinities or NaN in the results that they enter (an infinite value beside bf16 keys:
+ * that infinity or NaN, as the terms of its probability have it and where its tile lies).
  * Rows of Q, out and lse that belong to no token are not touched.
  * Logits, softmax statistics and sums are fp32.  bf16 keys and values: probabilities are carried as two bf16 terms (off by 2^-17 at most) where results are bf16, and as
  * three where they are fp32.

@@ -100,3 +100,30 @@ def test_biases_as_large_as_floats_get(pb, dtype, out, n_qh, H, D, lens, new):
         want = got.clone()
         call()
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype,out,n_qh,H,D", [(BF, BF, 4, 2, 128), (BF, F32, 4, 2, 128), (BF, BF, 1, 1, 64), (BF, F32, 2, 1, 256), (F32, F32, 4, 2, 64)])
+@pytest.mark.parametrize("m", [1, 300])
+def test_infinite_values_anywhere_are_that_infinity_or_nan(pb, dtype, out, n_qh, H, D, m):
+    """In the first tile, which all tokens see in full, between, and in the last one: in the tokens that see the row an infinity of that sign or NaN, in its columns alone; and the same of the
+    attention of one token."""
+    n, page = 2000, 16
+    g = torch.Generator(device="cuda").manual_seed(D)
+    K, V = (torch.randn(n // page, H, page, D, generator=g, device="cuda").to(dtype) for _ in range(2))
+    Q, table = torch.randn(m, n_qh, D, generator=g, device="cuda").to(dtype), torch.arange(n // page, dtype=I32, device="cuda")[None]
+    ctx, clean, got = context(pb, n_qh, H, D, dtype, out), torch.zeros(m, n_qh, D, dtype=out, device="cuda"), torch.zeros(m, n_qh, D, dtype=out, device="cuda")
+    ctx.pact_chunk_attention(pb.PagedCache(K, V), Q, table, i32([n]), i32([m]), clean, row_start=i32([0]))
+    for at in (0, 5, 700, n - m, n - 1):
+        kept = V[at // page, 0, at % page].clone()
+        V[at // page, 0, at % page, 1], V[at // page, 0, at % page, D - 1] = float("inf"), -float("inf")
+        first, heads, rest = max(0, at - (n - m)), n_qh // H, [c for c in range(D) if c not in (1, D - 1)]
+        ctx.pact_chunk_attention(pb.PagedCache(K, V), Q, table, i32([n]), i32([m]), got, row_start=i32([0]))
+        assert torch.equal(got[:first], clean[:first]) and torch.equal(got[:, heads:], clean[:, heads:]) and torch.equal(got[first:, :heads][..., rest], clean[first:, :heads][..., rest]), at
+        for c, sign in ((1, 1), (D - 1, -1)):
+            hit = got[first:, :heads, c]
+            assert (hit.isnan() | (hit == sign * float("inf"))).all(), at
+        if m == 1:
+            one = torch.zeros(1, n_qh, D, dtype=out, device="cuda")
+            ctx.pact_paged_attention(pb.PagedCache(K, V), Q, table, i32([n]), one)
+            assert all((x.isnan() | (x == s * float("inf"))).all() for x, s in ((one[0, :heads, 1], 1), (one[0, :heads, D - 1], -1))) and torch.isfinite(one[0, :heads][:, rest]).all()
+        V[at // page, 0, at % page] = kept
