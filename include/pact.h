@@ -461,6 +461,7 @@ pact_status pact_chunk_attention(pact_ctx *ctx, const pact_paged_cache *cache /*
  * another's.  Whole pages are shared.  A page that the last rows fill in part is kept by the first request that ends in it if nobody else holds it afterwards; every other such
  * request gets a page of its own, off the top of the free stack, and an entry {from, to, rows} in `copies`, which pact_page_copy carries out for every layer (in the order of the requests).  Pages that
  * nobody holds any more are pushed on the stack first, in the order of the first places (request, then place) that named them.
+ * This call and pact_cache_compact take a cluster of 16 CTAs: PACT_ERR_UNSUPPORTED where the device, or the part of it that a process has, cannot launch one.
  * A call that cannot be served as a whole leaves everything as it is: the tables, lengths, counts, stack and n_free_out repeat the old ones, there are no copies, and status becomes PACT_ERR_NO_PAGES or
  * PACT_ERR_INVALID_ARG (a length outside 0 .. max_pages * page_rows, a source that is none, rows outside 0 .. the source's length, a page id outside the cache, n_free outside 0 .. n_pages, a page named
  * by more requests than it has holders). */

@@ -225,13 +225,13 @@ pact_status pact_create(pact_ctx **out, int d, int n_qh, int n_kvh, int d_h, pac
   }
   c->umma = in == PACT_BF16 && umma_supported(c->d_k);
   e = paged_configure(&c->paged, c->dev, n_qh, n_kvh, d_h, in == PACT_BF16);
-  if (e == cudaSuccess) e = share_configure();
   if (e == cudaSuccess) e = chunk_configure(&c->chunk, c->dev, d_h, in == PACT_BF16, c->out == PACT_BF16);
   if (e != cudaSuccess) {
     fail_cuda(ctx, e, "pact_create");
     delete c;
     return PACT_ERR_CUDA;
   }
+  c->no_share = !share_fits();
   c->spin_limit = kSpinLimit;
   c->sweep_limit = kSpinLimit;
   c->copy_polls = INT32_MAX;

@@ -408,6 +408,24 @@ cudaError_t launch(void (*kernel)(ShareArgs), const ShareArgs &a, cudaStream_t s
   return launch_opt(opt, kernel, dim3(kShareCtas), dim3(kShareThreads), sizeof(ShareSmem), st, a);
 }
 
+bool cluster_fits(void (*kernel)(ShareArgs)) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ShareSmem)) != cudaSuccess ||
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+    return false;
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3(kShareCtas);
+  lc.blockDim = dim3(kShareThreads);
+  lc.dynamicSmemBytes = sizeof(ShareSmem);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kShareCtas;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  lc.attrs = attr;
+  lc.numAttrs = 1;
+  int n = 0;
+  return cudaOccupancyMaxActiveClusters(&n, kernel, &lc) == cudaSuccess && n >= 1;
+}
+
 }  // namespace
 
 size_t fork_scratch(int requests, int max_pages, int n_pages, ShareArgs *a, char *base) {
@@ -442,13 +460,13 @@ size_t compact_scratch(int n_pages, ShareArgs *a, char *base) {
   return at;
 }
 
-cudaError_t share_configure() {
-  for (auto kernel : {k_cache_fork, k_cache_compact}) {
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ShareSmem));
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return e;
-  }
-  return cudaSuccess;
+bool share_fits() {
+  for (auto kernel : {k_cache_fork, k_cache_compact})
+    if (!cluster_fits(kernel)) {
+      (void)cudaGetLastError();
+      return false;
+    }
+  return true;
 }
 
 cudaError_t launch_cache_fork(const ShareArgs &a, cudaStream_t st) { return launch(k_cache_fork, a, st); }

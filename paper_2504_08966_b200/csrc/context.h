@@ -18,6 +18,7 @@ struct pact_ctx {
   bool umma;               // bf16 keys of a width the tcgen05 tile kernels take
   pact::PagedCfg paged;    // the paged cache's kernels for these heads
   pact::ChunkCfg chunk;    // the attention of several new tokens per request for them
+  bool no_share;           // the device cannot launch the clusters of pact_cache_fork and pact_cache_compact
   int device;
   char err[256];
   long long launches;      // kernels launched by this context so far

@@ -33,7 +33,7 @@ struct ShareArgs {
 __host__ __device__ inline int page_of(uint64_t page_mul, unsigned n) { return (int)((n >> 4) * page_mul >> 33); }
 size_t fork_scratch(int requests, int max_pages, int n_pages, ShareArgs *a, char *base);
 size_t compact_scratch(int n_pages, ShareArgs *a, char *base);
-cudaError_t share_configure();
+bool share_fits();                         // whether the device can launch that cluster; before the first launch
 cudaError_t launch_cache_fork(const ShareArgs &a, cudaStream_t st);
 cudaError_t launch_cache_compact(const ShareArgs &a, cudaStream_t st);
 

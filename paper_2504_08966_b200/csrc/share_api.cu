@@ -34,6 +34,7 @@ pact_status pact_cache_fork(pact_ctx *ctx, const pact_fork *f, void *stream) {
   if (!f->source || !f->shared || !f->free_pages || !f->n_free || !f->block_table_out || !f->length_out || !f->shared_out || !f->free_out || !f->n_free_out || !f->copies || !f->n_copies)
     return PACT_ERR_INVALID_ARG;
   if (f->block_table_out == f->block_table || f->length_out == f->length) return PACT_ERR_INVALID_ARG;
+  if (ctx->no_share) return PACT_ERR_UNSUPPORTED;
   s = check_ws(f->ws, f->ws_bytes, fork_scratch(f->n_requests, f->max_pages, f->n_pages, nullptr, nullptr));
   if (s != PACT_OK) return s;
   ShareArgs a;
@@ -55,6 +56,7 @@ pact_status pact_cache_compact(pact_ctx *ctx, const pact_compact *c, void *strea
   if (s != PACT_OK) return s;
   if (!c->shared || !c->free_pages || !c->n_free || !c->block_table_out || !c->shared_out || !c->free_out || !c->moved_to || !c->copies || !c->n_copies || c->n_list < c->n_pages / 2)
     return PACT_ERR_INVALID_ARG;
+  if (ctx->no_share) return PACT_ERR_UNSUPPORTED;
   s = check_ws(c->ws, c->ws_bytes, compact_scratch(c->n_pages, nullptr, nullptr));
   if (s != PACT_OK) return s;
   ShareArgs a;
