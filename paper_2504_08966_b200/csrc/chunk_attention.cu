@@ -34,9 +34,6 @@ namespace {
 constexpr int kSoftmaxWarps = 8;
 constexpr int kCopyWarp = 8, kMmaWarp = 9, kValueWarp = 10, kCutWarp = 11;
 constexpr int kChunkThreads = 12 * 32;
-// Registers of a thread: a row of logits and what is made of it take more than the 168 that 384 threads may have each, the other warps need fewer.
-constexpr int kRowRegs = 208, kOtherRegs = 88;
-static_assert(kSoftmaxWarps * 32 * kRowRegs + (kChunkThreads - kSoftmaxWarps * 32) * kOtherRegs <= kChunkThreads * 168, "what the CTA is launched with");
 constexpr float kLag = 8.f;                // of the reference behind the maximum, in powers of two
 constexpr size_t kChunkSmem = 227 * 1024;
 
@@ -201,8 +198,7 @@ __device__ __forceinline__ LoadAt chunk_load_at(int x, int n, int ahead) {
 }
 __device__ __forceinline__ int chunk_v_load(int j, int n, int ahead) { return ahead == 1 ? 2 * j + 1 : min(2 * j + 2, 2 * n - 1); }
 
-// A warp's bounded wait: false once kWaitNs or `polls` have run out, or another warp has given up.  Without a call: a kernel that moves registers from one group of
-// warps to another cannot have any there.
+// A warp's bounded wait: false once kWaitNs or `polls` have run out, or another warp has given up.
 struct ChunkWait {
   int *abort;
   int32_t *status;
@@ -277,7 +273,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   bool ok = true;
 
   if (warp < kSoftmaxWarps) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRowRegs));
     // ---- rows: softmax and results ----
     const int t = warp >> 2, row = tid & 127;                        // of the block
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;
@@ -618,7 +613,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     }
     if (being_read) asm volatile("bar.sync 2, %0;" ::"n"(kSoftmaxWarps * 32) : "memory");
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kCopyWarp) {
       // ---- pages ----
       constexpr int kAtOnce = 32 / C::kGroups;                         // tiles whose pages the lanes hold: 16 rows each
