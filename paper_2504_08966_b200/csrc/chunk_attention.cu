@@ -3,9 +3,8 @@
 //   s_ip = scale q_i.k_p + logw_p  (p up to the token's own row, or all),   out_i = sum_p exp(s_ip - m) v_p / sum_p exp(s_ip - m)
 //
 // Work.  The query heads of a key head read the same rows, so an item is 256 rows (token, head) of one key head: two blocks of 128, a tensor-memory lane
-// per row, against tiles of 128 cached rows that arrive once for both.  Per tile and SM 4 x 512 clocks of tcgen05 (128 x 128 x 128, logits and values, two
-// blocks), 2048 clocks of exponentials (16 a clock) and 64 KB from the L2: the three balance, and the two blocks take turns at the
-// first two.  Items of up to 128 rows (a few tokens: HBM bounds them) have one block; its even and odd tiles then take the place of the two blocks, each with a running
+// per row, against tiles of 128 cached rows that arrive once for both.  Per tile and SM 6 x 512 clocks of tcgen05 (128 x 128 x 128, logits and two terms of values, two
+// blocks), 2048 clocks of exponentials (16 a clock) and 64 KB from the L2.  None of them bounds a tile: a block's steps follow one another, and the two blocks take turns.  Items of up to 128 rows (a few tokens: HBM bounds them) have one block; its even and odd tiles then take the place of the two blocks, each with a running
 // maximum and sums of its own.
 // Above 128 columns there is one block (tensor memory has room for one result), with tiles of 64.
 //
@@ -15,17 +14,19 @@
 // Logits lie in tensor memory, probabilities take their place there, and results stay in it until the end.  The maximum that logits are taken from lags behind
 // the true one by at most 2^8 of a probability, so that results are rescaled a few times per item only.
 //
-// Measured: 1,024 tokens of 32 heads of 128 on 8 key heads over 65,536 rows 1.14 ms, 960 TFLOP/s (a tile 4,500 clocks: 1,000 for the maximum, 1,500 for probabilities, 300 to hand them on, 1,650
-// until the next logits are there); 12 prompts of up to 2,948 rows 0.70 ms, 500 TFLOP/s of what the mask leaves (nine tiles an item, then 7,000 clocks for results and the next queries);
-// 32 requests of five tokens over up to 8,192 rows 165 us, 4.1 TB/s; with fp32 results eight times 256 tokens over up to 2,916 rows 270 us (adding up the results of two tiles took 4,700 of
-// their 13,500 clocks with all sums in the L2; 64 columns in shared memory: 277 -> 270 us there, 1,154 -> 1,045 us for 30 times 879 tokens, 406 -> 382 us with heads of 64, all of whose columns fit).  What is done once per item is mostly fetching of its code: results 32 columns at a time took 3 % longer, the queries' loop unrolled 1 %.
+// Measured (four calls in a graph): 1,024 tokens of 32 heads of 128 on 8 key heads over 65,536 rows 1.51 ms, 720 TFLOP/s, and 1.65 ms once the power limit has brought the clock down (1.70 launched one by
+// one; a tile 5,700 clocks: 1,000 to 1,250 for the maximum, 2,000 to 2,350 for probabilities, 550 at its beginning, 1,800 until the next logits are there); 12 prompts of up to 2,948 rows 0.73 ms, 480
+// TFLOP/s of what the mask leaves (nine tiles an item, then 7,000 clocks for results and the next queries), with 16 heads of 192 and 256 on 4: 0.91 and 1.05 ms; 32 requests of five tokens over up to 8,192
+// rows 160 us, 4.2 TB/s; with fp32 results eight times 256 tokens over up to 2,916 rows 242 us (64 columns of the sums of earlier tiles in shared memory instead of all in the L2: 277 -> 270 us then), 30
+// times 879 tokens 937 us, heads of 64, all of whose columns fit, 360 us.  What is done once per item is mostly fetching of its code: results 32 columns at a time took 3 % longer, the queries' loop unrolled 1 %.
 //
 // Rounding: probabilities go into the products with bf16 values as two bf16 terms where results are bf16 (off by 2^-17 of a weight at most: 2 to 4 of
 // 1,000 results differ from those of fp32 probabilities; with one term 240 to 370 did), as three, which hold all of fp32's 24 bits, where they are fp32.  The tensor cores cut their running sums
 // off towards 0 (some 2^-25 at each of 16 rows and terms), so the products of 32 tiles (fp32 results: of two) at a time are added with rounding: 512 cuts of sums that grow from nothing, 2^-16 in the mean.
 // Sums of probabilities are taken before the rounding.
-// The second term took the long case from 1.14 to 1.50 ms, the prompts from 0.70 to 0.73 and left the drafts as they were, with the loops over a tile rolled: each is 32 columns of code, logits go back to tensor memory with their
-// biases.  All of a tile's columns in registers and straight code for them, as one term had it, took 1.99, 1.02 and 0.26 ms: the warps waited for instructions (1.4 warps per one that was issued, instead of 0.5).
+// The second term took the long case from 1.14 to 1.51 ms, the prompts from 0.70 to 0.73, those with heads of 192 and 256 from 0.75 and 0.80 to 0.91 and 1.05; the drafts, 165 us then, and fp32 results, 265, are faster.  For that the loops over
+// a tile are rolled: each is 32 columns of code, and logits go back to tensor memory with their biases.  All of a tile's columns in registers and straight code for them, as one term had it, took 1.99, 1.02
+// and, for the drafts, 0.26 ms: the warps waited for instructions (1.4 warps per one that was issued, instead of 0.3).  Columns 16 at a time: 1.66 ms; two loads of 32 under way at once: 1.57.
 #include "chunk_row.cuh"
 
 namespace pact {
