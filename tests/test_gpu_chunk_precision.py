@@ -127,3 +127,28 @@ def test_infinite_values_anywhere_are_that_infinity_or_nan(pb, dtype, out, n_qh,
             ctx.pact_paged_attention(pb.PagedCache(K, V), Q, table, i32([n]), one)
             assert all((x.isnan() | (x == s * float("inf"))).all() for x, s in ((one[0, :heads, 1], 1), (one[0, :heads, D - 1], -1))) and torch.isfinite(one[0, :heads][:, rest]).all()
         V[at // page, 0, at % page] = kept
+
+
+@pytest.mark.parametrize("out", [BF, F32])
+@pytest.mark.parametrize("m,n,slope,D", [(200, 4200, 64, 64), (200, 4400, 1024, 128), (200, 8300, 256, 64), (3, 8300, 64, 64), (3, 8450, 1024, 128), (100, 4200, 256, 256)])
+def test_logits_that_grow_from_tile_to_tile(pb, out, m, n, slope, D):
+    # Biases that rise with the rows (queries 0), so that sums of earlier tiles are rescaled before and after they are put aside, and so many key heads that some have all their tiles in one CTA.
+    # 2^-17 and 2^-15 as above; a factor 2^-22 and a rounding or two 2^-24 for each of up to 60 times that the reference moves: 2^-15.8; the argument of an exponential, up to 2^5 where its weight
+    # is 2^-24 or more, 2^-19; everything else 2^-20: less than 2^-13.9 (fp32 results: their rounding is within it).
+    B, H, page = (10, 32, 32) if D == 256 else (5, 64, 32)
+    P = (n + page - 1) // page
+    g = torch.Generator(device="cuda").manual_seed(n + m)
+    K = torch.zeros(P, H, page, D, dtype=BF, device="cuda")
+    V = (1 + torch.rand(P, H, page, D, generator=g, device="cuda")).to(BF)
+    w = torch.arange(P * page, device="cuda", dtype=F32).reshape(P, page) / slope
+    got, lse = torch.empty(B * m, H, D, dtype=out, device="cuda"), torch.empty(B * m, H, device="cuda")
+    context(pb, H, H, D, BF, out).pact_chunk_attention(pb.PagedCache(K, V, w), torch.zeros(B * m, H, D, dtype=BF, device="cuda"), torch.arange(P, dtype=I32, device="cuda").repeat(B, 1), i32([n] * B),
+                                                       i32([m] * B), got, row_stride=m, lse=lse)
+    s = w.reshape(-1)[:n].double()
+    p = torch.exp(s - s[-1])
+    sums, v = p.cumsum(0)[n - m:], V.transpose(0, 1).reshape(H, -1, D)[:, :n]
+    last = torch.arange(n - m, n, device="cuda")
+    want = torch.stack([((x.double() * p[:, None]).cumsum(0)[last] / sums[:, None]) for x in v], 1).cpu().numpy()
+    err = np.abs(f64(got).reshape(B, m, H, D) - want)
+    assert (err <= 2.0 ** -13.9 * want + (half_step(want) if out == BF else 0)).all()
+    assert ((lse.double().view(B, m, H) - (s[-1] + torch.log(sums))[None, :, None]).abs() <= 2.0 ** -13.9 + 2.0 ** -23 * n / slope).all()
